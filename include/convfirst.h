@@ -40,6 +40,7 @@
 #define CONVFIRST_H
 
 #include <stddef.h>
+#include <stdint.h>
 
 #ifdef __cplusplus
 extern "C" {
@@ -401,6 +402,119 @@ cf_status cf_block_autotune(const void *x, void *y, const cf_block_params *p,
 /* The cached configuration id for a key (0 = default kernel and tiling), or -1
  * for invalid arguments. */
 int cf_block_tuned_config(int N, int H, int W, int C, int E, int k, cf_dtype dt, cf_act act);
+
+/* ------------------------------------------------------------------------
+ * Training and scoring operators: what a network's norm, FFN and classifier
+ * need next to the fused blocks when they are fine-tuned over its features, or
+ * when classes or tokens are scored.  They work on rows (an NHWC tensor's
+ * pixels, tokens): x[rows][C], channels fastest, consecutive rows ld* elements
+ * apart.  Inputs may have any row stride from 0 (one row for all) on, outputs
+ * at least C.  Pointers need the alignment of their elements only.  rows = 0
+ * is a call with nothing to do.  An output may share memory with an input only
+ * where that is stated; views of one buffer with the same row stride and
+ * different columns do not share memory.  Everything else is as above:
+ * asynchronous, no device memory allocated, arguments checked first, results
+ * deterministic.  Sums are held in fp32, and each result is rounded once.
+ *
+ * Checkpoints in 8 bits.  Activations kept for the backward pass: q [rows][C]
+ * bytes and scale [rows][ceil(C/CF_CKPT_BLOCK)] floats, dense.  For each block
+ * of 64 channels of a row (the last may be shorter), with a = max |x|,
+ *   q = rint(x * (127 / a)),   scale = a * (1 / 127),   x ~ q * scale,
+ * each operation rounded in fp32: |x - q * scale| <= a / 254, up to rounding.
+ * A block with a < 2^-119 is kept as zeros (scale 0); one with infinities or
+ * NaN has a NaN scale, and so do all values read from it. */
+#define CF_CKPT_BLOCK 64
+#define CF_NORM_MAX_C 16384
+#define CF_TOP_MAX 32
+
+/* Layer norm over the C channels of each row:
+ *   mean = 1/C sum x,  rstd = 1 / sqrt(1/C sum (x - mean)^2 + eps)
+ *   y = weight * (x - mean) * rstd + bias
+ * weight, bias [C] may be NULL.  For the backward pass, each NULL unless
+ * wanted: stats [rows][2] receives mean and rstd; q and scale (both or
+ * neither) the checkpoint of x, in the same pass over it.  y may equal x with
+ * ldy = ldx.  C above CF_NORM_MAX_C returns CF_ERR_UNSUPPORTED. */
+cf_status cf_layer_norm_forward(const void *x, void *y, const float *weight, const float *bias, float *stats,
+                                int8_t *q, float *scale, int64_t rows, int C, int64_t ldx, int64_t ldy, float eps,
+                                cf_dtype dt, void *stream);
+
+/* Its gradients, with xh = (x - mean) * rstd and g = weight * dy:
+ *   dx = rstd * (g - 1/C sum g - xh * 1/C sum g xh)
+ *   dweight = sum over rows of dy * xh,  dbias = sum over rows of dy
+ * x is given as it was (x, ldx), or as the checkpoint that the forward call
+ * wrote (q, scale; x NULL); stats are the forward call's.  dx may equal dy
+ * with lddx = lddy.  dweight and dbias [C]: both or, where they are not
+ * wanted, neither.  ws (16-byte aligned; NULL for 0 bytes) holds the fp32
+ * partial sums of dweight and dbias, added in a fixed order. */
+cf_status cf_layer_norm_backward(const void *dy, const void *x, const int8_t *q, const float *scale,
+                                 const float *stats, const float *weight, void *dx, float *dweight, float *dbias,
+                                 void *ws, size_t ws_bytes, int64_t rows, int C, int64_t lddy, int64_t ldx,
+                                 int64_t lddx, cf_dtype dt, void *stream);
+size_t cf_layer_norm_backward_workspace_bytes(int64_t rows, int C);
+
+/* Checkpoint of x (cf_checkpoint_pack) and its values back (unpack). */
+cf_status cf_checkpoint_pack(const void *x, int8_t *q, float *scale, int64_t rows, int C, int64_t ldx, cf_dtype dt,
+                             void *stream);
+cf_status cf_checkpoint_unpack(const int8_t *q, const float *scale, void *x, int64_t rows, int C, int64_t ldx,
+                               cf_dtype dt, void *stream);
+
+/* h = act(u), with fp32 GELU, and in the same pass the checkpoints of u (for
+ * cf_act_backward) and of the rounded h (for the gradient of the linear layer
+ * that reads h); either pair of pointers may be NULL.  h may equal u with
+ * ldh = ldu. */
+cf_status cf_act_forward(const void *u, void *h, int8_t *qu, float *scale_u, int8_t *qh, float *scale_h, int64_t rows,
+                         int C, int64_t ldu, int64_t ldh, cf_dtype dt, cf_act act, void *stream);
+
+/* du = dh * act'(u) with u from its checkpoint (ReLU: act'(0) = 0).  du may
+ * equal dh with lddu = lddh. */
+cf_status cf_act_backward(const void *dh, const int8_t *qu, const float *scale_u, void *du, int64_t rows, int C,
+                          int64_t lddh, int64_t lddu, cf_dtype dt, cf_act act, void *stream);
+
+/* Gradients of a linear (point-wise) layer's weight and bias from the
+ * checkpoint of its input x:
+ *   dw[k][c] = sum over rows of dy[r][k] * x[r][c],  db[k] = sum over rows of dy[r][k]
+ * with dy [rows][K] (row stride lddy), x = q * scale; or, with stats [rows][2]
+ * of cf_layer_norm_forward, x = weight * (q * scale - mean) * rstd + bias (the
+ * layer read the norm's output, of which nothing else is kept; weight and bias
+ * may be NULL).  On the matrix cores: the factor from the checkpoint is
+ * rounded to dt before its products, sums are fp32.  dw [K][C] in dt, dense;
+ * db [K] fp32.  rows = 0 gives zeros.  ws (16-byte aligned; NULL for 0 bytes)
+ * holds fp32 partial sums, added in a fixed order.  K and C up to 2^20
+ * (CF_ERR_UNSUPPORTED above). */
+cf_status cf_linear_weight_grad(const void *dy, const int8_t *q, const float *scale, const float *stats,
+                                const float *weight, const float *bias, void *dw, float *db, void *ws,
+                                size_t ws_bytes, int64_t rows, int K, int C, int64_t lddy, cf_dtype dt, void *stream);
+size_t cf_linear_weight_grad_workspace_bytes(int64_t rows, int K, int C);
+
+/* Log probabilities from logits z [rows][V] (row stride ldz), fp16, bf16 or
+ * fp32 (cf_logits_dtype).  With m the largest logit and s the sum of exp(z - m):
+ *   logp[r] = z[r][token] - m - log s     of the given token (tokens, logp: both or neither NULL);
+ *             0 for a negative token (nothing asked), NaN for one of V or more
+ *   entropy[r] = -sum p log p             (fp32, natural logarithms)
+ *   stats[r] = {m, log s}                 for cf_log_probs_backward; may be NULL
+ *   top_logp[r][n], top_ids[r][n]         the `top` most probable tokens and their log
+ *             probabilities in order, equal logits by index (top = 0: both NULL)
+ * A logit of -inf has probability 0; a row with nothing else has logp and
+ * top_logp -inf and entropy 0.  A row with +inf or NaN has NaN logp, entropy,
+ * stats and top_logp (of its ids, NaN logits come first).  top is at most
+ * CF_TOP_MAX and at most V.  ws (16-byte aligned; NULL for 0 bytes): a few rows are cut into
+ * chunks whose results it holds. */
+typedef enum { CF_LOGITS_F16 = 0, CF_LOGITS_BF16 = 1, CF_LOGITS_F32 = 2 } cf_logits_dtype;
+cf_status cf_log_probs_forward(const void *z, const int64_t *tokens, float *logp, float *entropy, float *stats,
+                               float *top_logp, int64_t *top_ids, int top, void *ws, size_t ws_bytes, int64_t rows,
+                               int V, int64_t ldz, cf_logits_dtype dt, void *stream);
+size_t cf_log_probs_workspace_bytes(int64_t rows, int V, int top);
+
+/* The gradient of sum(d_logp * logp) + sum(d_entropy * entropy):
+ *   dz[r][j] = d_logp[r] (1[j = token] - p_j) - d_entropy[r] p_j (log p_j + entropy[r])
+ * stats and entropy are the forward call's.  d_logp needs tokens; either of
+ * d_logp and d_entropy may be NULL.  Rows without a finite logit, and d_logp
+ * of a negative token, have no gradient; rows with NaN results, and those that
+ * asked for a token of V or more, have a NaN gradient.  dz may equal z with
+ * lddz = ldz. */
+cf_status cf_log_probs_backward(const void *z, const int64_t *tokens, const float *stats, const float *entropy,
+                                const float *d_logp, const float *d_entropy, void *dz, int64_t rows, int V,
+                                int64_t ldz, int64_t lddz, cf_logits_dtype dt, void *stream);
 
 /* Thread-local message describing the most recent non-CF_OK status. */
 const char *cf_last_error(void);

@@ -34,6 +34,9 @@ __all__ = [
     "CFError", "EXPORTED_SYMBOLS", "dw_weight_from_conv2d", "grouped_weight_from_conv2d",
     "pw_weight_from_conv2d", "down_weight_from_conv2d", "fold_batchnorm", "block_params_from_modules",
     "grouped_block_params_from_modules", "down_params_from_modules", "stem_params_from_modules",
+    "Checkpoint", "LogProbs", "layer_norm_forward", "layer_norm_forward_save", "layer_norm_backward",
+    "checkpoint_pack", "checkpoint_unpack", "act_forward", "act_forward_save", "act_backward",
+    "linear_weight_grad", "log_probs_forward", "log_probs_backward",
 ]
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -52,6 +55,10 @@ EXPORTED_SYMBOLS = (
     "cf_mbconv_workspace_bytes", "cf_mbconv_s2_forward", "cf_mbconv_s2_workspace_bytes", "cf_stem_forward",
     "cf_stem_gblock_forward", "cf_block_autotune",
     "cf_block_tuned_config", "cf_last_error", "cf_status_string", "cf_abi_version",
+    "cf_layer_norm_forward", "cf_layer_norm_backward", "cf_layer_norm_backward_workspace_bytes",
+    "cf_checkpoint_pack", "cf_checkpoint_unpack", "cf_act_forward", "cf_act_backward",
+    "cf_linear_weight_grad", "cf_linear_weight_grad_workspace_bytes",
+    "cf_log_probs_forward", "cf_log_probs_workspace_bytes", "cf_log_probs_backward",
 )
 
 
@@ -205,6 +212,21 @@ def lib():
             "cf_status_string": (ctypes.c_char_p, [i]),
             "cf_abi_version": (i, []),
         }
+        l, f = ctypes.c_int64, ctypes.c_float
+        sig.update({
+            "cf_layer_norm_forward": (i, [vp] * 7 + [l, i, l, l, f, i, vp]),
+            "cf_layer_norm_backward": (i, [vp] * 10 + [sz, l, i, l, l, l, i, vp]),
+            "cf_layer_norm_backward_workspace_bytes": (sz, [l, i]),
+            "cf_checkpoint_pack": (i, [vp] * 3 + [l, i, l, i, vp]),
+            "cf_checkpoint_unpack": (i, [vp] * 3 + [l, i, l, i, vp]),
+            "cf_act_forward": (i, [vp] * 6 + [l, i, l, l, i, i, vp]),
+            "cf_act_backward": (i, [vp] * 4 + [l, i, l, l, i, i, vp]),
+            "cf_linear_weight_grad": (i, [vp] * 9 + [sz, l, i, i, l, i, vp]),
+            "cf_linear_weight_grad_workspace_bytes": (sz, [l, i, i]),
+            "cf_log_probs_forward": (i, [vp] * 7 + [i, vp, sz, l, i, l, i, vp]),
+            "cf_log_probs_workspace_bytes": (sz, [l, i, i]),
+            "cf_log_probs_backward": (i, [vp] * 7 + [l, i, l, l, i, vp]),
+        })
         for name, (res, args) in sig.items():
             f = getattr(L, name)
             f.restype = res
@@ -367,12 +389,12 @@ def _allocating_for(x: torch.Tensor, stream):
     return contextlib.nullcontext() if stream is None else torch.cuda.stream(_torch_stream(x, stream))
 
 
-def _new(x: torch.Tensor, shape, stream):
+def _new(x: torch.Tensor, shape, stream, dtype=None):
     """A new output of a call on `stream`: from that stream's pool, as scratch
     is, and not handed out again before the current stream, on which the caller
     goes on, has done what it has queued when the output is dropped."""
     with _allocating_for(x, stream):
-        y = torch.empty(shape, dtype=x.dtype, device=x.device)
+        y = torch.empty(shape, dtype=dtype or x.dtype, device=x.device)
     if stream is not None:
         y.record_stream(torch.cuda.current_stream(x.device))
     return y
@@ -996,3 +1018,8 @@ class ConvFirstBlock(torch.nn.Module):
 
     def forward(self, x: torch.Tensor) -> torch.Tensor:
         return block_forward(x, self.params(), act=self.act)
+
+
+from .training import (Checkpoint, LogProbs, act_backward, act_forward, act_forward_save,  # noqa: E402
+                       checkpoint_pack, checkpoint_unpack, layer_norm_backward, layer_norm_forward,
+                       layer_norm_forward_save, linear_weight_grad, log_probs_backward, log_probs_forward)

@@ -2,6 +2,7 @@
 // host (no HIP call before every check has passed), dispatch to the launchers
 // of cf_fused.hip / cf_unfused.hip, and error reporting.
 #include "convfirst.h"
+#include "cf_api.h"
 #include "cf_kernels.h"
 
 #include <hip/hip_runtime.h>
@@ -330,6 +331,21 @@ cf_status mbconv_call(const char *what, const void *x, void *y, void *ws, size_t
 }
 
 }  // namespace
+
+cf_status cf::api_fail(cf_status s, const char *fmt, ...) {
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(g_err, sizeof g_err, fmt, ap);
+    va_end(ap);
+    return s;
+}
+
+cf_status cf::api_done(hipError_t e, const char *what) {
+    if (e != hipSuccess)
+        return hip_fail(e, what);
+    g_err[0] = 0;
+    return CF_OK;
+}
 
 extern "C" {
 

@@ -1,0 +1,656 @@
+// cf_logprobs.hip -- log probabilities of given tokens (classes), entropy and
+// the most probable alternatives from rows of logits z, and the gradient.
+//
+//   m = max_j z_j,  s = sum_j exp(z_j - m),  log p_j = (z_j - m) - log s
+//   H = -sum_j p_j log p_j = log s - 1/s sum_j exp(z_j - m) (z_j - m)
+//   dz_j = g (1[j = token] - p_j) - h p_j (log p_j + H)     for gradients g of log p, h of H
+//
+// The forward pass reads the logits once: every thread keeps the running
+// maximum of its share of the row with the two sums relative to it (fp32;
+// exponentials in base 2) and rescales them when the maximum grows; the
+// threads' triples are joined at the end.  Few rows are cut into chunks for
+// workgroups of their own, whose triples a second launch joins.
+//
+// A logit of -inf has probability 0 and adds nothing.  A row with nothing else
+// has log p = -inf, H = 0 and no gradient; one with +inf or NaN has NaN
+// everywhere.  References to the maximum stay at or above the lowest finite
+// number, so that rows masked with it are as good as any other.
+//
+// Alternatives: the n-th largest of the 64 maxima over four threads each bounds
+// the n-th largest logit from below, so only the few threads whose maximum
+// reaches it look at their share again and collect what does.  Equal logits
+// rank by index; where more are equal than fit the list (a row with few
+// classes left), those above the bound are collected and the equal ones taken
+// in the order of the row.
+#include "cf_rows.h"
+#include "cf_kernels.h"
+#include "cf_train.h"
+
+namespace cf {
+
+namespace {
+
+constexpr float LOG2E = 1.44269504f, LN2 = 0.693147181f, LOWEST = -3.40282347e38f;
+// exponents below this give 0; also stands in for -inf, whose product with 0 is not 0
+constexpr float FLOOR2 = -1000.0f;
+
+// 16 bytes of logits: VE values, of which n are in the row (the rest -inf)
+template <typename T>
+struct Z16 {
+    typedef uint16_t elem;
+    static constexpr int VE = 8;
+    typedef u32x4 raw;
+    static __device__ __forceinline__ raw load(const elem *p, int n) { return load8(p, n); }
+    static __device__ __forceinline__ void values(const raw &r, int n, float *z) {
+        unpack8<T>(r, z);
+        if (n < 8)
+#pragma unroll
+            for (int i = 0; i < 8; i++)
+                z[i] = i < n ? z[i] : -INFINITY;
+    }
+    static __device__ __forceinline__ float one(const elem *p) { return T::lo(*p); }
+    static __device__ __forceinline__ void store(elem *p, const float *z, int n) { store8(p, pack8<T>(z), n); }
+};
+struct Z32 {
+    typedef float elem;
+    static constexpr int VE = 4;
+    typedef float4v raw;
+    struct __attribute__((packed, aligned(4))) Any {
+        float4v v;
+    };
+    static __device__ __forceinline__ raw load(const elem *p, int n) {
+        if (n >= 4)
+            return reinterpret_cast<const Any *>(p)->v;
+        raw r = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < 3; i++)
+            if (i < n)
+                r[i] = p[i];
+        return r;
+    }
+    static __device__ __forceinline__ void values(const raw &r, int n, float *z) {
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+            z[i] = i < n ? r[i] : -INFINITY;
+    }
+    static __device__ __forceinline__ float one(const elem *p) { return *p; }
+    static __device__ __forceinline__ void store(elem *p, const float *z, int n) {
+        if (n >= 4) {
+            reinterpret_cast<Any *>(p)->v = float4v{z[0], z[1], z[2], z[3]};
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < 3; i++)
+            if (i < n)
+                p[i] = z[i];
+    }
+};
+
+// ---------------------------------------------------------------------------
+// Maximum m (NaN if any logit is), s and t = sum exp2(d) d of the logits seen,
+// d = (z - max(m, LOWEST)) log2 e.
+struct Stat {
+    float m, s, t;
+};
+__device__ __forceinline__ float ref_of(float m) { return fmaxf(m, LOWEST); }
+
+// the sums of a relative to a maximum m >= a.m instead
+__device__ __forceinline__ void rebase(Stat &a, float m) {
+    const float d = fmaxf((ref_of(a.m) - ref_of(m)) * LOG2E, FLOOR2), f = __builtin_amdgcn_exp2f(d);
+    a.t = f * fmaf(d, a.s, a.t);
+    a.s *= f;
+    a.m = m;
+}
+
+template <int N>
+__device__ __forceinline__ void add(Stat &a, const float *z) {
+    float m = a.m;
+#pragma unroll
+    for (int i = 0; i < N; i++)
+        m = Max::of(m, z[i]);
+    if (!(m == a.m))
+        rebase(a, m);
+    const float ref = ref_of(m);
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        const float d = fmaxf((z[i] - ref) * LOG2E, FLOOR2), e = __builtin_amdgcn_exp2f(d);
+        a.s += e;
+        a.t = fmaf(e, d, a.t);
+    }
+}
+
+__device__ __forceinline__ Stat wave_join(Stat a) {
+    const float m = lanes<Max, 64>(a.m);
+    rebase(a, m);
+    return {m, lanes<Add, 64>(a.s), lanes<Add, 64>(a.t)};
+}
+
+// ---------------------------------------------------------------------------
+// Order of the alternatives: larger logits first, NaN before all, equal ones
+// by index.  Key 0 is none.
+__device__ __forceinline__ uint64_t key_of(float z, uint32_t i) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, z + 0.0f);  // -0 equals 0
+    const uint32_t o = z != z ? 0xffffffffu : u & 0x80000000u ? ~u : u | 0x80000000u;
+    return (uint64_t)o << 32 | (0xffffffffu - i);
+}
+__device__ __forceinline__ float logit_of(uint64_t k) {
+    const uint32_t o = (uint32_t)(k >> 32);
+    return o == 0xffffffffu ? NAN : __builtin_bit_cast(float, o & 0x80000000u ? o & 0x7fffffffu : ~o);
+}
+__device__ __forceinline__ int64_t index_of(uint64_t k) { return (int64_t)(0xffffffffu - (uint32_t)k); }
+
+template <int CTRL>
+__device__ __forceinline__ uint64_t dpp64(uint64_t k) {
+    const int lo = (int)(uint32_t)k, hi = (int)(uint32_t)(k >> 32);
+    return (uint64_t)(uint32_t)__builtin_amdgcn_update_dpp(hi, hi, CTRL, 0xf, 0xf, true) << 32 |
+           (uint32_t)__builtin_amdgcn_update_dpp(lo, lo, CTRL, 0xf, 0xf, true);
+}
+__device__ __forceinline__ uint64_t later(uint64_t a, uint64_t b) { return a > b ? a : b; }
+__device__ __forceinline__ uint64_t wave_max(uint64_t k) {
+    k = later(k, dpp64<DPP_XOR1>(k));
+    k = later(k, dpp64<DPP_XOR2>(k));
+    k = later(k, dpp64<DPP_MIRROR8>(k));
+    k = later(k, dpp64<DPP_MIRROR16>(k));
+    const auto l = __builtin_amdgcn_permlane16_swap((uint32_t)k, (uint32_t)k, false, false);
+    const auto h = __builtin_amdgcn_permlane16_swap((uint32_t)(k >> 32), (uint32_t)(k >> 32), false, false);
+    k = later((uint64_t)h[0] << 32 | (uint32_t)l[0], (uint64_t)h[1] << 32 | (uint32_t)l[1]);
+    const auto l2 = __builtin_amdgcn_permlane32_swap((uint32_t)k, (uint32_t)k, false, false);
+    const auto h2 = __builtin_amdgcn_permlane32_swap((uint32_t)(k >> 32), (uint32_t)(k >> 32), false, false);
+    return later((uint64_t)h2[0] << 32 | (uint32_t)l2[0], (uint64_t)h2[1] << 32 | (uint32_t)l2[1]);
+}
+
+struct Args {
+    const void *z;
+    const int64_t *tokens;
+    float *logp, *entropy;
+    float2 *stats;
+    float *top_logp;
+    int64_t *top_ids;
+    float4 *part;        // [rows][chunks]: m, s, t
+    uint64_t *part_key;  // [rows][chunks][top], in order
+    int64_t ldz;
+    int V, top, chunks, chunk;  // logits of a chunk, a multiple of 8
+};
+
+// what a row's sums say; one thread
+template <typename Z>
+__device__ __forceinline__ void finish(const Args &a, int64_t row, const Stat &s) {
+    const typename Z::elem *z = (const typename Z::elem *)a.z + row * a.ldz;
+    const bool bad = !(s.m < INFINITY), empty = s.s == 0.0f;
+    const float ref = ref_of(s.m), ls = bad ? NAN : empty ? 0.0f : logf(s.s);
+    const int64_t t = a.tokens ? a.tokens[row] : -1;
+    if (a.logp) {
+        float lp = 0.0f;
+        if (t >= a.V)
+            lp = NAN;
+        else if (t >= 0)
+            lp = bad ? NAN : (Z::one(z + t) - ref) - ls;
+        a.logp[row] = lp;
+    }
+    a.entropy[row] = bad ? NAN : empty ? 0.0f : fmaxf(ls - LN2 * (s.t / s.s), 0.0f);
+    if (a.stats)
+        a.stats[row] = bad ? make_float2(NAN, NAN) : empty ? make_float2(-INFINITY, 0.0f) : make_float2(s.m, ls);
+}
+
+// one alternative of a row
+__device__ __forceinline__ void put_top(const Args &a, int64_t row, int n, uint64_t key, const Stat &s) {
+    const bool bad = !(s.m < INFINITY);
+    const float z = logit_of(key);
+    a.top_logp[row * a.top + n] = bad ? NAN : s.s == 0.0f ? z : (z - ref_of(s.m)) - logf(s.s);
+    a.top_ids[row * a.top + n] = index_of(key);
+}
+
+constexpr int TH = 256;    // threads of a workgroup
+constexpr int NV = 4;      // vectors a thread loads together
+constexpr int LIST = 512;  // logits collected before equal ones are counted
+
+// Scan of the n <= `end` logits from `begin`: f(value, index) for every logit
+// of this thread's share.
+template <typename Z, typename F>
+__device__ __forceinline__ void each(const typename Z::elem *z, int begin, int end, F &&f) {
+    for (int i = begin + (int)threadIdx.x * Z::VE; i < end; i += TH * Z::VE) {
+        float v[Z::VE];
+        const int n = end - i;
+        Z::values(Z::load(z + i, n), n, v);
+#pragma unroll
+        for (int e = 0; e < Z::VE; e++)
+            if (e < n)
+                f(v[e], (uint32_t)(i + e));
+    }
+}
+
+struct TopSpace {
+    float gm[64];
+    uint64_t list[LIST];
+    uint64_t out[TOP_MAX];
+    uint64_t best[TH / 64];
+    int n, cnt[TH / 64];
+};
+
+// The `top` first logits of [begin, end) in order into sp.out (0 where there
+// are fewer); tm is the maximum of this thread's share.  Every thread calls it
+// and may read sp.out afterwards.
+template <typename Z>
+__device__ void find_top(const typename Z::elem *z, int begin, int end, int top, float tm, TopSpace &sp) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const float g = lanes<Max, 4>(tm);
+    if ((tid & 3) == 0)
+        sp.gm[tid >> 2] = g;
+    if (tid == 0)
+        sp.n = 0;
+    if (tid < top)
+        sp.out[tid] = 0;
+    __syncthreads();
+    // the n-th largest of the 64 maxima: the least one with fewer than n above it
+    const float mine = sp.gm[lane];
+    int above = 0;
+    bool nan = false;
+#pragma unroll
+    for (int j = 0; j < 64; j += 4) {
+        const float4 o = *reinterpret_cast<const float4 *>(&sp.gm[j]);
+        above += (o.x > mine) + (o.y > mine) + (o.z > mine) + (o.w > mine);
+        nan |= o.x != o.x || o.y != o.y || o.z != o.z || o.w != o.w;
+    }
+    const float bound = -lanes<Max, 64>(above < top ? -mine : -INFINITY);
+    // nan is the same in every thread
+    bool done = false;
+    if (!nan) {
+        if (tm >= bound)
+            each<Z>(z, begin, end, [&](float v, uint32_t i) {
+                if (v >= bound) {
+                    const int at = atomicAdd(&sp.n, 1);
+                    if (at < LIST)
+                        sp.list[at] = key_of(v, i);
+                }
+            });
+        __syncthreads();
+        int n = sp.n;
+        done = n <= LIST;
+        if (!done) {  // many are equal: those above the bound, then the first of the equal ones
+            __syncthreads();
+            if (tid == 0)
+                sp.n = 0;
+            __syncthreads();
+            if (tm > bound)
+                each<Z>(z, begin, end, [&](float v, uint32_t i) {
+                    if (v > bound) {
+                        const int at = atomicAdd(&sp.n, 1);
+                        if (at < LIST)
+                            sp.list[at] = key_of(v, i);
+                    }
+                });
+            __syncthreads();
+            n = sp.n;
+            done = n + TOP_MAX <= LIST;
+            if (done && n < top) {
+                const int above_n = n, want = top - n;
+                int found = 0;
+                for (int i0 = begin; i0 < end && found < want; i0 += TH * Z::VE) {
+                    const int i = i0 + tid * Z::VE;
+                    float v[Z::VE];
+                    unsigned eq = 0;
+                    if (i < end) {
+                        Z::values(Z::load(z + i, end - i), end - i, v);
+#pragma unroll
+                        for (int e = 0; e < Z::VE; e++)
+                            eq |= (unsigned)(v[e] == bound && e < end - i) << e;
+                    }
+                    int c = __popc(eq), before = c;
+#pragma unroll
+                    for (int o = 1; o < 64; o <<= 1) {
+                        const int up = __shfl_up(before, o);
+                        before += lane >= o ? up : 0;
+                    }
+                    if (lane == 63)
+                        sp.cnt[wave] = before;
+                    __syncthreads();
+                    int at = found + before - c, all = 0;
+#pragma unroll
+                    for (int w = 0; w < TH / 64; w++) {
+                        at += w < wave ? sp.cnt[w] : 0;
+                        all += sp.cnt[w];
+                    }
+#pragma unroll
+                    for (int e = 0; e < Z::VE; e++)
+                        if (eq >> e & 1) {
+                            if (at < want)
+                                sp.list[above_n + at] = key_of(bound, (uint32_t)(i + e));
+                            at++;
+                        }
+                    found += all;
+                    __syncthreads();
+                }
+                n += found < want ? found : want;
+            }
+        }
+        if (done) {
+            for (int i = tid; i < n; i += TH) {
+                const uint64_t k = sp.list[i];
+                int rank = 0;
+                for (int j = 0; j < n; j++)
+                    rank += sp.list[j] > k;
+                if (rank < top)
+                    sp.out[rank] = k;
+            }
+        }
+    }
+    if (!done) {  // NaN, or hundreds above the bound in few threads: one pass for each
+        uint64_t last = ~0ull;
+        bool first = true;
+        for (int r = 0; r < top; r++) {
+            uint64_t best = 0;
+            each<Z>(z, begin, end, [&](float v, uint32_t i) {
+                const uint64_t k = key_of(v, i);
+                best = (first || k < last) && k > best ? k : best;
+            });
+            best = wave_max(best);
+            __syncthreads();
+            if (lane == 0)
+                sp.best[wave] = best;
+            __syncthreads();
+            best = sp.best[0];
+#pragma unroll
+            for (int w = 1; w < TH / 64; w++)
+                best = later(best, sp.best[w]);
+            if (tid == 0)
+                sp.out[r] = best;
+            if (best == 0)
+                break;
+            last = best;
+            first = false;
+        }
+    }
+    __syncthreads();
+}
+
+// One chunk of one row a workgroup; a row of one chunk is finished here.
+template <typename Z, bool TOP>
+__global__ __launch_bounds__(TH) void log_probs_kernel(Args a) {
+    __shared__ Stat join[TH / 64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t row = blockIdx.x / (unsigned)a.chunks;
+    const int part = (int)(blockIdx.x - (unsigned)row * (unsigned)a.chunks);
+    const typename Z::elem *const z = (const typename Z::elem *)a.z + row * a.ldz;
+    const int begin = part * a.chunk, end = a.V - begin < a.chunk ? a.V : begin + a.chunk;
+    constexpr int STEP = TH * Z::VE;
+
+    Stat st = {-INFINITY, 0.0f, 0.0f};
+    typename Z::raw next[NV] = {};
+    auto fetch = [&](int i) {
+#pragma unroll
+        for (int v = 0; v < NV; v++)
+            if (i + v * STEP < end)
+                next[v] = Z::load(z + i + v * STEP, end - (i + v * STEP));
+    };
+    int i = begin + tid * Z::VE;
+    fetch(i);
+    for (; i < end; i += NV * STEP) {
+        typename Z::raw cur[NV];
+#pragma unroll
+        for (int v = 0; v < NV; v++)
+            cur[v] = next[v];
+        fetch(i + NV * STEP);
+        float x[NV * Z::VE];
+#pragma unroll
+        for (int v = 0; v < NV; v++)
+            Z::values(cur[v], end - (i + v * STEP), x + v * Z::VE);
+        add<NV * Z::VE>(st, x);
+    }
+    const float tm = st.m;
+    st = wave_join(st);
+    if (lane == 0)
+        join[wave] = st;
+    __syncthreads();
+    float m = join[0].m;
+#pragma unroll
+    for (int w = 1; w < TH / 64; w++)
+        m = Max::of(m, join[w].m);
+    Stat all = {m, 0.0f, 0.0f};
+#pragma unroll
+    for (int w = 0; w < TH / 64; w++) {
+        Stat o = join[w];
+        rebase(o, m);
+        all.s += o.s;
+        all.t += o.t;
+    }
+    if (tid == 0) {
+        if (a.chunks > 1)
+            a.part[row * a.chunks + part] = make_float4(all.m, all.s, all.t, 0.0f);
+        else
+            finish<Z>(a, row, all);
+    }
+    if constexpr (TOP) {
+        __shared__ TopSpace sp;
+        find_top<Z>(z, begin, end, a.top, tm, sp);
+        if (tid < a.top) {
+            if (a.chunks > 1)
+                a.part_key[(row * a.chunks + part) * a.top + tid] = sp.out[tid];
+            else
+                put_top(a, row, tid, sp.out[tid], all);
+        }
+    }
+}
+
+constexpr int CHUNKS = 64;  // at most, one a lane of the joining wave
+
+// The chunks of a row: a lane each; alternatives by merging their lists.
+template <typename Z, bool TOP>
+__global__ __launch_bounds__(64) void log_probs_join_kernel(Args a) {
+    const int lane = threadIdx.x;
+    const int64_t row = blockIdx.x;
+    const bool on = lane < a.chunks;
+    Stat st = {-INFINITY, 0.0f, 0.0f};
+    if (on) {
+        const float4 p = a.part[row * a.chunks + lane];
+        st = {p.x, p.y, p.z};
+    }
+    st = wave_join(st);
+    if (lane == 0)
+        finish<Z>(a, row, st);
+    if constexpr (TOP) {
+        __shared__ uint64_t key[CHUNKS * TOP_MAX];
+        const uint64_t *const from = a.part_key + row * a.chunks * a.top;
+        for (int i = lane; i < a.chunks * a.top; i += 64)
+            key[i] = from[i];
+        __syncthreads();
+        int at = 0;
+        uint64_t head = on ? key[lane * a.top] : 0, mine = 0;
+        for (int n = 0; n < a.top; n++) {
+            const uint64_t best = wave_max(head);
+            if (n == lane)
+                mine = best;
+            if (head == best && best != 0) {
+                at++;
+                head = at < a.top ? key[lane * a.top + at] : 0;
+            }
+        }
+        if (lane < a.top)
+            put_top(a, row, lane, mine, st);
+    }
+}
+
+// ---------------------------------------------------------------------------
+struct BackArgs {
+    const void *z;
+    void *dz;
+    const int64_t *tokens;
+    const float2 *stats;
+    const float *entropy, *d_logp, *d_entropy;
+    int64_t ldz, lddz;
+    int V;
+    uint32_t n;       // vectors of all rows
+    FastDiv per_row;  // vectors of a row
+};
+
+// What the vectors of a row share:  dz_j = p_j (a + b l_j), l_j = log2 p_j.
+struct RowGrad {
+    float ref, off, a, b, g;
+    int64_t token;
+};
+__device__ __forceinline__ RowGrad row_grad(const BackArgs &k, int64_t row) {
+    RowGrad r;
+    const float2 st = k.stats[row];
+    const bool bad = !(st.x < INFINITY), empty = st.x == -INFINITY;
+    const float h = k.d_entropy ? k.d_entropy[row] : 0.0f;
+    r.token = k.tokens ? k.tokens[row] : -1;
+    r.g = r.token >= 0 && k.d_logp ? k.d_logp[row] : 0.0f;
+    r.ref = ref_of(st.x);
+    r.off = -st.y * LOG2E;
+    r.a = k.d_entropy ? -r.g - h * k.entropy[row] : -r.g;
+    r.b = -h * LN2;
+    if (empty)
+        r.a = r.b = r.g = 0.0f;
+    if (bad || r.token >= k.V)  // no such class: the forward pass said NaN
+        r.a = NAN;
+    return r;
+}
+
+template <typename Z>
+__device__ __forceinline__ void grad8(const BackArgs &k, const RowGrad &r, const typename Z::elem *z,
+                                      typename Z::elem *dz, int i) {
+    const int n = k.V - i;
+    float x[Z::VE];
+    Z::values(Z::load(z + i, n), n, x);
+#pragma unroll
+    for (int e = 0; e < Z::VE; e++) {
+        const float l = fmaxf(fmaf(x[e] - r.ref, LOG2E, r.off), FLOOR2);
+        x[e] = __builtin_amdgcn_exp2f(l) * fmaf(r.b, l, r.a);
+    }
+    if (r.token >= i && r.token < i + Z::VE)
+#pragma unroll
+        for (int e = 0; e < Z::VE; e++)
+            if (r.token == i + e)
+                x[e] += r.g;
+    Z::store(dz + i, x, n);
+}
+
+// Short rows: a thread takes a vector of any row.
+template <typename Z>
+__global__ __launch_bounds__(256) void log_probs_backward_kernel(BackArgs k) {
+    const uint32_t v = blockIdx.x * 256 + threadIdx.x;
+    if (v >= k.n)
+        return;
+    const uint32_t row = fdiv(v, k.per_row);
+    const int i = (int)(v - row * k.per_row.d) * Z::VE;
+    grad8<Z>(k, row_grad(k, row), (const typename Z::elem *)k.z + row * k.ldz,
+             (typename Z::elem *)k.dz + row * k.lddz, i);
+}
+
+// Long rows: a workgroup takes BACK_NV * 256 vectors of one row, whose numbers
+// it reads once.
+constexpr int BACK_NV = 4;
+template <typename Z>
+__global__ __launch_bounds__(256) void log_probs_backward_row_kernel(BackArgs k, uint32_t chunks) {
+    const uint32_t row = blockIdx.x / chunks, part = blockIdx.x - row * chunks;
+    const RowGrad r = row_grad(k, row);
+    const typename Z::elem *const z = (const typename Z::elem *)k.z + row * k.ldz;
+    typename Z::elem *const dz = (typename Z::elem *)k.dz + row * k.lddz;
+#pragma unroll
+    for (int v = 0; v < BACK_NV; v++) {
+        const int64_t i = ((int64_t)part * BACK_NV + v) * 256 * Z::VE + threadIdx.x * Z::VE;
+        if (i < k.V)
+            grad8<Z>(k, r, z, dz, (int)i);
+    }
+}
+
+// Chunks of a row, and their length: rows enough to fill the chip stay whole;
+// otherwise about four workgroups a CU, of at least a vector for each thread.
+void chunks_of(int64_t rows, int V, int *chunks, int *chunk) {
+    int64_t n = (4 * device_cu_count() + rows - 1) / rows;
+    const int64_t most = (V + 2047) / 2048;
+    n = n < most ? n : most;
+    n = n < CHUNKS ? n : CHUNKS;
+    n = rows >= 2 * device_cu_count() || n < 1 ? 1 : n;
+    *chunk = (int)((V + n - 1) / n + 7) / 8 * 8;
+    *chunks = (V + *chunk - 1) / *chunk;
+}
+
+template <typename Z>
+hipError_t forward(const Args &a, int64_t rows, hipStream_t st) {
+    const dim3 grid((unsigned)(rows * a.chunks));
+    if (a.top)
+        log_probs_kernel<Z, true><<<grid, dim3(TH), 0, st>>>(a);
+    else
+        log_probs_kernel<Z, false><<<grid, dim3(TH), 0, st>>>(a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.chunks == 1)
+        return e;
+    if (a.top)
+        log_probs_join_kernel<Z, true><<<dim3((unsigned)rows), dim3(64), 0, st>>>(a);
+    else
+        log_probs_join_kernel<Z, false><<<dim3((unsigned)rows), dim3(64), 0, st>>>(a);
+    return hipGetLastError();
+}
+
+template <typename Z>
+hipError_t backward(BackArgs &a, int64_t rows, hipStream_t st) {
+    constexpr int SPAN = BACK_NV * 256 * Z::VE;
+    if (a.V >= SPAN / 2) {
+        const uint32_t chunks = (uint32_t)((a.V + SPAN - 1) / SPAN);
+        log_probs_backward_row_kernel<Z><<<dim3((unsigned)(rows * chunks)), dim3(256), 0, st>>>(a, chunks);
+    } else {
+        const uint32_t per_row = (uint32_t)((a.V + Z::VE - 1) / Z::VE);
+        a.per_row = make_fastdiv(per_row);
+        a.n = (uint32_t)(rows * per_row);
+        log_probs_backward_kernel<Z><<<dim3((a.n + 255) / 256), dim3(256), 0, st>>>(a);
+    }
+    return hipGetLastError();
+}
+
+size_t keys_at(int64_t rows, int chunks) { return (size_t)rows * chunks * sizeof(float4); }
+
+}  // namespace
+
+// Grids stay below 2^32 threads, vectors of short rows below 2^31.
+bool log_probs_fit(int64_t rows, int V) {
+    const double limit = 16777216.0;
+    return rows < limit && (V >= 4096 ? (double)rows * ((V + 4095) / 4096) < limit
+                                      : (double)rows * ((V + 3) / 4) < 2147483648.0);
+}
+
+size_t log_probs_workspace_bytes(int64_t rows, int V, int top) {
+    int chunks, chunk;
+    chunks_of(rows, V, &chunks, &chunk);
+    return chunks > 1 ? keys_at(rows, chunks) + (size_t)rows * chunks * top * sizeof(uint64_t) : 0;
+}
+
+hipError_t launch_log_probs(const LogProbs &p, int64_t rows, int V, int top, int dt, void *ws, hipStream_t st) {
+    Args a;
+    a.z = p.z;
+    a.tokens = p.tokens;
+    a.logp = p.logp;
+    a.entropy = p.entropy;
+    a.stats = (float2 *)p.stats;
+    a.top_logp = p.top_logp;
+    a.top_ids = p.top_ids;
+    a.ldz = p.ldz;
+    a.V = V;
+    a.top = top;
+    chunks_of(rows, V, &a.chunks, &a.chunk);
+    a.part = (float4 *)ws;
+    a.part_key = (uint64_t *)((char *)ws + keys_at(rows, a.chunks));
+    return dt == LOGITS_F32 ? forward<Z32>(a, rows, st)
+           : dt == LOGITS_BF16 ? forward<Z16<BF16>>(a, rows, st)
+                               : forward<Z16<F16>>(a, rows, st);
+}
+
+hipError_t launch_log_probs_backward(const LogProbsBackward &p, int64_t rows, int V, int dt, hipStream_t st) {
+    BackArgs a;
+    a.z = p.z;
+    a.dz = p.dz;
+    a.tokens = p.tokens;
+    a.stats = (const float2 *)p.stats;
+    a.entropy = p.entropy;
+    a.d_logp = p.d_logp;
+    a.d_entropy = p.d_entropy;
+    a.ldz = p.ldz;
+    a.lddz = p.lddz;
+    a.V = V;
+    a.n = 0;
+    a.per_row = FastDiv{1, 0, 0};
+    return dt == LOGITS_F32 ? backward<Z32>(a, rows, st)
+           : dt == LOGITS_BF16 ? backward<Z16<BF16>>(a, rows, st)
+                               : backward<Z16<F16>>(a, rows, st);
+}
+
+}  // namespace cf

@@ -1,0 +1,462 @@
+// cf_norm.hip -- layer norm over the channels of each row (an NHWC pixel, a
+// token), forward and backward, with the 8-bit checkpoint of the input.
+//
+//   mean = 1/C sum_c x,  var = 1/C sum_c (x - mean)^2,  rstd = 1 / sqrt(var + eps)
+//   xh = (x - mean) rstd,  y = w xh + b
+//   g = w dy,  dx = rstd (g - 1/C sum_c g - xh 1/C sum_c g xh)
+//   dw = sum_r dy xh,  db = sum_r dy
+//
+// Both passes are bound by memory: a row is read once, held in registers as
+// fp32 (so the variance is a second pass over registers, without the
+// cancellation of E[x^2] - mean^2) and written once.  G lanes share a row,
+// 8 V channels each, in vectors of 8 that alternate between the lanes so that
+// a group's loads are contiguous: narrow rows of 64 channels take 8 lanes, a
+// wave then holds 8 rows, rows above 2048 channels take several waves.
+#include "cf_rows.h"
+#include "cf_kernels.h"
+#include "cf_train.h"
+
+namespace cf {
+
+namespace {
+
+// Sums over the G lanes of a row.  Groups of up to a wave exchange registers;
+// larger ones go through LDS, slot `buf` of `red`, with one barrier that every
+// thread of the workgroup passes.  The slot may be used again after one more
+// such barrier.
+template <int G, int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], float (*red)[16][N], int buf) {
+#pragma unroll
+    for (int i = 0; i < N; i++)
+        v[i] = lanes<Add, (G < 64 ? G : 64)>(v[i]);
+    if constexpr (G > 64) {
+        const int wave = threadIdx.x >> 6, w0 = wave / (G / 64) * (G / 64);
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int i = 0; i < N; i++)
+                red[buf][wave][i] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            float s = red[buf][w0][i];
+#pragma unroll
+            for (int k = 1; k < G / 64; k++)
+                s += red[buf][w0 + k][i];
+            v[i] = s;
+        }
+    }
+}
+
+// s / C, rounded like a division: with 1 / C alone the mean of a row of large
+// equal values is off by a rounding that its spread of 0 does not hide.
+__device__ __forceinline__ float mean_of(float s, float c, float inv_c) {
+    const float m = s * inv_c;
+    return fmaf(fmaf(-m, c, s), inv_c, m);
+}
+
+struct NormArgs {
+    const uint16_t *x;
+    uint16_t *y;
+    const float *w, *b;
+    float2 *stats;
+    int8_t *q;
+    float *scale;
+    int64_t ldx, ldy, rows;
+    int C, blocks;
+    float eps;
+};
+
+// U rows a group: their loads are issued together.
+template <typename T, int G, int V, int U>
+__global__ __launch_bounds__(G > 256 ? G : 256) void norm_forward_kernel(NormArgs a) {
+    constexpr int TH = G > 256 ? G : 256, NG = TH / G;
+    __shared__ float red[2][16][U];
+    const int grp = threadIdx.x / G, gl = threadIdx.x % G;
+    const int64_t r0 = (int64_t)blockIdx.x * (NG * U) + grp;
+    const float fc = (float)a.C, inv_c = 1.0f / fc;
+    u32x4 raw[U][V];
+#pragma unroll
+    for (int u = 0; u < U; u++)
+#pragma unroll
+        for (int v = 0; v < V; v++) {
+            const int64_t r = r0 + u * NG;
+            const int c = (gl + v * G) * 8;
+            raw[u][v] = r < a.rows ? load8(a.x + r * a.ldx + c, a.C - c) : u32x4{0u, 0u, 0u, 0u};
+        }
+    float x[U][V * 8], s[U];
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+        s[u] = 0.0f;
+#pragma unroll
+        for (int v = 0; v < V; v++) {
+            unpack8<T>(raw[u][v], &x[u][8 * v]);
+#pragma unroll
+            for (int i = 0; i < 8; i++)
+                s[u] += x[u][8 * v + i];
+        }
+    }
+    if (a.q) {
+#pragma unroll
+        for (int u = 0; u < U; u++)
+#pragma unroll
+            for (int v = 0; v < V; v++) {
+                const int64_t r = r0 + u * NG;
+                const int c = (gl + v * G) * 8;
+                const Quant z = quant_of(lanes<Max, 8>(amax8(&x[u][8 * v])));
+                if (r < a.rows && c < a.C) {
+                    store8b(a.q + r * a.C + c, quant8(&x[u][8 * v], z.inv), a.C - c);
+                    if ((threadIdx.x & 7) == 0)
+                        a.scale[r * a.blocks + c / CKPT_BLOCK] = z.scale;
+                }
+            }
+    }
+    row_sums<G>(s, red, 0);
+    float mean[U];
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+        mean[u] = mean_of(s[u], fc, inv_c);
+        s[u] = 0.0f;
+#pragma unroll
+        for (int v = 0; v < V; v++) {
+            const int n = a.C - (gl + v * G) * 8;
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                float &d = x[u][8 * v + i];
+                d -= mean[u];
+                s[u] = i < n ? fmaf(d, d, s[u]) : s[u];
+            }
+        }
+    }
+    row_sums<G>(s, red, 1);
+    float rstd[U];
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+        rstd[u] = 1.0f / sqrtf(fmaf(s[u], inv_c, a.eps));
+        const int64_t r = r0 + u * NG;
+        if (a.stats && gl == 0 && r < a.rows)
+            a.stats[r] = make_float2(mean[u], rstd[u]);
+    }
+#pragma unroll
+    for (int v = 0; v < V; v++) {
+        const int c = (gl + v * G) * 8, n = a.C - c;
+        float w[8], b[8];
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            w[i] = a.w && i < n ? a.w[c + i] : 1.0f;
+            b[i] = a.b && i < n ? a.b[c + i] : 0.0f;
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int64_t r = r0 + u * NG;
+            float y[8];
+#pragma unroll
+            for (int i = 0; i < 8; i++)
+                y[i] = fmaf(x[u][8 * v + i] * rstd[u], w[i], b[i]);
+            if (r < a.rows && n > 0)
+                store8(a.y + r * a.ldy + c, pack8<T>(y), n);
+        }
+    }
+}
+
+struct NormBackArgs {
+    const uint16_t *dy, *x;
+    const int8_t *q;
+    const float *scale;
+    const float2 *stats;
+    const float *w;
+    uint16_t *dx;
+    float *dw, *db;  // the gradients, or [workgroup][2][C] partial sums from dw on (db null)
+    int64_t lddy, ldx, lddx, rows;
+    int C, blocks;
+};
+
+// Threads of a workgroup of the backward kernel: its register accumulators of
+// dw and db cover C / G of each row a lane, and one workgroup's groups add
+// theirs before they are written, so few large workgroups write little.
+constexpr int back_threads(int G) { return G > 512 ? G : 512; }
+
+// CK: x from its checkpoint.  Persistent: a group takes rows a grid apart, the
+// next row's loads in flight while the current one is worked on.
+template <typename T, bool CK, int G, int V>
+__global__ __launch_bounds__(back_threads(G)) void norm_backward_kernel(NormBackArgs a) {
+    constexpr int TH = back_threads(G), NG = TH / G, WAVES = TH / 64;
+    __shared__ float red[2][16][2];
+    const int grp = threadIdx.x / G, gl = threadIdx.x % G, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const float fc = (float)a.C, inv_c = 1.0f / fc;
+    float w[V * 8], dw[V * 8], db[V * 8];
+#pragma unroll
+    for (int v = 0; v < V; v++)
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const int c = (gl + v * G) * 8 + i;
+            w[8 * v + i] = a.w && c < a.C ? a.w[c] : 1.0f;
+            dw[8 * v + i] = db[8 * v + i] = 0.0f;
+        }
+    struct Row {
+        u32x4 dy[V], x[V];
+        float scale[V];
+        float2 st;
+    };
+    auto fetch = [&](int64_t r) {
+        Row t;
+        t.st = make_float2(0.0f, 0.0f);
+        if (r < a.rows)
+            t.st = a.stats[r];
+#pragma unroll
+        for (int v = 0; v < V; v++) {
+            const int c = (gl + v * G) * 8;
+            t.dy[v] = t.x[v] = u32x4{0u, 0u, 0u, 0u};
+            t.scale[v] = 0.0f;
+            if (r < a.rows && c < a.C) {
+                t.dy[v] = load8(a.dy + r * a.lddy + c, a.C - c);
+                if constexpr (CK) {
+                    const u32x2 q = load8b(a.q + r * a.C + c, a.C - c);
+                    t.x[v].x = q.x;
+                    t.x[v].y = q.y;
+                    t.scale[v] = a.scale[r * a.blocks + c / CKPT_BLOCK];
+                } else {
+                    t.x[v] = load8(a.x + r * a.ldx + c, a.C - c);
+                }
+            }
+        }
+        return t;
+    };
+    const int64_t step = (int64_t)gridDim.x * NG;
+    int64_t base = (int64_t)blockIdx.x * NG;
+    Row next = fetch(base + grp);
+    for (int it = 0; base < a.rows; base += step, it ^= 1) {
+        const Row t = next;
+        const int64_t r = base + grp;
+        next = fetch(r + step);
+        // the row's values, from the registers they were loaded into: held as
+        // 16 (or 8) bits and converted again after the sums, they leave room
+        // for the next row
+        auto values = [&](int v, float *dy, float *x) {
+            unpack8<T>(t.dy[v], dy);
+            if constexpr (CK)
+                dequant8(u32x2{t.x[v].x, t.x[v].y}, t.scale[v], x);
+            else
+                unpack8<T>(t.x[v], x);
+        };
+        float s[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int v = 0; v < V; v++) {
+            float dy[8], x[8];
+            values(v, dy, x);
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const int j = 8 * v + i;
+                const float xh = (x[i] - t.st.x) * t.st.y, g = dy[i] * w[j];
+                dw[j] = fmaf(dy[i], xh, dw[j]);
+                db[j] += dy[i];
+                s[0] += g;
+                s[1] = fmaf(g, xh, s[1]);
+            }
+        }
+        row_sums<G>(s, red, it);
+        const float m0 = mean_of(s[0], fc, inv_c), m1 = mean_of(s[1], fc, inv_c);
+#pragma unroll
+        for (int v = 0; v < V; v++) {
+            const int c = (gl + v * G) * 8;
+            float dy[8], x[8], dx[8];
+            values(v, dy, x);
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const float xh = (x[i] - t.st.x) * t.st.y;
+                dx[i] = t.st.y * (fmaf(dy[i], w[8 * v + i], -m0) - xh * m1);
+            }
+            if (r < a.rows && c < a.C)
+                store8(a.dx + r * a.lddx + c, pack8<T>(dx), a.C - c);
+        }
+    }
+    if (!a.dw)
+        return;
+    // Lanes of a wave that hold the same channels, then the waves, 4 channels
+    // of each lane at a time.
+    float *const pw = a.db ? a.dw : a.dw + (int64_t)blockIdx.x * 2 * a.C;
+    float *const pb = a.db ? a.db : pw + a.C;
+    __shared__ float4 part[2][WAVES][64];
+    constexpr int SUB = G > 64 ? G / 64 : 1;  // waves that share a row
+#pragma unroll
+    for (int j = 0; j < V * 8; j += 4) {
+        float4 t[2];
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+#pragma unroll
+            for (int k = 0; k < 2; k++) {
+                float f = k ? db[j + i] : dw[j + i];
+                if constexpr (G <= 8)
+                    f += dpp<0x128>(f);  // 8 lanes further in the row of 16
+                if constexpr (G <= 16) {
+                    const Two h = swap16(f);
+                    f = h.a + h.b;
+                }
+                if constexpr (G <= 32) {
+                    const Two h = swap32(f);
+                    f = h.a + h.b;
+                }
+                (&t[k].x)[i] = f;
+            }
+        __syncthreads();
+        part[0][wave][lane] = t[0];
+        part[1][wave][lane] = t[1];
+        __syncthreads();
+        constexpr int LANES = G < 64 ? G : 64, OUT = 2 * SUB * LANES * 4;
+        for (int o = threadIdx.x; o < OUT; o += TH) {
+            const int i = o & 3, l = (o >> 2) % LANES, rest = (o >> 2) / LANES, sub = rest % SUB, k = rest / SUB;
+            float f = 0.0f;
+#pragma unroll
+            for (int n = 0; n < WAVES / SUB; n++)
+                f += (&part[k][n * SUB + sub][l].x)[i];
+            const int c = (sub * 64 + l + (j / 8) * G) * 8 + (j & 7) + i;
+            if (c < a.C)
+                (k ? pb : pw)[c] = f;
+        }
+    }
+}
+
+// Sum of `n` partials [n][2][C] into dw [C] and db [C]: 16 columns a
+// workgroup, 64 threads share a column and add every 64th partial.
+__global__ __launch_bounds__(1024) void norm_reduce_kernel(const float *part, float *dw, float *db, int n, int C) {
+    __shared__ float s[64][17];
+    const int col = threadIdx.x & 15, at = threadIdx.x >> 4;
+    const int64_t i = (int64_t)blockIdx.x * 16 + col;
+    float f = 0.0f;
+    if (i < 2 * (int64_t)C)
+        for (int k = at; k < n; k += 64)
+            f += part[(int64_t)k * 2 * C + i];
+    s[at][col] = f;
+    __syncthreads();
+#pragma unroll
+    for (int h = 32; h > 0; h >>= 1) {
+        if (at < h)
+            s[at][col] += s[at + h][col];
+        __syncthreads();
+    }
+    if (at == 0 && i < 2 * (int64_t)C)
+        (i < C ? dw[i] : db[i - C]) = s[0][col];
+}
+
+// Lanes and vectors of a row of C channels.
+#define CF_NORM_SHAPES(F)                                                                                              \
+    if (C <= 64) return F(8, 1);                                                                                       \
+    if (C <= 128) return F(16, 1);                                                                                     \
+    if (C <= 256) return F(32, 1);                                                                                     \
+    if (C <= 512) return F(64, 1);                                                                                     \
+    if (C <= 1024) return F(64, 2);                                                                                    \
+    if (C <= 2048) return F(128, 2);                                                                                   \
+    if (C <= 4096) return F(256, 2);                                                                                   \
+    if (C <= 8192) return F(512, 2);                                                                                   \
+    return F(1024, 2);
+
+template <typename T, int G, int V>
+hipError_t forward_shape(const NormArgs &a, hipStream_t st) {
+    constexpr int NG = (G > 256 ? G : 256) / G, TH = G > 256 ? G : 256;
+    // Four rows a group where that leaves eight workgroups a CU.
+    constexpr int U = 4 / V;
+    const int64_t many = (a.rows + NG * U - 1) / (NG * U);
+    if (many >= 8 * device_cu_count()) {
+        norm_forward_kernel<T, G, V, U><<<dim3((unsigned)many), dim3(TH), 0, st>>>(a);
+    } else {
+        norm_forward_kernel<T, G, V, 1><<<dim3((unsigned)((a.rows + NG - 1) / NG)), dim3(TH), 0, st>>>(a);
+    }
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t forward_type(const NormArgs &a, hipStream_t st) {
+    const int C = a.C;
+#define F(G, V) (forward_shape<T, G, V>(a, st))
+    CF_NORM_SHAPES(F)
+#undef F
+}
+
+// Workgroups of the backward pass: as many as run at once; and the groups of
+// one.
+int back_groups_of(int C) {
+#define F(G, V) (back_threads(G) / G)
+    CF_NORM_SHAPES(F)
+#undef F
+}
+int64_t back_grid(int64_t rows, int C) {
+    const int64_t ng = back_groups_of(C), need = (rows + ng - 1) / ng;
+    const int64_t most = (int64_t)device_cu_count() * (C <= 4096 ? 2 : 1);
+    return need < 1 ? 1 : need < most ? need : most;
+}
+
+int lanes_of(int C) {
+#define F(G, V) (G)
+    CF_NORM_SHAPES(F)
+#undef F
+}
+
+template <typename T, bool CK>
+hipError_t backward_type(const NormBackArgs &a, unsigned grid, hipStream_t st) {
+    const int C = a.C;
+#define F(G, V)                                                                                                        \
+    (norm_backward_kernel<T, CK, G, V><<<dim3(grid), dim3(back_threads(G)), 0, st>>>(a), hipGetLastError())
+    CF_NORM_SHAPES(F)
+#undef F
+}
+
+}  // namespace
+
+// The forward grid stays below 2^32 threads.
+bool norm_fits(int64_t rows, int C) { return C <= NORM_MAX_C && ((double)rows + 256) * lanes_of(C) < 4294967296.0; }
+
+hipError_t launch_norm_forward(const void *x, int64_t ldx, void *y, int64_t ldy, const float *weight,
+                               const float *bias, float *stats, const Ckpt &ckpt, int64_t rows, int C, float eps,
+                               int bf16, hipStream_t st) {
+    NormArgs a;
+    a.x = (const uint16_t *)x;
+    a.y = (uint16_t *)y;
+    a.w = weight;
+    a.b = bias;
+    a.stats = (float2 *)stats;
+    a.q = ckpt.q;
+    a.scale = ckpt.scale;
+    a.ldx = ldx;
+    a.ldy = ldy;
+    a.rows = rows;
+    a.C = C;
+    a.blocks = blocks_of(C);
+    a.eps = eps;
+    return bf16 ? forward_type<BF16>(a, st) : forward_type<F16>(a, st);
+}
+
+size_t norm_backward_workspace_bytes(int64_t rows, int C) {
+    const int64_t grid = back_grid(rows, C);
+    return grid > 1 ? (size_t)grid * 2 * C * sizeof(float) : 0;
+}
+
+hipError_t launch_norm_backward(const NormBackward &n, int64_t rows, int C, int bf16, void *ws, hipStream_t st) {
+    const unsigned grid = (unsigned)back_grid(rows, C);
+    NormBackArgs a;
+    a.dy = (const uint16_t *)n.dy;
+    a.x = (const uint16_t *)n.x;
+    a.q = n.ckpt.q;
+    a.scale = n.ckpt.scale;
+    a.stats = (const float2 *)n.stats;
+    a.w = n.weight;
+    a.dx = (uint16_t *)n.dx;
+    a.dw = !n.dweight || grid == 1 ? n.dweight : (float *)ws;
+    a.db = grid == 1 ? n.dbias : nullptr;
+    a.lddy = n.lddy;
+    a.ldx = n.ldx;
+    a.lddx = n.lddx;
+    a.rows = rows;
+    a.C = C;
+    a.blocks = blocks_of(C);
+    hipError_t e;
+    if (n.ckpt.q)
+        e = bf16 ? backward_type<BF16, true>(a, grid, st) : backward_type<F16, true>(a, grid, st);
+    else
+        e = bf16 ? backward_type<BF16, false>(a, grid, st) : backward_type<F16, false>(a, grid, st);
+    if (e != hipSuccess || !n.dweight || grid == 1)
+        return e;
+    norm_reduce_kernel<<<dim3((2 * C + 15) / 16), dim3(1024), 0, st>>>((const float *)ws, n.dweight, n.dbias,
+                                                                       (int)grid, C);
+    return hipGetLastError();
+}
+
+}  // namespace cf

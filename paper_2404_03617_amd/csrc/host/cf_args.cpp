@@ -183,6 +183,67 @@ PyObject *collect(PyObject *, PyObject *args) {
     return PyBytes_FromStringAndSize(reinterpret_cast<const char *>(out), (Py_ssize_t)(8 * spec->size()));
 }
 
+// Dtype codes of rows() and flat(); the first three as in the C ABI.
+bool code_of(at::ScalarType t, int *code) {
+    switch (t) {
+    case at::kHalf: *code = 0; return true;
+    case at::kBFloat16: *code = 1; return true;
+    case at::kFloat: *code = 2; return true;
+    case at::kChar: *code = 3; return true;
+    case at::kLong: *code = 4; return true;
+    default: return false;
+    }
+}
+
+// rows(x) -> (address, rows, C, row stride, dtype code) of a GPU tensor [.., C]
+// whose last dimension is contiguous and whose others are rows at one stride,
+// else None
+PyObject *rows(PyObject *, PyObject *o) {
+    if (!THPVariable_CheckExact(o))
+        Py_RETURN_NONE;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    int code = 0;
+    if (!t.defined() || t.layout() != at::kStrided || !t.is_cuda() || t.is_conj() || t.is_neg() || t.dim() < 1 ||
+        !code_of(t.scalar_type(), &code))
+        Py_RETURN_NONE;
+    const int64_t last = t.dim() - 1;
+    const long long C = t.size(last);
+    if (C > 1 && t.stride(last) != 1)
+        Py_RETURN_NONE;
+    long long n = 1, ld = -1;  // rows so far and their stride
+    for (int64_t d = last - 1; d >= 0; d--) {
+        if (t.size(d) != 1) {
+            if (ld < 0)
+                ld = t.stride(d);
+            else if (t.stride(d) != ld * n)
+                Py_RETURN_NONE;
+        }
+        n *= t.size(d);
+        if (n == 0)
+            break;
+    }
+    return Py_BuildValue("KLLLi", (unsigned long long)(uintptr_t)t.data_ptr(), n, C, ld < 0 || n == 0 ? C : ld, code);
+}
+
+// flat(x, t, code, rows, last) -> address of a contiguous tensor t of that
+// dtype on x's device with rows * last elements and a last dimension of `last`
+// (last = 0: `rows` elements in any shape), else None
+PyObject *flat(PyObject *, PyObject *args) {
+    PyObject *xo, *to;
+    int code, have;
+    long long n, last;
+    if (!PyArg_ParseTuple(args, "OOiLL", &xo, &to, &code, &n, &last))
+        return nullptr;
+    if (!THPVariable_CheckExact(xo) || !THPVariable_CheckExact(to))
+        Py_RETURN_NONE;
+    const at::Tensor &x = THPVariable_Unpack(xo), &t = THPVariable_Unpack(to);
+    if (!plain(t) || !code_of(t.scalar_type(), &have) || have != code || t.device() != x.device())
+        Py_RETURN_NONE;
+    if (last ? t.numel() != n * last || t.dim() < 1 || t.size(t.dim() - 1) != last : t.numel() != n)
+        Py_RETURN_NONE;
+    return PyLong_FromUnsignedLongLong((unsigned long long)(uintptr_t)t.data_ptr());
+}
+
 // C++ exceptions (a tensor without storage, say) end here: the binding's own
 // checks take over
 template <PyObject *(*F)(PyObject *, PyObject *)>
@@ -200,6 +261,8 @@ PyMethodDef methods[] = {{"spec", guarded<make_spec>, METH_O, nullptr},
                          {"like", guarded<like>, METH_VARARGS, nullptr},
                          {"shape", guarded<shape>, METH_VARARGS, nullptr},
                          {"collect", guarded<collect>, METH_VARARGS, nullptr},
+                         {"rows", guarded<rows>, METH_O, nullptr},
+                         {"flat", guarded<flat>, METH_VARARGS, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_cf_args", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

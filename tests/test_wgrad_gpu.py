@@ -1,0 +1,180 @@
+"""Weight gradients from checkpoints against the product in 64 bits.
+
+Tolerances.  A factor from the checkpoint is rounded once to the 16-bit type
+(ROUND of its value; a normalised one errs by 8 fp32 roundings of its parts
+before), products of 16-bit numbers are exact in fp32, their sum of R terms
+errs by at most R/16 + 64 roundings of the sum of magnitudes, and the result is
+rounded once."""
+import pytest
+import torch
+
+import paper_2404_03617_amd as cf
+from paper_2404_03617_amd import training
+
+from _rows import DT, F32, ROUND, TINY, assert_within, dequantise, quantise, randn, rows_in
+
+pytestmark = pytest.mark.gpu
+
+# rows, K, C: one of each, ragged, tiles of every size, rows split over workgroups
+SHAPES = [(1, 1, 1), (2, 3, 5), (63, 16, 64), (64, 64, 64), (65, 65, 63), (130, 100, 72), (1, 300, 200),
+          (257, 128, 128), (100, 129, 257), (49, 2048, 512), (1000, 1000, 512), (5000, 24, 40), (20000, 64, 64),
+          (3001, 256, 64), (700, 8, 1000), (300, 2816, 2304), (513, 4096, 4096), (40, 4100, 4111)]
+
+
+def case(seed, rows, K, C, dt, norm):
+    x = (randn(seed, (rows, C)) * torch.exp(0.5 * randn(seed + 1, (C,))) + 0.3).to(dt)
+    q, scale, _ = quantise(x)
+    dy = randn(seed + 2, (rows, K), dt, 0.05)
+    kept = dequantise(q, scale)
+    stats = w = b = None
+    spread = torch.zeros(())
+    if norm:
+        xd = x.double()
+        mean = xd.mean(1)
+        stats = torch.stack([mean, ((xd - mean[:, None]).square().mean(1) + 1e-6).rsqrt()], 1).float()
+        w, b = 1 + 0.3 * randn(seed + 3, (C,)), 0.2 * randn(seed + 4, (C,))
+        mean, rstd = stats[:, :1].double(), stats[:, 1:].double()
+        spread = 8 * F32 * (kept.abs() + mean.abs() + 128 * scale.double().repeat_interleave(64, 1)[:, :C]) * rstd
+        kept = (kept - mean) * rstd
+    return dy, q, scale, stats, w, b, kept, spread
+
+
+def reference(dy, kept, w, b, spread, dt, rows):
+    d = dy.double()
+    s, db = d.t() @ kept, d.sum(0)
+    mag = d.abs().t() @ kept.abs()
+    err = mag * (ROUND[dt] + F32 * (rows / 16 + 64)) + d.abs().t() @ (spread * torch.ones_like(kept) + TINY[dt])
+    edb = F32 * (rows / 16 + 64) * d.abs().sum(0) + 1e-30
+    if w is not None:
+        s, err = s * w.double(), err * w.double().abs()
+        s, err = s + db[:, None] * b.double(), err + edb[:, None] * b.double().abs()
+    return s, err + ROUND[dt] * (s.abs() + err) + TINY[dt], db, edb
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("norm", [False, True])
+@pytest.mark.parametrize("rows,K,C", SHAPES)
+def test_weight_grad(rows, K, C, norm, dtype):
+    dt = DT[dtype]
+    dy, q, scale, stats, w, b, kept, spread = case(rows + K + C, rows, K, C, dt, norm)
+    dw, tw, db, tb = reference(dy, kept, w, b, spread, dt, rows)
+    ck = cf.Checkpoint(q.cuda(), scale.cuda(), dt)
+    more = dict(stats=stats.cuda(), weight=w.cuda(), bias=b.cuda()) if norm else {}
+    for kind in ("dense", "slice"):
+        got = cf.linear_weight_grad(rows_in(kind, dy), ck, **more)
+        assert_within(got[0], dw, tw, "%s dW" % kind)
+        assert_within(got[1], db, tb, "%s db" % kind)
+    again = cf.linear_weight_grad(dy.cuda(), ck, **more)
+    assert torch.equal(again[0], got[0]) and torch.equal(again[1], got[1])
+
+
+@pytest.mark.parametrize("which", ["weight", "bias", "neither"])
+def test_norm_without_weight_or_bias(which):
+    rows, K, C, dt = 900, 40, 100, torch.bfloat16
+    dy, q, scale, stats, w, b, kept, spread = case(3, rows, K, C, dt, True)
+    w = w if which == "weight" else None
+    b = b if which == "bias" else None
+    dw, tw, db, tb = reference(dy, kept, torch.ones(C) if w is None else w, torch.zeros(C) if b is None else b, spread,
+                               dt, rows)
+    got = cf.linear_weight_grad(dy.cuda(), cf.Checkpoint(q.cuda(), scale.cuda(), dt), stats.cuda(),
+                                None if w is None else w.cuda(), None if b is None else b.cuda())
+    assert_within(got[0], dw, tw, "dW")
+    assert_within(got[1], db, tb, "db")
+
+
+def test_layout_with_distinct_values():
+    """Whole numbers that fp32 sums exactly, every entry of dW another: a
+    misplaced row, column or tile shows as a wrong number."""
+    rows, K, C = 70, 137, 150
+    q = torch.zeros(rows, C, dtype=torch.int8)
+    for r in range(64):
+        q[r] = (torch.arange(C) >> (r % 8)) & 1
+    scale = torch.ones(rows, 3)
+    dy = torch.zeros(rows, K)
+    for r in range(8):
+        dy[r] = 2.0**r * (1 + torch.arange(K) % 4)
+    dy = dy.half()
+    got = cf.linear_weight_grad(dy.cuda(), cf.Checkpoint(q.cuda(), scale.cuda(), torch.float16))
+    assert torch.equal(got[0].cpu(), (dy.double().t() @ q.double()).half())
+    assert torch.equal(got[1].cpu().double(), dy.double().sum(0))
+
+
+def test_broadcast_rows_nan_and_no_rows():
+    rows, K, C = 300, 33, 70
+    dy, q, scale, *_ = case(8, rows, K, C, torch.float16, False)
+    one = dy[:1].cuda()
+    ck = cf.Checkpoint(q.cuda(), scale.cuda(), torch.float16)
+    a = cf.linear_weight_grad(one.expand(rows, K), ck)
+    b = cf.linear_weight_grad(one.expand(rows, K).contiguous(), ck)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    bad = scale.clone()
+    bad[200, 1] = float("nan")  # a block that held infinities
+    n = cf.linear_weight_grad(dy.cuda(), cf.Checkpoint(q.cuda(), bad.cuda(), torch.float16))[0]
+    assert bool(torch.isnan(n[:, 64:]).all()) and bool(torch.isfinite(n[:, :64]).all())
+    e = cf.Checkpoint(q[:0].cuda(), scale[:0].cuda(), torch.float16)
+    dw, db = cf.linear_weight_grad(dy[:0].cuda(), e)
+    assert torch.equal(dw, torch.zeros_like(dw)) and torch.equal(db, torch.zeros_like(db)) and dw.shape == (K, C)
+
+
+def test_offsets_past_32_bits():
+    """dy rows 2^15 elements apart; checkpoint rows past 2^31 bytes."""
+    rows, ld, K = 70000, 32768, 40
+    buf = torch.zeros(rows * ld, dtype=torch.bfloat16, device="cuda").view(rows, ld)
+    dy = buf[:, 7:7 + K]
+    q = torch.zeros(rows, ld, dtype=torch.int8, device="cuda")
+    scale = torch.ones(rows, ld // 64, device="cuda")
+    some = torch.tensor([0, 65535, 65537, 69999]).cuda()
+    vals = randn(5, (4, K), torch.bfloat16)
+    dy[some] = vals.cuda()
+    g = torch.Generator().manual_seed(1)
+    qs = torch.randint(-127, 128, (4, ld), generator=g, dtype=torch.int8)
+    q[some] = qs.cuda()
+    got = cf.linear_weight_grad(dy, cf.Checkpoint(q, scale, torch.bfloat16))
+    want = vals.double().t() @ qs.double()
+    mag = vals.double().abs().t() @ qs.double().abs()
+    assert_within(got[0], want, 2.0**-8 * want.abs() + 64 * F32 * mag + 1e-30, "dW")
+    assert_within(got[1], vals.double().sum(0), 64 * F32 * vals.double().abs().sum(0), "db")
+
+
+def test_workspace_stream_and_graph():
+    rows, K, C, dt = 9000, 72, 100, torch.float16
+    dy, q, scale, stats, w, b, *_ = case(11, rows, K, C, dt, True)
+    d, s, w, b = dy.cuda(), stats.cuda(), w.cuda(), b.cuda()
+    ck = cf.Checkpoint(q.cuda(), scale.cuda(), dt)
+    need = training.linear_weight_grad_workspace_bytes(rows, K, C)
+    assert need > 0
+    ws = torch.full((need + 64,), 0xA5, dtype=torch.uint8, device="cuda")
+    want = [t.clone() for t in cf.linear_weight_grad(d, ck, s, w, b, ws=ws[:need])]
+    assert bool((ws[need:] == 0xA5).all())
+    with pytest.raises(ValueError):
+        cf.linear_weight_grad(d, ck, s, w, b, ws=ws[:need - 1])
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = cf.linear_weight_grad(d, ck, s, w, b, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(u, v) for u, v in zip(got, want))
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        rec = cf.linear_weight_grad(d, ck, s, w, b)
+    first, other = d.clone(), randn(2, (rows, K), dt).cuda()
+    for v in (first, other, first):
+        d.copy_(v)
+        g.replay()
+        eager = cf.linear_weight_grad(d, ck, s, w, b)
+        torch.cuda.synchronize()
+        assert all(torch.equal(u, r) for u, r in zip(rec, eager))
+
+
+def test_refusals():
+    dy = torch.zeros(10, 8, dtype=torch.float16, device="cuda")
+    ck = cf.checkpoint_pack(torch.zeros(10, 70, dtype=torch.float16, device="cuda"))
+    w = torch.ones(70, device="cuda")
+    for args in ((dy[:9], ck), (dy.float(), ck), (dy, ck, torch.ones(9, 2, device="cuda")),
+                 (dy, ck, torch.ones(10, 2, device="cuda"), w[:69])):
+        with pytest.raises(ValueError):
+            cf.linear_weight_grad(*args)
+    with pytest.raises(TypeError):
+        cf.linear_weight_grad(dy, dy)
+    with pytest.raises(cf.CFError) as e:
+        cf.linear_weight_grad(dy, ck, None, w)
+    assert e.value.status == cf.CF_ERR_INVALID and "stats" in str(e.value)

@@ -74,7 +74,7 @@ __device__ __forceinline__ void keep(const Ckpt &k, const At &p, const ActArgs &
     const Quant z = quant_of(lanes<Max, 8>(amax8(x)));
     if (p.n <= 0)
         return;
-    store8b(k.q + p.r * a.C + p.c, quant8(x, z.inv), p.n);
+    store8b(k.q + p.r * a.C, p.c, a.C, quant8(x, z.inv));
     if ((threadIdx.x & 7) == 0)
         k.scale[p.r * a.blocks + p.c / CKPT_BLOCK] = z.scale;
 }
@@ -85,7 +85,7 @@ __global__ __launch_bounds__(256) void act_forward_kernel(ActArgs a) {
     if (i >= a.n)  // whole groups of 8 lanes
         return;
     const At p = place(a, i);
-    const u32x4 raw = p.n > 0 ? load8(a.in + p.r * a.ldi + p.c, p.n) : u32x4{0u, 0u, 0u, 0u};
+    const u32x4 raw = load8(a.in + p.r * a.ldi, p.c, a.C);
     float x[8];
     unpack8<T>(raw, x);
     if (a.u.q)
@@ -97,7 +97,7 @@ __global__ __launch_bounds__(256) void act_forward_kernel(ActArgs a) {
         x[e] = act_of<ACT>(x[e]);
     const u32x4 y = pack8<T>(x);
     if (a.out && p.n > 0)
-        store8(a.out + p.r * a.ldo + p.c, y, p.n);
+        store8(a.out + p.r * a.ldo, p.c, a.C, y);
     if (a.h.q) {
         unpack8<T>(y, x);  // the checkpoint is of the values the next layer reads
         keep(a.h, p, a, x);
@@ -112,18 +112,18 @@ __global__ __launch_bounds__(256) void act_backward_kernel(ActArgs a) {
     const At p = place(a, i);
     if (p.n <= 0)
         return;
-    const u32x2 q = load8b(a.u.q + p.r * a.C + p.c, p.n);
+    const u32x2 q = load8b(a.u.q + p.r * a.C, p.c, a.C);
     const float scale = a.u.scale[p.r * a.blocks + p.c / CKPT_BLOCK];
     float u[8];
     dequant8(q, scale, u);
     if (a.in) {
         float d[8];
-        unpack8<T>(load8(a.in + p.r * a.ldi + p.c, p.n), d);
+        unpack8<T>(load8(a.in + p.r * a.ldi, p.c, a.C), d);
 #pragma unroll
         for (int e = 0; e < 8; e++)
             u[e] = d[e] * act_slope<ACT>(u[e]);
     }
-    store8(a.out + p.r * a.ldo + p.c, pack8<T>(u), p.n);
+    store8(a.out + p.r * a.ldo, p.c, a.C, pack8<T>(u));
 }
 
 ActArgs args_of(const void *in, int64_t ldi, void *out, int64_t ldo, const Ckpt &u, const Ckpt &h, int64_t rows,

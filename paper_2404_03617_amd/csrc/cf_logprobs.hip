@@ -34,13 +34,14 @@ constexpr float LOG2E = 1.44269504f, LN2 = 0.693147181f, LOWEST = -3.40282347e38
 // exponents below this give 0; also stands in for -inf, whose product with 0 is not 0
 constexpr float FLOOR2 = -1000.0f;
 
-// 16 bytes of logits: VE values, of which n are in the row (the rest -inf)
+// 16 bytes of logits: VE values, of which n are before `end` (the rest -inf).
+// `end` is the row's end or, in a chunk, a multiple of 8.
 template <typename T>
 struct Z16 {
     typedef uint16_t elem;
     static constexpr int VE = 8;
     typedef u32x4 raw;
-    static __device__ __forceinline__ raw load(const elem *p, int n) { return load8(p, n); }
+    static __device__ __forceinline__ raw load(const elem *row, int i, int end) { return load8(row, i, end); }
     static __device__ __forceinline__ void values(const raw &r, int n, float *z) {
         unpack8<T>(r, z);
         if (n < 8)
@@ -49,7 +50,9 @@ struct Z16 {
                 z[i] = i < n ? z[i] : -INFINITY;
     }
     static __device__ __forceinline__ float one(const elem *p) { return T::lo(*p); }
-    static __device__ __forceinline__ void store(elem *p, const float *z, int n) { store8(p, pack8<T>(z), n); }
+    static __device__ __forceinline__ void store(elem *row, int i, int end, const float *z) {
+        store8(row, i, end, pack8<T>(z));
+    }
 };
 struct Z32 {
     typedef float elem;
@@ -58,7 +61,9 @@ struct Z32 {
     struct __attribute__((packed, aligned(4))) Any {
         float4v v;
     };
-    static __device__ __forceinline__ raw load(const elem *p, int n) {
+    static __device__ __forceinline__ raw load(const elem *row, int at, int end) {
+        const elem *const p = row + at;
+        const int n = end - at;
         if (n >= 4)
             return reinterpret_cast<const Any *>(p)->v;
         raw r = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -74,7 +79,9 @@ struct Z32 {
             z[i] = i < n ? r[i] : -INFINITY;
     }
     static __device__ __forceinline__ float one(const elem *p) { return *p; }
-    static __device__ __forceinline__ void store(elem *p, const float *z, int n) {
+    static __device__ __forceinline__ void store(elem *row, int at, int end, const float *z) {
+        elem *const p = row + at;
+        const int n = end - at;
         if (n >= 4) {
             reinterpret_cast<Any *>(p)->v = float4v{z[0], z[1], z[2], z[3]};
             return;
@@ -211,7 +218,7 @@ __device__ __forceinline__ void each(const typename Z::elem *z, int begin, int e
     for (int i = begin + (int)threadIdx.x * Z::VE; i < end; i += TH * Z::VE) {
         float v[Z::VE];
         const int n = end - i;
-        Z::values(Z::load(z + i, n), n, v);
+        Z::values(Z::load(z, i, end), n, v);
 #pragma unroll
         for (int e = 0; e < Z::VE; e++)
             if (e < n)
@@ -290,7 +297,7 @@ __device__ void find_top(const typename Z::elem *z, int begin, int end, int top,
                     float v[Z::VE];
                     unsigned eq = 0;
                     if (i < end) {
-                        Z::values(Z::load(z + i, end - i), end - i, v);
+                        Z::values(Z::load(z, i, end), end - i, v);
 #pragma unroll
                         for (int e = 0; e < Z::VE; e++)
                             eq |= (unsigned)(v[e] == bound && e < end - i) << e;
@@ -380,7 +387,7 @@ __global__ __launch_bounds__(TH) void log_probs_kernel(Args a) {
 #pragma unroll
         for (int v = 0; v < NV; v++)
             if (i + v * STEP < end)
-                next[v] = Z::load(z + i + v * STEP, end - (i + v * STEP));
+                next[v] = Z::load(z, i + v * STEP, end);
     };
     int i = begin + tid * Z::VE;
     fetch(i);
@@ -510,7 +517,7 @@ __device__ __forceinline__ void grad8(const BackArgs &k, const RowGrad &r, const
                                       typename Z::elem *dz, int i) {
     const int n = k.V - i;
     float x[Z::VE];
-    Z::values(Z::load(z + i, n), n, x);
+    Z::values(Z::load(z, i, k.V), n, x);
 #pragma unroll
     for (int e = 0; e < Z::VE; e++) {
         const float l = fmaxf(fmaf(x[e] - r.ref, LOG2E, r.off), FLOOR2);
@@ -521,7 +528,7 @@ __device__ __forceinline__ void grad8(const BackArgs &k, const RowGrad &r, const
         for (int e = 0; e < Z::VE; e++)
             if (r.token == i + e)
                 x[e] += r.g;
-    Z::store(dz + i, x, n);
+    Z::store(dz, i, k.V, x);
 }
 
 // Short rows: a thread takes a vector of any row.

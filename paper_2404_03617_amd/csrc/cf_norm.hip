@@ -81,7 +81,7 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void norm_forward_kernel(NormArg
         for (int v = 0; v < V; v++) {
             const int64_t r = r0 + u * NG;
             const int c = (gl + v * G) * 8;
-            raw[u][v] = r < a.rows ? load8(a.x + r * a.ldx + c, a.C - c) : u32x4{0u, 0u, 0u, 0u};
+            raw[u][v] = r < a.rows ? load8(a.x + r * a.ldx, c, a.C) : u32x4{0u, 0u, 0u, 0u};
         }
     float x[U][V * 8], s[U];
 #pragma unroll
@@ -104,7 +104,7 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void norm_forward_kernel(NormArg
                 const int c = (gl + v * G) * 8;
                 const Quant z = quant_of(lanes<Max, 8>(amax8(&x[u][8 * v])));
                 if (r < a.rows && c < a.C) {
-                    store8b(a.q + r * a.C + c, quant8(&x[u][8 * v], z.inv), a.C - c);
+                    store8b(a.q + r * a.C, c, a.C, quant8(&x[u][8 * v], z.inv));
                     if ((threadIdx.x & 7) == 0)
                         a.scale[r * a.blocks + c / CKPT_BLOCK] = z.scale;
                 }
@@ -140,11 +140,8 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void norm_forward_kernel(NormArg
     for (int v = 0; v < V; v++) {
         const int c = (gl + v * G) * 8, n = a.C - c;
         float w[8], b[8];
-#pragma unroll
-        for (int i = 0; i < 8; i++) {
-            w[i] = a.w && i < n ? a.w[c + i] : 1.0f;
-            b[i] = a.b && i < n ? a.b[c + i] : 0.0f;
-        }
+        load8f(a.w ? a.w + c : nullptr, n, 1.0f, w);
+        load8f(a.b ? a.b + c : nullptr, n, 0.0f, b);
 #pragma unroll
         for (int u = 0; u < U; u++) {
             const int64_t r = r0 + u * NG;
@@ -153,7 +150,7 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void norm_forward_kernel(NormArg
             for (int i = 0; i < 8; i++)
                 y[i] = fmaf(x[u][8 * v + i] * rstd[u], w[i], b[i]);
             if (r < a.rows && n > 0)
-                store8(a.y + r * a.ldy + c, pack8<T>(y), n);
+                store8(a.y + r * a.ldy, c, a.C, pack8<T>(y));
         }
     }
 }
@@ -175,23 +172,48 @@ struct NormBackArgs {
 // theirs before they are written, so few large workgroups write little.
 constexpr int back_threads(int G) { return G > 512 ? G : 512; }
 
+constexpr int RED_BYTES = 2 * 16 * 2 * sizeof(float);
+
 // CK: x from its checkpoint.  Persistent: a group takes rows a grid apart, the
 // next row's loads in flight while the current one is worked on.
 template <typename T, bool CK, int G, int V>
-__global__ __launch_bounds__(back_threads(G)) void norm_backward_kernel(NormBackArgs a) {
+__global__ __launch_bounds__(back_threads(G), 4) void norm_backward_kernel(NormBackArgs a) {
     constexpr int TH = back_threads(G), NG = TH / G, WAVES = TH / 64;
-    __shared__ float red[2][16][2];
+    // the waves' sums of a row, then the weight while rows are worked on and
+    // what the waves add up after that
+    extern __shared__ float4 dynamic[];
+    float(*const red)[16][2] = reinterpret_cast<float(*)[16][2]>(dynamic);
+    float4 *const space = dynamic + RED_BYTES / 16;
     const int grp = threadIdx.x / G, gl = threadIdx.x % G, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const float fc = (float)a.C, inv_c = 1.0f / fc;
-    float w[V * 8], dw[V * 8], db[V * 8];
+    float w[8], dw[V * 8], db[V * 8];
 #pragma unroll
-    for (int v = 0; v < V; v++)
-#pragma unroll
-        for (int i = 0; i < 8; i++) {
-            const int c = (gl + v * G) * 8 + i;
-            w[8 * v + i] = a.w && c < a.C ? a.w[c] : 1.0f;
-            dw[8 * v + i] = db[8 * v + i] = 0.0f;
+    for (int v = 0; v < V; v++) {
+        const int c = (gl + v * G) * 8;
+        load8f(a.w ? a.w + c : nullptr, a.C - c, 1.0f, w);
+        if (V > 1 && grp == 0) {
+            space[(2 * v) * G + gl] = make_float4(w[0], w[1], w[2], w[3]);
+            space[(2 * v + 1) * G + gl] = make_float4(w[4], w[5], w[6], w[7]);
         }
+#pragma unroll
+        for (int i = 0; i < 8; i++)
+            dw[8 * v + i] = db[8 * v + i] = 0.0f;
+    }
+    if (V > 1)
+        __syncthreads();
+    // the weight of a lane's vector: from its registers, or (two vectors) from
+    // LDS, as the registers hold the sums of both
+    auto weight = [&](int v, float *f) {
+        if constexpr (V > 1) {
+            const float4 lo = space[(2 * v) * G + gl], hi = space[(2 * v + 1) * G + gl];
+            f[0] = lo.x, f[1] = lo.y, f[2] = lo.z, f[3] = lo.w;
+            f[4] = hi.x, f[5] = hi.y, f[6] = hi.z, f[7] = hi.w;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; i++)
+                f[i] = w[i];
+        }
+    };
     struct Row {
         u32x4 dy[V], x[V];
         float scale[V];
@@ -208,14 +230,14 @@ __global__ __launch_bounds__(back_threads(G)) void norm_backward_kernel(NormBack
             t.dy[v] = t.x[v] = u32x4{0u, 0u, 0u, 0u};
             t.scale[v] = 0.0f;
             if (r < a.rows && c < a.C) {
-                t.dy[v] = load8(a.dy + r * a.lddy + c, a.C - c);
+                t.dy[v] = load8(a.dy + r * a.lddy, c, a.C);
                 if constexpr (CK) {
-                    const u32x2 q = load8b(a.q + r * a.C + c, a.C - c);
+                    const u32x2 q = load8b(a.q + r * a.C, c, a.C);
                     t.x[v].x = q.x;
                     t.x[v].y = q.y;
                     t.scale[v] = a.scale[r * a.blocks + c / CKPT_BLOCK];
                 } else {
-                    t.x[v] = load8(a.x + r * a.ldx + c, a.C - c);
+                    t.x[v] = load8(a.x + r * a.ldx, c, a.C);
                 }
             }
         }
@@ -241,12 +263,13 @@ __global__ __launch_bounds__(back_threads(G)) void norm_backward_kernel(NormBack
         float s[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int v = 0; v < V; v++) {
-            float dy[8], x[8];
+            float dy[8], x[8], f[8];
             values(v, dy, x);
+            weight(v, f);
 #pragma unroll
             for (int i = 0; i < 8; i++) {
                 const int j = 8 * v + i;
-                const float xh = (x[i] - t.st.x) * t.st.y, g = dy[i] * w[j];
+                const float xh = (x[i] - t.st.x) * t.st.y, g = dy[i] * f[i];
                 dw[j] = fmaf(dy[i], xh, dw[j]);
                 db[j] += dy[i];
                 s[0] += g;
@@ -258,15 +281,16 @@ __global__ __launch_bounds__(back_threads(G)) void norm_backward_kernel(NormBack
 #pragma unroll
         for (int v = 0; v < V; v++) {
             const int c = (gl + v * G) * 8;
-            float dy[8], x[8], dx[8];
+            float dy[8], x[8], dx[8], f[8];
             values(v, dy, x);
+            weight(v, f);
 #pragma unroll
             for (int i = 0; i < 8; i++) {
                 const float xh = (x[i] - t.st.x) * t.st.y;
-                dx[i] = t.st.y * (fmaf(dy[i], w[8 * v + i], -m0) - xh * m1);
+                dx[i] = t.st.y * (fmaf(dy[i], f[i], -m0) - xh * m1);
             }
             if (r < a.rows && c < a.C)
-                store8(a.dx + r * a.lddx + c, pack8<T>(dx), a.C - c);
+                store8(a.dx + r * a.lddx, c, a.C, pack8<T>(dx));
         }
     }
     if (!a.dw)
@@ -275,7 +299,7 @@ __global__ __launch_bounds__(back_threads(G)) void norm_backward_kernel(NormBack
     // of each lane at a time.
     float *const pw = a.db ? a.dw : a.dw + (int64_t)blockIdx.x * 2 * a.C;
     float *const pb = a.db ? a.db : pw + a.C;
-    __shared__ float4 part[2][WAVES][64];
+    float4(*const part)[WAVES][64] = reinterpret_cast<float4(*)[WAVES][64]>(space);
     constexpr int SUB = G > 64 ? G / 64 : 1;  // waves that share a row
 #pragma unroll
     for (int j = 0; j < V * 8; j += 4) {
@@ -315,26 +339,32 @@ __global__ __launch_bounds__(back_threads(G)) void norm_backward_kernel(NormBack
     }
 }
 
-// Sum of `n` partials [n][2][C] into dw [C] and db [C]: 16 columns a
-// workgroup, 64 threads share a column and add every 64th partial.
+// Sum of `n` partials [n][2][C] into dw [C] and db [C]: 32 columns a
+// workgroup (a cache line), 32 threads share a column and add every 32nd
+// partial, eight loads at a time.
 __global__ __launch_bounds__(1024) void norm_reduce_kernel(const float *part, float *dw, float *db, int n, int C) {
-    __shared__ float s[64][17];
-    const int col = threadIdx.x & 15, at = threadIdx.x >> 4;
-    const int64_t i = (int64_t)blockIdx.x * 16 + col;
+    __shared__ float s[32][33];
+    const int col = threadIdx.x & 31, at = threadIdx.x >> 5;
+    const int64_t i = (int64_t)blockIdx.x * 32 + col, pitch = 2 * (int64_t)C;
     float f = 0.0f;
-    if (i < 2 * (int64_t)C)
-        for (int k = at; k < n; k += 64)
-            f += part[(int64_t)k * 2 * C + i];
+    if (i < pitch) {
+        int k = at;
+        for (; k + 7 * 32 < n; k += 8 * 32) {
+            float t[8];
+#pragma unroll
+            for (int u = 0; u < 8; u++)
+                t[u] = part[(k + u * 32) * pitch + i];
+            f += ((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7]));
+        }
+        for (; k < n; k += 32)
+            f += part[k * pitch + i];
+    }
     s[at][col] = f;
     __syncthreads();
-#pragma unroll
-    for (int h = 32; h > 0; h >>= 1) {
-        if (at < h)
-            s[at][col] += s[at + h][col];
-        __syncthreads();
-    }
-    if (at == 0 && i < 2 * (int64_t)C)
-        (i < C ? dw[i] : db[i - C]) = s[0][col];
+    f = lanes<Add, 32>(s[col][at]);  // transposed: 32 lanes hold one column
+    const int64_t o = (int64_t)blockIdx.x * 32 + at;
+    if (col == 0 && o < pitch)
+        (o < C ? dw[o] : db[o - C]) = f;
 }
 
 // Lanes and vectors of a row of C channels.
@@ -390,11 +420,23 @@ int lanes_of(int C) {
 #undef F
 }
 
+template <typename T, bool CK, int G, int V>
+hipError_t backward_shape(const NormBackArgs &a, unsigned grid, hipStream_t st) {
+    constexpr int SUMS = 2 * back_threads(G) * 16, WEIGHT = V > 1 ? G * V * 32 : 0;
+    constexpr int LDS = RED_BYTES + (SUMS > WEIGHT ? SUMS : WEIGHT);
+    if (LDS > 64 * 1024) {
+        const hipError_t e = allow_full_lds((const void *)norm_backward_kernel<T, CK, G, V>);
+        if (e != hipSuccess)
+            return e;
+    }
+    norm_backward_kernel<T, CK, G, V><<<dim3(grid), dim3(back_threads(G)), LDS, st>>>(a);
+    return hipGetLastError();
+}
+
 template <typename T, bool CK>
 hipError_t backward_type(const NormBackArgs &a, unsigned grid, hipStream_t st) {
     const int C = a.C;
-#define F(G, V)                                                                                                        \
-    (norm_backward_kernel<T, CK, G, V><<<dim3(grid), dim3(back_threads(G)), 0, st>>>(a), hipGetLastError())
+#define F(G, V) (backward_shape<T, CK, G, V>(a, grid, st))
     CF_NORM_SHAPES(F)
 #undef F
 }
@@ -454,7 +496,7 @@ hipError_t launch_norm_backward(const NormBackward &n, int64_t rows, int C, int 
         e = bf16 ? backward_type<BF16, false>(a, grid, st) : backward_type<F16, false>(a, grid, st);
     if (e != hipSuccess || !n.dweight || grid == 1)
         return e;
-    norm_reduce_kernel<<<dim3((2 * C + 15) / 16), dim3(1024), 0, st>>>((const float *)ws, n.dweight, n.dbias,
+    norm_reduce_kernel<<<dim3((2 * C + 31) / 32), dim3(1024), 0, st>>>((const float *)ws, n.dweight, n.dbias,
                                                                        (int)grid, C);
     return hipGetLastError();
 }

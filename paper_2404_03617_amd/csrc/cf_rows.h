@@ -26,50 +26,112 @@ struct __attribute__((packed, aligned(1))) Any8 {
     u32x2 v;
 };
 
-// 8 elements of p, zeros from element n on (n < 8 at the end of a row only).
-__device__ __forceinline__ u32x4 load8(const uint16_t *p, int n) {
+struct __attribute__((packed, aligned(2))) Any4h {
+    uint32_t v;
+};
+struct __attribute__((packed, aligned(2))) Any8h {
+    u32x2 v;
+};
+
+// the last n of 16 (8) bytes' values, of 16 (8) bits each, moved to the front
+__device__ __forceinline__ u32x4 from_end(const u32x4 &r, int n) {
+    const int s = 16 * (8 - n);  // 16 .. 112
+    const uint64_t lo = __builtin_bit_cast(uint64_t, u32x2{r[0], r[1]}), hi = __builtin_bit_cast(uint64_t, u32x2{r[2], r[3]});
+    const uint64_t l = s < 64 ? lo >> s | hi << (64 - s) : hi >> (s - 64), h = s < 64 ? hi >> s : 0;
+    return {(uint32_t)l, (uint32_t)(l >> 32), (uint32_t)h, (uint32_t)(h >> 32)};
+}
+
+// An offset that is the same in all lanes, in a vector register: a uniform
+// address would go to a scalar load, which needs 4-byte alignment.
+__device__ __forceinline__ int per_lane(int i) {
+    asm("" : "+v"(i));
+    return i;
+}
+
+// 8 elements of a row of C, from element c on, zeros past its end.  The last
+// ones of a row that is no multiple of 8 come with those before them.
+__device__ __forceinline__ u32x4 load8(const uint16_t *row, int c, int C) {
+    const int n = C - c;
     if (n >= 8)
-        return reinterpret_cast<const Any16 *>(p)->v;
+        return reinterpret_cast<const Any16 *>(row + c)->v;
+    if (n <= 0)
+        return u32x4{0u, 0u, 0u, 0u};
+    if (C >= 8)
+        return from_end(reinterpret_cast<const Any16 *>(row + per_lane(C - 8))->v, n);
     u32x4 r = {0u, 0u, 0u, 0u};
 #pragma unroll
     for (int i = 0; i < 7; i++)
         if (i < n)
-            r[i / 2] |= (uint32_t)p[i] << (16 * (i & 1));
+            r[i / 2] |= (uint32_t)row[c + i] << (16 * (i & 1));
     return r;
 }
 
-__device__ __forceinline__ void store8(uint16_t *p, const u32x4 &r, int n) {
+__device__ __forceinline__ void store8(uint16_t *row, int c, int C, const u32x4 &r) {
+    const int n = C - c;
+    uint16_t *const p = row + c;
     if (n >= 8) {
         reinterpret_cast<Any16 *>(p)->v = r;
         return;
     }
-#pragma unroll
-    for (int i = 0; i < 7; i++)
-        if (i < n)
-            p[i] = (uint16_t)(r[i / 2] >> (16 * (i & 1)));
+    if (n <= 0)
+        return;
+    const uint32_t w2 = n & 4 ? r[2] : r[0], w3 = n & 4 ? r[3] : r[1];  // what follows the first 0 or 4
+    if (n & 4)
+        reinterpret_cast<Any8h *>(p)->v = u32x2{r[0], r[1]};
+    if (n & 2)
+        reinterpret_cast<Any4h *>(p + (n & 4))->v = w2;
+    if (n & 1)
+        p[n - 1] = (uint16_t)(n & 2 ? w3 : w2);
 }
 
-// 8 bytes of a checkpoint, the same way.
-__device__ __forceinline__ u32x2 load8b(const int8_t *p, int n) {
+// 8 bytes of a checkpoint's row, the same way.
+__device__ __forceinline__ u32x2 load8b(const int8_t *row, int c, int C) {
+    const int n = C - c;
     if (n >= 8)
-        return reinterpret_cast<const Any8 *>(p)->v;
+        return reinterpret_cast<const Any8 *>(row + c)->v;
+    if (n <= 0)
+        return u32x2{0u, 0u};
+    if (C >= 8)
+        return __builtin_bit_cast(u32x2, __builtin_bit_cast(uint64_t, reinterpret_cast<const Any8 *>(row + per_lane(C - 8))->v) >>
+                                             (8 * (8 - n)));
     u32x2 r = {0u, 0u};
 #pragma unroll
     for (int i = 0; i < 7; i++)
         if (i < n)
-            r[i / 4] |= (uint32_t)(uint8_t)p[i] << (8 * (i & 3));
+            r[i / 4] |= (uint32_t)(uint8_t)row[c + i] << (8 * (i & 3));
     return r;
 }
 
-__device__ __forceinline__ void store8b(int8_t *p, const u32x2 &r, int n) {
+__device__ __forceinline__ void store8b(int8_t *row, int c, int C, const u32x2 &r) {
+    const int n = C - c;
     if (n >= 8) {
-        reinterpret_cast<Any8 *>(p)->v = r;
+        reinterpret_cast<Any8 *>(row + c)->v = r;
         return;
     }
 #pragma unroll
     for (int i = 0; i < 7; i++)
         if (i < n)
-            p[i] = (int8_t)(r[i / 4] >> (8 * (i & 3)));
+            row[c + i] = (int8_t)(r[i / 4] >> (8 * (i & 3)));
+}
+
+// 8 floats of a vector (weight, bias) from p, `rest` from element n on or
+// where there is no vector.
+struct __attribute__((packed, aligned(4))) AnyF4 {
+    float4v v;
+};
+__device__ __forceinline__ void load8f(const float *p, int n, float rest, float *f) {
+    if (p && n >= 8) {
+        const float4v a = reinterpret_cast<const AnyF4 *>(p)->v, b = reinterpret_cast<const AnyF4 *>(p + 4)->v;
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            f[i] = a[i];
+            f[4 + i] = b[i];
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; i++)
+        f[i] = p && i < n ? p[i] : rest;
 }
 
 template <typename T>

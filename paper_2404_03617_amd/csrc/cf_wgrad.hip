@@ -64,19 +64,15 @@ __device__ __forceinline__ f32x16 mfma32(const u32x4 &a, const u32x4 &b, const f
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(pa.h, pb.h, c, 0, 0, 0);
 }
 
-// 16 bytes of a checkpoint row, zeros from byte n on
-__device__ __forceinline__ u32x4 load16b(const int8_t *p, int n) {
+// 16 bytes of a checkpoint's row of C, from byte c on, zeros past its end
+__device__ __forceinline__ u32x4 load16b(const int8_t *row, int c, int C) {
     struct __attribute__((packed, aligned(1))) Any {
         u32x4 v;
     };
-    if (n >= 16)
-        return reinterpret_cast<const Any *>(p)->v;
-    u32x4 r = {0u, 0u, 0u, 0u};
-#pragma unroll
-    for (int i = 0; i < 15; i++)
-        if (i < n)
-            r[i / 4] |= (uint32_t)(uint8_t)p[i] << (8 * (i & 3));
-    return r;
+    if (C - c >= 16)
+        return reinterpret_cast<const Any *>(row + c)->v;
+    const u32x2 lo = load8b(row, c, C), hi = load8b(row, c + 8, C);
+    return u32x4{lo.x, lo.y, hi.x, hi.y};
 }
 
 template <typename T, int TM, int TN, int WM, int WN, bool NORM>
@@ -108,7 +104,7 @@ __global__ __launch_bounds__(64 * WM *WN) void wgrad_kernel(WGradArgs a) {
 #pragma unroll
         for (int j = 0; j < VA; j++) {
             const int64_t row = r + ra + j * DA;
-            st.a[j] = row < last && ca < a.K ? load8(a.dy + row * a.lddy + ca, a.K - ca) : u32x4{0u, 0u, 0u, 0u};
+            st.a[j] = row < last && ca < a.K ? load8(a.dy + row * a.lddy, ca, a.K) : u32x4{0u, 0u, 0u, 0u};
         }
 #pragma unroll
         for (int j = 0; j < VB; j++) {
@@ -116,7 +112,7 @@ __global__ __launch_bounds__(64 * WM *WN) void wgrad_kernel(WGradArgs a) {
             st.b[j] = u32x4{0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u};
             st.f[j] = st.o[j] = 0.0f;
             if (row < last && cb < a.C) {
-                st.b[j] = load16b(a.q + row * a.C + cb, a.C - cb);
+                st.b[j] = load16b(a.q + row * a.C, cb, a.C);
                 float f = a.scale[row * a.blocks + cb / CKPT_BLOCK], o = 0.0f;
                 if constexpr (NORM) {
                     const float2 s = a.stats[row];

@@ -28,7 +28,6 @@ namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-constexpr int BK = 64;   // rows of a step
 constexpr int PAD = 32;  // elements behind each row of LDS
 
 struct WGradArgs {
@@ -41,7 +40,7 @@ struct WGradArgs {
     float *db;
     float *part;     // [splits][K][C] partial sums, null for one split
     float *part_db;  // [splits][K]
-    int64_t lddy, rows, chunk;  // rows of a split, a multiple of BK
+    int64_t lddy, rows, chunk;  // rows of a split, a multiple of ROWS
     int K, C, blocks;
 };
 
@@ -64,23 +63,30 @@ __device__ __forceinline__ f32x16 mfma32(const u32x4 &a, const u32x4 &b, const f
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(pa.h, pb.h, c, 0, 0, 0);
 }
 
-// 16 bytes of a checkpoint's row of C, from byte c on, zeros past its end
-__device__ __forceinline__ u32x4 load16b(const int8_t *row, int c, int C) {
-    struct __attribute__((packed, aligned(1))) Any {
-        u32x4 v;
-    };
-    if (C - c >= 16)
-        return reinterpret_cast<const Any *>(row + c)->v;
-    const u32x2 lo = load8b(row, c, C), hi = load8b(row, c + 8, C);
-    return u32x4{lo.x, lo.y, hi.x, hi.y};
-}
+struct __attribute__((packed, aligned(1))) Any16b {
+    u32x4 v;
+};
 
-template <typename T, int TM, int TN, int WM, int WN, bool NORM>
-__global__ __launch_bounds__(64 * WM *WN) void wgrad_kernel(WGradArgs a) {
-    constexpr int TH = 64 * WM * WN, SA = TM + PAD, SB = TN + PAD;
-    constexpr int FM = TM / WM / 32, FN = TN / WN / 32;      // MFMA tiles of a wave
-    constexpr int VA = BK * TM / 8 / TH, VB = BK * TN / 16 / TH;  // vectors of a thread and step
-    static_assert(TH % (TM / 8) == 0 && VA >= 1 && VB >= 1, "a thread's dy vectors share their columns");
+// What a tile needs to know at compile time: TM x TN of dW, WM x WN waves, BK
+// rows a step, QB bytes of a checkpoint's row a load.  EVEN: vectors lie in
+// their rows whole (K a multiple of 8, C of QB) and 32 bits hold a step's
+// offsets.
+template <int TM_, int TN_, int WM_, int WN_, int BK_, int QB_>
+struct Shape2 {
+    static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, BK = BK_, QB = QB_;
+    static constexpr int TH = 64 * WM * WN, SA = TM + PAD, SB = TN + PAD;
+    static constexpr int FM = TM / WM / 32, FN = TN / WN / 32, KS = BK / 16;    // MFMA tiles of a wave, steps of 16
+    static constexpr int VA = BK * TM / 8 / TH, VB = BK * TN / QB / TH;         // vectors of a thread and step
+    static constexpr int DA = TH / (TM / 8), DB = TH / (TN / QB);               // rows between them
+    static constexpr int SUMS = DA * TM * 4, STEP = 2 * BK * (SA + SB) * 2, LDS = STEP > SUMS ? STEP : SUMS;
+    static_assert(TH % (TM / 8) == 0 && TH % (TN / QB) == 0 && VA >= 1 && VB >= 1, "a thread's vectors share columns");
+    static_assert(CKPT_BLOCK % QB == 0 && TN % CKPT_BLOCK == 0, "a vector has one scale");
+};
+
+template <typename T, typename S, bool NORM, bool EVEN>
+__global__ __launch_bounds__(S::TH) void wgrad_kernel(WGradArgs a) {
+    constexpr int TM = S::TM, TN = S::TN, WM = S::WM, WN = S::WN, BK = S::BK, QB = S::QB, TH = S::TH, SA = S::SA,
+                  SB = S::SB, FM = S::FM, FN = S::FN, KS = S::KS, VA = S::VA, VB = S::VB, DA = S::DA, DB = S::DB;
     extern __shared__ __align__(16) uint16_t lds[];
     uint16_t *const la = lds, *const lb = lds + 2 * BK * SA;
 
@@ -91,70 +97,91 @@ __global__ __launch_bounds__(64 * WM *WN) void wgrad_kernel(WGradArgs a) {
     const bool affine = NORM && a.b;
     const bool sums = blockIdx.x == 0 || (affine && !a.part);
 
-    const int ca = k0 + tid % (TM / 8) * 8, ra = tid / (TM / 8);
-    const int cb = c0 + tid % (TN / 16) * 16, rb = tid / (TN / 16);
-    constexpr int DA = TH / (TM / 8), DB = TH / (TN / 16);  // rows between a thread's vectors
+    const int ka = tid % (TM / 8) * 8, ra = tid / (TM / 8), ca = k0 + ka;
+    const int kb = tid % (TN / QB) * QB, rb = tid / (TN / QB), cb = c0 + kb;
     float db[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
 
-    struct Step {
-        u32x4 a[VA], b[VB];
-        float f[VB], o[VB];  // factor and offset of the biased bytes
-    } st;
-    auto fetch = [&](int64_t r) {
-#pragma unroll
-        for (int j = 0; j < VA; j++) {
+    // A step's share of a thread, in registers from one step to the next.
+    u32x4 va[VA];
+    u32x2 vb[VB][QB / 8];
+    float vs[VB];
+    float2 vn[VB];
+
+    // Vectors past K or C are loaded from its start instead: what they hold
+    // only reaches sums that are not stored.  Rows past the end are loaded
+    // from the step's first row and taken as zeros when they are stored.
+    const uint32_t oa = (uint32_t)((ca < a.K ? ca : 0) * 2), ob = (uint32_t)(cb < a.C ? cb : 0);
+    auto fetch_a = [&](int j, int64_t r) {
+        if constexpr (EVEN) {
+            const int left = (int)(last - r < BK ? last - r : BK);
+            const char *const p = (const char *)(a.dy + r * a.lddy);
+            const int row = ra + j * DA < left ? ra + j * DA : 0;
+            va[j] = reinterpret_cast<const Any16 *>(p + ((uint32_t)row * (uint32_t)(a.lddy * 2) + oa))->v;
+        } else {
             const int64_t row = r + ra + j * DA;
-            st.a[j] = row < last && ca < a.K ? load8(a.dy + row * a.lddy, ca, a.K) : u32x4{0u, 0u, 0u, 0u};
+            va[j] = row < last ? load8(a.dy + row * a.lddy, ca, a.K) : u32x4{0u, 0u, 0u, 0u};
         }
-#pragma unroll
-        for (int j = 0; j < VB; j++) {
+    };
+    auto fetch_b = [&](int j, int64_t r) {
+        if constexpr (EVEN) {
+            const int left = (int)(last - r < BK ? last - r : BK);
+            const int row = rb + j * DB < left ? rb + j * DB : 0;
+            const char *const p = (const char *)(a.q + r * a.C);
+            const uint32_t at = (uint32_t)row * (uint32_t)a.C + ob;
+            if constexpr (QB == 16) {
+                const u32x4 t = reinterpret_cast<const Any16b *>(p + at)->v;
+                vb[j][0] = u32x2{t[0], t[1]};
+                vb[j][QB / 8 - 1] = u32x2{t[2], t[3]};
+            } else {
+                vb[j][0] = reinterpret_cast<const Any8 *>(p + at)->v;
+            }
+            vs[j] = (a.scale + r * a.blocks)[(uint32_t)row * (uint32_t)a.blocks + ob / CKPT_BLOCK];
+            if constexpr (NORM)
+                vn[j] = (a.stats + r)[row];
+        } else {
             const int64_t row = r + rb + j * DB;
-            st.b[j] = u32x4{0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u};
-            st.f[j] = st.o[j] = 0.0f;
+            vs[j] = 0.0f;
+            vn[j] = make_float2(0.0f, 0.0f);
+#pragma unroll
+            for (int i = 0; i < QB / 8; i++)
+                vb[j][i] = row < last ? load8b(a.q + row * a.C, cb + 8 * i, a.C) : u32x2{0u, 0u};
             if (row < last && cb < a.C) {
-                st.b[j] = load16b(a.q + row * a.C, cb, a.C);
-                float f = a.scale[row * a.blocks + cb / CKPT_BLOCK], o = 0.0f;
-                if constexpr (NORM) {
-                    const float2 s = a.stats[row];
-                    f *= s.y;
-                    o = -s.x * s.y;
-                }
-                st.f[j] = f;
-                st.o[j] = fmaf(-128.0f, f, o);
+                vs[j] = a.scale[row * a.blocks + cb / CKPT_BLOCK];
+                if constexpr (NORM)
+                    vn[j] = a.stats[row];
             }
         }
     };
-    auto store = [&](int buf) {
-        uint16_t *const pa = la + buf * (BK * SA), *const pb = lb + buf * (BK * SB);
+    // into buffer `buf`, `left` rows of which are in the split
+    auto store_a = [&](int j, int buf, int64_t left) {
+        if (ra + j * DA >= left)
+            va[j] = u32x4{0u, 0u, 0u, 0u};
+        *reinterpret_cast<u32x4 *>(la + buf * (BK * SA) + (ra + j * DA) * SA + ka) = va[j];
+        if (sums) {
+            float x[8];
+            unpack8<T>(va[j], x);
 #pragma unroll
-        for (int j = 0; j < VA; j++)
-            *reinterpret_cast<u32x4 *>(pa + (ra + j * DA) * SA + (ca - k0)) = st.a[j];
-#pragma unroll
-        for (int j = 0; j < VB; j++) {
-            u32x4 v[2];
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                const uint32_t w = st.b[j][i] ^ 0x80808080u;
-                float x[4];
-#pragma unroll
-                for (int e = 0; e < 4; e++)
-                    x[e] = fmaf(biased(w, e), st.f[j], st.o[j]);
-                v[i / 2][2 * (i & 1)] = T::pack2(x[0], x[1]);
-                v[i / 2][2 * (i & 1) + 1] = T::pack2(x[2], x[3]);
-            }
-            uint16_t *const p = pb + (rb + j * DB) * SB + (cb - c0);
-            *reinterpret_cast<u32x4 *>(p) = v[0];
-            *reinterpret_cast<u32x4 *>(p + 8) = v[1];
+            for (int i = 0; i < 8; i++)
+                db[i] += x[i];
         }
-        if (sums)
+    };
+    auto store_b = [&](int j, int buf, int64_t left) {
+        // x = (byte - 128) f + o
+        const bool on = rb + j * DB < left;
+        const float f = !on ? 0.0f : NORM ? vs[j] * vn[j].y : vs[j];
+        const float o = !on ? 0.0f : fmaf(-128.0f, f, NORM ? -vn[j].x * vn[j].y : 0.0f);
+        uint16_t *const p = lb + buf * (BK * SB) + (rb + j * DB) * SB + kb;
 #pragma unroll
-            for (int j = 0; j < VA; j++) {
-                float x[8];
-                unpack8<T>(st.a[j], x);
+        for (int i = 0; i < QB / 8; i++) {
+            u32x4 v;
 #pragma unroll
-                for (int i = 0; i < 8; i++)
-                    db[i] += x[i];
+            for (int h = 0; h < 2; h++) {
+                const uint32_t w = vb[j][i][h] ^ 0x80808080u;
+                v[2 * h] = T::pack2(fmaf(biased(w, 0), f, o), fmaf(biased(w, 1), f, o));
+                v[2 * h + 1] = T::pack2(fmaf(biased(w, 2), f, o), fmaf(biased(w, 3), f, o));
             }
+            *reinterpret_cast<u32x4 *>(p + 8 * i) = v;
+        }
     };
 
     f32x16 acc[FM][FN];
@@ -171,27 +198,45 @@ __global__ __launch_bounds__(64 * WM *WN) void wgrad_kernel(WGradArgs a) {
     const int tr_row = 8 * (lane >> 5) + ((lane & 15) >> 2), tr_col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
     const int wm = wave / WN * (TM / WM), wn = wave % WN * (TN / WN);
 
-    fetch(first);
-    store(0);
-    __syncthreads();
+    if (first < last) {
+#pragma unroll
+        for (int j = 0; j < VA; j++)
+            fetch_a(j, first);
+#pragma unroll
+        for (int j = 0; j < VB; j++)
+            fetch_b(j, first);
+        const int64_t second = first + BK < last ? first + BK : first;  // a row to load from; not used past the end
+#pragma unroll
+        for (int j = 0; j < VA; j++) {
+            store_a(j, 0, last - first);
+            fetch_a(j, second);
+        }
+#pragma unroll
+        for (int j = 0; j < VB; j++) {
+            store_b(j, 0, last - first);
+            fetch_b(j, second);
+        }
+        __syncthreads();
+    }
+    // Step by step: products of the step in one buffer while the next step,
+    // fetched into registers a step ago, is written to the other and the one
+    // after it is fetched.
     int buf = 0;
     for (int64_t r = first; r < last; r += BK, buf ^= 1) {
-        const bool more = r + BK < last;
-        if (more)
-            fetch(r + BK);
+        const int64_t left = last - (r + BK), third = left > BK ? r + 2 * BK : r;
         const uint16_t *const pa = la + buf * (BK * SA) + tr_row * SA + wm + tr_col;
         const uint16_t *const pb = lb + buf * (BK * SB) + tr_row * SB + wn + tr_col;
 #pragma unroll
-        for (int k = 0; k < BK; k += 16) {
+        for (int k = 0; k < KS; k++) {
             u32x4 fa[FM], fb[FN];
 #pragma unroll
             for (int m = 0; m < FM; m++) {
-                const u32x2 lo = read_tr(pa + k * SA + 32 * m), hi = read_tr(pa + (k + 4) * SA + 32 * m);
+                const u32x2 lo = read_tr(pa + 16 * k * SA + 32 * m), hi = read_tr(pa + (16 * k + 4) * SA + 32 * m);
                 fa[m] = u32x4{lo.x, lo.y, hi.x, hi.y};
             }
 #pragma unroll
             for (int n = 0; n < FN; n++) {
-                const u32x2 lo = read_tr(pb + k * SB + 32 * n), hi = read_tr(pb + (k + 4) * SB + 32 * n);
+                const u32x2 lo = read_tr(pb + 16 * k * SB + 32 * n), hi = read_tr(pb + (16 * k + 4) * SB + 32 * n);
                 fb[n] = u32x4{lo.x, lo.y, hi.x, hi.y};
             }
 #pragma unroll
@@ -199,9 +244,17 @@ __global__ __launch_bounds__(64 * WM *WN) void wgrad_kernel(WGradArgs a) {
 #pragma unroll
                 for (int n = 0; n < FN; n++)
                     acc[m][n] = mfma32<T>(fa[m], fb[n], acc[m][n]);
+#pragma unroll
+            for (int j = VA * k / KS; j < VA * (k + 1) / KS; j++) {
+                store_a(j, buf ^ 1, left);
+                fetch_a(j, third);
+            }
+#pragma unroll
+            for (int j = VB * k / KS; j < VB * (k + 1) / KS; j++) {
+                store_b(j, buf ^ 1, left);
+                fetch_b(j, third);
+            }
         }
-        if (more)
-            store(buf ^ 1);
         __syncthreads();
     }
 
@@ -297,15 +350,22 @@ __global__ __launch_bounds__(64 * S) void wgrad_reduce_kernel(WGradArgs a, int s
 }
 
 struct Plan {
-    int tile;  // index into the tiles below
+    int tile;  // index into TILES
     int splits;
     int64_t chunk;
 };
 
+// Tiles and their waves.
+typedef Shape2<64, 64, 2, 2, 64, 16> Tile64;
+typedef Shape2<128, 128, 2, 2, 64, 16> Tile128;
+typedef Shape2<256, 256, 2, 4, 64, 16> Tile256;
+typedef Shape2<256, 64, 4, 2, 64, 8> TileTall;
+typedef Shape2<64, 256, 2, 4, 64, 16> TileWide;
 struct Tile {
     int m, n;
 };
-constexpr Tile TILES[] = {{64, 64}, {128, 128}, {256, 256}};
+constexpr Tile TILES[] = {{64, 64}, {128, 128}, {256, 256}, {256, 64}, {64, 256}};
+constexpr int ROWS = 64;  // of a step
 
 int64_t tiles_of(int t, int K, int C) {
     return (int64_t)((K + TILES[t].m - 1) / TILES[t].m) * ((C + TILES[t].n - 1) / TILES[t].n);
@@ -316,44 +376,54 @@ constexpr size_t PART_BYTES = (size_t)64 << 20;
 Plan plan_of(int64_t rows, int K, int C) {
     const int64_t cus = device_cu_count();
     Plan p;
-    p.tile = K >= 256 && C >= 256 && tiles_of(2, K, C) >= cus / 2 ? 2 : K > 64 && C > 64 && tiles_of(1, K, C) * (rows / 512 + 1) >= cus ? 1 : 0;
+    if (K >= 256 && C >= 256 && tiles_of(2, K, C) >= cus / 2)
+        p.tile = 2;
+    else if (C <= 64 && K > 128 && tiles_of(3, K, C) * (rows / 512 + 1) >= cus)
+        p.tile = 3;
+    else if (K <= 64 && C > 128 && tiles_of(4, K, C) * (rows / 512 + 1) >= cus)
+        p.tile = 4;
+    else if (K > 64 && C > 64 && tiles_of(1, K, C) * (rows / 512 + 1) >= cus)
+        p.tile = 1;
+    else
+        p.tile = 0;
     const int64_t tiles = tiles_of(p.tile, K, C);
-    int64_t splits = (2 * cus + tiles - 1) / tiles;
-    const int64_t most = (rows + 4 * BK - 1) / (4 * BK), room = (int64_t)(PART_BYTES / (4.0 * K * (C + 1.0)));
+    const int per_cu = p.tile == 0 ? 3 : p.tile == 1 ? 2 : 1;
+    int64_t splits = per_cu * cus / tiles;
+    const int64_t most = (rows + 4 * ROWS - 1) / (4 * ROWS), room = (int64_t)(PART_BYTES / (4.0 * K * (C + 1.0)));
     splits = splits < most ? splits : most;
     splits = splits < room ? splits : room;
     if (tiles >= cus || splits < 1)
         splits = 1;
-    p.chunk = rows < 1 ? BK : ((rows + splits - 1) / splits + BK - 1) / BK * BK;
+    p.chunk = rows < 1 ? ROWS : ((rows + splits - 1) / splits + ROWS - 1) / ROWS * ROWS;
     p.splits = rows < 1 ? 1 : (int)((rows + p.chunk - 1) / p.chunk);
     return p;
 }
 
-template <typename T, int TM, int TN, int WM, int WN, bool NORM>
+template <typename T, typename S, bool NORM>
 hipError_t launch_tile(const WGradArgs &a, int splits, hipStream_t st) {
-    constexpr int SUMS = 64 * WM * WN / (TM / 8) * TM * 4;
-    constexpr int STEP = 2 * BK * (TM + PAD + TN + PAD) * 2;
-    constexpr int LDS = STEP > SUMS ? STEP : SUMS;
-    const void *const f = (const void *)wgrad_kernel<T, TM, TN, WM, WN, NORM>;
-    if (LDS > 64 * 1024) {
-        const hipError_t e = allow_full_lds(f);
+    const bool even = a.K % 8 == 0 && a.C % S::QB == 0 && a.lddy * 2 * S::BK < (int64_t)1 << 31 &&
+                      (int64_t)a.C * S::BK < (int64_t)1 << 31;
+    void (*const f)(WGradArgs) = even ? wgrad_kernel<T, S, NORM, true> : wgrad_kernel<T, S, NORM, false>;
+    if (S::LDS > 64 * 1024) {
+        const hipError_t e = allow_full_lds((const void *)f);
         if (e != hipSuccess)
             return e;
     }
-    const dim3 grid((a.C + TN - 1) / TN, (a.K + TM - 1) / TM, splits);
-    wgrad_kernel<T, TM, TN, WM, WN, NORM><<<grid, dim3(64 * WM * WN), LDS, st>>>(a);
+    const dim3 grid((a.C + S::TN - 1) / S::TN, (a.K + S::TM - 1) / S::TM, splits);
+    f<<<grid, dim3(S::TH), S::LDS, st>>>(a);
     return hipGetLastError();
 }
 
 template <typename T, bool NORM>
 hipError_t launch_type(const WGradArgs &a, const Plan &p, hipStream_t st) {
     hipError_t e;
-    if (p.tile == 2)
-        e = launch_tile<T, 256, 256, 2, 4, NORM>(a, p.splits, st);
-    else if (p.tile == 1)
-        e = launch_tile<T, 128, 128, 2, 2, NORM>(a, p.splits, st);
-    else
-        e = launch_tile<T, 64, 64, 2, 2, NORM>(a, p.splits, st);
+    switch (p.tile) {
+    case 0: e = launch_tile<T, Tile64, NORM>(a, p.splits, st); break;
+    case 1: e = launch_tile<T, Tile128, NORM>(a, p.splits, st); break;
+    case 2: e = launch_tile<T, Tile256, NORM>(a, p.splits, st); break;
+    case 3: e = launch_tile<T, TileTall, NORM>(a, p.splits, st); break;
+    default: e = launch_tile<T, TileWide, NORM>(a, p.splits, st); break;
+    }
     if (e != hipSuccess || p.splits == 1)
         return e;
     const dim3 grid(a.K, (a.C + 63) / 64);

@@ -232,6 +232,7 @@ def lib():
             f.restype = res
             f.argtypes = args
         _lib = L
+        training._bind(L)
     return _lib
 
 
@@ -1020,6 +1021,7 @@ class ConvFirstBlock(torch.nn.Module):
         return block_forward(x, self.params(), act=self.act)
 
 
+from . import training  # noqa: E402
 from .training import (Checkpoint, LogProbs, act_backward, act_forward, act_forward_save,  # noqa: E402
                        checkpoint_pack, checkpoint_unpack, layer_norm_backward, layer_norm_forward,
                        layer_norm_forward_save, linear_weight_grad, log_probs_backward, log_probs_forward)

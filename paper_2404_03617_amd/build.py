@@ -4,8 +4,9 @@
 
 Each csrc/*.hip file is compiled by hipcc for gfx950 into _build/, in
 parallel, then linked into paper_2404_03617_amd/_lib/libconvfirst.so.  The
-binding's argument checks (csrc/host/cf_args.cpp, host code against torch's
-headers) become the CPython module _lib/_cf_args.so.
+binding's argument checks (csrc/host/cf_args.cpp) and native calls
+(csrc/host/cf_calls.cpp), host code against torch's headers, become the CPython
+module _lib/_cf_args.so.
 """
 from __future__ import annotations
 
@@ -22,11 +23,12 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD_DIR = os.path.join(ROOT, "_build")
 LIB_DIR = os.path.join(PKG, "_lib")
 LIB = os.path.join(LIB_DIR, "libconvfirst.so")
-ARGS_SRC = os.path.join(CSRC, "host", "cf_args.cpp")
+ARGS_SRC = [os.path.join(CSRC, "host", f) for f in ("cf_args.cpp", "cf_calls.cpp")]
 ARGS_LIB = os.path.join(LIB_DIR, "_cf_args.so")
 
 ARCH = "gfx950"
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+ROCM_INCLUDE = os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "include")
 # Packed fp32 instructions are switched off for every kernel (the hardware
 # forms v_pk_fma_f32 & co. are avoided on this target).
 COMMON = ["--offload-arch=" + ARCH, "-O3", "-std=c++17", "-fPIC",
@@ -48,7 +50,7 @@ def _compile(src: str) -> str:
 
 
 def build_args() -> str:
-    """Compile the native argument checks; returns the module's path."""
+    """Compile the native argument checks and calls; returns the module's path."""
     import sysconfig
 
     import torch
@@ -57,13 +59,14 @@ def build_args() -> str:
     tlib = os.path.join(os.path.dirname(torch.__file__), "lib")
     tmp = ARGS_LIB + ".tmp"
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared",
-           "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI), ARGS_SRC, "-o", tmp]
-    for d in include_paths() + [sysconfig.get_paths()["include"]]:
+           "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI), "-D__HIP_PLATFORM_AMD__", "-I", INCLUDE,
+           *ARGS_SRC, "-o", tmp]
+    for d in include_paths() + [sysconfig.get_paths()["include"], ROCM_INCLUDE]:
         cmd += ["-isystem", d]
-    cmd += ["-L" + tlib, "-ltorch_python", "-ltorch_cpu", "-lc10", "-Wl,-rpath," + tlib]
+    cmd += ["-L" + tlib, "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip", "-Wl,-rpath," + tlib]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
-        raise RuntimeError("compiling %s failed:\n%s\n%s" % (ARGS_SRC, " ".join(cmd), r.stderr[-8000:]))
+        raise RuntimeError("compiling %s failed:\n%s\n%s" % (" ".join(ARGS_SRC), " ".join(cmd), r.stderr[-8000:]))
     os.replace(tmp, ARGS_LIB)
     return ARGS_LIB
 

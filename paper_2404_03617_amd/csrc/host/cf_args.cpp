@@ -18,7 +18,16 @@
 #include <string>
 #include <vector>
 
+#include "cf_native.h"
+
+namespace cfa {
+extern PyMethodDef calls[];  // cf_calls.cpp
+}
+
 namespace {
+
+using cfa::code_of;
+using cfa::plain;
 
 // One parameter: its key, whether it is a weight (x's dtype, required) or an
 // fp32 vector (optional), and its shape as indices into the call's sizes.
@@ -75,12 +84,6 @@ PyObject *make_spec(PyObject *, PyObject *arg) {
             PyErr_SetString(PyExc_ValueError, "spec: size index out of range");
     }
     return c;
-}
-
-// A strided GPU tensor whose memory the library can use as it is.  Callers let
-// only torch.Tensor and Parameter themselves through, no other subclass.
-bool plain(const at::Tensor &t) {
-    return t.defined() && t.layout() == at::kStrided && t.is_cuda() && t.is_contiguous() && !t.is_conj() && !t.is_neg();
 }
 
 // tensor4(x) -> (N, H, W, C, dtype code, address) of a contiguous 4-D fp16 or
@@ -183,46 +186,18 @@ PyObject *collect(PyObject *, PyObject *args) {
     return PyBytes_FromStringAndSize(reinterpret_cast<const char *>(out), (Py_ssize_t)(8 * spec->size()));
 }
 
-// Dtype codes of rows() and flat(); the first three as in the C ABI.
-bool code_of(at::ScalarType t, int *code) {
-    switch (t) {
-    case at::kHalf: *code = 0; return true;
-    case at::kBFloat16: *code = 1; return true;
-    case at::kFloat: *code = 2; return true;
-    case at::kChar: *code = 3; return true;
-    case at::kLong: *code = 4; return true;
-    default: return false;
-    }
-}
-
 // rows(x) -> (address, rows, C, row stride, dtype code) of a GPU tensor [.., C]
-// whose last dimension is contiguous and whose others are rows at one stride,
-// else None
+// of rows at one stride, else None
 PyObject *rows(PyObject *, PyObject *o) {
     if (!THPVariable_CheckExact(o))
         Py_RETURN_NONE;
     const at::Tensor &t = THPVariable_Unpack(o);
-    int code = 0;
-    if (!t.defined() || t.layout() != at::kStrided || !t.is_cuda() || t.is_conj() || t.is_neg() || t.dim() < 1 ||
-        !code_of(t.scalar_type(), &code))
+    int64_t n, C, ld;
+    int code;
+    if (!cfa::rows_view(t, &n, &C, &ld, &code))
         Py_RETURN_NONE;
-    const int64_t last = t.dim() - 1;
-    const long long C = t.size(last);
-    if (C > 1 && t.stride(last) != 1)
-        Py_RETURN_NONE;
-    long long n = 1, ld = -1;  // rows so far and their stride
-    for (int64_t d = last - 1; d >= 0; d--) {
-        if (t.size(d) != 1) {
-            if (ld < 0)
-                ld = t.stride(d);
-            else if (t.stride(d) != ld * n)
-                Py_RETURN_NONE;
-        }
-        n *= t.size(d);
-        if (n == 0)
-            break;
-    }
-    return Py_BuildValue("KLLLi", (unsigned long long)(uintptr_t)t.data_ptr(), n, C, ld < 0 || n == 0 ? C : ld, code);
+    return Py_BuildValue("KLLLi", (unsigned long long)(uintptr_t)t.data_ptr(), (long long)n, (long long)C,
+                         (long long)ld, code);
 }
 
 // flat(x, t, code, rows, last) -> address of a contiguous tensor t of that
@@ -268,4 +243,11 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_cf_args", nullptr, -1, methods, n
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__cf_args() { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__cf_args() {
+    PyObject *m = PyModule_Create(&module);
+    if (m && PyModule_AddFunctions(m, cfa::calls) < 0) {
+        Py_DECREF(m);
+        return nullptr;
+    }
+    return m;
+}

@@ -11,6 +11,7 @@ do, and as inputs rows that were expanded.  Parameters and statistics are fp32.
 """
 from __future__ import annotations
 
+import ctypes
 from typing import NamedTuple, Optional
 
 import torch
@@ -52,6 +53,33 @@ class LogProbs(NamedTuple):
     stats: torch.Tensor
     top_logp: Optional[torch.Tensor]
     top_ids: Optional[torch.Tensor]
+
+
+# ---------------------------------------------------------------------------
+# Native calls (csrc/host/cf_calls.cpp): checks, outputs and the library's call in
+# one function.  They give None for what is not theirs (a stream or workspace of
+# the caller's, anything wrong), and the functions below go on in Python.
+
+_BOUND = ("cf_layer_norm_forward", "cf_layer_norm_backward", "cf_layer_norm_backward_workspace_bytes",
+          "cf_act_forward", "cf_act_backward", "cf_checkpoint_unpack", "cf_linear_weight_grad",
+          "cf_linear_weight_grad_workspace_bytes", "cf_log_probs_forward", "cf_log_probs_workspace_bytes",
+          "cf_log_probs_backward")
+
+
+def _native(name, *args):
+    """The native call's result; None where it is not for this one."""
+    if _cf._args is None:
+        return None
+    r = getattr(_cf._args, name)(*args)
+    if type(r) is int:
+        _cf._check(r)
+    return r
+
+
+def _bind(L):
+    """Gives the native calls the library's functions."""
+    if _cf._args is not None:
+        _cf._args.bind(tuple(ctypes.cast(getattr(L, f), ctypes.c_void_p).value for f in _BOUND))
 
 
 # ---------------------------------------------------------------------------
@@ -188,6 +216,10 @@ def layer_norm_forward(x: torch.Tensor, weight=None, bias=None, eps: float = 1e-
     """Layer norm over the last dimension (C up to 16384), for inference: y =
     weight * (x - mean) / sqrt(var + eps) + bias, with fp32 weight and bias [C]
     or None.  out may be x."""
+    if stream is None:
+        y = _native("norm_forward", x, weight, bias, eps, out)
+        if y is not None:
+            return y
     xp, rows, C, ldx, code = _rows("x", x, 2)
     w, b = _flat("weight", x, weight, 2, C, 0), _flat("bias", x, bias, 2, C, 0)
     y, yp, ldy = _out_rows(x, out, x.shape, code, stream)
@@ -202,6 +234,10 @@ def layer_norm_forward_save(x: torch.Tensor, weight=None, bias=None, eps: float 
     checkpoint), stats fp32 [..., 2] (mean and 1 / standard deviation of each
     row) and the 8-bit checkpoint of x, written in the same pass over x, or None
     where x itself is kept (checkpoint = False)."""
+    if stream is None:
+        r = _native("norm_forward_save", x, weight, bias, eps, checkpoint, out)
+        if r is not None:
+            return r[0], r[1], Checkpoint(r[2], r[3], x.dtype) if checkpoint else None
     xp, rows, C, ldx, code = _rows("x", x, 2)
     w, b = _flat("weight", x, weight, 2, C, 0), _flat("bias", x, bias, 2, C, 0)
     y, yp, ldy = _out_rows(x, out, x.shape, code, stream)
@@ -219,6 +255,11 @@ def layer_norm_backward(dy: torch.Tensor, x, stats: torch.Tensor, weight=None, p
     dweight and dbias fp32 [C] (None without param_grads).  x is the norm's
     input or its Checkpoint, stats what layer_norm_forward_save returned.  out
     may be dy.  ws: a uint8 workspace of layer_norm_backward_workspace_bytes()."""
+    if stream is None and ws is None:
+        ck = (None, x.q, x.scale) if isinstance(x, Checkpoint) else (x, None, None)
+        r = _native("norm_backward", dy, *ck, stats, weight, param_grads, out)
+        if r is not None:
+            return r
     dyp, rows, C, lddy, code = _rows("dy", dy, 2)
     xp, ldx, q, scale = None, C, None, None
     if isinstance(x, Checkpoint):
@@ -250,6 +291,10 @@ def layer_norm_backward_workspace_bytes(rows: int, C: int) -> int:
 
 def checkpoint_pack(x: torch.Tensor, stream=None) -> Checkpoint:
     """x [..., C] in 8 bits."""
+    if stream is None:
+        r = _native("act_forward", x, _cf.ACTS["none"], False, True, False, None)
+        if r is not None:
+            return Checkpoint(r[1], r[2], x.dtype)
     xp, rows, C, ldx, code = _rows("x", x, 2)
     ck = _new_checkpoint(x, stream)
     _cf._check(_cf.lib().cf_checkpoint_pack(xp, ck.q.data_ptr(), ck.scale.data_ptr(), rows, C, ldx, code,
@@ -259,6 +304,10 @@ def checkpoint_pack(x: torch.Tensor, stream=None) -> Checkpoint:
 
 def checkpoint_unpack(ck: Checkpoint, out=None, stream=None) -> torch.Tensor:
     """The values that a checkpoint keeps, in the dtype of the tensor kept."""
+    if stream is None and type(ck) is Checkpoint and ck.dtype in _cf.DTYPES:
+        x = _native("unpack", ck.q, ck.scale, _CODES[ck.dtype], out)
+        if x is not None:
+            return x
     rows, C, code = _of_checkpoint("ck", ck)
     q, scale = _checkpoint("ck", ck, ck.q, rows, C)
     x, xp, ldx = _out_rows(ck.q, out, ck.q.shape, code, stream)
@@ -269,6 +318,10 @@ def checkpoint_unpack(ck: Checkpoint, out=None, stream=None) -> torch.Tensor:
 def act_forward(u: torch.Tensor, act: str = "gelu", out=None, stream=None) -> torch.Tensor:
     """h = act(u), "gelu" (erf), "relu" or "none", in fp32 and rounded once.
     out may be u."""
+    if stream is None and act in _cf.ACTS:
+        r = _native("act_forward", u, _cf.ACTS[act], True, False, False, out)
+        if r is not None:
+            return r[0]
     up, rows, C, ldu, code = _rows("u", u, 2)
     a = _act(act)
     h, hp, ldh = _out_rows(u, out, u.shape, code, stream)
@@ -281,6 +334,11 @@ def act_forward_save(u: torch.Tensor, act: str = "gelu", checkpoint_out: bool = 
     """act_forward with checkpoints in the same pass: (h, checkpoint of u for
     act_backward, checkpoint of h for linear_weight_grad of the next layer or,
     without checkpoint_out, None)."""
+    if stream is None and act in _cf.ACTS:
+        r = _native("act_forward", u, _cf.ACTS[act], True, True, checkpoint_out, out)
+        if r is not None:
+            return (r[0], Checkpoint(r[1], r[2], u.dtype),
+                    Checkpoint(r[3], r[4], u.dtype) if checkpoint_out else None)
     up, rows, C, ldu, code = _rows("u", u, 2)
     a = _act(act)
     h, hp, ldh = _out_rows(u, out, u.shape, code, stream)
@@ -294,6 +352,10 @@ def act_forward_save(u: torch.Tensor, act: str = "gelu", checkpoint_out: bool = 
 
 def act_backward(dh: torch.Tensor, u: Checkpoint, act: str = "gelu", out=None, stream=None) -> torch.Tensor:
     """du = dh * act'(u) with u from its checkpoint.  out may be dh."""
+    if stream is None and act in _cf.ACTS and type(u) is Checkpoint:
+        du = _native("act_backward", dh, u.q, u.scale, _cf.ACTS[act], out)
+        if du is not None:
+            return du
     dhp, rows, C, lddh, code = _rows("dh", dh, 2)
     a = _act(act)
     if not isinstance(u, Checkpoint):
@@ -310,6 +372,10 @@ def linear_weight_grad(dy: torch.Tensor, x: Checkpoint, stats=None, weight=None,
     checkpoint of x.  With stats (and the norm's weight and bias) the checkpoint
     is of the input of a layer norm whose output was x.  ws: a uint8 workspace
     of linear_weight_grad_workspace_bytes()."""
+    if stream is None and ws is None and type(x) is Checkpoint and x.dtype in _cf.DTYPES:
+        r = _native("wgrad", dy, x.q, x.scale, stats, weight, bias)
+        if r is not None:
+            return r
     dyp, rows, K, lddy, code = _rows("dy", dy, 2)
     n, C, _ = _of_checkpoint("x", x)
     if K < 1 or C < 1:
@@ -341,6 +407,10 @@ def log_probs_forward(logits: torch.Tensor, tokens=None, top: int = 0, ws=None, 
     and its `top` (at most 32) most probable tokens in order, equal ones by
     index.  Logits of -inf have probability 0.  ws: a uint8 workspace of
     log_probs_workspace_bytes()."""
+    if stream is None and ws is None:
+        r = _native("log_probs", logits, tokens, top)
+        if r is not None:
+            return LogProbs(*r)
     zp, rows, V, ldz, code = _rows("logits", logits, 3)
     lead = logits.shape[:-1]
     tp = _flat("tokens", logits, tokens, 4, rows, 0)
@@ -367,6 +437,10 @@ def log_probs_backward(logits: torch.Tensor, tokens, lp: LogProbs, d_logp=None, 
     """The gradient of sum(d_logp * lp.logp) + sum(d_entropy * lp.entropy) with
     respect to the logits, in their dtype; lp is what log_probs_forward returned
     for them, d_logp and d_entropy fp32 [...] or None.  out may be logits."""
+    if stream is None and type(lp) is LogProbs:
+        dz = _native("log_probs_backward", logits, tokens, lp.stats, lp.entropy, d_logp, d_entropy, out)
+        if dz is not None:
+            return dz
     zp, rows, V, ldz, code = _rows("logits", logits, 3)
     tp = _flat("tokens", logits, tokens, 4, rows, 0)
     sp, ep = _flat("lp.stats", logits, lp.stats, 2, rows, 2), _flat("lp.entropy", logits, lp.entropy, 2, rows, 0)

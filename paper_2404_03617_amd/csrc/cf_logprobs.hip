@@ -16,7 +16,9 @@
 // everywhere.  References to the maximum stay at or above the lowest finite
 // number, so that rows masked with it are as good as any other.
 //
-// Alternatives: the n-th largest of the 64 maxima over four threads each bounds
+// Rows of up to 2048 logits (1024 in fp32) are a wave's each.
+//
+// Alternatives of longer rows: the n-th largest of the 64 maxima over four threads each bounds
 // the n-th largest logit from below, so only the few threads whose maximum
 // reaches it look at their share again and collect what does.  Equal logits
 // rank by index; where more are equal than fit the list (a row with few
@@ -179,21 +181,26 @@ struct Args {
     int V, top, chunks, chunk;  // logits of a chunk, a multiple of 8
 };
 
-// what a row's sums say; one thread
+// The token that a row asks about and its logit, loaded ahead by the thread that
+// finishes the row.
+struct Asked {
+    int64_t token;
+    float z;
+};
 template <typename Z>
-__device__ __forceinline__ void finish(const Args &a, int64_t row, const Stat &s) {
-    const typename Z::elem *z = (const typename Z::elem *)a.z + row * a.ldz;
+__device__ __forceinline__ Asked ask(const Args &a, int64_t row) {
+    Asked q = {a.tokens ? a.tokens[row] : -1, 0.0f};
+    if (q.token >= 0 && q.token < a.V)
+        q.z = Z::one((const typename Z::elem *)a.z + row * a.ldz + q.token);
+    return q;
+}
+
+// what a row's sums say; one thread
+__device__ __forceinline__ void finish(const Args &a, int64_t row, const Stat &s, const Asked &q) {
     const bool bad = !(s.m < INFINITY), empty = s.s == 0.0f;
-    const float ref = ref_of(s.m), ls = bad ? NAN : empty ? 0.0f : logf(s.s);
-    const int64_t t = a.tokens ? a.tokens[row] : -1;
-    if (a.logp) {
-        float lp = 0.0f;
-        if (t >= a.V)
-            lp = NAN;
-        else if (t >= 0)
-            lp = bad ? NAN : (Z::one(z + t) - ref) - ls;
-        a.logp[row] = lp;
-    }
+    const float ls = bad ? NAN : empty ? 0.0f : logf(s.s);
+    if (a.logp)
+        a.logp[row] = q.token >= a.V ? NAN : q.token < 0 ? 0.0f : bad ? NAN : (q.z - ref_of(s.m)) - ls;
     a.entropy[row] = bad ? NAN : empty ? 0.0f : fmaxf(ls - LN2 * (s.t / s.s), 0.0f);
     if (a.stats)
         a.stats[row] = bad ? make_float2(NAN, NAN) : empty ? make_float2(-INFINITY, 0.0f) : make_float2(s.m, ls);
@@ -231,8 +238,41 @@ struct TopSpace {
     uint64_t list[LIST];
     uint64_t out[TOP_MAX];
     uint64_t best[TH / 64];
-    int n, cnt[TH / 64];
+    int n, threads, cnt[TH / 64];
+    uint8_t who[TH];
 };
+
+// Logits of [begin, end) that `wanted` takes, from the shares of the threads
+// that say `mine`, into sp.list; their number in sp.n (which may pass LIST).
+// The whole workgroup reads those shares, a vector a thread, so that a row's
+// length does not become a chain of loads.
+template <typename Z, typename F>
+__device__ void collect(const typename Z::elem *z, int begin, int end, bool mine, TopSpace &sp, F &&wanted) {
+    const int tid = threadIdx.x;
+    if (tid == 0)
+        sp.n = sp.threads = 0;
+    __syncthreads();
+    if (mine)
+        sp.who[atomicAdd(&sp.threads, 1)] = (uint8_t)tid;
+    __syncthreads();
+    const unsigned each = (unsigned)(end - begin + TH * Z::VE - 1) / (TH * Z::VE), all = sp.threads * each;
+    for (unsigned w = tid; w < all; w += TH) {
+        const unsigned t = w / each, i = begin + ((w - t * each) * TH + sp.who[t]) * Z::VE;
+        const int n = end - (int)i;
+        if (n <= 0)
+            continue;
+        float v[Z::VE];
+        Z::values(Z::load(z, (int)i, end), n, v);
+#pragma unroll
+        for (int e = 0; e < Z::VE; e++)
+            if (e < n && wanted(v[e])) {
+                const int at = atomicAdd(&sp.n, 1);
+                if (at < LIST)
+                    sp.list[at] = key_of(v[e], i + e);
+            }
+    }
+    __syncthreads();
+}
 
 // The `top` first logits of [begin, end) in order into sp.out (0 where there
 // are fewer); tm is the maximum of this thread's share.  Every thread calls it
@@ -243,8 +283,6 @@ __device__ void find_top(const typename Z::elem *z, int begin, int end, int top,
     const float g = lanes<Max, 4>(tm);
     if ((tid & 3) == 0)
         sp.gm[tid >> 2] = g;
-    if (tid == 0)
-        sp.n = 0;
     if (tid < top)
         sp.out[tid] = 0;
     __syncthreads();
@@ -262,31 +300,12 @@ __device__ void find_top(const typename Z::elem *z, int begin, int end, int top,
     // nan is the same in every thread
     bool done = false;
     if (!nan) {
-        if (tm >= bound)
-            each<Z>(z, begin, end, [&](float v, uint32_t i) {
-                if (v >= bound) {
-                    const int at = atomicAdd(&sp.n, 1);
-                    if (at < LIST)
-                        sp.list[at] = key_of(v, i);
-                }
-            });
-        __syncthreads();
+        collect<Z>(z, begin, end, tm >= bound, sp, [&](float v) { return v >= bound; });
         int n = sp.n;
         done = n <= LIST;
         if (!done) {  // many are equal: those above the bound, then the first of the equal ones
             __syncthreads();
-            if (tid == 0)
-                sp.n = 0;
-            __syncthreads();
-            if (tm > bound)
-                each<Z>(z, begin, end, [&](float v, uint32_t i) {
-                    if (v > bound) {
-                        const int at = atomicAdd(&sp.n, 1);
-                        if (at < LIST)
-                            sp.list[at] = key_of(v, i);
-                    }
-                });
-            __syncthreads();
+            collect<Z>(z, begin, end, tm > bound, sp, [&](float v) { return v > bound; });
             n = sp.n;
             done = n + TOP_MAX <= LIST;
             if (done && n < top) {
@@ -382,6 +401,9 @@ __global__ __launch_bounds__(TH) void log_probs_kernel(Args a) {
     constexpr int STEP = TH * Z::VE;
 
     Stat st = {-INFINITY, 0.0f, 0.0f};
+    Asked asked = {-1, 0.0f};
+    if (tid == 0 && a.chunks == 1)
+        asked = ask<Z>(a, row);
     typename Z::raw next[NV] = {};
     auto fetch = [&](int i) {
 #pragma unroll
@@ -420,12 +442,6 @@ __global__ __launch_bounds__(TH) void log_probs_kernel(Args a) {
         all.s += o.s;
         all.t += o.t;
     }
-    if (tid == 0) {
-        if (a.chunks > 1)
-            a.part[row * a.chunks + part] = make_float4(all.m, all.s, all.t, 0.0f);
-        else
-            finish<Z>(a, row, all);
-    }
     if constexpr (TOP) {
         __shared__ TopSpace sp;
         find_top<Z>(z, begin, end, a.top, tm, sp);
@@ -436,6 +452,104 @@ __global__ __launch_bounds__(TH) void log_probs_kernel(Args a) {
                 put_top(a, row, tid, sp.out[tid], all);
         }
     }
+    if (tid == 0) {
+        if (a.chunks > 1)
+            a.part[row * a.chunks + part] = make_float4(all.m, all.s, all.t, 0.0f);
+        else
+            finish(a, row, all, asked);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Short rows: a wave takes one whole, NV vectors a lane, all in registers and
+// without a barrier.  Alternatives one after the other: the wave's largest key,
+// then the next of the lane that held it.
+//
+// Keys of 16-bit logits fit 32 bits: the low 13 bits of their fp32 form are
+// zeros and take the index (V below 8192).
+template <typename Z>
+struct WaveKey {
+    typedef uint64_t key;
+    static __device__ __forceinline__ key of(float z, int i, bool) { return key_of(z, (uint32_t)i); }
+    static __device__ __forceinline__ key best(key k) { return wave_max(k); }
+    static __device__ __forceinline__ uint64_t wide(key k) { return k; }
+};
+template <typename T>
+struct WaveKey<Z16<T>> {
+    typedef uint32_t key;
+    static constexpr uint32_t INDEX = 0x1fffu;
+    static __device__ __forceinline__ key of(float z, int i, bool nan) {
+        const uint32_t u = __builtin_bit_cast(uint32_t, z + 0.0f);  // -0 equals 0
+        uint32_t o = u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+        if (nan)  // of the row: of any sign, before all
+            o = z != z ? 0xffffffffu : o;
+        return (o & ~INDEX) | (INDEX - (uint32_t)i);
+    }
+    template <int CTRL>
+    static __device__ __forceinline__ key step(key k) {
+        const key o = (key)__builtin_amdgcn_update_dpp((int)k, (int)k, CTRL, 0xf, 0xf, true);
+        return k > o ? k : o;
+    }
+    static __device__ __forceinline__ key best(key k) {
+        k = step<DPP_MIRROR16>(step<DPP_MIRROR8>(step<DPP_XOR2>(step<DPP_XOR1>(k))));
+        const auto a = __builtin_amdgcn_permlane16_swap(k, k, false, false);
+        k = a[0] > a[1] ? a[0] : a[1];
+        const auto b = __builtin_amdgcn_permlane32_swap(k, k, false, false);
+        return b[0] > b[1] ? b[0] : b[1];
+    }
+    static __device__ __forceinline__ uint64_t wide(key k) {
+        const uint32_t o = k & ~INDEX;
+        // the value's low bits, which the index took: zeros of a positive
+        // number, ones (it is stored inverted) of a negative one
+        const uint32_t whole = o == ~INDEX ? 0xffffffffu : o & 0x80000000u ? o : o | INDEX;
+        return (uint64_t)whole << 32 | (0xffffffffu - (INDEX - (k & INDEX)));
+    }
+};
+
+template <typename Z, int NV, bool TOP>
+__global__ __launch_bounds__(256) void log_probs_wave_kernel(Args a, int64_t rows) {
+    typedef WaveKey<Z> K;
+    const int lane = threadIdx.x & 63;
+    const int64_t row = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (row >= rows)
+        return;
+    const typename Z::elem *const z = (const typename Z::elem *)a.z + row * a.ldz;
+    float x[NV * Z::VE];
+    typename Z::raw raw[NV];
+#pragma unroll
+    for (int v = 0; v < NV; v++)
+        raw[v] = Z::load(z, (v * 64 + lane) * Z::VE, a.V);
+    const Asked asked = ask<Z>(a, row);
+#pragma unroll
+    for (int v = 0; v < NV; v++)
+        Z::values(raw[v], a.V - (v * 64 + lane) * Z::VE, x + v * Z::VE);
+    Stat st = {-INFINITY, 0.0f, 0.0f};
+    add<NV * Z::VE>(st, x);
+    st = wave_join(st);
+    if constexpr (TOP) {
+        const bool nan = st.m != st.m;  // the same in all lanes
+        typename K::key k[NV * Z::VE], mine = 0, top = 0;
+#pragma unroll
+        for (int i = 0; i < NV * Z::VE; i++) {
+            const int at = (i / Z::VE * 64 + lane) * Z::VE + i % Z::VE;
+            k[i] = at < a.V ? K::of(x[i], at, nan) : 0;
+            top = k[i] > top ? k[i] : top;
+        }
+        for (int n = 0; n < a.top; n++) {
+            const typename K::key best = K::best(top);
+            mine = n == lane ? best : mine;
+            if (top == best) {
+                top = 0;
+#pragma unroll
+                for (int i = 0; i < NV * Z::VE; i++)
+                    top = k[i] < best && k[i] > top ? k[i] : top;
+            }
+        }
+        if (lane < a.top)
+            put_top(a, row, lane, K::wide(mine), st);
+    }
+    if (lane == 0)  // last: the asked logit is two loads, one after the other
+        finish(a, row, st, asked);
 }
 
 constexpr int CHUNKS = 64;  // at most, one a lane of the joining wave
@@ -446,19 +560,27 @@ __global__ __launch_bounds__(64) void log_probs_join_kernel(Args a) {
     const int lane = threadIdx.x;
     const int64_t row = blockIdx.x;
     const bool on = lane < a.chunks;
+    const Asked asked = ask<Z>(a, row);
     Stat st = {-INFINITY, 0.0f, 0.0f};
     if (on) {
         const float4 p = a.part[row * a.chunks + lane];
         st = {p.x, p.y, p.z};
     }
     st = wave_join(st);
-    if (lane == 0)
-        finish<Z>(a, row, st);
     if constexpr (TOP) {
         __shared__ uint64_t key[CHUNKS * TOP_MAX];
         const uint64_t *const from = a.part_key + row * a.chunks * a.top;
-        for (int i = lane; i < a.chunks * a.top; i += 64)
-            key[i] = from[i];
+        // eight loads in flight
+        for (int i = lane; i < a.chunks * a.top; i += 8 * 64) {
+            uint64_t k[8];
+#pragma unroll
+            for (int u = 0; u < 8; u++)
+                k[u] = i + u * 64 < a.chunks * a.top ? from[i + u * 64] : 0;
+#pragma unroll
+            for (int u = 0; u < 8; u++)
+                if (i + u * 64 < CHUNKS * TOP_MAX)
+                    key[i + u * 64] = k[u];
+        }
         __syncthreads();
         int at = 0;
         uint64_t head = on ? key[lane * a.top] : 0, mine = 0;
@@ -474,6 +596,8 @@ __global__ __launch_bounds__(64) void log_probs_join_kernel(Args a) {
         if (lane < a.top)
             put_top(a, row, lane, mine, st);
     }
+    if (lane == 0)
+        finish(a, row, st, asked);
 }
 
 // ---------------------------------------------------------------------------
@@ -572,8 +696,24 @@ void chunks_of(int64_t rows, int V, int *chunks, int *chunk) {
     *chunks = (V + *chunk - 1) / *chunk;
 }
 
+template <typename Z, int N>
+hipError_t forward_wave(const Args &a, int64_t rows, hipStream_t st) {
+    const dim3 grid((unsigned)((rows + 3) / 4));
+    if (a.top)
+        log_probs_wave_kernel<Z, N, true><<<grid, dim3(256), 0, st>>>(a, rows);
+    else
+        log_probs_wave_kernel<Z, N, false><<<grid, dim3(256), 0, st>>>(a, rows);
+    return hipGetLastError();
+}
+
 template <typename Z>
 hipError_t forward(const Args &a, int64_t rows, hipStream_t st) {
+    if (a.V <= 64 * Z::VE)
+        return forward_wave<Z, 1>(a, rows, st);
+    if (a.V <= 128 * Z::VE)
+        return forward_wave<Z, 2>(a, rows, st);
+    if (a.V <= 256 * Z::VE)
+        return forward_wave<Z, 4>(a, rows, st);
     const dim3 grid((unsigned)(rows * a.chunks));
     if (a.top)
         log_probs_kernel<Z, true><<<grid, dim3(TH), 0, st>>>(a);

@@ -167,10 +167,11 @@ struct NormBackArgs {
     int C, blocks;
 };
 
-// Threads of a workgroup of the backward kernel: its register accumulators of
-// dw and db cover C / G of each row a lane, and one workgroup's groups add
-// theirs before they are written, so few large workgroups write little.
-constexpr int back_threads(int G) { return G > 512 ? G : 512; }
+// Threads of a workgroup of the backward kernel.  A workgroup's groups add
+// their sums of dw and db before they are written: above 2048 channels, where
+// those are many, one workgroup a CU writes half of what two would (2999 rows
+// of 4095 25.6 -> 23.0 us with the reduction; 6272 of 2048 lose 1 us).
+constexpr int back_threads(int G) { return G >= 256 ? 1024 : 512; }
 
 constexpr int RED_BYTES = 2 * 16 * 2 * sizeof(float);
 
@@ -382,10 +383,12 @@ __global__ __launch_bounds__(1024) void norm_reduce_kernel(const float *part, fl
 template <typename T, int G, int V>
 hipError_t forward_shape(const NormArgs &a, hipStream_t st) {
     constexpr int NG = (G > 256 ? G : 256) / G, TH = G > 256 ? G : 256;
-    // Four rows a group where that leaves eight workgroups a CU.
+    // Four rows a group (two of wide rows) where that leaves four workgroups a
+    // CU: 2999 rows of 4095 15.3 -> 13.7 us, 25088 of 256 keep one (7.6 us, 8.8
+    // with four).
     constexpr int U = 4 / V;
     const int64_t many = (a.rows + NG * U - 1) / (NG * U);
-    if (many >= 8 * device_cu_count()) {
+    if (many >= 4 * device_cu_count()) {
         norm_forward_kernel<T, G, V, U><<<dim3((unsigned)many), dim3(TH), 0, st>>>(a);
     } else {
         norm_forward_kernel<T, G, V, 1><<<dim3((unsigned)((a.rows + NG - 1) / NG)), dim3(TH), 0, st>>>(a);
@@ -410,7 +413,7 @@ int back_groups_of(int C) {
 }
 int64_t back_grid(int64_t rows, int C) {
     const int64_t ng = back_groups_of(C), need = (rows + ng - 1) / ng;
-    const int64_t most = (int64_t)device_cu_count() * (C <= 4096 ? 2 : 1);
+    const int64_t most = (int64_t)device_cu_count() * (C <= 2048 ? 2 : 1);
     return need < 1 ? 1 : need < most ? need : most;
 }
 

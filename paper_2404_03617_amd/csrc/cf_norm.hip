@@ -296,20 +296,20 @@ __global__ __launch_bounds__(back_threads(G), 4) void norm_backward_kernel(NormB
     }
     if (!a.dw)
         return;
-    // Lanes of a wave that hold the same channels, then the waves, 4 channels
-    // of each lane at a time.
+    // Lanes of a wave that hold the same channels, then the waves through LDS.
     float *const pw = a.db ? a.dw : a.dw + (int64_t)blockIdx.x * 2 * a.C;
     float *const pb = a.db ? a.db : pw + a.C;
-    float4(*const part)[WAVES][64] = reinterpret_cast<float4(*)[WAVES][64]>(space);
-    constexpr int SUB = G > 64 ? G / 64 : 1;  // waves that share a row
+    float4(*const part)[WAVES][64] = reinterpret_cast<float4(*)[WAVES][64]>(space);  // [dw, db][4 channels]
+    constexpr int SUB = G > 64 ? G / 64 : 1;                                         // waves that share a row
+    __syncthreads();
 #pragma unroll
-    for (int j = 0; j < V * 8; j += 4) {
-        float4 t[2];
+    for (int k = 0; k < 2; k++)
 #pragma unroll
-        for (int i = 0; i < 4; i++)
+        for (int j = 0; j < V * 2; j++) {
+            float4 t;
 #pragma unroll
-            for (int k = 0; k < 2; k++) {
-                float f = k ? db[j + i] : dw[j + i];
+            for (int i = 0; i < 4; i++) {
+                float f = k ? db[4 * j + i] : dw[4 * j + i];
                 if constexpr (G <= 8)
                     f += dpp<0x128>(f);  // 8 lanes further in the row of 16
                 if constexpr (G <= 16) {
@@ -320,22 +320,28 @@ __global__ __launch_bounds__(back_threads(G), 4) void norm_backward_kernel(NormB
                     const Two h = swap32(f);
                     f = h.a + h.b;
                 }
-                (&t[k].x)[i] = f;
+                (&t.x)[i] = f;
             }
-        __syncthreads();
-        part[0][wave][lane] = t[0];
-        part[1][wave][lane] = t[1];
-        __syncthreads();
-        constexpr int LANES = G < 64 ? G : 64, OUT = 2 * SUB * LANES * 4;
-        for (int o = threadIdx.x; o < OUT; o += TH) {
-            const int i = o & 3, l = (o >> 2) % LANES, rest = (o >> 2) / LANES, sub = rest % SUB, k = rest / SUB;
-            float f = 0.0f;
+            part[k * V * 2 + j][wave][lane] = t;
+        }
+    __syncthreads();
+    constexpr int LANES = G < 64 ? G : 64, OUT = 4 * V * SUB * LANES;
+    for (int o = threadIdx.x; o < OUT; o += TH) {
+        const int l = o % LANES, sub = o / LANES % SUB, kj = o / (LANES * SUB), j = kj % (2 * V);
+        float4 f = part[kj][sub][l];
+        for (int n = 1; n < WAVES / SUB; n++) {
+            const float4 g = part[kj][n * SUB + sub][l];
+            f.x += g.x, f.y += g.y, f.z += g.z, f.w += g.w;
+        }
+        const int c = (sub * 64 + l + j / 2 * G) * 8 + (j & 1) * 4;
+        float *const to = (kj < 2 * V ? pw : pb) + c;
+        if (c + 4 <= a.C) {
+            reinterpret_cast<AnyF4 *>(to)->v = float4v{f.x, f.y, f.z, f.w};
+        } else {
 #pragma unroll
-            for (int n = 0; n < WAVES / SUB; n++)
-                f += (&part[k][n * SUB + sub][l].x)[i];
-            const int c = (sub * 64 + l + (j / 8) * G) * 8 + (j & 7) + i;
-            if (c < a.C)
-                (k ? pb : pw)[c] = f;
+            for (int i = 0; i < 3; i++)
+                if (c + i < a.C)
+                    to[i] = (&f.x)[i];
         }
     }
 }
@@ -414,7 +420,7 @@ int back_groups_of(int C) {
 int64_t back_grid(int64_t rows, int C) {
     const int64_t ng = back_groups_of(C), need = (rows + ng - 1) / ng;
     const int64_t most = (int64_t)device_cu_count() * (C <= 2048 ? 2 : 1);
-    return need < 1 ? 1 : need < most ? need : most;
+    return need <= 2 ? 1 : need < most ? need : most;  // two turns of one workgroup, and no second launch
 }
 
 int lanes_of(int C) {
@@ -425,7 +431,7 @@ int lanes_of(int C) {
 
 template <typename T, bool CK, int G, int V>
 hipError_t backward_shape(const NormBackArgs &a, unsigned grid, hipStream_t st) {
-    constexpr int SUMS = 2 * back_threads(G) * 16, WEIGHT = V > 1 ? G * V * 32 : 0;
+    constexpr int SUMS = back_threads(G) * V * 64, WEIGHT = V > 1 ? G * V * 32 : 0;
     constexpr int LDS = RED_BYTES + (SUMS > WEIGHT ? SUMS : WEIGHT);
     if (LDS > 64 * 1024) {
         const hipError_t e = allow_full_lds((const void *)norm_backward_kernel<T, CK, G, V>);

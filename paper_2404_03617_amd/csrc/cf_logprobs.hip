@@ -218,18 +218,40 @@ constexpr int TH = 256;    // threads of a workgroup
 constexpr int NV = 4;      // vectors a thread loads together
 constexpr int LIST = 512;  // logits collected before equal ones are counted
 
-// Scan of the n <= `end` logits from `begin`: f(value, index) for every logit
-// of this thread's share.
+// The logits [begin, end) of a row in vectors that start at multiples of 16
+// bytes, whatever the row's own start: the first vector holds what comes
+// before the first such place (4096 rows of 100003 in bf16: 186 -> 166 us).  Vector v has n logits from index i on (none: n <= 0).
+template <typename Z>
+struct Piece {
+    const typename Z::elem *z;
+    int begin, end, V, pad;
+    __device__ __forceinline__ Piece(const typename Z::elem *row, int b, int e, int len)
+        : z(row), begin(b), end(e), V(len), pad((int)((uintptr_t)(row + b) & 15u) / (int)sizeof(*row)) {}
+    struct At {
+        int i, n;
+    };
+    __device__ __forceinline__ At at(int v) const {
+        const int i = begin - pad + v * Z::VE;
+        const int from = i > begin ? i : begin, to = i + Z::VE < end ? i + Z::VE : end;
+        return {from, to - from};
+    }
+    __device__ __forceinline__ int vectors() const { return (end - begin + pad + Z::VE - 1) / Z::VE; }
+    // the logits' bits, and the logits (-inf past n)
+    __device__ __forceinline__ typename Z::raw load(const At &a) const { return Z::load(z, a.i, V); }
+    __device__ __forceinline__ void values(const At &a, float *x) const { Z::values(load(a), a.n, x); }
+};
+
+// f(value, index) for every logit of this thread's share.
 template <typename Z, typename F>
-__device__ __forceinline__ void each(const typename Z::elem *z, int begin, int end, F &&f) {
-    for (int i = begin + (int)threadIdx.x * Z::VE; i < end; i += TH * Z::VE) {
-        float v[Z::VE];
-        const int n = end - i;
-        Z::values(Z::load(z, i, end), n, v);
+__device__ __forceinline__ void each(const Piece<Z> &p, F &&f) {
+    for (int v = threadIdx.x; v < p.vectors(); v += TH) {
+        const auto a = p.at(v);
+        float x[Z::VE];
+        p.values(a, x);
 #pragma unroll
         for (int e = 0; e < Z::VE; e++)
-            if (e < n)
-                f(v[e], (uint32_t)(i + e));
+            if (e < a.n)
+                f(x[e], (uint32_t)(a.i + e));
     }
 }
 
@@ -242,12 +264,12 @@ struct TopSpace {
     uint8_t who[TH];
 };
 
-// Logits of [begin, end) that `wanted` takes, from the shares of the threads
+// Logits of the piece that `wanted` takes, from the shares of the threads
 // that say `mine`, into sp.list; their number in sp.n (which may pass LIST).
 // The whole workgroup reads those shares, a vector a thread, so that a row's
 // length does not become a chain of loads.
 template <typename Z, typename F>
-__device__ void collect(const typename Z::elem *z, int begin, int end, bool mine, TopSpace &sp, F &&wanted) {
+__device__ void collect(const Piece<Z> &p, bool mine, TopSpace &sp, F &&wanted) {
     const int tid = threadIdx.x;
     if (tid == 0)
         sp.n = sp.threads = 0;
@@ -255,30 +277,31 @@ __device__ void collect(const typename Z::elem *z, int begin, int end, bool mine
     if (mine)
         sp.who[atomicAdd(&sp.threads, 1)] = (uint8_t)tid;
     __syncthreads();
-    const unsigned each = (unsigned)(end - begin + TH * Z::VE - 1) / (TH * Z::VE), all = sp.threads * each;
+    const unsigned each = (unsigned)(p.vectors() + TH - 1) / TH, all = sp.threads * each;
     for (unsigned w = tid; w < all; w += TH) {
-        const unsigned t = w / each, i = begin + ((w - t * each) * TH + sp.who[t]) * Z::VE;
-        const int n = end - (int)i;
-        if (n <= 0)
+        const unsigned t = w / each;
+        const int v = (int)((w - t * each) * TH + sp.who[t]);
+        if (v >= p.vectors())
             continue;
-        float v[Z::VE];
-        Z::values(Z::load(z, (int)i, end), n, v);
+        const auto a = p.at(v);
+        float x[Z::VE];
+        p.values(a, x);
 #pragma unroll
         for (int e = 0; e < Z::VE; e++)
-            if (e < n && wanted(v[e])) {
+            if (e < a.n && wanted(x[e])) {
                 const int at = atomicAdd(&sp.n, 1);
                 if (at < LIST)
-                    sp.list[at] = key_of(v[e], i + e);
+                    sp.list[at] = key_of(x[e], (uint32_t)(a.i + e));
             }
     }
     __syncthreads();
 }
 
-// The `top` first logits of [begin, end) in order into sp.out (0 where there
+// The `top` first logits of the piece in order into sp.out (0 where there
 // are fewer); tm is the maximum of this thread's share.  Every thread calls it
 // and may read sp.out afterwards.
 template <typename Z>
-__device__ void find_top(const typename Z::elem *z, int begin, int end, int top, float tm, TopSpace &sp) {
+__device__ void find_top(const Piece<Z> &p, int top, float tm, TopSpace &sp) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const float g = lanes<Max, 4>(tm);
     if ((tid & 3) == 0)
@@ -300,26 +323,27 @@ __device__ void find_top(const typename Z::elem *z, int begin, int end, int top,
     // nan is the same in every thread
     bool done = false;
     if (!nan) {
-        collect<Z>(z, begin, end, tm >= bound, sp, [&](float v) { return v >= bound; });
+        collect<Z>(p, tm >= bound, sp, [&](float v) { return v >= bound; });
         int n = sp.n;
         done = n <= LIST;
         if (!done) {  // many are equal: those above the bound, then the first of the equal ones
             __syncthreads();
-            collect<Z>(z, begin, end, tm > bound, sp, [&](float v) { return v > bound; });
+            collect<Z>(p, tm > bound, sp, [&](float v) { return v > bound; });
             n = sp.n;
             done = n + TOP_MAX <= LIST;
             if (done && n < top) {
                 const int above_n = n, want = top - n;
                 int found = 0;
-                for (int i0 = begin; i0 < end && found < want; i0 += TH * Z::VE) {
-                    const int i = i0 + tid * Z::VE;
-                    float v[Z::VE];
+                for (int v0 = 0; v0 < p.vectors() && found < want; v0 += TH) {
+                    typename Piece<Z>::At a = {0, 0};
                     unsigned eq = 0;
-                    if (i < end) {
-                        Z::values(Z::load(z, i, end), end - i, v);
+                    if (v0 + tid < p.vectors()) {
+                        a = p.at(v0 + tid);
+                        float x[Z::VE];
+                        p.values(a, x);
 #pragma unroll
                         for (int e = 0; e < Z::VE; e++)
-                            eq |= (unsigned)(v[e] == bound && e < end - i) << e;
+                            eq |= (unsigned)(x[e] == bound && e < a.n) << e;
                     }
                     int c = __popc(eq), before = c;
 #pragma unroll
@@ -340,7 +364,7 @@ __device__ void find_top(const typename Z::elem *z, int begin, int end, int top,
                     for (int e = 0; e < Z::VE; e++)
                         if (eq >> e & 1) {
                             if (at < want)
-                                sp.list[above_n + at] = key_of(bound, (uint32_t)(i + e));
+                                sp.list[above_n + at] = key_of(bound, (uint32_t)(a.i + e));
                             at++;
                         }
                     found += all;
@@ -365,7 +389,7 @@ __device__ void find_top(const typename Z::elem *z, int begin, int end, int top,
         bool first = true;
         for (int r = 0; r < top; r++) {
             uint64_t best = 0;
-            each<Z>(z, begin, end, [&](float v, uint32_t i) {
+            each<Z>(p, [&](float v, uint32_t i) {
                 const uint64_t k = key_of(v, i);
                 best = (first || k < last) && k > best ? k : best;
             });
@@ -398,31 +422,32 @@ __global__ __launch_bounds__(TH) void log_probs_kernel(Args a) {
     const int part = (int)(blockIdx.x - (unsigned)row * (unsigned)a.chunks);
     const typename Z::elem *const z = (const typename Z::elem *)a.z + row * a.ldz;
     const int begin = part * a.chunk, end = a.V - begin < a.chunk ? a.V : begin + a.chunk;
-    constexpr int STEP = TH * Z::VE;
+    const Piece<Z> piece(z, begin, end, a.V);
+    const int vectors = piece.vectors();
 
     Stat st = {-INFINITY, 0.0f, 0.0f};
     Asked asked = {-1, 0.0f};
     if (tid == 0 && a.chunks == 1)
         asked = ask<Z>(a, row);
     typename Z::raw next[NV] = {};
-    auto fetch = [&](int i) {
+    auto fetch = [&](int v) {
 #pragma unroll
-        for (int v = 0; v < NV; v++)
-            if (i + v * STEP < end)
-                next[v] = Z::load(z, i + v * STEP, end);
+        for (int u = 0; u < NV; u++)
+            if (v + u * TH < vectors)
+                next[u] = piece.load(piece.at(v + u * TH));
     };
-    int i = begin + tid * Z::VE;
-    fetch(i);
-    for (; i < end; i += NV * STEP) {
+    int v = tid;
+    fetch(v);
+    for (; v < vectors; v += NV * TH) {
         typename Z::raw cur[NV];
 #pragma unroll
-        for (int v = 0; v < NV; v++)
-            cur[v] = next[v];
-        fetch(i + NV * STEP);
+        for (int u = 0; u < NV; u++)
+            cur[u] = next[u];
+        fetch(v + NV * TH);
         float x[NV * Z::VE];
 #pragma unroll
-        for (int v = 0; v < NV; v++)
-            Z::values(cur[v], end - (i + v * STEP), x + v * Z::VE);
+        for (int u = 0; u < NV; u++)
+            Z::values(cur[u], piece.at(v + u * TH).n, x + u * Z::VE);
         add<NV * Z::VE>(st, x);
     }
     const float tm = st.m;
@@ -444,7 +469,7 @@ __global__ __launch_bounds__(TH) void log_probs_kernel(Args a) {
     }
     if constexpr (TOP) {
         __shared__ TopSpace sp;
-        find_top<Z>(z, begin, end, a.top, tm, sp);
+        find_top<Z>(piece, a.top, tm, sp);
         if (tid < a.top) {
             if (a.chunks > 1)
                 a.part_key[(row * a.chunks + part) * a.top + tid] = sp.out[tid];
@@ -636,10 +661,10 @@ __device__ __forceinline__ RowGrad row_grad(const BackArgs &k, int64_t row) {
     return r;
 }
 
+// n (at most a vector's) logits from index i on
 template <typename Z>
 __device__ __forceinline__ void grad8(const BackArgs &k, const RowGrad &r, const typename Z::elem *z,
-                                      typename Z::elem *dz, int i) {
-    const int n = k.V - i;
+                                      typename Z::elem *dz, int i, int n) {
     float x[Z::VE];
     Z::values(Z::load(z, i, k.V), n, x);
 #pragma unroll
@@ -647,12 +672,12 @@ __device__ __forceinline__ void grad8(const BackArgs &k, const RowGrad &r, const
         const float l = fmaxf(fmaf(x[e] - r.ref, LOG2E, r.off), FLOOR2);
         x[e] = __builtin_amdgcn_exp2f(l) * fmaf(r.b, l, r.a);
     }
-    if (r.token >= i && r.token < i + Z::VE)
+    if (r.token >= i && r.token < i + n)
 #pragma unroll
         for (int e = 0; e < Z::VE; e++)
             if (r.token == i + e)
                 x[e] += r.g;
-    Z::store(dz, i, k.V, x);
+    Z::store(dz, i, i + n, x);
 }
 
 // Short rows: a thread takes a vector of any row.
@@ -664,7 +689,7 @@ __global__ __launch_bounds__(256) void log_probs_backward_kernel(BackArgs k) {
     const uint32_t row = fdiv(v, k.per_row);
     const int i = (int)(v - row * k.per_row.d) * Z::VE;
     grad8<Z>(k, row_grad(k, row), (const typename Z::elem *)k.z + row * k.ldz,
-             (typename Z::elem *)k.dz + row * k.lddz, i);
+             (typename Z::elem *)k.dz + row * k.lddz, i, k.V - i);
 }
 
 // Long rows: a workgroup takes BACK_NV * 256 vectors of one row, whose numbers
@@ -676,11 +701,14 @@ __global__ __launch_bounds__(256) void log_probs_backward_row_kernel(BackArgs k,
     const RowGrad r = row_grad(k, row);
     const typename Z::elem *const z = (const typename Z::elem *)k.z + row * k.ldz;
     typename Z::elem *const dz = (typename Z::elem *)k.dz + row * k.lddz;
+    const Piece<Z> piece(z, 0, k.V, k.V);
 #pragma unroll
-    for (int v = 0; v < BACK_NV; v++) {
-        const int64_t i = ((int64_t)part * BACK_NV + v) * 256 * Z::VE + threadIdx.x * Z::VE;
-        if (i < k.V)
-            grad8<Z>(k, r, z, dz, (int)i);
+    for (int u = 0; u < BACK_NV; u++) {
+        const int v = (int)(part * BACK_NV + u) * 256 + (int)threadIdx.x;
+        if (v < piece.vectors()) {
+            const auto a = piece.at(v);
+            grad8<Z>(k, r, z, dz, a.i, a.n);
+        }
     }
 }
 
@@ -733,7 +761,9 @@ template <typename Z>
 hipError_t backward(BackArgs &a, int64_t rows, hipStream_t st) {
     constexpr int SPAN = BACK_NV * 256 * Z::VE;
     if (a.V >= SPAN / 2) {
-        const uint32_t chunks = (uint32_t)((a.V + SPAN - 1) / SPAN);
+        // room for a first vector that is not whole, unless every row starts a vector
+        const bool whole = ((uintptr_t)a.z | (uintptr_t)a.ldz * sizeof(typename Z::elem)) % 16 == 0;
+        const uint32_t chunks = (uint32_t)((a.V + (whole ? 0 : Z::VE - 1) + SPAN - 1) / SPAN);
         log_probs_backward_row_kernel<Z><<<dim3((unsigned)(rows * chunks)), dim3(256), 0, st>>>(a, chunks);
     } else {
         const uint32_t per_row = (uint32_t)((a.V + Z::VE - 1) / Z::VE);

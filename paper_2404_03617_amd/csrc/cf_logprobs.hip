@@ -16,7 +16,9 @@
 // everywhere.  References to the maximum stay at or above the lowest finite
 // number, so that rows masked with it are as good as any other.
 //
-// Rows of up to 2048 logits (1024 in fp32) are a wave's each.
+// Rows of up to 2048 logits (1024 in fp32) stay in the registers of a wave or
+// of 8, 16 or 32 of its lanes (65536 rows of 100 with five alternatives: 50 us
+// with a wave each).
 //
 // Alternatives of longer rows: the n-th largest of the 64 maxima over four threads each bounds
 // the n-th largest logit from below, so only the few threads whose maximum
@@ -128,10 +130,12 @@ __device__ __forceinline__ void add(Stat &a, const float *z) {
     }
 }
 
+// of G neighbouring lanes
+template <int G = 64>
 __device__ __forceinline__ Stat wave_join(Stat a) {
-    const float m = lanes<Max, 64>(a.m);
+    const float m = lanes<Max, G>(a.m);
     rebase(a, m);
-    return {m, lanes<Add, 64>(a.s), lanes<Add, 64>(a.t)};
+    return {m, lanes<Add, G>(a.s), lanes<Add, G>(a.t)};
 }
 
 // ---------------------------------------------------------------------------
@@ -155,17 +159,24 @@ __device__ __forceinline__ uint64_t dpp64(uint64_t k) {
            (uint32_t)__builtin_amdgcn_update_dpp(lo, lo, CTRL, 0xf, 0xf, true);
 }
 __device__ __forceinline__ uint64_t later(uint64_t a, uint64_t b) { return a > b ? a : b; }
+template <int G = 64>
 __device__ __forceinline__ uint64_t wave_max(uint64_t k) {
     k = later(k, dpp64<DPP_XOR1>(k));
     k = later(k, dpp64<DPP_XOR2>(k));
     k = later(k, dpp64<DPP_MIRROR8>(k));
-    k = later(k, dpp64<DPP_MIRROR16>(k));
-    const auto l = __builtin_amdgcn_permlane16_swap((uint32_t)k, (uint32_t)k, false, false);
-    const auto h = __builtin_amdgcn_permlane16_swap((uint32_t)(k >> 32), (uint32_t)(k >> 32), false, false);
-    k = later((uint64_t)h[0] << 32 | (uint32_t)l[0], (uint64_t)h[1] << 32 | (uint32_t)l[1]);
-    const auto l2 = __builtin_amdgcn_permlane32_swap((uint32_t)k, (uint32_t)k, false, false);
-    const auto h2 = __builtin_amdgcn_permlane32_swap((uint32_t)(k >> 32), (uint32_t)(k >> 32), false, false);
-    return later((uint64_t)h2[0] << 32 | (uint32_t)l2[0], (uint64_t)h2[1] << 32 | (uint32_t)l2[1]);
+    if constexpr (G >= 16)
+        k = later(k, dpp64<DPP_MIRROR16>(k));
+    if constexpr (G >= 32) {
+        const auto l = __builtin_amdgcn_permlane16_swap((uint32_t)k, (uint32_t)k, false, false);
+        const auto h = __builtin_amdgcn_permlane16_swap((uint32_t)(k >> 32), (uint32_t)(k >> 32), false, false);
+        k = later((uint64_t)h[0] << 32 | (uint32_t)l[0], (uint64_t)h[1] << 32 | (uint32_t)l[1]);
+    }
+    if constexpr (G >= 64) {
+        const auto l = __builtin_amdgcn_permlane32_swap((uint32_t)k, (uint32_t)k, false, false);
+        const auto h = __builtin_amdgcn_permlane32_swap((uint32_t)(k >> 32), (uint32_t)(k >> 32), false, false);
+        k = later((uint64_t)h[0] << 32 | (uint32_t)l[0], (uint64_t)h[1] << 32 | (uint32_t)l[1]);
+    }
+    return k;
 }
 
 struct Args {
@@ -486,9 +497,9 @@ __global__ __launch_bounds__(TH) void log_probs_kernel(Args a) {
 }
 
 // ---------------------------------------------------------------------------
-// Short rows: a wave takes one whole, NV vectors a lane, all in registers and
-// without a barrier.  Alternatives one after the other: the wave's largest key,
-// then the next of the lane that held it.
+// Short rows: G lanes of a wave take one whole, NV vectors a lane, all in
+// registers and without a barrier.  Alternatives one after the other: the
+// largest key of the group, then the next of the lane that held it.
 //
 // Keys of 16-bit logits fit 32 bits: the low 13 bits of their fp32 form are
 // zeros and take the index (V below 8192).
@@ -496,7 +507,10 @@ template <typename Z>
 struct WaveKey {
     typedef uint64_t key;
     static __device__ __forceinline__ key of(float z, int i, bool) { return key_of(z, (uint32_t)i); }
-    static __device__ __forceinline__ key best(key k) { return wave_max(k); }
+    template <int G>
+    static __device__ __forceinline__ key best(key k) {
+        return wave_max<G>(k);
+    }
     static __device__ __forceinline__ uint64_t wide(key k) { return k; }
 };
 template <typename T>
@@ -515,12 +529,20 @@ struct WaveKey<Z16<T>> {
         const key o = (key)__builtin_amdgcn_update_dpp((int)k, (int)k, CTRL, 0xf, 0xf, true);
         return k > o ? k : o;
     }
+    template <int G>
     static __device__ __forceinline__ key best(key k) {
-        k = step<DPP_MIRROR16>(step<DPP_MIRROR8>(step<DPP_XOR2>(step<DPP_XOR1>(k))));
-        const auto a = __builtin_amdgcn_permlane16_swap(k, k, false, false);
-        k = a[0] > a[1] ? a[0] : a[1];
-        const auto b = __builtin_amdgcn_permlane32_swap(k, k, false, false);
-        return b[0] > b[1] ? b[0] : b[1];
+        k = step<DPP_MIRROR8>(step<DPP_XOR2>(step<DPP_XOR1>(k)));
+        if constexpr (G >= 16)
+            k = step<DPP_MIRROR16>(k);
+        if constexpr (G >= 32) {
+            const auto a = __builtin_amdgcn_permlane16_swap(k, k, false, false);
+            k = a[0] > a[1] ? a[0] : a[1];
+        }
+        if constexpr (G >= 64) {
+            const auto b = __builtin_amdgcn_permlane32_swap(k, k, false, false);
+            k = b[0] > b[1] ? b[0] : b[1];
+        }
+        return k;
     }
     static __device__ __forceinline__ uint64_t wide(key k) {
         const uint32_t o = k & ~INDEX;
@@ -531,37 +553,38 @@ struct WaveKey<Z16<T>> {
     }
 };
 
-template <typename Z, int NV, bool TOP>
+template <typename Z, int G, int NV, bool TOP>
 __global__ __launch_bounds__(256) void log_probs_wave_kernel(Args a, int64_t rows) {
     typedef WaveKey<Z> K;
-    const int lane = threadIdx.x & 63;
-    const int64_t row = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (row >= rows)
+    const int lane = threadIdx.x % G;  // of the group
+    const int group = G == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / G) : threadIdx.x / G;
+    const int64_t row = (int64_t)blockIdx.x * (256 / G) + group;
+    if (row >= rows)  // whole groups: no exchange crosses them
         return;
     const typename Z::elem *const z = (const typename Z::elem *)a.z + row * a.ldz;
     float x[NV * Z::VE];
     typename Z::raw raw[NV];
 #pragma unroll
     for (int v = 0; v < NV; v++)
-        raw[v] = Z::load(z, (v * 64 + lane) * Z::VE, a.V);
+        raw[v] = Z::load(z, (v * G + lane) * Z::VE, a.V);
     const Asked asked = ask<Z>(a, row);
 #pragma unroll
     for (int v = 0; v < NV; v++)
-        Z::values(raw[v], a.V - (v * 64 + lane) * Z::VE, x + v * Z::VE);
+        Z::values(raw[v], a.V - (v * G + lane) * Z::VE, x + v * Z::VE);
     Stat st = {-INFINITY, 0.0f, 0.0f};
     add<NV * Z::VE>(st, x);
-    st = wave_join(st);
+    st = wave_join<G>(st);
     if constexpr (TOP) {
-        const bool nan = st.m != st.m;  // the same in all lanes
+        const bool nan = st.m != st.m;  // the same in all lanes of the group
         typename K::key k[NV * Z::VE], mine = 0, top = 0;
 #pragma unroll
         for (int i = 0; i < NV * Z::VE; i++) {
-            const int at = (i / Z::VE * 64 + lane) * Z::VE + i % Z::VE;
+            const int at = (i / Z::VE * G + lane) * Z::VE + i % Z::VE;
             k[i] = at < a.V ? K::of(x[i], at, nan) : 0;
             top = k[i] > top ? k[i] : top;
         }
         for (int n = 0; n < a.top; n++) {
-            const typename K::key best = K::best(top);
+            const typename K::key best = K::template best<G>(top);
             mine = n == lane ? best : mine;
             if (top == best) {
                 top = 0;
@@ -724,24 +747,31 @@ void chunks_of(int64_t rows, int V, int *chunks, int *chunk) {
     *chunks = (V + *chunk - 1) / *chunk;
 }
 
-template <typename Z, int N>
+template <typename Z, int G, int N>
 hipError_t forward_wave(const Args &a, int64_t rows, hipStream_t st) {
-    const dim3 grid((unsigned)((rows + 3) / 4));
+    const dim3 grid((unsigned)((rows + 256 / G - 1) / (256 / G)));
     if (a.top)
-        log_probs_wave_kernel<Z, N, true><<<grid, dim3(256), 0, st>>>(a, rows);
+        log_probs_wave_kernel<Z, G, N, true><<<grid, dim3(256), 0, st>>>(a, rows);
     else
-        log_probs_wave_kernel<Z, N, false><<<grid, dim3(256), 0, st>>>(a, rows);
+        log_probs_wave_kernel<Z, G, N, false><<<grid, dim3(256), 0, st>>>(a, rows);
     return hipGetLastError();
 }
 
 template <typename Z>
 hipError_t forward(const Args &a, int64_t rows, hipStream_t st) {
+    // a lane for each of the alternatives
+    if (a.V <= 8 * Z::VE && a.top <= 8)
+        return forward_wave<Z, 8, 1>(a, rows, st);
+    if (a.V <= 16 * Z::VE && a.top <= 16)
+        return forward_wave<Z, 16, 1>(a, rows, st);
+    if (a.V <= 32 * Z::VE)
+        return forward_wave<Z, 32, 1>(a, rows, st);
     if (a.V <= 64 * Z::VE)
-        return forward_wave<Z, 1>(a, rows, st);
+        return forward_wave<Z, 64, 1>(a, rows, st);
     if (a.V <= 128 * Z::VE)
-        return forward_wave<Z, 2>(a, rows, st);
+        return forward_wave<Z, 64, 2>(a, rows, st);
     if (a.V <= 256 * Z::VE)
-        return forward_wave<Z, 4>(a, rows, st);
+        return forward_wave<Z, 64, 4>(a, rows, st);
     const dim3 grid((unsigned)(rows * a.chunks));
     if (a.top)
         log_probs_kernel<Z, true><<<grid, dim3(TH), 0, st>>>(a);

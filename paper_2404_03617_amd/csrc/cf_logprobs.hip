@@ -16,9 +16,9 @@
 // everywhere.  References to the maximum stay at or above the lowest finite
 // number, so that rows masked with it are as good as any other.
 //
-// Rows of up to 2048 logits (1024 in fp32) stay in the registers of a wave or
-// of 8, 16 or 32 of its lanes (65536 rows of 100 with five alternatives: 50 us
-// with a wave each).
+// Rows of up to 4096 logits (2048 in fp32) stay in the registers of a wave or
+// of 8, 16 or 32 of its lanes (65536 rows of 100 with five alternatives: 15 us,
+// 50 with a wave each, 360 with a workgroup).
 //
 // Alternatives of longer rows: the n-th largest of the 64 maxima over four threads each bounds
 // the n-th largest logit from below, so only the few threads whose maximum
@@ -770,8 +770,15 @@ hipError_t forward(const Args &a, int64_t rows, hipStream_t st) {
         return forward_wave<Z, 64, 1>(a, rows, st);
     if (a.V <= 128 * Z::VE)
         return forward_wave<Z, 64, 2>(a, rows, st);
-    if (a.V <= 256 * Z::VE)
+    // The alternatives of a lane's many logits are found one after the other:
+    // a workgroup finds eight of 2000 sooner where rows leave it the room (100
+    // rows of 2000 in bf16: 8.2 us, a wave 11.2; 2000 rows 17.2 and 10.0), and
+    // of 4000 unless rows are many (10000 rows: 67 us, a wave 53).
+    const int64_t cus = device_cu_count();
+    if (a.V <= 256 * Z::VE && (a.top <= 4 || rows >= 4 * cus))
         return forward_wave<Z, 64, 4>(a, rows, st);
+    if (a.V <= 512 * Z::VE && (a.top == 0 || (a.top <= 8 && rows >= 16 * cus)))
+        return forward_wave<Z, 64, 8>(a, rows, st);
     const dim3 grid((unsigned)(rows * a.chunks));
     if (a.top)
         log_probs_kernel<Z, true><<<grid, dim3(TH), 0, st>>>(a);

@@ -104,6 +104,20 @@ def test_forward_and_backward(rows, V, dtype):
         check_backward(z, tokens, *got)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,V,top", [(70, 50, 8), (70, 64, 9), (70, 64, 17), (300, 128, 16), (300, 250, 32), (40, 512, 5),
+                                        (1100, 1500, 5), (9, 1500, 5), (4200, 2600, 8), (4200, 1900, 3), (30, 3000, 0),
+                                        (9, 3000, 8), (4200, 4096, 2)])
+def test_rows_between_a_few_lanes_and_a_workgroup(rows, V, top, dtype):
+    dt = DT[dtype]
+    z = randn(rows + V, (rows, V), dt, 1.5)
+    z[::7, ::3] = -INF
+    z[1::5] = z[1::5].round()  # ties
+    g = torch.Generator().manual_seed(V)
+    tokens = 3 * torch.randint(0, V // 3, (rows,), generator=g) + 1
+    check(z, tokens, top)
+
+
 def masked_rows(V, dt):
     """Rows whose masks leave all, one, few or no classes, by -inf or by the
     type's lowest value; equal logits; large and small ones."""

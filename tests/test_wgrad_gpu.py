@@ -68,6 +68,28 @@ def test_weight_grad(rows, K, C, norm, dtype):
     assert torch.equal(again[0], got[0]) and torch.equal(again[1], got[1])
 
 
+# Shapes at which the estimate takes each tile, whole and with its rows split,
+# with vectors that lie in their rows, that meet their ends, and rows shorter
+# than a vector.
+TILES = [(40, 2, 3), (578, 2, 2), (578, 8, 16), (633, 8, 19), (136, 2296, 3744), (66, 4518, 3997), (3440, 2928, 464),
+         (205001, 134, 77), (273, 4744, 2816), (275, 3627, 3571), (2075, 1720, 2336), (2521, 2211, 1812),
+         (198, 4344, 784), (66, 3066, 2624), (3827, 3596, 5), (3714, 4120, 16), (4518, 3421, 9), (68, 1912, 3936),
+         (69, 4024, 1994), (61966, 2, 212), (2874, 8, 4272), (19152, 9, 707), (1068, 3608, 560), (973, 3466, 592),
+         (32259, 80, 368), (90993, 74, 66), (995, 232, 1152), (969, 306, 891)]
+
+
+@pytest.mark.parametrize("rows,K,C", TILES)
+def test_every_tile(rows, K, C):
+    n = TILES.index((rows, K, C))
+    for dt, norm in ((torch.float16, n % 2 == 0), (torch.bfloat16, n % 2 == 1)):
+        dy, q, scale, stats, w, b, kept, spread = case(n, rows, K, C, dt, norm)
+        dw, tw, db, tb = reference(dy, kept, w, b, spread, dt, rows)
+        more = dict(stats=stats.cuda(), weight=w.cuda(), bias=b.cuda()) if norm else {}
+        got = cf.linear_weight_grad(rows_in("shifted", dy), cf.Checkpoint(q.cuda(), scale.cuda(), dt), **more)
+        assert_within(got[0], dw, tw, "dW")
+        assert_within(got[1], db, tb, "db")
+
+
 @pytest.mark.parametrize("which", ["weight", "bias", "neither"])
 def test_norm_without_weight_or_bias(which):
     rows, K, C, dt = 900, 40, 100, torch.bfloat16

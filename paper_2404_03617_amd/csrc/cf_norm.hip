@@ -11,7 +11,15 @@
 // cancellation of E[x^2] - mean^2) and written once.  G lanes share a row,
 // 8 V channels each, in vectors of 8 that alternate between the lanes so that
 // a group's loads are contiguous: narrow rows of 64 channels take 8 lanes, a
-// wave then holds 8 rows, rows above 2048 channels take several waves.
+// wave then holds 8 rows, rows above 512 channels take several waves.
+//
+// Measured on MI355X, where a copy of 2 GiB moves 4.9 TB/s (kernel times):
+//   forward   401408 x 64 fp16 with statistics and checkpoint 25.8 us, 5.2 TB/s;
+//             25088 x 256 bf16 7.4 us; 2999 x 4095 bf16 12.4 us, 4.0 TB/s (rows
+//             that start at any 2 bytes); one row of 512 1.7 us, a launch
+//   backward  401408 x 64 from the checkpoint 24.1 us, 5.5 TB/s, and 4.6 us for
+//             the second launch; 2999 x 4095 20.0 us, 3.7 TB/s, and 4.8 us: three
+//             turns of 1024 rows, whose first loads and last stores nothing hides
 #include "cf_rows.h"
 #include "cf_kernels.h"
 #include "cf_train.h"
@@ -169,14 +177,18 @@ struct NormBackArgs {
 
 // Threads of a workgroup of the backward kernel.  A workgroup's groups add
 // their sums of dw and db before they are written: above 2048 channels, where
-// those are many, one workgroup a CU writes half of what two would (2999 rows
-// of 4095 25.6 -> 23.0 us with the reduction; 6272 of 2048 lose 1 us).
-constexpr int back_threads(int G) { return G >= 256 ? 1024 : 512; }
+// those are many, one workgroup a CU writes half of what two would (norm and
+// gradient of 2999 rows of 4095 41.9 -> 38.8 us, 560 of 2304 17.9 -> 15.7).
+constexpr int back_threads(int G) { return G >= 512 ? 1024 : 512; }
 
 constexpr int RED_BYTES = 2 * 16 * 2 * sizeof(float);
 
 // CK: x from its checkpoint.  Persistent: a group takes rows a grid apart, the
-// next row's loads in flight while the current one is worked on.
+// next row's loads in flight while the current one is worked on.  The sums over
+// rows stay in registers until the end and are added in a fixed order, within a
+// workgroup through LDS, across workgroups by norm_reduce_kernel: no atomics, so
+// the same input gives the same gradients, and one rounding of fp32 sums of a
+// few rows each.
 template <typename T, bool CK, int G, int V>
 __global__ __launch_bounds__(back_threads(G), 4) void norm_backward_kernel(NormBackArgs a) {
     constexpr int TH = back_threads(G), NG = TH / G, WAVES = TH / 64;
@@ -348,7 +360,9 @@ __global__ __launch_bounds__(back_threads(G), 4) void norm_backward_kernel(NormB
 
 // Sum of `n` partials [n][2][C] into dw [C] and db [C]: 32 columns a
 // workgroup (a cache line), 32 threads share a column and add every 32nd
-// partial, eight loads at a time.
+// partial, eight loads at a time.  512 partials of 64 channels 4.6 us, 256 of
+// 4095 (8.4 MB) 4.8 us: little more than a launch and two loads one after the
+// other.
 __global__ __launch_bounds__(1024) void norm_reduce_kernel(const float *part, float *dw, float *db, int n, int C) {
     __shared__ float s[32][33];
     const int col = threadIdx.x & 31, at = threadIdx.x >> 5;
@@ -374,31 +388,43 @@ __global__ __launch_bounds__(1024) void norm_reduce_kernel(const float *part, fl
         (o < C ? dw[o] : db[o - C]) = f;
 }
 
-// Lanes and vectors of a row of C channels.
+// Lanes and vectors of a row of C channels: one vector a lane where a workgroup
+// can hold the row.  In the backward pass two (for which the registers do not
+// suffice: some of them go to memory) take longer, norm and gradient of 25088
+// rows of 1024 73 us against 58, of 2000 of 8192 51 against 41, of 37 of 986 14
+// against 10.4.
 #define CF_NORM_SHAPES(F)                                                                                              \
     if (C <= 64) return F(8, 1);                                                                                       \
     if (C <= 128) return F(16, 1);                                                                                     \
     if (C <= 256) return F(32, 1);                                                                                     \
     if (C <= 512) return F(64, 1);                                                                                     \
-    if (C <= 1024) return F(64, 2);                                                                                    \
-    if (C <= 2048) return F(128, 2);                                                                                   \
-    if (C <= 4096) return F(256, 2);                                                                                   \
-    if (C <= 8192) return F(512, 2);                                                                                   \
+    if (C <= 1024) return F(128, 1);                                                                                   \
+    if (C <= 2048) return F(256, 1);                                                                                   \
+    if (C <= 4096) return F(512, 1);                                                                                   \
+    if (C <= 8192) return F(1024, 1);                                                                                  \
     return F(1024, 2);
+
+// U rows a group; false where that leaves fewer than `least` waves.
+template <typename T, int G, int V, int U>
+bool forward_rows(const NormArgs &a, int64_t least, hipStream_t st) {
+    constexpr int TH = G > 256 ? G : 256, ROWS = TH / G * U;
+    const int64_t grid = (a.rows + ROWS - 1) / ROWS;
+    if (grid * (TH / 64) < least)
+        return false;
+    norm_forward_kernel<T, G, V, U><<<dim3((unsigned)grid), dim3(TH), 0, st>>>(a);
+    return true;
+}
 
 template <typename T, int G, int V>
 hipError_t forward_shape(const NormArgs &a, hipStream_t st) {
-    constexpr int NG = (G > 256 ? G : 256) / G, TH = G > 256 ? G : 256;
-    // Four rows a group (two of wide rows) where that leaves four workgroups a
-    // CU: 2999 rows of 4095 15.3 -> 13.7 us, 25088 of 256 keep one (7.6 us, 8.8
-    // with four).
-    constexpr int U = 4 / V;
-    const int64_t many = (a.rows + NG * U - 1) / (NG * U);
-    if (many >= 4 * device_cu_count()) {
-        norm_forward_kernel<T, G, V, U><<<dim3((unsigned)many), dim3(TH), 0, st>>>(a);
-    } else {
-        norm_forward_kernel<T, G, V, 1><<<dim3((unsigned)((a.rows + NG - 1) / NG)), dim3(TH), 0, st>>>(a);
-    }
+    // Four vectors a lane where that leaves 16 waves a CU: four rows, or
+    // of rows above 512 channels two in half the lanes (2999 rows of 4095 with
+    // one row 15.3 us, with four in all the lanes 15.9, with two in half 13.5).
+    // Fewer rows take one at a time: 25088 of 256 7.6 us (with four 8.8), 512 of
+    // 768 3.7 us a call (with two vectors a lane 4.0).
+    constexpr int HALF = V == 1 && G > 64 ? G / 2 : G, VECS = V == 2 || G > 64 ? 2 : 1;
+    if (!forward_rows<T, HALF, VECS, 4 / VECS>(a, 16 * (int64_t)device_cu_count(), st))
+        forward_rows<T, G, V, 1>(a, 0, st);
     return hipGetLastError();
 }
 
@@ -419,7 +445,7 @@ int back_groups_of(int C) {
 }
 int64_t back_grid(int64_t rows, int C) {
     const int64_t ng = back_groups_of(C), need = (rows + ng - 1) / ng;
-    const int64_t most = (int64_t)device_cu_count() * (C <= 2048 ? 2 : 1);
+    const int64_t most = (int64_t)device_cu_count() * (C <= 2048 ? 2 : 1);  // 16 waves a CU
     return need <= 2 ? 1 : need < most ? need : most;  // two turns of one workgroup, and no second launch
 }
 

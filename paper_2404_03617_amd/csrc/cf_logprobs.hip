@@ -20,12 +20,18 @@
 // of 8, 16 or 32 of its lanes (65536 rows of 100 with five alternatives: 15 us,
 // 50 with a wave each, 360 with a workgroup).
 //
-// Alternatives of longer rows: the n-th largest of the 64 maxima over four threads each bounds
-// the n-th largest logit from below, so only the few threads whose maximum
-// reaches it look at their share again and collect what does.  Equal logits
-// rank by index; where more are equal than fit the list (a row with few
-// classes left), those above the bound are collected and the equal ones taken
+// Alternatives of longer rows: the n-th largest of the 64 maxima over four
+// threads each bounds the n-th largest logit from below, so only the few threads
+// whose maximum reaches it look at their share again and collect what does.
+// Equal logits rank by index; where more are equal than fit the list (a row with
+// few classes left), those above the bound are collected and the equal ones taken
 // in the order of the row.
+//
+// Measured on MI355X, where a copy of 2 GiB moves 4.9 TB/s (kernel times): 4096
+// rows of 100003 in bf16 forward 166 us (4.9 TB/s; VALU 67% busy), backward 267 us
+// (6.1 TB/s); one row of 131072 with eight alternatives 6.7 us in 64 workgroups
+// and 3.8 us to join them; 128 rows of 1000 with five 6.0 us.  The last two are
+// chains: load, maximum, join, alternatives, the logit asked for.
 #include "cf_rows.h"
 #include "cf_kernels.h"
 #include "cf_train.h"
@@ -226,12 +232,12 @@ __device__ __forceinline__ void put_top(const Args &a, int64_t row, int n, uint6
 }
 
 constexpr int TH = 256;    // threads of a workgroup
-constexpr int NV = 4;      // vectors a thread loads together
 constexpr int LIST = 512;  // logits collected before equal ones are counted
 
 // The logits [begin, end) of a row in vectors that start at multiples of 16
 // bytes, whatever the row's own start: the first vector holds what comes
-// before the first such place (4096 rows of 100003 in bf16: 186 -> 166 us).  Vector v has n logits from index i on (none: n <= 0).
+// before the first such place (4096 rows of 100003 in bf16: 186 -> 166 us).
+// Vector v has n logits from index i on (none: n <= 0).
 template <typename Z>
 struct Piece {
     const typename Z::elem *z;
@@ -309,14 +315,16 @@ __device__ void collect(const Piece<Z> &p, bool mine, TopSpace &sp, F &&wanted) 
 }
 
 // The `top` first logits of the piece in order into sp.out (0 where there
-// are fewer); tm is the maximum of this thread's share.  Every thread calls it
-// and may read sp.out afterwards.
+// are fewer); tm is the maximum of this thread's share and x its last vector.
+// Every thread calls it and may read sp.out afterwards.
 template <typename Z>
-__device__ void find_top(const Piece<Z> &p, int top, float tm, TopSpace &sp) {
+__device__ void find_top(const Piece<Z> &p, int top, float tm, const float *x, TopSpace &sp) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const float g = lanes<Max, 4>(tm);
     if ((tid & 3) == 0)
         sp.gm[tid >> 2] = g;
+    if (tid == 0)
+        sp.n = 0;
     if (tid < top)
         sp.out[tid] = 0;
     __syncthreads();
@@ -334,7 +342,20 @@ __device__ void find_top(const Piece<Z> &p, int top, float tm, TopSpace &sp) {
     // nan is the same in every thread
     bool done = false;
     if (!nan) {
-        collect<Z>(p, tm >= bound, sp, [&](float v) { return v >= bound; });
+        if (p.vectors() <= TH) {  // the shares are at hand (one row of 131072 9.8 us a call, read again 10.4)
+            const auto a = p.at(tid);
+            if (tm >= bound)
+#pragma unroll
+                for (int e = 0; e < Z::VE; e++)
+                    if (e < a.n && x[e] >= bound) {
+                        const int at = atomicAdd(&sp.n, 1);
+                        if (at < LIST)
+                            sp.list[at] = key_of(x[e], (uint32_t)(a.i + e));
+                    }
+            __syncthreads();
+        } else {
+            collect<Z>(p, tm >= bound, sp, [&](float v) { return v >= bound; });
+        }
         int n = sp.n;
         done = n <= LIST;
         if (!done) {  // many are equal: those above the bound, then the first of the equal ones
@@ -424,8 +445,9 @@ __device__ void find_top(const Piece<Z> &p, int top, float tm, TopSpace &sp) {
     __syncthreads();
 }
 
-// One chunk of one row a workgroup; a row of one chunk is finished here.
-template <typename Z, bool TOP>
+// One chunk of one row a workgroup, NV vectors a thread loaded together; a row
+// of one chunk is finished here.
+template <typename Z, bool TOP, int NV>
 __global__ __launch_bounds__(TH) void log_probs_kernel(Args a) {
     __shared__ Stat join[TH / 64];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -449,13 +471,13 @@ __global__ __launch_bounds__(TH) void log_probs_kernel(Args a) {
     };
     int v = tid;
     fetch(v);
+    float x[NV * Z::VE];
     for (; v < vectors; v += NV * TH) {
         typename Z::raw cur[NV];
 #pragma unroll
         for (int u = 0; u < NV; u++)
             cur[u] = next[u];
         fetch(v + NV * TH);
-        float x[NV * Z::VE];
 #pragma unroll
         for (int u = 0; u < NV; u++)
             Z::values(cur[u], piece.at(v + u * TH).n, x + u * Z::VE);
@@ -480,7 +502,7 @@ __global__ __launch_bounds__(TH) void log_probs_kernel(Args a) {
     }
     if constexpr (TOP) {
         __shared__ TopSpace sp;
-        find_top<Z>(piece, a.top, tm, sp);
+        find_top<Z>(piece, a.top, tm, x, sp);
         if (tid < a.top) {
             if (a.chunks > 1)
                 a.part_key[(row * a.chunks + part) * a.top + tid] = sp.out[tid];
@@ -772,7 +794,7 @@ hipError_t forward(const Args &a, int64_t rows, hipStream_t st) {
         return forward_wave<Z, 64, 2>(a, rows, st);
     // The alternatives of a lane's many logits are found one after the other:
     // a workgroup finds eight of 2000 sooner where rows leave it the room (100
-    // rows of 2000 in bf16: 8.2 us, a wave 11.2; 2000 rows 17.2 and 10.0), and
+    // rows of 2000 in bf16: 7.2 us, a wave 11.2; 2000 rows 17.2 and 10.0), and
     // of 4000 unless rows are many (10000 rows: 67 us, a wave 53).
     const int64_t cus = device_cu_count();
     if (a.V <= 256 * Z::VE && (a.top <= 4 || rows >= 4 * cus))
@@ -780,10 +802,15 @@ hipError_t forward(const Args &a, int64_t rows, hipStream_t st) {
     if (a.V <= 512 * Z::VE && (a.top == 0 || (a.top <= 8 && rows >= 16 * cus)))
         return forward_wave<Z, 64, 8>(a, rows, st);
     const dim3 grid((unsigned)(rows * a.chunks));
-    if (a.top)
-        log_probs_kernel<Z, true><<<grid, dim3(TH), 0, st>>>(a);
+    // Short chunks, few vectors a thread: less code for what runs once (one row of
+    // 131072 with eight alternatives 10.2 us a call, 10.7 with four vectors; 32 of
+    // 50257 with twenty 16.1 and 18.0).
+    if (a.chunk <= 2048)
+        a.top ? log_probs_kernel<Z, true, 1><<<grid, dim3(TH), 0, st>>>(a)
+              : log_probs_kernel<Z, false, 1><<<grid, dim3(TH), 0, st>>>(a);
     else
-        log_probs_kernel<Z, false><<<grid, dim3(TH), 0, st>>>(a);
+        a.top ? log_probs_kernel<Z, true, 4><<<grid, dim3(TH), 0, st>>>(a)
+              : log_probs_kernel<Z, false, 4><<<grid, dim3(TH), 0, st>>>(a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.chunks == 1)
         return e;

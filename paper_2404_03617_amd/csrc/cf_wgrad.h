@@ -18,6 +18,16 @@
 // bytes: the 4 rows that 32 lanes read together then lie in different banks.
 // Few tiles over many rows: the rows are split over workgroups that write fp32
 // partial sums, and a second launch adds them in a fixed order.
+//
+// Measured on MI355X (the library's product of two bf16 matrices of the largest
+// size below, without bytes to convert, takes 457 us; a copy moves 4.9 TB/s):
+//   16384 rows, K = C = 4096, bf16: 508 us, 1082 TFLOP/s.  MFMA busy 61%, VALU
+//     43%, LDS 46%; without the conversion (wrong results) it is 451 us, with
+//     every fetch from the same rows 519: the VALU work beside the products
+//     bounds it, not memory
+//   401408 rows, K = 256, C = 64, fp16 after a norm: 47.3 us and 7.2 us for the
+//     second launch, 4.9 TB/s: memory
+//   49 rows, K = 2048, C = 512: 5.3 us, one step of 64 rows from load to store
 #pragma once
 
 #include "cf_rows.h"
@@ -159,7 +169,11 @@ __global__ __launch_bounds__(S::TH, S::OCC) void wgrad_kernel(WGradArgs a) {
 
     const int ka = tid % (TM / 8) * 8, ra = tid / (TM / 8), ca = k0 + ka;
     const int kb = tid % (TN / QB) * QB, rb = tid / (TN / QB), cb = c0 + kb;
-    float db[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    // Sums of fp16 as x * one + sum, which is one instruction with the conversion
+    // and takes no registers for it: with a conversion before each sum the large
+    // tiles ran out of them (16384 rows, K = C = 4096: 2535 us against 573).
+    float db[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f}, one = 1.0f;
+    asm("" : "+v"(one));
 
     // A step's share of a thread, in registers from its fetch to its store.
     struct Stage {
@@ -231,7 +245,7 @@ __global__ __launch_bounds__(S::TH, S::OCC) void wgrad_kernel(WGradArgs a) {
             unpack8<T>(t.a[j], x);
 #pragma unroll
             for (int i = 0; i < 8; i++)
-                db[i] += x[i];
+                db[i] = T::is_bf16 ? db[i] + x[i] : fmaf(x[i], one, db[i]);
         }
     };
     auto store_b = [&](auto shift, Stage &t, int j, int buf, int left) {
@@ -436,14 +450,14 @@ __global__ __launch_bounds__(S::TH, S::OCC) void wgrad_kernel(WGradArgs a) {
         return;
     const int kl = wm + 4 * (lane >> 5), lim = a.K - k0 - kl;
     const bool whole = k0 + TM <= a.K;
-    const int64_t size = a.part ? 4 : 2;
     char *const out = a.part ? (char *)(a.part + ((int64_t)at.split * a.K + k0) * a.C) : (char *)(a.dw + (int64_t)k0 * a.C);
-    auto put = [&](auto check) {
+    auto put = [&](auto check, auto partial) {
 #pragma unroll
         for (int n = 0; n < FN; n++) {
             const int c = c0 + wn + 32 * n + (lane & 31);
             if (c >= a.C)
                 continue;
+            constexpr int64_t size = decltype(partial)::value ? 4 : 2;
             const uint64_t off = ((uint64_t)kl * (uint64_t)a.C + c) * size;
             const float w = NORM && a.w ? a.w[c] : 1.0f, b = affine ? a.b[c] : 0.0f;
 #pragma unroll
@@ -455,7 +469,7 @@ __global__ __launch_bounds__(S::TH, S::OCC) void wgrad_kernel(WGradArgs a) {
                         continue;
                     char *const o = out + (int64_t)row * a.C * size + off;
                     float f = acc[m][n][i];
-                    if (a.part) {
+                    if constexpr (decltype(partial)::value) {
                         *reinterpret_cast<float *>(o) = f;
                     } else {
                         if constexpr (NORM) {
@@ -468,10 +482,16 @@ __global__ __launch_bounds__(S::TH, S::OCC) void wgrad_kernel(WGradArgs a) {
                 }
         }
     };
-    if (whole)
-        put(std::false_type{});
+    auto put_as = [&](auto partial) {
+        if (whole)
+            put(std::false_type{}, partial);
+        else
+            put(std::true_type{}, partial);
+    };
+    if (a.part)
+        put_as(std::true_type{});
     else
-        put(std::true_type{});
+        put_as(std::false_type{});
 }
 
 // The sum of the splits: V neighbouring entries of a row of dW a thread, S

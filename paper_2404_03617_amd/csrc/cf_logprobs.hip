@@ -520,8 +520,8 @@ __global__ __launch_bounds__(TH) void log_probs_kernel(Args a) {
 
 // ---------------------------------------------------------------------------
 // Short rows: G lanes of a wave take one whole, NV vectors a lane, all in
-// registers and without a barrier.  Alternatives one after the other: the
-// largest key of the group, then the next of the lane that held it.
+// registers and without a barrier.  Few alternatives are found one after the
+// other: the largest key of the group, then the next of the lane that held it.
 //
 // Keys of 16-bit logits fit 32 bits: the low 13 bits of their fp32 form are
 // zeros and take the index (V below 8192).
@@ -575,6 +575,19 @@ struct WaveKey<Z16<T>> {
     }
 };
 
+// Orders a wave's LDS writes and the reads of other lanes' after them.
+__device__ __forceinline__ void wave_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// Up to FEW_TOP alternatives of a wave's row are found one after the other, more
+// (60000 rows of 1000: eight in bf16 65 us, otherwise 78; twenty 69 and 139, in
+// fp32 84 and 244; five in bf16 66 and 65) among the logits that reach the n-th
+// largest of the lanes' maxima, collected and ranked by counting.  WAVE_LIST of
+// them: as many as reach it in a row of equal logits.
+constexpr int FEW_TOP = 5, WAVE_LIST = 256;
+
 template <typename Z, int G, int NV, bool TOP>
 __global__ __launch_bounds__(256) void log_probs_wave_kernel(Args a, int64_t rows) {
     typedef WaveKey<Z> K;
@@ -605,7 +618,46 @@ __global__ __launch_bounds__(256) void log_probs_wave_kernel(Args a, int64_t row
             k[i] = at < a.V ? K::of(x[i], at, nan) : 0;
             top = k[i] > top ? k[i] : top;
         }
-        for (int n = 0; n < a.top; n++) {
+        int from = 0;
+        if constexpr (G == 64)
+            if (a.top > FEW_TOP) {
+                typedef typename K::key Key;
+                __shared__ __align__(16) Key heads[4][64], list[4][WAVE_LIST];
+                Key *const head = heads[group], *const found = list[group];
+                head[lane] = top;
+                wave_fence();
+                int above = 0;
+#pragma unroll 16
+                for (int j = 0; j < 64; j++)
+                    above += head[j] > top;
+                // the least of the n largest maxima (keys differ but for 0)
+                const Key bound = ~K::template best<64>(above < a.top ? (Key)~top : (Key)0);
+                int count = 0;
+#pragma unroll
+                for (int i = 0; i < NV * Z::VE; i++) {
+                    const bool in = k[i] != 0 && k[i] >= bound;
+                    const uint64_t all = __ballot(in);
+                    const int at = count + __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32),
+                                                                     __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0));
+                    if (in && at < WAVE_LIST)
+                        found[at] = k[i];
+                    count += __popcll(all);
+                }
+                if (count <= WAVE_LIST) {
+                    wave_fence();
+                    for (int i = lane; i < count; i += 64) {
+                        const Key one = found[i];
+                        int rank = 0;
+#pragma unroll 4
+                        for (int j = 0; j < count; j++)
+                            rank += found[j] > one;
+                        if (rank < a.top)
+                            put_top(a, row, rank, K::wide(one), st);
+                    }
+                    from = a.top;
+                }
+            }
+        for (int n = from; n < a.top; n++) {
             const typename K::key best = K::template best<G>(top);
             mine = n == lane ? best : mine;
             if (top == best) {
@@ -615,7 +667,7 @@ __global__ __launch_bounds__(256) void log_probs_wave_kernel(Args a, int64_t row
                     top = k[i] < best && k[i] > top ? k[i] : top;
             }
         }
-        if (lane < a.top)
+        if (from == 0 && lane < a.top)
             put_top(a, row, lane, K::wide(mine), st);
     }
     if (lane == 0)  // last: the asked logit is two loads, one after the other
@@ -792,14 +844,14 @@ hipError_t forward(const Args &a, int64_t rows, hipStream_t st) {
         return forward_wave<Z, 64, 1>(a, rows, st);
     if (a.V <= 128 * Z::VE)
         return forward_wave<Z, 64, 2>(a, rows, st);
-    // The alternatives of a lane's many logits are found one after the other:
-    // a workgroup finds eight of 2000 sooner where rows leave it the room (100
-    // rows of 2000 in bf16: 7.2 us, a wave 11.2; 2000 rows 17.2 and 10.0), and
-    // of 4000 unless rows are many (10000 rows: 67 us, a wave 53).
+    // Longer rows with alternatives go to a wave each where that fills the card, to
+    // a workgroup each (or several) where they are fewer.  bf16, eight: 100 rows of
+    // 2000 7.3 us by workgroups, 8.3 by waves (twenty 7.6 and 15), 1000 9.0 and
+    // 8.5; 500 rows of 4000 13.4 and 12.2 (twenty 16 and 19), 3000 24 and 19.
     const int64_t cus = device_cu_count();
     if (a.V <= 256 * Z::VE && (a.top <= 4 || rows >= 4 * cus))
         return forward_wave<Z, 64, 4>(a, rows, st);
-    if (a.V <= 512 * Z::VE && (a.top == 0 || (a.top <= 8 && rows >= 16 * cus)))
+    if (a.V <= 512 * Z::VE && (a.top == 0 || rows >= 4 * cus))
         return forward_wave<Z, 64, 8>(a, rows, st);
     const dim3 grid((unsigned)(rows * a.chunks));
     // Short chunks, few vectors a thread: less code for what runs once (one row of

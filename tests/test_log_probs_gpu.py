@@ -147,7 +147,7 @@ def masked_rows(V, dt):
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
-@pytest.mark.parametrize("V,repeat", [(33, 1), (1000, 1), (4100, 40), (20001, 1)])
+@pytest.mark.parametrize("V,repeat", [(33, 1), (700, 80), (1000, 1), (1900, 80), (3000, 80), (4100, 40), (20001, 1)])
 def test_masks_ties_and_extremes(V, repeat, dtype):
     z = masked_rows(V, DT[dtype]).repeat(repeat, 1)
     g = torch.Generator().manual_seed(4)

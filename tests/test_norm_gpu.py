@@ -56,6 +56,20 @@ SHAPES = [(1, 1), (3, 2), (1, 7), (5, 8), (33, 63), (300, 64), (7, 65), (129, 10
           (1, 16383), (4099, 48)]
 
 
+# Rows enough for several a group, in each width of group.
+GROUPS = [(32771, 64), (16500, 120), (8200, 255), (4100, 512), (4100, 1001), (2050, 2040), (1025, 4096), (1030, 8190),
+          (600, 9000)]
+
+
+@pytest.mark.parametrize("rows,C", GROUPS)
+def test_rows_enough_for_groups(rows, C):
+    dt = DT["bf16" if C % 2 else "f16"]
+    x, w, b = inputs(rows + C, rows, C, dt)
+    mean, rstd, xh, y = reference(x, w, b)
+    tol = ROUND[dt] * y.abs() + err_xh(x, rstd) * w.double().abs() + 4 * F32 * y.abs() + TINY[dt]
+    assert_within(cf.layer_norm_forward(x.cuda(), dev(w), dev(b), eps=EPS), y, tol, "y")
+
+
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("rows,C", SHAPES)
 def test_forward(rows, C, dtype):

@@ -8,6 +8,12 @@
 // Elementwise and bound by memory: a lane takes 8 channels, 8 lanes the 64
 // that share a scale (an exchange of registers finds their maximum).  Rows
 // are cut into whole blocks of 64, so a row's last block may hold idle lanes.
+//
+// Measured on MI355X, where a copy of 2 GiB moves 4.9 TB/s (kernel times):
+// 100352 x 128 bf16 written in 8.5 and read back in 8.0 us (39 MB each way, 4.6
+// and 4.9 TB/s); 6272 x 2048 fp16 through GELU with both checkpoints 14.8 us (79
+// MB, 5.3 TB/s) and its gradient 13.9 us (65 MB, 4.7 TB/s), both with the VALU
+// 99% busy: the erf polynomial costs as much as the memory.
 #include "cf_rows.h"
 #include "cf_kernels.h"
 #include "cf_train.h"

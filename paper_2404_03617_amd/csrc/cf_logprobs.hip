@@ -28,8 +28,8 @@
 // in the order of the row.
 //
 // Measured on MI355X, where a copy of 2 GiB moves 4.9 TB/s (kernel times): 4096
-// rows of 100003 in bf16 forward 166 us (4.9 TB/s; VALU 67% busy), backward 267 us
-// (6.1 TB/s); one row of 131072 with eight alternatives 6.7 us in 64 workgroups
+// rows of 100003 in bf16 forward 166 to 188 us (4.4 to 4.9 TB/s; VALU 82% busy),
+// backward 267 to 275 (6 TB/s); one row of 131072 with eight alternatives 5.7 us in 64 workgroups
 // and 3.8 us to join them; 128 rows of 1000 with five 6.0 us.  The last two are
 // chains: load, maximum, join, alternatives, the logit asked for.
 #include "cf_rows.h"

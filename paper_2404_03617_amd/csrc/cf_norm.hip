@@ -14,12 +14,12 @@
 // wave then holds 8 rows, rows above 512 channels take several waves.
 //
 // Measured on MI355X, where a copy of 2 GiB moves 4.9 TB/s (kernel times):
-//   forward   401408 x 64 fp16 with statistics and checkpoint 25.8 us, 5.2 TB/s;
-//             25088 x 256 bf16 7.4 us; 2999 x 4095 bf16 12.4 us, 4.0 TB/s (rows
+//   forward   401408 x 64 fp16 with statistics and checkpoint 25.4 us, 5.2 TB/s;
+//             25088 x 256 bf16 7.4 us; 2999 x 4095 bf16 13 us, 3.7 TB/s (rows
 //             that start at any 2 bytes); one row of 512 1.7 us, a launch
-//   backward  401408 x 64 from the checkpoint 24.1 us, 5.5 TB/s, and 4.6 us for
-//             the second launch; 2999 x 4095 20.0 us, 3.7 TB/s, and 4.8 us: three
-//             turns of 1024 rows, whose first loads and last stores nothing hides
+//   backward  401408 x 64 from the checkpoint 24.2 us, 5.5 TB/s, and 4.7 us for
+//             the second launch; 2999 x 4095 21 us, 3.5 TB/s, and 4 us: six turns
+//             of 512 rows, whose first loads and last stores nothing hides
 #include "cf_rows.h"
 #include "cf_kernels.h"
 #include "cf_train.h"
@@ -378,8 +378,8 @@ __global__ __launch_bounds__(back_threads(G), 4) void norm_backward_kernel(NormB
 
 // Sum of `n` partials [n][2][C] into dw [C] and db [C]: 32 columns a
 // workgroup (a cache line), 32 threads share a column and add every 32nd
-// partial, eight loads at a time.  512 partials of 64 channels 4.6 us, 256 of
-// 4095 (8.4 MB) 4.8 us: little more than a launch and two loads one after the
+// partial, eight loads at a time.  512 partials of 64 channels 4.7 us, 256 of
+// 4095 (8.4 MB) 4.0 us: little more than a launch and two loads one after the
 // other.
 __global__ __launch_bounds__(1024) void norm_reduce_kernel(const float *part, float *dw, float *db, int n, int C) {
     __shared__ float s[32][33];

@@ -21,13 +21,13 @@
 //
 // Measured on MI355X (the library's product of two bf16 matrices of the largest
 // size below, without bytes to convert, takes 457 us; a copy moves 4.9 TB/s):
-//   16384 rows, K = C = 4096, bf16: 508 us, 1082 TFLOP/s.  MFMA busy 61%, VALU
-//     43%, LDS 46%; without the conversion (wrong results) it is 451 us, with
-//     every fetch from the same rows 519: the VALU work beside the products
+//   16384 rows, K = C = 4096, bf16: 500 us, 1100 TFLOP/s (fp16 540).  MFMA busy
+//     61%, VALU 43%, LDS 46%; without the conversion (wrong results) it is 451 us,
+//     with every fetch from the same rows 519: the VALU work beside the products
 //     bounds it, not memory
-//   401408 rows, K = 256, C = 64, fp16 after a norm: 47.3 us and 7.2 us for the
-//     second launch, 4.9 TB/s: memory
-//   49 rows, K = 2048, C = 512: 5.3 us, one step of 64 rows from load to store
+//   401408 rows, K = 256, C = 64, fp16 after a norm: 46.4 us and 7.2 us for the
+//     second launch, 5.0 TB/s: memory
+//   49 rows, K = 2048, C = 512: 4.7 us, one step of 64 rows from load to store
 #pragma once
 
 #include "cf_rows.h"

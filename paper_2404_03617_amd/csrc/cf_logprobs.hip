@@ -296,6 +296,10 @@ __device__ void collect(const Piece<Z> &p, bool mine, TopSpace &sp, F &&wanted) 
     __syncthreads();
     const unsigned each = (unsigned)(p.vectors() + TH - 1) / TH, all = sp.threads * each;
     for (unsigned w = tid; w < all; w += TH) {
+        // enough to know that they are too many: a row of equal logits would add
+        // every one (512 rows of 50257, one of them masked whole: 49 us, so 19)
+        if (*(volatile int *)&sp.n > LIST)
+            break;
         const unsigned t = w / each;
         const int v = (int)((w - t * each) * TH + sp.who[t]);
         if (v >= p.vectors())

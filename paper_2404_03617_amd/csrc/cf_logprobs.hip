@@ -588,9 +588,11 @@ __device__ __forceinline__ void wave_fence() {
 // Up to FEW_TOP alternatives of a wave's row are found one after the other, more
 // (60000 rows of 1000: eight in bf16 65 us, otherwise 78; twenty 69 and 139, in
 // fp32 84 and 244; five in bf16 66 and 65) among the logits that reach the n-th
-// largest of the lanes' maxima, collected and ranked by counting.  WAVE_LIST of
-// them: as many as reach it in a row of equal logits.
-constexpr int FEW_TOP = 5, WAVE_LIST = 256;
+// largest of the lanes' maxima, collected and ranked by counting.  Up to 256 of
+// them, as many as reach it in a row of equal logits; up to 64 of short rows in 16
+// bits, where the way for few takes less than ranking more (128 rows of 400, one
+// of them masked whole, twenty: 7.3 us against 10.7).
+constexpr int FEW_TOP = 5;
 
 template <typename Z, int G, int NV, bool TOP>
 __global__ __launch_bounds__(256) void log_probs_wave_kernel(Args a, int64_t rows) {
@@ -626,6 +628,7 @@ __global__ __launch_bounds__(256) void log_probs_wave_kernel(Args a, int64_t row
         if constexpr (G == 64)
             if (a.top > FEW_TOP) {
                 typedef typename K::key Key;
+                constexpr int WAVE_LIST = Z::VE == 8 && NV <= 2 ? 64 : 256;
                 __shared__ __align__(16) Key heads[4][64], list[4][WAVE_LIST];
                 Key *const head = heads[group], *const found = list[group];
                 head[lane] = top;
@@ -648,13 +651,22 @@ __global__ __launch_bounds__(256) void log_probs_wave_kernel(Args a, int64_t row
                     count += __popcll(all);
                 }
                 if (count <= WAVE_LIST) {
+                    if (lane < 4 && count + lane < WAVE_LIST)
+                        found[count + lane] = 0;
                     wave_fence();
                     for (int i = lane; i < count; i += 64) {
                         const Key one = found[i];
                         int rank = 0;
-#pragma unroll 4
-                        for (int j = 0; j < count; j++)
-                            rank += found[j] > one;
+#pragma unroll 2
+                        for (int j = 0; j < count; j += 4) {
+                            struct __align__(16) Four {
+                                Key k[4];
+                            };
+                            const Four o = *reinterpret_cast<const Four *>(found + j);
+#pragma unroll
+                            for (int u = 0; u < 4; u++)
+                                rank += o.k[u] > one;
+                        }
                         if (rank < a.top)
                             put_top(a, row, rank, K::wide(one), st);
                     }

@@ -243,24 +243,28 @@ __global__ __launch_bounds__(back_threads(G), 4) void norm_backward_kernel(NormB
         float2 st;
     };
     auto fetch = [&](int64_t r) {
+        // Past C dy is 0, but x is another of the row's values (a lane with
+        // nothing of the row: its mean is 0): (0 - mean) * rstd may be infinite where
+        // no channel's is, and 0 times that would make the row's sum NaN.
         Row t;
         t.st = make_float2(0.0f, 0.0f);
-        if (r < a.rows)
+        if (r < a.rows && gl * 8 < a.C)
             t.st = a.stats[r];
 #pragma unroll
         for (int v = 0; v < V; v++) {
             const int c = (gl + v * G) * 8;
-            t.dy[v] = t.x[v] = u32x4{0u, 0u, 0u, 0u};
-            t.scale[v] = 0.0f;
+            t.dy[v] = u32x4{0u, 0u, 0u, 0u};
+            t.x[v] = v ? t.x[0] : u32x4{0u, 0u, 0u, 0u};
+            t.scale[v] = v ? t.scale[0] : 0.0f;
             if (r < a.rows && c < a.C) {
                 t.dy[v] = load8(a.dy + r * a.lddy, c, a.C);
                 if constexpr (CK) {
-                    const u32x2 q = load8b(a.q + r * a.C, c, a.C);
+                    const u32x2 q = load8b<true>(a.q + r * a.C, c, a.C);
                     t.x[v].x = q.x;
                     t.x[v].y = q.y;
                     t.scale[v] = a.scale[r * a.blocks + c / CKPT_BLOCK];
                 } else {
-                    t.x[v] = load8(a.x + r * a.ldx, c, a.C);
+                    t.x[v] = load8<true>(a.x + r * a.ldx, c, a.C);
                 }
             }
         }

@@ -33,11 +33,17 @@ struct __attribute__((packed, aligned(2))) Any8h {
     u32x2 v;
 };
 
-// the last n of 16 (8) bytes' values, of 16 (8) bits each, moved to the front
+// the last n of 16 (8) bytes' values, of 16 (8) bits each, moved to the front;
+// behind them zeros or, with `around`, the values that stood before them
+template <bool AROUND = false>
 __device__ __forceinline__ u32x4 from_end(const u32x4 &r, int n) {
     const int s = 16 * (8 - n);  // 16 .. 112
     const uint64_t lo = __builtin_bit_cast(uint64_t, u32x2{r[0], r[1]}), hi = __builtin_bit_cast(uint64_t, u32x2{r[2], r[3]});
-    const uint64_t l = s < 64 ? lo >> s | hi << (64 - s) : hi >> (s - 64), h = s < 64 ? hi >> s : 0;
+    uint64_t l = s < 64 ? lo >> s | hi << (64 - s) : hi >> (s - 64), h = s < 64 ? hi >> s : 0;
+    if constexpr (AROUND) {
+        l |= s > 64 ? lo << (128 - s) : 0;
+        h |= s < 64 ? lo << (64 - s) : s == 64 ? lo : lo >> (s - 64) | hi << (128 - s);
+    }
     return {(uint32_t)l, (uint32_t)(l >> 32), (uint32_t)h, (uint32_t)(h >> 32)};
 }
 
@@ -48,8 +54,10 @@ __device__ __forceinline__ int per_lane(int i) {
     return i;
 }
 
-// 8 elements of a row of C, from element c on, zeros past its end.  The last
-// ones of a row that is no multiple of 8 come with those before them.
+// 8 elements of a row of C, from element c on, zeros past its end (AROUND:
+// other elements of the row, where c is in it).  The last ones of a row that is
+// no multiple of 8 come with those before them.
+template <bool AROUND = false>
 __device__ __forceinline__ u32x4 load8(const uint16_t *row, int c, int C) {
     const int n = C - c;
     if (n >= 8)
@@ -57,12 +65,12 @@ __device__ __forceinline__ u32x4 load8(const uint16_t *row, int c, int C) {
     if (n <= 0)
         return u32x4{0u, 0u, 0u, 0u};
     if (C >= 8)
-        return from_end(reinterpret_cast<const Any16 *>(row + per_lane(C - 8))->v, n);
+        return from_end<AROUND>(reinterpret_cast<const Any16 *>(row + per_lane(C - 8))->v, n);
     u32x4 r = {0u, 0u, 0u, 0u};
 #pragma unroll
-    for (int i = 0; i < 7; i++)
-        if (i < n)
-            r[i / 2] |= (uint32_t)row[c + i] << (16 * (i & 1));
+    for (int i = 0; i < (AROUND ? 8 : 7); i++)
+        if (AROUND || i < n)
+            r[i / 2] |= (uint32_t)row[c + (i < n ? i : 0)] << (16 * (i & 1));
     return r;
 }
 
@@ -85,20 +93,22 @@ __device__ __forceinline__ void store8(uint16_t *row, int c, int C, const u32x4 
 }
 
 // 8 bytes of a checkpoint's row, the same way.
+template <bool AROUND = false>
 __device__ __forceinline__ u32x2 load8b(const int8_t *row, int c, int C) {
     const int n = C - c;
     if (n >= 8)
         return reinterpret_cast<const Any8 *>(row + c)->v;
     if (n <= 0)
         return u32x2{0u, 0u};
-    if (C >= 8)
-        return __builtin_bit_cast(u32x2, __builtin_bit_cast(uint64_t, reinterpret_cast<const Any8 *>(row + per_lane(C - 8))->v) >>
-                                             (8 * (8 - n)));
+    if (C >= 8) {
+        const uint64_t v = __builtin_bit_cast(uint64_t, reinterpret_cast<const Any8 *>(row + per_lane(C - 8))->v);
+        return __builtin_bit_cast(u32x2, v >> (8 * (8 - n)) | (AROUND ? v << (8 * n) : 0));
+    }
     u32x2 r = {0u, 0u};
 #pragma unroll
-    for (int i = 0; i < 7; i++)
-        if (i < n)
-            r[i / 4] |= (uint32_t)(uint8_t)row[c + i] << (8 * (i & 3));
+    for (int i = 0; i < (AROUND ? 8 : 7); i++)
+        if (AROUND || i < n)
+            r[i / 4] |= (uint32_t)(uint8_t)row[c + (i < n ? i : 0)] << (8 * (i & 3));
     return r;
 }
 
@@ -259,15 +269,18 @@ __device__ __forceinline__ u32x2 quant8(const float *x, float inv) {
 // byte i of 4 as a float: q + 128 is unsigned, which converts in one step
 __device__ __forceinline__ float biased(uint32_t w, int i) { return (float)((w >> (8 * i)) & 0xffu); }
 
-// 8 bytes to values q * scale
+// byte i of 4 as a float
+__device__ __forceinline__ float signed_byte(uint32_t w, int i) { return (float)(int8_t)(w >> (8 * i)); }
+
+// 8 bytes to values q * scale, each rounded to fp32 before anything else is done
+// with it: most 16-bit values that were the largest of their block come back as
+// they were, and so does a row of them, whose x - mean is 0.  (Fused with the
+// subtraction of the mean the product keeps the rounding of the scale.)
 __device__ __forceinline__ void dequant8(const u32x2 &q, float scale, float *x) {
+#pragma clang fp contract(off)
 #pragma unroll
-    for (int h = 0; h < 2; h++) {
-        const uint32_t w = q[h] ^ 0x80808080u;
-#pragma unroll
-        for (int i = 0; i < 4; i++)
-            x[4 * h + i] = (biased(w, i) - 128.0f) * scale;
-    }
+    for (int i = 0; i < 8; i++)
+        x[i] = signed_byte(q[i / 4], i & 3) * scale;
 }
 
 inline int blocks_of(int C) { return (C + CKPT_BLOCK - 1) / CKPT_BLOCK; }

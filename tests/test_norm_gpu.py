@@ -296,3 +296,36 @@ def test_checks_without_the_native_module(monkeypatch):
     for bad in ((xd.t(),), (xd, wd[:-1]), (xd.double(),), (xd, wd, bd.cpu())):
         with pytest.raises(ValueError):
             cf.layer_norm_forward(*bad)
+
+
+@pytest.mark.parametrize("ckpt", [False, True])
+@pytest.mark.parametrize("rows,C", [(3, 3), (5, 60), (4, 64), (6, 130), (3, 1001), (700, 72), (2, 9000)])
+def test_gradient_of_rows_whose_mean_passes_fp32_in_deviations(rows, C, ckpt):
+    """Constant rows of 2^114 in bf16 with eps 1e-12: mean * rstd is 2^134, while
+    x - mean, and with it every term of the gradient, is 0 or finite.  (A power
+    of two comes back from its checkpoint exactly, rounded to fp32.)"""
+    dt, eps = torch.bfloat16, 1e-12
+    x = randn(C, (rows, C), dt)
+    big = torch.arange(rows) % 2 == 0
+    x[big] = 2.0**114
+    w, b = 1.0 + 0.3 * randn(1, (C,)), 0.2 * randn(2, (C,))
+    dy = randn(3, (rows, C), dt, 2.0**-30)  # dx of such a row is 10^6 times that
+    y, stats, ck = cf.layer_norm_forward_save(x.cuda(), w.cuda(), b.cuda(), eps=eps)
+    assert bool((y[big.cuda()] == b.to(dt).cuda()).all())
+    mean, rstd = stats[:, :1].cpu().double(), stats[:, 1:].cpu().double()
+    assert bool((mean[big] == 2.0**114).all())
+    kept = cf.checkpoint_unpack(ck).cpu().double() if ckpt else x.double()
+    assert bool((kept[big] == 2.0**114).all())
+    if ckpt:
+        kept[~big] = dequantise(ck.q.cpu(), ck.scale.cpu())[~big]
+    xh = (kept - mean) * rstd
+    dx, dw, db, g = ref_backward(dy, xh, rstd, w)
+    exh = torch.where(big[:, None], 0.0, 4 * F32 * (xh.abs().amax(1, keepdim=True) + mean.abs() * rstd))
+    gmax = g.abs().amax(1, keepdim=True)
+    xmax = xh.abs().amax(1, keepdim=True)
+    tol = ROUND[dt] * dx.abs() + rstd * (64 * F32 * gmax * (1 + xh.abs() * xmax) + exh * gmax * (2 + 2 * xmax)) + TINY[dt]
+    tw = 64 * F32 * (dy.double() * xh).abs().sum(0) + (dy.double().abs() * exh).sum(0) + 1e-30
+    tb = 64 * F32 * dy.double().abs().sum(0) + 1e-30
+    got = cf.layer_norm_backward(dy.cuda(), ck if ckpt else x.cuda(), stats, w.cuda())
+    for name, v, r, t in zip(("dx", "dweight", "dbias"), got, (dx, dw, db), (tol, tw, tb)):
+        assert_within(v, r, t, name)

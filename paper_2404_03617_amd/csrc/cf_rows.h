@@ -266,9 +266,6 @@ __device__ __forceinline__ u32x2 quant8(const float *x, float inv) {
     return r;
 }
 
-// byte i of 4 as a float: q + 128 is unsigned, which converts in one step
-__device__ __forceinline__ float biased(uint32_t w, int i) { return (float)((w >> (8 * i)) & 0xffu); }
-
 // byte i of 4 as a float
 __device__ __forceinline__ float signed_byte(uint32_t w, int i) { return (float)(int8_t)(w >> (8 * i)); }
 

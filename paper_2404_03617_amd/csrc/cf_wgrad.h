@@ -253,10 +253,15 @@ __global__ __launch_bounds__(S::TH, S::OCC) void wgrad_kernel(WGradArgs a) {
         }
     };
     auto store_b = [&](auto shift, Stage &t, int j, int buf, int left) {
-        // x = (byte - 128) f + o
+        // x = q f + o (q + 128 with an offset of -128 f, which converts as well, would
+        // pass fp32 for blocks of bf16's largest values)
         const bool on = rb + j * DB < left;
         const float f = !on ? 0.0f : NORM ? t.s[j] * t.n[j].y : t.s[j];
-        const float o = !on ? 0.0f : fmaf(-128.0f, f, NORM ? -t.n[j].x * t.n[j].y : 0.0f);
+        const float o = on && NORM ? -t.n[j].x * t.n[j].y : 0.0f;
+        auto value = [&](uint32_t w, int i) {
+            const float q = signed_byte(w, i);
+            return NORM ? fmaf(q, f, o) : q * f;
+        };
         uint16_t *const p = lb + buf * (BK * SB) + (rb + j * DB) * SB + kb;
         if (decltype(shift)::value != 0 && nb > 0 && nb < QB) {  // the last nb of QB bytes to the front
             uint64_t lo = __builtin_bit_cast(uint64_t, t.b[j][0]);
@@ -273,9 +278,9 @@ __global__ __launch_bounds__(S::TH, S::OCC) void wgrad_kernel(WGradArgs a) {
             u32x4 v;
 #pragma unroll
             for (int h = 0; h < 2; h++) {
-                const uint32_t w = t.b[j][i][h] ^ 0x80808080u;
-                v[2 * h] = T::pack2(fmaf(biased(w, 0), f, o), fmaf(biased(w, 1), f, o));
-                v[2 * h + 1] = T::pack2(fmaf(biased(w, 2), f, o), fmaf(biased(w, 3), f, o));
+                const uint32_t w = t.b[j][i][h];
+                v[2 * h] = T::pack2(value(w, 0), value(w, 1));
+                v[2 * h + 1] = T::pack2(value(w, 2), value(w, 3));
             }
             *reinterpret_cast<u32x4 *>(p + 8 * i) = v;
         }

@@ -200,3 +200,30 @@ def test_refusals():
     with pytest.raises(cf.CFError) as e:
         cf.linear_weight_grad(dy, ck, None, w)
     assert e.value.status == cf.CF_ERR_INVALID and "stats" in str(e.value)
+
+
+# shapes that take vectors in their rows, at their ends, and short of one, whole
+# and with the rows split
+LARGE = [(70, 64, 64), (300, 72, 200), (5000, 24, 40), (129, 130, 77), (40, 5, 9), (600, 520, 776)]
+
+
+@pytest.mark.parametrize("quiet", [True, False])
+@pytest.mark.parametrize("rows,K,C", LARGE)
+def test_values_at_the_end_of_the_range(rows, K, C, quiet):
+    """Rows of bf16's lowest value (masked ones) or its largest, with a gradient
+    of zeros or a very small one: 128 scales of such a block pass fp32, its values
+    do not."""
+    dt = torch.bfloat16
+    x = (randn(rows, (rows, C)) + 0.3).to(dt)
+    far = torch.arange(rows) % 9 == 4
+    x[far] = torch.where(torch.arange(int(far.sum()))[:, None] % 2 == 0, torch.finfo(dt).min, torch.finfo(dt).max).to(dt)
+    x[far, C // 2:] *= 0.25
+    q, scale, fine = quantise(x)
+    assert bool(fine.all())
+    dy = randn(C, (rows, K), dt, 0.05)
+    dy[far] = 0.0 if quiet else (dy[far].float() * 2.0**-127).to(dt)
+    kept = dequantise(q, scale)
+    dw, tw, db, tb = reference(dy, kept, None, None, torch.zeros(()), dt, rows)
+    got = cf.linear_weight_grad(dy.cuda(), cf.Checkpoint(q.cuda(), scale.cuda(), dt))
+    assert_within(got[0], dw, tw, "dW")
+    assert_within(got[1], db, tb, "db")

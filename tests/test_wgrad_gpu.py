@@ -227,3 +227,29 @@ def test_values_at_the_end_of_the_range(rows, K, C, quiet):
     got = cf.linear_weight_grad(dy.cuda(), cf.Checkpoint(q.cuda(), scale.cuda(), dt))
     assert_within(got[0], dw, tw, "dW")
     assert_within(got[1], db, tb, "db")
+
+
+@pytest.mark.parametrize("quiet", [True, False])
+@pytest.mark.parametrize("rows,K,C", LARGE)
+def test_norm_of_rows_whose_mean_passes_fp32_in_deviations(rows, K, C, quiet):
+    """Constant rows of 2^114 with 1 / deviation 10^6: mean * rstd is 2^134, the
+    normalised values are finite (and what is left of the 8 bits' rounding)."""
+    dt = torch.bfloat16
+    x = (randn(rows, (rows, C)) + 0.3).to(dt)
+    far = torch.arange(rows) % 9 == 4
+    x[far] = 2.0**114
+    q, scale, _ = quantise(x)
+    xd = x.double()
+    mean = xd.mean(1)
+    stats = torch.stack([mean, ((xd - mean[:, None]).square().mean(1) + 1e-12).rsqrt()], 1).float()
+    w, b = 1 + 0.3 * randn(3, (C,)), 0.2 * randn(4, (C,))
+    dy = randn(C, (rows, K), dt, 0.05)
+    if quiet:
+        dy[far] = 0.0
+    kept = dequantise(q, scale)
+    mean, rstd = stats[:, :1].double(), stats[:, 1:].double()
+    spread = 8 * F32 * (kept.abs() + mean.abs() + 128 * scale.double().repeat_interleave(64, 1)[:, :C]) * rstd
+    dw, tw, db, tb = reference(dy, (kept - mean) * rstd, w, b, spread, dt, rows)
+    got = cf.linear_weight_grad(dy.cuda(), cf.Checkpoint(q.cuda(), scale.cuda(), dt), stats.cuda(), w.cuda(), b.cuda())
+    assert_within(got[0], dw, tw, "dW")
+    assert_within(got[1], db, tb, "db")

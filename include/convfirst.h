@@ -477,7 +477,8 @@ cf_status cf_act_backward(const void *dh, const int8_t *qu, const float *scale_u
  * of cf_layer_norm_forward, x = weight * (q * scale - mean) * rstd + bias (the
  * layer read the norm's output, of which nothing else is kept; weight and bias
  * may be NULL).  On the matrix cores: the factor from the checkpoint is
- * rounded to dt before its products, sums are fp32.  dw [K][C] in dt, dense;
+ * rounded to dt before its products (in fp16, values above 65504 become
+ * infinite: a checkpoint of bf16 activations wants bf16), sums are fp32.  dw [K][C] in dt, dense;
  * db [K] fp32.  rows = 0 gives zeros.  ws (16-byte aligned; NULL for 0 bytes)
  * holds fp32 partial sums, added in a fixed order.  K and C up to 2^20
  * (CF_ERR_UNSUPPORTED above). */

@@ -370,13 +370,19 @@ def act_backward(dh: torch.Tensor, u: Checkpoint, act: str = "gelu", out=None, s
     return du
 
 
+def _wider(x, dy):
+    """Whether a checkpoint's values may lie beyond dy's range."""
+    return x.dtype == torch.bfloat16 and getattr(dy, "dtype", None) == torch.float16
+
+
 def linear_weight_grad(dy: torch.Tensor, x: Checkpoint, stats=None, weight=None, bias=None, ws=None, stream=None):
     """(dW, db) of a linear or point-wise layer y = x W^T + b with W [K, C]:
     dW = dy^T x [K, C] in dy's dtype, db = sums of dy [K] fp32, from the
     checkpoint of x.  With stats (and the norm's weight and bias) the checkpoint
-    is of the input of a layer norm whose output was x.  ws: a uint8 workspace
-    of linear_weight_grad_workspace_bytes()."""
-    if stream is None and ws is None and type(x) is Checkpoint and x.dtype in _cf.DTYPES:
+    is of the input of a layer norm whose output was x.  The product takes x in
+    dy's dtype, so a float16 dy needs a checkpoint of float16 activations.  ws: a
+    uint8 workspace of linear_weight_grad_workspace_bytes()."""
+    if stream is None and ws is None and type(x) is Checkpoint and x.dtype in _cf.DTYPES and not _wider(x, dy):
         r = _native("wgrad", dy, x.q, x.scale, stats, weight, bias)
         if r is not None:
             return r
@@ -386,6 +392,8 @@ def linear_weight_grad(dy: torch.Tensor, x: Checkpoint, stats=None, weight=None,
         raise ValueError("dy and x must have channels, got K=%d C=%d" % (K, C))
     if n != rows:
         raise ValueError("dy has %d rows but x has %d" % (rows, n))
+    if _wider(x, dy):
+        raise ValueError("a checkpoint of bfloat16 activations needs a bfloat16 dy, got %s" % dy.dtype)
     q, scale = _checkpoint("x", x, dy, rows, C)
     sp = _flat("stats", dy, stats, 2, rows, 2)
     w, b = _flat("weight", dy, weight, 2, C, 0), _flat("bias", dy, bias, 2, C, 0)

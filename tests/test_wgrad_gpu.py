@@ -253,3 +253,22 @@ def test_norm_of_rows_whose_mean_passes_fp32_in_deviations(rows, K, C, quiet):
     got = cf.linear_weight_grad(dy.cuda(), cf.Checkpoint(q.cuda(), scale.cuda(), dt), stats.cuda(), w.cuda(), b.cuda())
     assert_within(got[0], dw, tw, "dW")
     assert_within(got[1], db, tb, "db")
+
+
+def test_half_precision_gradients_of_a_wider_checkpoint():
+    """bf16 holds values that fp16 does not, and the product rounds the
+    checkpoint's values to the gradient's type; the other way round it can."""
+    x = torch.full((30, 70), 1e5, dtype=torch.bfloat16)
+    x[::2] = randn(1, (15, 70), torch.bfloat16)
+    dy = randn(2, (30, 24), torch.float16)
+    ck = cf.checkpoint_pack(x.cuda())
+    stats, w = torch.ones(30, 2, device="cuda"), torch.ones(70, device="cuda")
+    for more in ((), (stats,), (stats, w, w)):
+        with pytest.raises(ValueError, match="bfloat16"):
+            cf.linear_weight_grad(dy.cuda(), ck, *more)
+    narrow = cf.checkpoint_pack(x[::2].half().cuda())
+    got = cf.linear_weight_grad(dy[::2].bfloat16().cuda(), narrow)
+    dw, tw, db, tb = reference(dy[::2].bfloat16(), dequantise(narrow.q.cpu(), narrow.scale.cpu()), None, None,
+                               torch.zeros(()), torch.bfloat16, 15)
+    assert_within(got[0], dw, tw, "dW")
+    assert_within(got[1], db, tb, "db")

@@ -310,7 +310,7 @@ cf_status cf_linear_weight_grad(const void *dy, const int8_t *q, const float *sc
         return api_fail(CF_ERR_INVALID, "%s: dw and db must be non-NULL", what);
     if (rows > 0 && (!dy || !q || !scale))
         return api_fail(CF_ERR_INVALID, "%s: dy, q and scale must be non-NULL", what);
-    if (!stats && (weight || bias))
+    if (rows > 0 && !stats && (weight || bias))
         return api_fail(CF_ERR_INVALID, "%s: weight and bias are the layer norm's and need stats", what);
     const Span t[] = {{"dy", dy, rows, K, lddy, 2},
                       dense("q", q, rows, C, 1),

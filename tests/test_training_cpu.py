@@ -172,3 +172,12 @@ def test_checkpoint_sizes():
     ck = cf.Checkpoint(torch.zeros(6, 130, dtype=torch.int8), torch.zeros(6, 3), torch.float16)
     assert ck.shape == (6, 130) and ck.nbytes() == 6 * 130 + 4 * 18
     assert training.CKPT_BLOCK == 64
+
+
+@needs_library
+def test_no_rows_need_no_statistics():
+    """The address of an empty tensor is null: with weight and bias of a norm but
+    no statistics, only the next check (of the size) refuses a call without rows."""
+    L, K = cf.lib(), (1 << 20) + 1
+    for rows, status in ((0, UNSUPPORTED), (1, INVALID)):
+        assert L.cf_linear_weight_grad(A, Q, S, None, W, B, OUT, G1, None, 0, rows, K, 64, K, 0, None) == status

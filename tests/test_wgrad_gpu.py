@@ -272,3 +272,12 @@ def test_half_precision_gradients_of_a_wider_checkpoint():
                                torch.zeros(()), torch.bfloat16, 15)
     assert_within(got[0], dw, tw, "dW")
     assert_within(got[1], db, tb, "db")
+
+
+def test_no_rows_after_a_norm():
+    """An empty batch has no statistics either (their address is null)."""
+    dy, q, scale, stats, w, b, *_ = case(4, 5, 33, 70, torch.float16, True)
+    ck = cf.Checkpoint(q[:0].cuda(), scale[:0].cuda(), torch.float16)
+    for more in ((), (w.cuda(),), (w.cuda(), b.cuda())):
+        dw, db = cf.linear_weight_grad(dy[:0].cuda(), ck, stats[:0].cuda(), *more)
+        assert dw.shape == (33, 70) and torch.equal(dw, torch.zeros_like(dw)) and torch.equal(db, torch.zeros_like(db))

@@ -273,13 +273,15 @@ __device__ __forceinline__ void each(const Piece<Z> &p, F &&f) {
 }
 
 struct TopSpace {
-    float gm[64];
+    alignas(16) float gm[64];  // read by fours
     uint64_t list[LIST];
     uint64_t out[TOP_MAX];
     uint64_t best[TH / 64];
     int n, threads, cnt[TH / 64];
     uint8_t who[TH];
 };
+static_assert(alignof(TopSpace) % alignof(float4) == 0 && offsetof(TopSpace, gm) % alignof(float4) == 0,
+              "gm is read as float4");
 
 // Logits of the piece that `wanted` takes, from the shares of the threads
 // that say `mine`, into sp.list; their number in sp.n (which may pass LIST).

@@ -312,3 +312,69 @@ def test_refusals():
     buf = torch.zeros(5, 40, dtype=torch.float16, device="cuda")
     with pytest.raises(cf.CFError):
         cf.log_probs_backward(buf[:4], t, r, g, out=buf[1:])
+
+
+def above_the_bound(z, top, lanes, together):
+    """How many logits of each row [rows, V] are strictly above the n-th largest
+    (n = top) of 64 maxima: `lanes` threads take vectors of 16 bytes in turn, and
+    `together` neighbouring threads share a maximum."""
+    vec = 16 // z.element_size()
+    owner = (torch.arange(z.shape[1]) // vec) % lanes // together
+    most = torch.full((z.shape[0], 64), -INF).scatter_reduce_(1, owner.expand(z.shape), z.float(), "amax")
+    bound = most.sort(1, descending=True).values[:, top - 1:top]
+    return (z.float() > bound).sum(1)
+
+
+def check_repeated(z, top, repeat):
+    """check() on the first rows of a call on many copies of them, and that every
+    copy gets the same answer."""
+    rows = z.shape[0]
+    tokens = torch.arange(rows)
+    r = cf.log_probs_forward(z.repeat(repeat, 1).cuda(), tokens.repeat(repeat).cuda(), top=top)
+    logp, _, h, lp, _ = reference(z, tokens)
+    ids, tl = order(z, top), tol_logp(z, logp)
+    for name, got, want, tol in (("entropy", r.entropy, h, 2 * E + E * h), ("logp", r.logp, lp, tl.gather(1, tokens[:, None])[:, 0]),
+                                 ("top_logp", r.top_logp, logp.gather(1, ids), tl.gather(1, ids))):
+        assert_within(got[:rows], want, tol, name)
+    assert torch.equal(r.top_ids[:rows].cpu(), ids)
+    for t in (r.entropy, r.logp, r.top_logp, r.top_ids):
+        assert torch.equal(t, t[:rows].repeat((repeat,) + (1,) * (t.dim() - 1)))
+
+
+def rows_with_large(V, dt, lanes, few):
+    """Small logits but for those of the first `few` threads of `lanes`."""
+    z = randn(3, (3, V), torch.float32, 0.01)
+    large = (torch.arange(V) // (16 // dt.itemsize)) % lanes < few
+    z[:, large] = 5.0 + torch.arange(int(large.sum())).float().remainder(977) * 0.01
+    z[1] = z[1].flip(0) if V % (lanes * 16 // dt.itemsize) == 0 else z[1]
+    return z.to(dt)
+
+
+@pytest.mark.parametrize("V,few,dtype", [(40000, 12, "f32"), (40000, 100, "f32"), (70000, 12, "bf16"), (70000, 120, "f16")])
+def test_more_above_the_bound_than_the_list_holds(V, few, dtype):
+    """Rows whole in a workgroup: more than 480 logits above the bound, in few
+    threads, so that each alternative takes a pass over the row."""
+    z = rows_with_large(V, DT[dtype], 256, few)
+    assert int(above_the_bound(z, 32, 256, 4).min()) > 480
+    cus = torch.cuda.get_device_properties(0).multi_processor_count
+    check_repeated(z, 32, (2 * cus + 2) // 3 + 1)
+
+
+@pytest.mark.parametrize("V,dtype", [(32768, "bf16"), (16384, "f16")])
+def test_more_above_the_bound_than_the_list_holds_in_a_chunk(V, dtype):
+    """The same in chunks of 2048, a vector a thread."""
+    z = rows_with_large(V, DT[dtype], 256, 100)
+    for c in range(0, V, 2048):
+        assert int(above_the_bound(z[:, c:c + 2048], 32, 256, 4).min()) > 480
+    check_repeated(z, 32, 1)
+
+
+@pytest.mark.parametrize("V,dtype,most", [(4000, "bf16", 256), (2000, "f16", 256), (2000, "f32", 256), (1000, "f32", 256),
+                                          (1000, "bf16", 64), (500, "f16", 64)])
+def test_more_above_the_bound_than_a_wave_collects(V, dtype, most):
+    """Rows of a wave each: more keys above the bound than its list holds."""
+    few = {"f32": 19, "f16": 19, "bf16": 12}[dtype]
+    z = rows_with_large(V, DT[dtype], 64, few)
+    assert int(above_the_bound(z, 20, 64, 1).min()) > most
+    cus = torch.cuda.get_device_properties(0).multi_processor_count
+    check_repeated(z, 20, (4 * cus + 2) // 3 + 1)

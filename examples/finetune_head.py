@@ -72,10 +72,15 @@ class Head:
 
 def evaluate(logits, labels, top=5):
     """Mean log probability of the labels, mean entropy, shares of rows whose
-    label is first and among the `top` first."""
-    r = cf.log_probs_forward(logits.reshape(-1, logits.shape[-1]), labels.reshape(-1), top=top)
-    hit = r.top_ids == labels.reshape(-1, 1)
-    return r.logp.mean(), r.entropy.mean(), hit[:, 0].float().mean(), hit.any(1).float().mean()
+    label is first and among the `top` first; over the rows with a label, as in
+    Head.step (all 0 where none has one)."""
+    labels = labels.reshape(-1)
+    r = cf.log_probs_forward(logits.reshape(-1, logits.shape[-1]), labels, top=top)
+    given = labels >= 0
+    hit = (r.top_ids == labels[:, None]).float()  # no id is negative
+    count = given.sum().clamp_min(1)
+    return (r.logp.sum() / count, r.entropy.masked_fill(~given, 0.0).sum() / count, hit[:, 0].sum() / count,
+            hit.sum() / count)
 
 
 def main():

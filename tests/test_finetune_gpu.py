@@ -50,3 +50,21 @@ def test_the_loss_falls(monkeypatch, capsys):
     m.main()
     losses = [float(line.split("loss ")[1].split(";")[0]) for line in capsys.readouterr().out.splitlines()]
     assert len(losses) == 3 and losses[-1] < 0.8 * losses[0], losses
+
+
+def test_evaluation_leaves_out_rows_without_a_label():
+    m = example()
+    g = torch.Generator().manual_seed(3)
+    z = (2.0 * torch.randn(6, 9, 40, generator=g)).half().cuda()
+    labels = torch.randint(0, 40, (6, 9), generator=g)
+    labels[0, 0] = z[0, 0].argmax().cpu()
+    none = torch.rand(6, 9, generator=g) < 0.4
+    none[0, 0] = False
+    padded = torch.where(none, -1 - labels, labels).cuda()
+    want = m.evaluate(z[~none.cuda()], labels[~none].cuda())
+    got = m.evaluate(z, padded)
+    assert float(want[2]) > 0
+    for a, b in zip(got, want):  # the same rows in another order of adding
+        assert abs(float(a) - float(b)) <= 1e-5 * abs(float(b)), (got, want)
+    nothing = m.evaluate(z, torch.full_like(padded, -1))
+    assert all(float(v) == 0.0 for v in nothing)

@@ -891,13 +891,19 @@ hipError_t forward(const Args &a, int64_t rows, hipStream_t st) {
     return hipGetLastError();
 }
 
+// Workgroups of a row of the backward pass (0: a short one); `size` bytes a logit.
+uint32_t back_chunks(const void *z, int64_t ldz, int V, int size) {
+    const int ve = 16 / size, span = BACK_NV * 256 * ve;
+    if (V < span / 2)
+        return 0;
+    // room for a first vector that is not whole, unless every row starts a vector
+    const bool whole = ((uintptr_t)z | (uintptr_t)ldz * size) % 16 == 0;
+    return (uint32_t)(((int64_t)V + (whole ? 0 : ve - 1) + span - 1) / span);
+}
+
 template <typename Z>
 hipError_t backward(BackArgs &a, int64_t rows, hipStream_t st) {
-    constexpr int SPAN = BACK_NV * 256 * Z::VE;
-    if (a.V >= SPAN / 2) {
-        // room for a first vector that is not whole, unless every row starts a vector
-        const bool whole = ((uintptr_t)a.z | (uintptr_t)a.ldz * sizeof(typename Z::elem)) % 16 == 0;
-        const uint32_t chunks = (uint32_t)((a.V + (whole ? 0 : Z::VE - 1) + SPAN - 1) / SPAN);
+    if (const uint32_t chunks = back_chunks(a.z, a.ldz, a.V, sizeof(typename Z::elem))) {
         log_probs_backward_row_kernel<Z><<<dim3((unsigned)(rows * chunks)), dim3(256), 0, st>>>(a, chunks);
     } else {
         const uint32_t per_row = (uint32_t)((a.V + Z::VE - 1) / Z::VE);
@@ -917,6 +923,11 @@ bool log_probs_fit(int64_t rows, int V) {
     const double limit = 16777216.0;
     return rows < limit && (V >= 4096 ? (double)rows * ((V + 4095) / 4096) < limit
                                       : (double)rows * ((V + 3) / 4) < 2147483648.0);
+}
+
+bool log_probs_backward_fits(const LogProbsBackward &p, int64_t rows, int V, int dt) {
+    const uint32_t chunks = back_chunks(p.z, p.ldz, V, dt == LOGITS_F32 ? 4 : 2);
+    return log_probs_fit(rows, V) && (double)rows * chunks < 16777216.0;
 }
 
 size_t log_probs_workspace_bytes(int64_t rows, int V, int top) {

@@ -87,8 +87,9 @@ struct LogProbsBackward {
     void *dz;
     int64_t lddz;
 };
-// whether the grids of both passes hold these rows
+// whether the grids of the passes hold these rows
 bool log_probs_fit(int64_t rows, int V);
+bool log_probs_backward_fits(const LogProbsBackward &a, int64_t rows, int V, int dt);
 hipError_t launch_log_probs_backward(const LogProbsBackward &a, int64_t rows, int V, int dt, hipStream_t st);
 
 }  // namespace cf

@@ -420,8 +420,6 @@ cf_status cf_log_probs_backward(const void *z, const int64_t *tokens, const floa
     if (!aligned(stats, 8))
         return api_fail(CF_ERR_INVALID, "%s: stats must be 8-byte aligned", what);
     CF_TRY(check_out(what, t[6], t, 6, t[0].name));
-    if (V > 1 << 30 || !cf::log_probs_fit(rows, V))
-        return api_fail(CF_ERR_UNSUPPORTED, "%s: no kernel for rows=%lld V=%d", what, (long long)rows, V);
     cf::LogProbsBackward a;
     a.z = z;
     a.ldz = ldz;
@@ -432,6 +430,8 @@ cf_status cf_log_probs_backward(const void *z, const int64_t *tokens, const floa
     a.d_entropy = d_entropy;
     a.dz = dz;
     a.lddz = lddz;
+    if (V > 1 << 30 || !cf::log_probs_backward_fits(a, rows, V, (int)dt))
+        return api_fail(CF_ERR_UNSUPPORTED, "%s: no kernel for rows=%lld V=%d", what, (long long)rows, V);
     return api_done(cf::launch_log_probs_backward(a, rows, V, (int)dt, (hipStream_t)stream), what);
 }
 

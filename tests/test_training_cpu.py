@@ -181,3 +181,12 @@ def test_no_rows_need_no_statistics():
     L, K = cf.lib(), (1 << 20) + 1
     for rows, status in ((0, UNSUPPORTED), (1, INVALID)):
         assert L.cf_linear_weight_grad(A, Q, S, None, W, B, OUT, G1, None, 0, rows, K, 64, K, 0, None) == status
+
+
+@needs_library
+def test_backward_of_long_rows_that_start_anywhere_has_a_grid():
+    """Rows of 4096 fp32 logits that do not start at 16 bytes take two workgroups
+    each: 2^23 of them are 2^32 threads."""
+    L, rows, V = cf.lib(), 1 << 23, 4096
+    for z, ldz in ((A + 4, V), (A, V + 1)):
+        assert L.cf_log_probs_backward(z, B, ST, S, G1, None, OUT, rows, V, ldz, V, 2, None) == UNSUPPORTED

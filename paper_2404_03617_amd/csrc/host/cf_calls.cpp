@@ -177,6 +177,11 @@ PyObject *call(PyObject *, PyObject *const *args, Py_ssize_t n) {
     }
 }
 
+bool truth(PyObject *o) {
+    const int v = PyObject_IsTrue(o);
+    must(v >= 0);
+    return v != 0;
+}
 float real(PyObject *o) {
     const double v = PyFloat_AsDouble(o);
     must(!(v == -1.0 && PyErr_Occurred()));
@@ -207,7 +212,7 @@ PyObject *norm_forward_save(PyObject *const *a, Py_ssize_t n) {
     const Out y = out_of(a[5], *x.t, x.code);
     const at::Tensor stats = fresh(*x.t, lead(*x.t, 2), at::kFloat);
     NewCheckpoint ck;
-    if (PyObject_IsTrue(a[4]))
+    if (truth(a[4]))
         ck.make(*x.t, x.C);
     check(lib.norm_forward(x.p, y.p, w, b, static_cast<float *>(stats.data_ptr()), ck.qp, ck.sp, x.n, x.C, x.ld, y.ld,
                            eps, (cf_dtype)x.code, stream()));
@@ -235,7 +240,7 @@ PyObject *norm_backward(PyObject *const *a, Py_ssize_t n) {
     const Out dx = out_of(a[7], *dy.t, dy.code);
     at::Tensor dw, db, ws;
     size_t bytes = 0;
-    if (PyObject_IsTrue(a[6])) {
+    if (truth(a[6])) {
         dw = fresh(*dy.t, {dy.C}, at::kFloat);
         db = fresh(*dy.t, {dy.C}, at::kFloat);
         bytes = lib.norm_ws(dy.n, dy.C);
@@ -255,12 +260,12 @@ PyObject *act_forward(PyObject *const *a, Py_ssize_t n) {
     const RowsOf u = rows_of(a[0], 2);
     const long act = whole(a[1]);
     Out h{at::Tensor(), nullptr, u.C};
-    if (PyObject_IsTrue(a[2]))
+    if (truth(a[2]))
         h = out_of(a[5], *u.t, u.code);
     NewCheckpoint cu, ch;
-    if (PyObject_IsTrue(a[3]))
+    if (truth(a[3]))
         cu.make(*u.t, u.C);
-    if (PyObject_IsTrue(a[4]))
+    if (truth(a[4]))
         ch.make(*u.t, u.C);
     check(lib.act_forward(u.p, h.p, cu.qp, cu.sp, ch.qp, ch.sp, u.n, u.C, u.ld, h.ld, (cf_dtype)u.code, (cf_act)act,
                           stream()));

@@ -118,3 +118,15 @@ def test_native_calls_accept_and_refuse_alike(name, monkeypatch):
         else:
             assert native[i] == want, (i, native[i], want)
     assert accepted >= 2 and isinstance(native[0], list)
+
+
+def test_choices_without_a_truth_value():
+    """A tensor of several elements where a call asks yes or no: torch's own error."""
+    x = randn(1, (4, 64), torch.float16).cuda()
+    _, stats, ck = cf.layer_norm_forward_save(x)
+    two = torch.ones(2)
+    for call in (lambda: cf.layer_norm_forward_save(x, checkpoint=two),
+                 lambda: cf.layer_norm_backward(x, ck, stats, param_grads=two),
+                 lambda: cf.act_forward_save(x, checkpoint_out=two)):
+        with pytest.raises(RuntimeError, match="ambiguous"):
+            call()

@@ -102,6 +102,12 @@ def _rows(name, t, kinds):
     return d
 
 
+def _not_negated(name, t):
+    """Memory that holds the negatives of a view's values is refused."""
+    if t.is_neg():
+        raise ValueError("%s is a negated view: resolve_neg() gives a tensor with its values" % name)
+
+
 def _rows_checked(name, t):
     if not isinstance(t, torch.Tensor):
         raise TypeError("%s must be a torch.Tensor" % name)
@@ -111,6 +117,7 @@ def _rows_checked(name, t):
         raise ValueError("%s has dtype %s" % (name, t.dtype))
     if t.device.type != "cuda":
         raise ValueError("%s must be a GPU tensor (got device %s)" % (name, t.device))
+    _not_negated(name, t)
     C = t.shape[-1]
     if C > 1 and t.stride(-1) != 1:
         raise ValueError("%s must be contiguous in its last dimension" % name)
@@ -145,6 +152,7 @@ def _flat(name, x, t, code, n, last):
                                                                       " rows of %d" % last if last else ""))
     if not t.is_contiguous():
         raise ValueError("%s must be contiguous" % name)
+    _not_negated(name, t)
     if t.device != x.device:
         raise ValueError("%s is on %s but the input is on %s" % (name, t.device, x.device))
     return t.data_ptr()

@@ -130,3 +130,16 @@ def test_choices_without_a_truth_value():
                  lambda: cf.act_forward_save(x, checkpoint_out=two)):
         with pytest.raises(RuntimeError, match="ambiguous"):
             call()
+
+
+def test_negated_views_are_refused():
+    """A view whose memory holds the negatives of its values (the imaginary part of
+    a conjugate) is not what a kernel would read."""
+    z = torch.randn(5, 1, dtype=torch.complex64, device="cuda").conj().imag
+    assert z.is_neg()
+    with pytest.raises(ValueError, match="negated"):
+        cf.log_probs_forward(z)
+    x = randn(1, (5, 1), torch.float16).cuda()
+    with pytest.raises(ValueError, match="negated"):
+        cf.layer_norm_forward(x, z[0])
+    assert cf.log_probs_forward(z.resolve_neg()).entropy.shape == (5,)

@@ -33,6 +33,7 @@
 #include "cf_rows.h"
 #include "cf_kernels.h"
 #include "cf_train.h"
+#include "cf_wgrad_plan.h"
 
 #include <type_traits>
 
@@ -52,25 +53,8 @@ struct WGradArgs {
     int K, C, blocks, tiles_k, tiles_c, splits;
 };
 
-// The tiles: m x n of dW; workgroups that run on a CU together; and what the
-// choice among them estimates with, in microseconds (cf_wgrad.hip).
-struct Tile {
-    int m, n, per_cu;
-    double alone, full, fixed;
-};
-constexpr int TILE_COUNT = 7;
-constexpr Tile TILES[TILE_COUNT] = {
-    {64, 64, 3, 0.50, 0.386, 4.5},   // 0: four waves
-    {128, 128, 3, 1.15, 0.72, 8.0},  // 1: four waves
-    {256, 256, 1, 1.45, 2.00, 12.0}, // 2: eight waves
-    {256, 64, 1, 0.90, 0.92, 6.5},   // 3: eight waves
-    {64, 256, 1, 0.90, 0.88, 6.5},   // 4: eight waves
-    {128, 128, 1, 0.73, 0.80, 8.0},  // 5: two groups of four waves
-    {64, 64, 1, 0.40, 0.362, 6.0},   // 6: four groups of four waves
-};
-
 // One instance a dtype, with and without a norm before the layer (tile: index
-// into TILES).
+// into wgrad::TILES).
 hipError_t launch_wgrad_f16(const WGradArgs &a, int tile, hipStream_t st);
 hipError_t launch_wgrad_bf16(const WGradArgs &a, int tile, hipStream_t st);
 hipError_t launch_wgrad_norm_f16(const WGradArgs &a, int tile, hipStream_t st);
@@ -592,8 +576,10 @@ typedef Shape2<64, 256, 2, 4, 1, 64, 16, 2, 2> TileWide;
 typedef Shape2<128, 128, 2, 2, 2, 64, 16, 2, 2> Deep128;
 typedef Shape2<64, 64, 2, 2, 4, 128, 8, 2, 4> Deep64;
 
-template <typename T, typename S, bool NORM>
+template <typename T, typename S, bool NORM, int TILE>
 hipError_t launch_tile(const WGradArgs &a, hipStream_t st) {
+    constexpr wgrad::Tile t = wgrad::TILES[TILE];
+    static_assert(S::TM == t.m && S::TN == t.n && S::TH == 64 * t.waves && S::QB == t.qb, "what the plan counts with");
     const bool small = a.lddy * 2 * S::BK < (int64_t)1 << 31 && (int64_t)a.C * S::BK < (int64_t)1 << 31;
     const int ends = a.K < 8 || a.C < S::QB || !small ? ANY : a.K % 8 || a.C % S::QB ? SHIFT : EVEN;
     void (*const f)(WGradArgs) = ends == EVEN    ? wgrad_kernel<T, S, NORM, EVEN>
@@ -613,13 +599,13 @@ template <typename T, bool NORM>
 hipError_t launch_type(const WGradArgs &a, int tile, hipStream_t st) {
     hipError_t e;
     switch (tile) {
-    case 0: e = launch_tile<T, Tile64, NORM>(a, st); break;
-    case 1: e = launch_tile<T, Tile128, NORM>(a, st); break;
-    case 2: e = launch_tile<T, Tile256, NORM>(a, st); break;
-    case 3: e = launch_tile<T, TileTall, NORM>(a, st); break;
-    case 4: e = launch_tile<T, TileWide, NORM>(a, st); break;
-    case 5: e = launch_tile<T, Deep128, NORM>(a, st); break;
-    default: e = launch_tile<T, Deep64, NORM>(a, st); break;
+    case 0: e = launch_tile<T, Tile64, NORM, 0>(a, st); break;
+    case 1: e = launch_tile<T, Tile128, NORM, 1>(a, st); break;
+    case 2: e = launch_tile<T, Tile256, NORM, 2>(a, st); break;
+    case 3: e = launch_tile<T, TileTall, NORM, 3>(a, st); break;
+    case 4: e = launch_tile<T, TileWide, NORM, 4>(a, st); break;
+    case 5: e = launch_tile<T, Deep128, NORM, 5>(a, st); break;
+    default: e = launch_tile<T, Deep64, NORM, 6>(a, st); break;
     }
     if (e != hipSuccess || a.splits == 1)
         return e;

@@ -281,3 +281,37 @@ def test_no_rows_after_a_norm():
     for more in ((), (w.cuda(),), (w.cuda(), b.cuda())):
         dw, db = cf.linear_weight_grad(dy[:0].cuda(), ck, stats[:0].cuda(), *more)
         assert dw.shape == (33, 70) and torch.equal(dw, torch.zeros_like(dw)) and torch.equal(db, torch.zeros_like(db))
+
+
+# What the shapes above leave out: few shapes take these.
+MORE_TILES = [(4324, 504, 512), (4200, 505, 507), (1108, 14941, 2)]
+
+
+@pytest.mark.parametrize("rows,K,C", MORE_TILES)
+def test_more_tiles(rows, K, C):
+    for dt, norm in ((torch.float16, True), (torch.bfloat16, False)):
+        dy, q, scale, stats, w, b, kept, spread = case(C, rows, K, C, dt, norm)
+        dw, tw, db, tb = reference(dy, kept, w, b, spread, dt, rows)
+        more = dict(stats=stats.cuda(), weight=w.cuda(), bias=b.cuda()) if norm else {}
+        got = cf.linear_weight_grad(rows_in("shifted", dy), cf.Checkpoint(q.cuda(), scale.cuda(), dt), **more)
+        assert_within(got[0], dw, tw, "dW")
+        assert_within(got[1], db, tb, "db")
+
+
+# Rows of dy 2^25 elements apart, whose steps pass 32 bits in each tile.
+FAR = [(128, 3956, 4269), (320, 3017, 4269), (832, 3330, 1139)]
+
+
+@pytest.mark.parametrize("rows,K,C", FAR)
+def test_steps_that_pass_32_bits(rows, K, C):
+    ld, dt = 1 << 25, torch.bfloat16
+    dy, q, scale, stats, w, b, kept, spread = case(rows, rows, K, C, dt, True)
+    dw, tw, db, tb = reference(dy, kept, w, b, spread, dt, rows)
+    far = torch.empty(rows * ld, dtype=dt, device="cuda").view(rows, ld)[:, 5:5 + K]
+    far.copy_(dy)
+    ck = cf.Checkpoint(q.cuda(), scale.cuda(), dt)
+    got = cf.linear_weight_grad(far, ck, stats.cuda(), w.cuda(), b.cuda())
+    assert_within(got[0], dw, tw, "dW")
+    assert_within(got[1], db, tb, "db")
+    del far
+    torch.cuda.empty_cache()

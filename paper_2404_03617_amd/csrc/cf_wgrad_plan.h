@@ -50,7 +50,9 @@ constexpr double PART_BYTES = 128 << 20;
 // rows over workgroups whose wave groups share a tile (fewer partial sums);
 // small ones over few rows take small tiles.
 inline double time_of(const Tile &t, int64_t rows, int K, int C, int64_t splits, int64_t cus) {
-    const double work = (double)tiles_of(t, K, C) * splits, steps = ((rows + splits - 1) / splits + 63) / 64;
+    const int64_t each = (rows + splits - 1) / splits;
+    // no rows still take a workgroup a tile: as many as one row
+    const double work = (double)tiles_of(t, K, C) * splits, steps = each < 1 ? 1 : (each + 63) / 64;
     const double rounds = std::ceil(work / (cus * t.per_cu)), load = std::ceil(work / cus);
     const double step = t.alone * rounds > t.full * load ? t.alone * rounds : t.full * load;
     return t.fixed + steps * step + (splits > 1 ? 4.0 + splits * 8.0 * K * C / 6.0e6 : 0.0);

@@ -44,3 +44,29 @@ def test_the_shapes_of_the_tile_tests_take_every_tile(tmp_path):
     tiles = int(lines[len(shapes)])
     missing = {(t, k) for t in range(tiles) for k in ("whole", "split", "any", "shift", "even")} - seen
     assert not missing, missing
+
+
+def test_splits_hold_all_rows_and_fit_the_room(tmp_path):
+    """Splits are whole steps of 64 rows, none is empty, together they are all of
+    the rows, their partial sums fit the room, and one workgroup per tile and split
+    stays below 2^32 threads."""
+    run_cpp(tmp_path, """
+    const int sizes[] = {1, 7, 64, 100, 511, 1000, 3008, 4096, 12288, 65536, 1 << 20};
+    for (int K : sizes)
+        for (int C : sizes)
+            for (int64_t rows = 0; rows < (int64_t)1 << 31; rows += rows / 2 + 1) {
+                if ((double)K * C > 1.5e11)
+                    continue;
+                const Plan p = plan_of(rows, K, C, %d);
+                const Tile &t = TILES[p.tile];
+                const double groups = (double)tiles_of(t, K, C) * p.splits;
+                const bool ok = p.splits >= 1 && p.chunk %% 64 == 0 && p.chunk * p.splits >= rows &&
+                                (p.splits == 1 || (p.chunk * (p.splits - 1) < rows && p.splits * 4.0 * K * (C + 1.0) <= PART_BYTES)) &&
+                                groups * 64 * t.waves < 4294967296.0;
+                if (!ok) {
+                    printf("rows %%lld K %%d C %%d: tile %%d, %%d splits of %%lld\\n", (long long)rows, K, C, p.tile, p.splits,
+                           (long long)p.chunk);
+                    return 1;
+                }
+            }
+    """ % CUS)

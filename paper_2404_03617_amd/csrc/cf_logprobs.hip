@@ -534,6 +534,7 @@ __global__ __launch_bounds__(TH) void log_probs_kernel(Args a) {
 template <typename Z>
 struct WaveKey {
     typedef uint64_t key;
+    static constexpr int FEW = 3;
     static __device__ __forceinline__ key of(float z, int i, bool) { return key_of(z, (uint32_t)i); }
     template <int G>
     static __device__ __forceinline__ key best(key k) {
@@ -544,6 +545,7 @@ struct WaveKey {
 template <typename T>
 struct WaveKey<Z16<T>> {
     typedef uint32_t key;
+    static constexpr int FEW = 5;
     static constexpr uint32_t INDEX = 0x1fffu;
     static __device__ __forceinline__ key of(float z, int i, bool nan) {
         const uint32_t u = __builtin_bit_cast(uint32_t, z + 0.0f);  // -0 equals 0
@@ -587,15 +589,16 @@ __device__ __forceinline__ void wave_fence() {
     __builtin_amdgcn_wave_barrier();
 }
 
-// Up to FEW_TOP alternatives of a wave's row are found one after the other, more
-// (60000 rows of 1000: eight in bf16 65 us, otherwise 78; twenty 69 and 139, in
-// fp32 84 and 244; five in bf16 66 and 65) among the logits that reach the n-th
-// largest of the lanes' maxima, collected and ranked by counting.  Up to 256 of
-// them, as many as reach it in a row of equal logits; up to 64 of short rows in 16
-// bits, where the way for few takes less than ranking more (128 rows of 400, one
-// of them masked whole, twenty: 7.3 us against 10.7).
-constexpr int FEW_TOP = 5;
-
+// A few alternatives of a wave's row (K::FEW) are found one after the other, more
+// among the logits that reach the n-th largest of the lanes' maxima, collected and
+// ranked by counting.  60000 rows of 1000, one after the other and collected: bf16
+// four 60 and 65 us, five 65 and 66, six 69 and 66, eight 78 and 66; fp32, whose
+// keys are twice as wide, three 75 and 79, four 85 and 79, eight 124 and 80.  10000 of
+// 4000 in bf16: five 40 and 41, six 43 and 41; 10000 of 400 in fp32: three 11.4 and
+// 12.6, five 13.9 and 12.8.  Up to 256 are collected, as many as reach the bound in
+// a row of equal logits; up to 64 of short rows in 16 bits, where the way for few
+// takes less than ranking more (128 rows of 400, one of them masked whole, twenty:
+// 7.3 us against 10.7).
 template <typename Z, int G, int NV, bool TOP>
 __global__ __launch_bounds__(256) void log_probs_wave_kernel(Args a, int64_t rows) {
     typedef WaveKey<Z> K;
@@ -628,7 +631,7 @@ __global__ __launch_bounds__(256) void log_probs_wave_kernel(Args a, int64_t row
         }
         int from = 0;
         if constexpr (G == 64)
-            if (a.top > FEW_TOP) {
+            if (a.top > K::FEW) {
                 typedef typename K::key Key;
                 constexpr int WAVE_LIST = Z::VE == 8 && NV <= 2 ? 64 : 256;
                 __shared__ __align__(16) Key heads[4][64], list[4][WAVE_LIST];

@@ -190,3 +190,19 @@ def test_backward_of_long_rows_that_start_anywhere_has_a_grid():
     L, rows, V = cf.lib(), 1 << 23, 4096
     for z, ldz in ((A + 4, V), (A, V + 1)):
         assert L.cf_log_probs_backward(z, B, ST, S, G1, None, OUT, rows, V, ldz, V, 2, None) == UNSUPPORTED
+
+
+def test_the_two_copies_of_gelus_tail_agree():
+    """GELU (cf_device.h) and its slope (cf_ckpt.hip) evaluate the same q(t)."""
+    import re
+
+    csrc = os.path.join(os.path.dirname(cf.__file__), "csrc")
+
+    def tail(name, function):
+        text = open(os.path.join(csrc, name)).read()
+        body = text[text.index(function):]
+        body = body[:body.index("exp2f")]
+        return re.findall(r"fmaf\([^;]*?(-?0\.\d{6,})f(?:, t, (-?0\.\d+)f)?\)", body)
+
+    a, b = tail("cf_device.h", "float gelu_f32("), tail("cf_ckpt.hip", "float gelu_slope(")
+    assert a == b and len(a) == 5, (a, b)

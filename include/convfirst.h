@@ -430,6 +430,8 @@ int cf_block_tuned_config(int N, int H, int W, int C, int E, int k, cf_dtype dt,
 /* Layer norm over the C channels of each row:
  *   mean = 1/C sum x,  rstd = 1 / sqrt(1/C sum (x - mean)^2 + eps)
  *   y = weight * (x - mean) * rstd + bias
+ * Statistics are fp32: a row whose sum passes its range is NaN, and where the sum
+ * of squared deviations does (bf16 values 1e19 and more apart) rstd is 0.
  * weight, bias [C] may be NULL.  For the backward pass, each NULL unless
  * wanted: stats [rows][2] receives mean and rstd; q and scale (both or
  * neither) the checkpoint of x, in the same pass over it.  y may equal x with

@@ -10,10 +10,10 @@
 // are cut into whole blocks of 64, so a row's last block may hold idle lanes.
 //
 // Measured on MI355X, where a copy of 2 GiB moves 4.9 TB/s (kernel times):
-// 100352 x 128 bf16 written in 8.5 and read back in 8.0 us (39 MB each way, 4.6
-// and 4.9 TB/s); 6272 x 2048 fp16 through GELU with both checkpoints 14.8 us (79
-// MB, 5.3 TB/s) and its gradient 13.9 us (65 MB, 4.7 TB/s), both with the VALU
-// 99% busy: the erf polynomial costs as much as the memory.
+// 100352 x 128 bf16 written in 8.3 and read back in 7.9 us (39 MB each way, 4.7
+// and 5.0 TB/s); 6272 x 2048 fp16 through GELU with its checkpoint 15.5 us (65 MB,
+// 4.2 TB/s), with the result's too 18.6 (79 MB), and its gradient 13.4 us (65 MB, 4.8
+// TB/s), with the VALU 99% busy: the erf polynomial costs as much as the memory.
 #include "cf_rows.h"
 #include "cf_kernels.h"
 #include "cf_train.h"
@@ -23,7 +23,8 @@ namespace cf {
 namespace {
 
 // gelu'(u) = Phi(u) + u phi(u), with the tail 1 - Phi(|u|) = q(t) exp(-u^2/2)
-// of gelu_f32 (1.5e-8): the exponential serves both terms.
+// of gelu_f32, whose coefficients these are (1.5e-8): the exponential serves both
+// terms.
 __device__ __forceinline__ float gelu_slope(float u) {
     const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(u), 0.32f, 1.0f));
     float q = fmaf(-0.129858347f, t, 0.495794653f);

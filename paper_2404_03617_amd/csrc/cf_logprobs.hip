@@ -17,7 +17,7 @@
 // number, so that rows masked with it are as good as any other.
 //
 // Rows of up to 4096 logits (2048 in fp32) stay in the registers of a wave or
-// of 8, 16 or 32 of its lanes (65536 rows of 100 with five alternatives: 15 us,
+// of 8, 16 or 32 of its lanes (65536 rows of 100 with five alternatives: 14 us,
 // 50 with a wave each, 360 with a workgroup).
 //
 // Alternatives of longer rows: the n-th largest of the 64 maxima over four
@@ -27,11 +27,15 @@
 // few classes left), those above the bound are collected and the equal ones taken
 // in the order of the row.
 //
-// Measured on MI355X, where a copy of 2 GiB moves 4.9 TB/s (kernel times): 4096
-// rows of 100003 in bf16 forward 166 to 188 us (4.4 to 4.9 TB/s; VALU 82% busy),
-// backward 267 to 275 (6 TB/s); one row of 131072 with eight alternatives 5.7 us in 64 workgroups
-// and 3.8 us to join them; 128 rows of 1000 with five 6.0 us.  The last two are
-// chains: load, maximum, join, alternatives, the logit asked for.
+// Measured on MI355X, where a copy of 2 GiB moves 4.9 TB/s: 4096 rows of 100003 in
+// bf16 forward 150 us among calls of its kind (5.5 TB/s; VALU 83% busy), 177 to 188
+// behind a backward pass, which takes 271 to 278 (6 TB/s); one row of 131072 with
+// eight alternatives 5.6 us in 64 workgroups and 4.0 us to join them; 128 rows of
+// 1000 with five 6.1 us.  The last two are chains: load, maximum, join,
+// alternatives, the logit asked for.  Rows of a wave each are bound by instructions
+// where they have alternatives, of which a key for every logit is the most: 60000
+// rows of 1000 with five or eight 65 us (none: 33), 10000 of 4000 with eight 41
+// (18), 20000 of 2000 with twenty 40 (19), 65536 of 100 with five 14 (7.6).
 #include "cf_rows.h"
 #include "cf_kernels.h"
 #include "cf_train.h"
@@ -236,7 +240,7 @@ constexpr int LIST = 512;  // logits collected before equal ones are counted
 
 // The logits [begin, end) of a row in vectors that start at multiples of 16
 // bytes, whatever the row's own start: the first vector holds what comes
-// before the first such place (4096 rows of 100003 in bf16: 186 -> 166 us).
+// before the first such place (4096 rows of 100003 in bf16: 170 -> 150 us).
 // Vector v has n logits from index i on (none: n <= 0).
 template <typename Z>
 struct Piece {
@@ -348,7 +352,7 @@ __device__ void find_top(const Piece<Z> &p, int top, float tm, const float *x, T
     // nan is the same in every thread
     bool done = false;
     if (!nan) {
-        if (p.vectors() <= TH) {  // the shares are at hand (one row of 131072 9.8 us a call, read again 10.4)
+        if (p.vectors() <= TH) {  // the shares are at hand (one row of 131072 9.7 us a call, read again 9.9)
             const auto a = p.at(tid);
             if (tm >= bound)
 #pragma unroll
@@ -876,8 +880,8 @@ hipError_t forward(const Args &a, int64_t rows, hipStream_t st) {
         return forward_wave<Z, 64, 8>(a, rows, st);
     const dim3 grid((unsigned)(rows * a.chunks));
     // Short chunks, few vectors a thread: less code for what runs once (one row of
-    // 131072 with eight alternatives 10.2 us a call, 10.7 with four vectors; 32 of
-    // 50257 with twenty 16.1 and 18.0).
+    // 131072 with eight alternatives 9.7 us a call, 9.9 with four vectors; 32 of
+    // 50257 with twenty 15.1 and 16.7).
     if (a.chunk <= 2048)
         a.top ? log_probs_kernel<Z, true, 1><<<grid, dim3(TH), 0, st>>>(a)
               : log_probs_kernel<Z, false, 1><<<grid, dim3(TH), 0, st>>>(a);

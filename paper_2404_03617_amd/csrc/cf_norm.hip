@@ -15,10 +15,10 @@
 //
 // Measured on MI355X, where a copy of 2 GiB moves 4.9 TB/s (kernel times):
 //   forward   401408 x 64 fp16 with statistics and checkpoint 25.4 us, 5.2 TB/s;
-//             25088 x 256 bf16 7.4 us; 2999 x 4095 bf16 13 us, 3.7 TB/s (rows
-//             that start at any 2 bytes); one row of 512 1.7 us, a launch
-//   backward  401408 x 64 from the checkpoint 24.2 us, 5.5 TB/s, and 4.7 us for
-//             the second launch; 2999 x 4095 21 us, 3.5 TB/s, and 4 us: six turns
+//             25088 x 256 bf16 7.7 us; 2999 x 4095 bf16 13 us, 3.8 TB/s (rows
+//             that start at any 2 bytes); one row of 512 1.8 us, a launch
+//   backward  401408 x 64 from the checkpoint 25.0 us, 5.3 TB/s, and 4.8 us for
+//             the second launch; 2999 x 4095 22 us, 3.4 TB/s, and 4 us: six turns
 //             of 512 rows, whose first loads and last stores nothing hides
 #include "cf_rows.h"
 #include "cf_kernels.h"

@@ -9,23 +9,27 @@
 // so that the main loop sees one factor and one offset for 64 channels of a
 // row, and w and b meet the sums in the epilogue.
 //
-// A workgroup makes a TM x TN tile of dW: 64 rows of dy and q at a time go
-// through registers into LDS, the bytes converted to the 16-bit type of dy on
-// the way (one rounding of q * scale or xh, 2^-9 in bf16 against the 2^-8 of
-// its block's largest value that 8 bits keep), two buffers, one barrier a
-// step.  Both operands have the summed index r outermost, so MFMA fragments
+// A workgroup makes a TM x TN tile of dW: 32 to 128 rows (by the tile) of dy and
+// q at a time go through registers into LDS, the bytes converted to the 16-bit type
+// of dy on the way (one rounding of q * scale or xh, 2^-9 in bf16 against the 2^-8
+// of its block's largest value that 8 bits keep), two buffers, one barrier a
+// step.  That rounding adds a third to the error of dW, most of which is the
+// rounding of the result: 2.8e-4 of its norm instead of 2.1e-4 in fp16, 2.2e-3
+// instead of 1.7e-3 in bf16.  Both operands have the summed index r outermost, so MFMA fragments
 // are read with the transposing LDS loads.  A row of LDS is padded by 64
 // bytes: the 4 rows that 32 lanes read together then lie in different banks.
 // Few tiles over many rows: the rows are split over workgroups that write fp32
 // partial sums, and a second launch adds them in a fixed order.
 //
-// Measured on MI355X (the library's product of two bf16 matrices of the largest
-// size below, without bytes to convert, takes 457 us; a copy moves 4.9 TB/s):
-//   16384 rows, K = C = 4096, bf16: 500 us, 1100 TFLOP/s (fp16 540).  MFMA busy
-//     61%, VALU 43%, LDS 46%; without the conversion (wrong results) it is 451 us,
-//     with every fetch from the same rows 519: the VALU work beside the products
-//     bounds it, not memory
-//   401408 rows, K = 256, C = 64, fp16 after a norm: 46.4 us and 7.2 us for the
+// Measured on MI355X (the library's product of two matrices of the largest size
+// below, without bytes to convert, takes 466 us in bf16 and 485 in fp16; a copy
+// moves 4.9 TB/s):
+//   16384 rows, K = C = 4096: bf16 502 us, 1095 TFLOP/s, fp16 509; after a norm 539
+//     and 567.  MFMA busy 65%, VALU 42%, LDS 49%: what stands beside the products, the
+//     way of both operands through registers into LDS, bounds it, not memory.  The
+//     sums of dy, in the tiles of the first columns alone, take 18 us of it in bf16
+//     and none in fp16
+//   401408 rows, K = 256, C = 64, fp16 after a norm: 45.8 us and 7.1 us for the
 //     second launch, 5.0 TB/s: memory
 //   49 rows, K = 2048, C = 512: 4.7 us, one step of 64 rows from load to store
 #pragma once

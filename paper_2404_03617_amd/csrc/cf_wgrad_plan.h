@@ -42,9 +42,9 @@ constexpr double PART_BYTES = 128 << 20;
 // microseconds, fitted to runs of every tile over 24 shapes (K and C from 21
 // to 8192, 27 to 401408 rows), where it picks the best or one within 15% of it:
 //   - a workgroup's start and end (`fixed`);
-//   - its steps of 64 rows, each as long as for a workgroup alone on its CU
-//     (`alone`) or as its share of a full one (`full` times the workgroups of
-//     the CU), whichever is longer;
+//   - its rows, by 64 (whatever a step of the tile stages), each as long as for a
+//     workgroup alone on its CU (`alone`) or as its share of a full one (`full`
+//     times the workgroups of the CU), whichever is longer;
 //   - partial sums written and read, at 6 TB/s, and a second launch.
 // Large dW fill the chip with large tiles; small ones over many rows split the
 // rows over workgroups whose wave groups share a tile (fewer partial sums);

@@ -8,6 +8,9 @@ Tensors are [..., C] in fp16 or bf16 (logits in fp32 too) on the GPU: NHWC
 activations, or rows of tokens.  Their last dimension is contiguous and the
 others are rows at one stride, so slices of the channels of a wider tensor will
 do, and as inputs rows that were expanded.  Parameters and statistics are fp32.
+Gradients are what the calls named _backward and _grad return: as everywhere in
+the package a tensor that requires gradients is read like any other, and results
+have no autograd graph.
 """
 from __future__ import annotations
 
@@ -60,9 +63,9 @@ class LogProbs(NamedTuple):
 # one function.  They give None for what is not theirs (a stream or workspace of
 # the caller's, anything wrong), and the functions below go on in Python.  A call
 # on little data, back to back, through Python's checks and ctypes and through
-# here: layer norm of one row of 512 7.6 and 4.2 us, weight gradient of 49 rows
-# 10.4 and 5.9, scoring of 128 rows of 1000 with five alternatives 16.6 and 7.6,
-# of one row of 131072 with eight 20.7 and 11.3.
+# here: layer norm of one row of 512 9.6 and 4.1 us, weight gradient of 49 rows
+# 13.5 and 5.8, scoring of 128 rows of 1000 with five alternatives 18.2 and 7.3,
+# of one row of 131072 with eight 22.5 and 10.9.
 
 _BOUND = ("cf_layer_norm_forward", "cf_layer_norm_backward", "cf_layer_norm_backward_workspace_bytes",
           "cf_act_forward", "cf_act_backward", "cf_checkpoint_unpack", "cf_linear_weight_grad",

@@ -65,8 +65,10 @@ typedef enum { CF_F16 = 0, CF_BF16 = 1 } cf_dtype;
  * hidden groups (cf_stage_forward) up to 128 pixels among them, works in fp32 with an
  * error below 1e-7 max(1, |u|) (the kernel for N*H*W <= 64: 3e-7, by the erf of
  * Abramowitz & Stegun 7.1.26).
- * CF_ACT_NONE makes the block affine (used by tests). */
-typedef enum { CF_ACT_GELU_ERF = 0, CF_ACT_RELU = 1, CF_ACT_NONE = 2 } cf_act;
+ * CF_ACT_NONE makes the block affine (used by tests).  CF_ACT_SILU, u / (1 +
+ * exp(-u)), is for the operators for heads at the end of this file; the others
+ * refuse it. */
+typedef enum { CF_ACT_GELU_ERF = 0, CF_ACT_RELU = 1, CF_ACT_NONE = 2, CF_ACT_SILU = 3 } cf_act;
 
 /* Weights of one block (all device pointers).
  *   dw_w  [k][k][C]     depth-wise taps (tap-major, channels fastest)
@@ -518,6 +520,99 @@ size_t cf_log_probs_workspace_bytes(int64_t rows, int V, int top);
 cf_status cf_log_probs_backward(const void *z, const int64_t *tokens, const float *stats, const float *entropy,
                                 const float *d_logp, const float *d_entropy, void *dz, int64_t rows, int V,
                                 int64_t ldz, int64_t lddz, cf_logits_dtype dt, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Operators for heads over features: group norm with an activation, the gated
+ * feed-forward block, and log probabilities straight from features, each with
+ * its gradients.  Rows, strides, pointers and workspaces as in the section
+ * above; act is any cf_act, in fp32.  Workspaces are 16-byte aligned, NULL for 0
+ * bytes, and need no clearing; calls that overlap in time need their own.
+ *
+ * The matrix products read rows in place that start at 16-byte aligned
+ * addresses, with strides that are multiples of 8 elements and below 2^22, and
+ * whose length is a multiple of 8; other operands are copied into the workspace
+ * first.  The queries' `aligned` says (not 0) that the call's 16-bit inputs
+ * have such addresses and strides, and w_gate and w_up one stride; without it they
+ * leave room for copies of all of them. */
+
+/* Group norm over NHWC feature maps: x [N][P][C], P pixels an image, G groups of
+ * C / G channels (at most CF_GROUP_MAX).  Over the P * C / G values of each group
+ *   mean = avg x,  rstd = 1 / sqrt(avg (x - mean)^2 + eps)
+ *   y = act(weight[c] * (x - mean) * rstd + bias[c])
+ * weight, bias [C] may be NULL.  stats [N][G][2] (mean and rstd, for the
+ * backward pass) may be NULL.  y may equal x with ldy = ldx. */
+#define CF_GROUP_MAX 4096
+cf_status cf_group_norm_forward(const void *x, void *y, const float *weight, const float *bias, float *stats, void *ws,
+                                size_t ws_bytes, int64_t N, int64_t P, int C, int G, int64_t ldx, int64_t ldy,
+                                float eps, cf_dtype dt, cf_act act, void *stream);
+size_t cf_group_norm_workspace_bytes(int64_t N, int64_t P, int C, int G);
+
+/* Its gradients, with xh = (x - mean) * rstd, du = dy * act'(weight * xh + bias),
+ * g = weight * du and averages over a group:
+ *   dx = rstd * (g - avg g - xh * avg g xh)
+ *   dweight = sum over images and pixels of du * xh,  dbias = sum of du
+ * x, weight, bias, act and stats as in the forward call.  dx may equal dy with
+ * lddx = lddy.  dweight and dbias [C]: both or neither. */
+cf_status cf_group_norm_backward(const void *dy, const void *x, const float *stats, const float *weight,
+                                 const float *bias, void *dx, float *dweight, float *dbias, void *ws, size_t ws_bytes,
+                                 int64_t N, int64_t P, int C, int G, int64_t lddy, int64_t ldx, int64_t lddx,
+                                 cf_dtype dt, cf_act act, void *stream);
+size_t cf_group_norm_backward_workspace_bytes(int64_t N, int64_t P, int C, int G);
+
+/* Gated feed-forward block, x and y [rows][C]:
+ *   a = x w_gate^T,  u = x w_up^T,  h = act(a) * u,  y = h w_down^T
+ * w_gate, w_up [H][C] and w_down [C][H] in dt, rows ld_* apart.  Sums are fp32; h is
+ * rounded to dt for its product.  saved [rows][2 H] fp32 receives a and u of each
+ * row for the backward pass; NULL for inference.  y may not overlap x. */
+cf_status cf_gated_ffn_forward(const void *x, const void *w_gate, const void *w_up, const void *w_down, void *y,
+                               float *saved, void *ws, size_t ws_bytes, int64_t rows, int C, int H, int64_t ldx,
+                               int64_t ld_gate, int64_t ld_up, int64_t ld_down, int64_t ldy, cf_dtype dt, cf_act act,
+                               void *stream);
+size_t cf_gated_ffn_workspace_bytes(int64_t rows, int C, int H, int aligned);
+
+/* Its gradients, from the forward call's inputs and saved:
+ *   dh = dy w_down,  da = dh * u * act'(a),  du = dh * act(a)
+ *   dx = da w_gate + du w_up
+ *   dw_gate = da^T x,  dw_up = du^T x,  dw_down = dy^T h
+ * da, du and h are rounded to dt for their products.  dw_gate, dw_up [H][C] and
+ * dw_down [C][H] in dt, dense; rows = 0 gives zeros.  No output may overlap an
+ * input. */
+cf_status cf_gated_ffn_backward(const void *dy, const void *x, const float *saved, const void *w_gate, const void *w_up,
+                                const void *w_down, void *dx, void *dw_gate, void *dw_up, void *dw_down, void *ws,
+                                size_t ws_bytes, int64_t rows, int C, int H, int64_t lddy, int64_t ldx, int64_t ld_gate,
+                                int64_t ld_up, int64_t ld_down, int64_t lddx, cf_dtype dt, cf_act act, void *stream);
+size_t cf_gated_ffn_backward_workspace_bytes(int64_t rows, int C, int H, int aligned);
+
+/* Log probabilities from features x [rows][C] and a classifier's weight [V][C]
+ * in dt, without its logits z = x weight^T, which stay in fp32 and are never
+ * stored:
+ *   lse[r] = log sum_v exp(z[r][v])
+ *   logp[r] = z[r][token] - lse[r]   (tokens, logp: both or neither NULL; 0 for a
+ *             negative token, NaN for one of V or more)
+ * A row whose logits are all -inf has lse and logp -inf; one with +inf or NaN
+ * has NaN. */
+cf_status cf_linear_log_probs_forward(const void *x, const void *weight, const int64_t *tokens, float *logp, float *lse,
+                                      void *ws, size_t ws_bytes, int64_t rows, int C, int V, int64_t ldx, int64_t ldw,
+                                      cf_dtype dt, void *stream);
+size_t cf_linear_log_probs_workspace_bytes(int64_t rows, int C, int V, int aligned);
+
+/* The gradients of sum(d_logp * logp) + sum(d_lse * lse), either of which may be
+ * NULL (d_logp needs tokens); lse is the forward call's:
+ *   dz[r][v] = (d_lse[r] - d_logp[r]) p_v + d_logp[r] 1[v = token],  p = exp(z - lse)
+ *   dx = dz weight,  dweight = dz^T x
+ * The logits are made again, a piece of the vocabulary at a time (dz of a piece,
+ * in dt, is in the workspace: 256 MiB, or rows * 8 KiB if that is more); in fp16 dz
+ * is scaled by a power of two a row, so that small probabilities keep their
+ * bits.  Rows whose d_logp and d_lse are 0 (d_logp counts as 0 for a negative token)
+ * or whose lse is -inf have no gradient and add nothing to dweight, whatever
+ * their features hold.  A token of V or more makes the gradients NaN.  dx
+ * [rows][C] and dweight [V][C], dense, in dt; rows = 0 gives zeros in dweight.  No
+ * output may overlap an input. */
+cf_status cf_linear_log_probs_backward(const void *x, const void *weight, const int64_t *tokens, const float *lse,
+                                       const float *d_logp, const float *d_lse, void *dx, void *dweight, void *ws,
+                                       size_t ws_bytes, int64_t rows, int C, int V, int64_t ldx, int64_t ldw,
+                                       int64_t lddx, cf_dtype dt, void *stream);
+size_t cf_linear_log_probs_backward_workspace_bytes(int64_t rows, int C, int V, int aligned);
 
 /* Thread-local message describing the most recent non-CF_OK status. */
 const char *cf_last_error(void);

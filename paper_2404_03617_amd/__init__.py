@@ -37,6 +37,9 @@ __all__ = [
     "Checkpoint", "LogProbs", "layer_norm_forward", "layer_norm_forward_save", "layer_norm_backward",
     "checkpoint_pack", "checkpoint_unpack", "act_forward", "act_forward_save", "act_backward",
     "linear_weight_grad", "log_probs_forward", "log_probs_backward",
+    "LinearLogProbs", "group_norm_forward", "group_norm_forward_save", "group_norm_backward",
+    "gated_ffn_forward", "gated_ffn_forward_save", "gated_ffn_backward",
+    "linear_log_probs_forward", "linear_log_probs_backward",
 ]
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -59,6 +62,11 @@ EXPORTED_SYMBOLS = (
     "cf_checkpoint_pack", "cf_checkpoint_unpack", "cf_act_forward", "cf_act_backward",
     "cf_linear_weight_grad", "cf_linear_weight_grad_workspace_bytes",
     "cf_log_probs_forward", "cf_log_probs_workspace_bytes", "cf_log_probs_backward",
+    "cf_group_norm_forward", "cf_group_norm_workspace_bytes", "cf_group_norm_backward",
+    "cf_group_norm_backward_workspace_bytes", "cf_gated_ffn_forward", "cf_gated_ffn_workspace_bytes",
+    "cf_gated_ffn_backward", "cf_gated_ffn_backward_workspace_bytes", "cf_linear_log_probs_forward",
+    "cf_linear_log_probs_workspace_bytes", "cf_linear_log_probs_backward",
+    "cf_linear_log_probs_backward_workspace_bytes",
 )
 
 
@@ -226,6 +234,18 @@ def lib():
             "cf_log_probs_forward": (i, [vp] * 7 + [i, vp, sz, l, i, l, i, vp]),
             "cf_log_probs_workspace_bytes": (sz, [l, i, i]),
             "cf_log_probs_backward": (i, [vp] * 7 + [l, i, l, l, i, vp]),
+            "cf_group_norm_forward": (i, [vp] * 6 + [sz, l, l, i, i, l, l, f, i, i, vp]),
+            "cf_group_norm_workspace_bytes": (sz, [l, l, i, i]),
+            "cf_group_norm_backward": (i, [vp] * 9 + [sz, l, l, i, i, l, l, l, i, i, vp]),
+            "cf_group_norm_backward_workspace_bytes": (sz, [l, l, i, i]),
+            "cf_gated_ffn_forward": (i, [vp] * 7 + [sz, l, i, i, l, l, l, l, l, i, i, vp]),
+            "cf_gated_ffn_workspace_bytes": (sz, [l, i, i, i]),
+            "cf_gated_ffn_backward": (i, [vp] * 11 + [sz, l, i, i, l, l, l, l, l, l, i, i, vp]),
+            "cf_gated_ffn_backward_workspace_bytes": (sz, [l, i, i, i]),
+            "cf_linear_log_probs_forward": (i, [vp] * 6 + [sz, l, i, i, l, l, i, vp]),
+            "cf_linear_log_probs_workspace_bytes": (sz, [l, i, i, i]),
+            "cf_linear_log_probs_backward": (i, [vp] * 9 + [sz, l, i, i, l, l, l, i, vp]),
+            "cf_linear_log_probs_backward_workspace_bytes": (sz, [l, i, i, i]),
         })
         for name, (res, args) in sig.items():
             f = getattr(L, name)
@@ -1021,7 +1041,10 @@ class ConvFirstBlock(torch.nn.Module):
         return block_forward(x, self.params(), act=self.act)
 
 
-from . import training  # noqa: E402
+from . import heads, training  # noqa: E402
+from .heads import (LinearLogProbs, gated_ffn_backward, gated_ffn_forward, gated_ffn_forward_save,  # noqa: E402
+                    group_norm_backward, group_norm_forward, group_norm_forward_save, linear_log_probs_backward,
+                    linear_log_probs_forward)
 from .training import (Checkpoint, LogProbs, act_backward, act_forward, act_forward_save,  # noqa: E402
                        checkpoint_pack, checkpoint_unpack, layer_norm_backward, layer_norm_forward,
                        layer_norm_forward_save, linear_weight_grad, log_probs_backward, log_probs_forward)

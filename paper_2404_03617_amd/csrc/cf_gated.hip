@@ -1,0 +1,175 @@
+// cf_gated.hip -- the gated feed-forward block
+//
+//   y = (act(x Wg^T) * (x Wu^T)) Wd^T,   x [rows][C], Wg, Wu [H][C], Wd [C][H]
+//
+// as two products (cf_mm.h): the first makes gate and up channels in the same
+// tile and leaves h = act(g) u; the second projects h.  Backward, from dy and
+// the g and u of the forward pass:
+//
+//   dh = dy Wd, in the same launch dg = dh u act'(g), du = dh act(g) and h again
+//   dWd = dy^T h;  dWg = dg^T x, dWu = du^T x (one launch);  dx = dg Wg + du Wu (one sum)
+//
+// h, dg and du are rounded to the type of x for the products that read them.
+#include "cf_head.h"
+#include "cf_mm_run.h"
+
+namespace cf {
+
+using namespace mm;
+
+namespace {
+
+// Which operands need a packed copy.  Gate and up are read with one stride.
+struct Copied {
+    bool x, dy, wgu, wd;
+};
+Copied copied_of(const GatedFfn &a, const RowsIn &dy) {
+    if (a.rows == 0)  // nothing is read
+        return {false, false, false, false};
+    return {!fits(a.x.p, a.x.ld, a.C), !fits(dy.p, dy.ld, a.C),
+            !fits(a.w_gate.p, a.w_gate.ld, a.C) || !fits(a.w_up.p, a.w_up.ld, a.C) || a.w_gate.ld != a.w_up.ld,
+            !fits(a.w_down.p, a.w_down.ld, a.H)};
+}
+Copied copied_at_most(int C, int H, bool aligned) {
+    const bool c = C % 8 != 0 || !aligned, h = H % 8 != 0 || !aligned;
+    return {c, c, c, h};
+}
+
+struct ForwardPlan {
+    Room room;
+    Operand x, wg, wu, wd;
+    int pad;
+    uint16_t *h;
+    Plan up, down;
+    void *part;
+};
+ForwardPlan forward_plan(const GatedFfn &a, const Copied &c, void *ws) {
+    ForwardPlan p;
+    p.room.p = (uint8_t *)ws;
+    p.pad = up8(a.H);
+    p.x = operand(a.x.p, a.x.ld, a.rows, a.C, c.x, p.room);
+    p.wg = operand(a.w_gate.p, a.w_gate.ld, a.H, a.C, c.wgu, p.room);
+    p.wu = operand(a.w_up.p, a.w_up.ld, a.H, a.C, c.wgu, p.room);
+    p.wd = operand(a.w_down.p, a.w_down.ld, a.C, a.H, c.wd, p.room);
+    p.h = (uint16_t *)p.room.take((size_t)a.rows * p.pad * 2);
+    p.up = plan(a.rows, 2 * (int64_t)a.H, a.C, false);
+    p.down = plan(a.rows, a.C, a.H, true);
+    p.part = p.room.take(part_bytes(p.down, a.rows, a.C, 1));
+    return p;
+}
+
+struct BackwardPlan {
+    Room room;
+    Operand x, dy, wg, wu, wd;
+    int pad;
+    uint16_t *d, *h;
+    Plan dh, dwd, dwu, dx;
+    void *part;
+};
+BackwardPlan backward_plan(const GatedFfn &a, const RowsIn &dy, const Copied &c, void *ws) {
+    BackwardPlan p;
+    p.room.p = (uint8_t *)ws;
+    p.pad = up8(a.H);
+    p.x = operand(a.x.p, a.x.ld, a.rows, a.C, c.x, p.room);
+    p.dy = operand(dy.p, dy.ld, a.rows, a.C, c.dy, p.room);
+    p.wg = operand(a.w_gate.p, a.w_gate.ld, a.H, a.C, c.wgu, p.room);
+    p.wu = operand(a.w_up.p, a.w_up.ld, a.H, a.C, c.wgu, p.room);
+    p.wd = operand(a.w_down.p, a.w_down.ld, a.C, a.H, c.wd, p.room);
+    p.d = (uint16_t *)p.room.take((size_t)a.rows * 2 * p.pad * 2);
+    p.h = (uint16_t *)p.room.take((size_t)a.rows * p.pad * 2);
+    p.dh = plan(a.rows, a.H, a.C, false);
+    p.dwd = plan(a.C, a.H, a.rows, true);
+    p.dwu = plan(a.H, a.C, a.rows, true, 2);
+    p.dx = plan(a.rows, a.C, a.H, true, 1, 2);
+    size_t part = part_bytes(p.dwd, a.C, a.H, 1);
+    const size_t two = part_bytes(p.dwu, a.H, a.C, 2), three = part_bytes(p.dx, a.rows, a.C, 1);
+    part = part > two ? part : two;
+    p.part = p.room.take(part > three ? part : three);
+    return p;
+}
+
+template <typename T>
+hipError_t forward(const GatedFfn &a, const ForwardPlan &p, void *y, int64_t ldy, float *saved, int bf16, hipStream_t st) {
+    CF_HIP(pack(p.x, bf16, st));
+    CF_HIP(pack(p.wg, bf16, st));
+    CF_HIP(pack(p.wu, bf16, st));
+    CF_HIP(pack(p.wd, bf16, st));
+    Args up = args_of(p.up, a.rows, 2 * a.H, a.C, p.x.m, a.rows, p.wg.m, a.H);
+    up.b[1] = p.wu.m.p;
+    CF_HIP(launch_gated<T>(up, GatedArgs{p.h, p.pad, saved, a.H, p.pad, a.act}, p.up.tile, st));
+    StoreArgs s = {};
+    s.out[0] = s.out[1] = (uint16_t *)y;
+    s.ldo = ldy;
+    return run_store<KC, KC>(args_of(p.down, a.rows, a.C, a.H, Matrix{p.h, p.pad, p.pad}, a.rows, p.wd.m, a.C), s,
+                             p.down, p.part, bf16, st);
+}
+
+template <typename T>
+hipError_t backward(const GatedFfn &a, const BackwardPlan &p, const float *saved, const GatedGrads &g, int bf16,
+                    hipStream_t st) {
+    CF_HIP(pack(p.x, bf16, st));
+    CF_HIP(pack(p.dy, bf16, st));
+    CF_HIP(pack(p.wg, bf16, st));
+    CF_HIP(pack(p.wu, bf16, st));
+    CF_HIP(pack(p.wd, bf16, st));
+    const Matrix h = {p.h, p.pad, p.pad}, d = {p.d, 2 * (int64_t)p.pad, p.pad};
+    if (a.rows > 0) {
+        CF_HIP(launch_gated_back<T>(args_of(p.dh, a.rows, a.H, a.C, p.dy.m, a.rows, p.wd.m, p.wd.m.ext),
+                                    GatedBackArgs{saved, p.d, p.h, a.H, p.pad, a.act}, p.dh.tile, st));
+        Args dx = args_of(p.dx, a.rows, a.C, a.H, d, a.rows, p.wg.m, p.wg.m.ext, true);
+        dx.a[1] = p.d + p.pad;
+        dx.b[1] = p.wu.m.p;
+        StoreArgs s = {};
+        s.out[0] = s.out[1] = (uint16_t *)g.dx;
+        s.ldo = g.lddx;
+        CF_HIP((run_store<KC, RC>(dx, s, p.dx, p.part, bf16, st)));
+    }
+    StoreArgs s = {};
+    s.out[0] = s.out[1] = (uint16_t *)g.dw_down;
+    s.ldo = a.H;
+    CF_HIP((run_store<RC, RC>(args_of(p.dwd, a.C, a.H, a.rows, p.dy.m, p.dy.m.ext, h, p.pad), s, p.dwd, p.part, bf16, st)));
+    Args w = args_of(p.dwu, a.H, a.C, a.rows, d, p.pad, p.x.m, p.x.m.ext, false, 2);
+    w.a[1] = p.d + p.pad;
+    s.out[0] = (uint16_t *)g.dw_gate;
+    s.out[1] = (uint16_t *)g.dw_up;
+    s.ldo = a.C;
+    return run_store<RC, RC>(w, s, p.dwu, p.part, bf16, st);
+}
+
+}  // namespace
+
+bool products_read(const void *p, int64_t ld, int cols) { return fits(p, ld, cols); }
+
+bool gated_fits(int64_t rows, int C, int H) {
+    return rows < (int64_t)1 << 30 && C <= 1 << 20 && H <= 1 << 20 && grid_fits(rows, C) && grid_fits(rows, 2 * (int64_t)H) &&
+           grid_fits(2 * (int64_t)H, C) && pack_fits(rows, C) && pack_fits(H, C) && pack_fits(C, H);
+}
+
+size_t gated_workspace_bytes(int64_t rows, int C, int H, bool aligned) {
+    GatedFfn a = {};
+    a.rows = (int)rows;
+    a.C = C;
+    a.H = H;
+    return forward_plan(a, copied_at_most(C, H, aligned), nullptr).room.used;
+}
+
+size_t gated_backward_workspace_bytes(int64_t rows, int C, int H, bool aligned) {
+    GatedFfn a = {};
+    a.rows = (int)rows;
+    a.C = C;
+    a.H = H;
+    return backward_plan(a, RowsIn{}, copied_at_most(C, H, aligned), nullptr).room.used;
+}
+
+hipError_t launch_gated(const GatedFfn &a, void *y, int64_t ldy, float *saved, int bf16, void *ws, hipStream_t st) {
+    const ForwardPlan p = forward_plan(a, copied_of(a, a.x), ws);
+    return bf16 ? forward<BF16>(a, p, y, ldy, saved, bf16, st) : forward<F16>(a, p, y, ldy, saved, bf16, st);
+}
+
+hipError_t launch_gated_backward(const GatedFfn &a, RowsIn dy, const float *saved, const GatedGrads &g, int bf16,
+                                 void *ws, hipStream_t st) {
+    const BackwardPlan p = backward_plan(a, dy, copied_of(a, dy), ws);
+    return bf16 ? backward<BF16>(a, p, saved, g, bf16, st) : backward<F16>(a, p, saved, g, bf16, st);
+}
+
+}  // namespace cf

@@ -1,0 +1,67 @@
+// cf_gnorm_plan.h -- how a group norm (cf_gnorm.hip) is cut into workgroups, in
+// plain C++ so that a test can ask without a GPU.
+#pragma once
+
+#include <stddef.h>
+#include <stdint.h>
+
+namespace cf {
+namespace gnorm {
+
+constexpr int FORWARD_NV = 32, BACKWARD_NV = 16;  // the most vectors that registers hold (backward: of x and of dy)
+
+// A workgroup takes `per_block` groups of one image, or a part of its pixels,
+// and holds them in registers: `nv` vectors of 8 channels a thread.
+struct Plan {
+    int per_block, blocks;  // groups of a workgroup, workgroups beside each other
+    int chunks;             // parts of an image's pixels
+    int64_t px;             // pixels of a part
+    int V, rows;            // vectors beside each other, pixels at a time
+    int threads, nv;
+};
+
+// The channels of a workgroup are a run of whole groups, at least `want` bytes
+// of each pixel.
+inline Plan shape(int64_t P, int C, int G, int want, int most_nv) {
+    const int D = C / G;
+    Plan p;
+    p.per_block = (want + 2 * D - 1) / (2 * D);
+    p.per_block = p.per_block > G ? G : p.per_block;
+    p.blocks = (G + p.per_block - 1) / p.per_block;
+    p.V = (p.per_block * D + 7) / 8;
+    const int64_t vectors = P * p.V;
+    p.threads = vectors > 1024 || p.V > 256 ? 512 : 256;
+    p.rows = p.threads / p.V;
+    const int64_t hold = p.rows > 0 ? (int64_t)p.rows * most_nv : 0;  // pixels that fit
+    p.chunks = hold ? (int)((P + hold - 1) / hold) : 0;
+    p.px = p.chunks ? (P + p.chunks - 1) / p.chunks : 0;
+    p.nv = p.rows ? (int)((p.px + p.rows - 1) / p.rows) : 0;
+    return p;
+}
+
+// 128 bytes of a pixel, a cache line, where that leaves a workgroup for every
+// CU and a whole image in one; else 64; images that are too large for either,
+// or too few, are cut.
+inline Plan plan_of(int64_t N, int64_t P, int C, int G, int most_nv, int64_t cus) {
+    Plan p = shape(P, C, G, 128, most_nv);
+    if (p.chunks != 1 || N * p.blocks < cus) {
+        const Plan half = shape(P, C, G, 64, most_nv);
+        if (half.chunks == 1)
+            p = half;
+    }
+    // few workgroups with much to do each: parts of at least 4 vectors a thread
+    if (p.chunks >= 1 && N * p.blocks * p.chunks < cus / 2 && p.nv > 4) {
+        int64_t chunks = (cus + N * p.blocks - 1) / (N * p.blocks);
+        const int64_t most = (P + 4 * p.rows - 1) / (4 * p.rows);
+        chunks = chunks < most ? chunks : most;
+        if (chunks > p.chunks) {
+            p.px = (P + chunks - 1) / chunks;
+            p.chunks = (int)((P + p.px - 1) / p.px);
+            p.nv = (int)((p.px + p.rows - 1) / p.rows);
+        }
+    }
+    return p;
+}
+
+}  // namespace gnorm
+}  // namespace cf

@@ -1,0 +1,272 @@
+// cf_linear_lp.hip -- log probabilities of classes or tokens from features and
+// a weight matrix, z = x W^T with W [V][C], without keeping the logits:
+//
+//   lse = log sum exp z,  logp = z[token] - lse
+//
+// Forward: every tile of logits (cf_mm.h) leaves the largest and the sum of exp(z -
+// largest) of its rows, and the token's logit where it has it; a second launch
+// joins the tiles of a row.
+//
+// Backward, with c = d_lse - d_logp and p = exp(z - lse):
+//
+//   dz = c p + d_logp 1[token];  dx = dz W;  dW = dz^T x
+//
+// piece by piece of the vocabulary: the piece's logits are made again and become dz
+// in 16 bits (at most PIECE_BYTES of them), which two products read.  dx runs
+// over the pieces in fp32.
+//
+// A gradient in 16 bits: in bf16 its range is that of fp32.  In fp16 a row's
+// values are scaled by a power of two, so that the largest of c and d_logp lies
+// in [2^13, 2^14) and a probability of 4e-9 still has all bits; dx is scaled
+// back by row, and the rows of x that dW sums are scaled against each other
+// (exactly, but for what falls below fp16 against the largest row) and the sums
+// back.  The same copy of x leaves out rows without a gradient: what their
+// features hold, NaN included, reaches nothing.
+#include "cf_head.h"
+#include "cf_mm_run.h"
+#include "cf_rows.h"
+
+namespace cf {
+
+using namespace mm;
+
+namespace {
+
+constexpr double PIECE_BYTES = 256 << 20;
+
+__global__ __launch_bounds__(256) void join_lse_kernel(const float2 *part, const float *picked, const int64_t *tokens,
+                                                       float *logp, float *lse, int rows, int V, int parts) {
+    const int lane = threadIdx.x & 15, r = blockIdx.x * 16 + (threadIdx.x >> 4);
+    float2 v = make_float2(-INFINITY, 0.0f);
+    if (r < rows)
+        for (int i = lane; i < parts; i += 16)
+            v = join_lse(v, part[(int64_t)i * rows + r]);
+#pragma unroll
+    for (int d = 1; d < 16; d *= 2)
+        v = join_lse(v, make_float2(__shfl_xor(v.x, d), __shfl_xor(v.y, d)));
+    if (lane || r >= rows)
+        return;
+    const float ls = logf(v.y);
+    lse[r] = v.x + ls;
+    if (logp) {
+        const int64_t t = tokens[r];
+        float l = 0.0f;
+        if (t >= V)
+            l = NAN;
+        else if (t >= 0)
+            l = v.x == -INFINITY && !(v.y != v.y) ? -INFINITY : picked[r] - v.x - ls;
+        logp[r] = l;
+    }
+}
+
+// What a row's gradient is made of; none for c = g = 0.
+__device__ __forceinline__ RowGrad grad_of(const LinearGrads &g, const int64_t *tokens, int V, int r) {
+    const int64_t t = tokens ? tokens[r] : -1;
+    float gl = g.d_logp && t >= 0 ? g.d_logp[r] : 0.0f;
+    if (t >= V && g.d_logp)
+        gl = NAN;
+    const float lse = g.lse[r];
+    RowGrad w = {(g.d_lse ? g.d_lse[r] : 0.0f) - gl, gl, lse, t < V ? (int)t : -1};
+    if (lse == -INFINITY)
+        w.c = w.g = 0.0f;
+    return w;
+}
+// 2^e <= the larger of |c| and |g| < 2^(e+1), within what fp32 can be scaled by
+constexpr int E_MIN = -100, E_MAX = 100;
+__device__ __forceinline__ int exponent_of(const RowGrad &w) {
+    const float a = fmaxf(fabsf(w.c), fabsf(w.g));
+    const int e = (int)(__float_as_uint(a) >> 23) - 127;
+    return e < E_MIN ? E_MIN : e > E_MAX ? E_MAX : e;
+}
+__device__ __forceinline__ float pow2(int e) { return e < -126 ? 0.0f : __uint_as_float((uint32_t)(e + 127) << 23); }
+
+// fp16: the largest exponent, and the factor of dW's sums.  One workgroup.
+__global__ __launch_bounds__(1024) void exponents_kernel(LinearGrads g, const int64_t *tokens, int V, int rows,
+                                                         int *most, float *scale) {
+    __shared__ int s[16];
+    int e = E_MIN;
+    for (int r = threadIdx.x; r < rows; r += 1024) {
+        const int k = exponent_of(grad_of(g, tokens, V, r));
+        e = k > e ? k : e;
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int k = __shfl_xor(e, d);
+        e = k > e ? k : e;
+    }
+    if ((threadIdx.x & 63) == 0)
+        s[threadIdx.x >> 6] = e;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < 16; i++)
+            e = s[i] > e ? s[i] : e;
+        *most = e;
+        *scale = pow2(e - 13);
+    }
+}
+
+__global__ __launch_bounds__(256) void row_grads_kernel(LinearGrads g, const int64_t *tokens, int V, int rows,
+                                                        const int *most, RowGrad *out, float *factor,
+                                                        float *row_scale) {
+    const int r = blockIdx.x * 256 + threadIdx.x;
+    if (r >= rows)
+        return;
+    RowGrad w = grad_of(g, tokens, V, r);
+    const bool none = w.c == 0.0f && w.g == 0.0f;
+    float f = none ? 0.0f : 1.0f;
+    if (most) {
+        const int e = exponent_of(w);
+        w.c *= pow2(13 - e);
+        w.g *= pow2(13 - e);
+        row_scale[r] = pow2(e - 13);
+        f = none ? 0.0f : pow2(e - *most);
+    }
+    out[r] = w;
+    factor[r] = f;
+}
+
+struct ForwardPlan {
+    Room room;
+    Operand x, w;
+    Plan z;
+    int parts;
+    float2 *part;
+    float *picked;
+};
+ForwardPlan forward_plan(const LinearLogProbs &a, bool copy_x, bool copy_w, void *ws) {
+    ForwardPlan p;
+    p.room.p = (uint8_t *)ws;
+    p.x = operand(a.x.p, a.x.ld, a.rows, a.C, copy_x, p.room);
+    p.w = operand(a.w.p, a.w.ld, a.V, a.C, copy_w, p.room);
+    p.z = plan(a.rows, a.V, a.C, false);
+    p.parts = (a.V + TILES[p.z.tile].n - 1) / TILES[p.z.tile].n;
+    p.part = (float2 *)p.room.take((size_t)p.parts * a.rows * sizeof(float2));
+    p.picked = (float *)p.room.take((size_t)a.rows * 4);
+    return p;
+}
+
+struct BackwardPlan {
+    Room room;
+    Operand x, w;
+    uint16_t *xs, *dz;
+    RowGrad *rows;
+    float *factor, *row_scale, *scale, *acc;
+    int *most;
+    int piece, pieces;
+    Plan z, dx, dw;
+    void *part;
+};
+BackwardPlan backward_plan(const LinearLogProbs &a, bool copy_x, bool copy_w, void *ws) {
+    BackwardPlan p;
+    p.room.p = (uint8_t *)ws;
+    p.x = operand(a.x.p, a.x.ld, a.rows, a.C, copy_x, p.room);
+    p.w = operand(a.w.p, a.w.ld, a.V, a.C, copy_w, p.room);
+    p.xs = (uint16_t *)p.room.take(packed_bytes(a.rows, a.C));
+    p.rows = (RowGrad *)p.room.take((size_t)a.rows * sizeof(RowGrad));
+    p.factor = (float *)p.room.take((size_t)a.rows * 4);
+    p.row_scale = (float *)p.room.take((size_t)a.rows * 4);
+    p.scale = (float *)p.room.take(4);
+    p.most = (int *)p.room.take(4);
+    // Pieces of at least 4096 columns, all but the last a multiple of a tile.
+    const double most = PIECE_BYTES / (2.0 * (a.rows > 0 ? a.rows : 1));
+    const int64_t at_most = most < 4096 ? 4096 : most > (1 << 30) ? 1 << 30 : (int64_t)most;
+    p.pieces = (int)((a.V + at_most - 1) / at_most);
+    p.piece = p.pieces == 1 ? a.V : ((a.V + p.pieces - 1) / p.pieces + 255) / 256 * 256;
+    p.pieces = (a.V + p.piece - 1) / p.piece;
+    p.dz = (uint16_t *)p.room.take((size_t)a.rows * up8(p.piece) * 2);
+    p.acc = p.pieces > 1 ? (float *)p.room.take((size_t)a.rows * a.C * 4) : nullptr;
+    p.z = plan(a.rows, p.piece, a.C, false);
+    p.dx = plan(a.rows, a.C, p.piece, true);
+    p.dw = plan(p.piece, a.C, a.rows, true);
+    const size_t one = part_bytes(p.dx, a.rows, a.C, 1), two = part_bytes(p.dw, p.piece, a.C, 1);
+    p.part = p.room.take(one > two ? one : two);
+    return p;
+}
+
+template <typename T>
+hipError_t forward(const LinearLogProbs &a, const ForwardPlan &p, float *logp, float *lse, int bf16, hipStream_t st) {
+    CF_HIP(pack(p.x, bf16, st));
+    CF_HIP(pack(p.w, bf16, st));
+    CF_HIP(launch_lse<T>(args_of(p.z, a.rows, a.V, a.C, p.x.m, a.rows, p.w.m, a.V),
+                         LseArgs{p.part, p.picked, logp ? a.tokens : nullptr}, p.z.tile, st));
+    join_lse_kernel<<<dim3((unsigned)((a.rows + 15) / 16)), 256, 0, st>>>(p.part, p.picked, a.tokens, logp, lse, a.rows,
+                                                                          a.V, p.parts);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t backward(const LinearLogProbs &a, const BackwardPlan &p, const LinearGrads &g, int bf16, hipStream_t st) {
+    CF_HIP(pack(p.x, bf16, st));
+    CF_HIP(pack(p.w, bf16, st));
+    if (a.rows > 0) {
+        if (!bf16)
+            exponents_kernel<<<1, 1024, 0, st>>>(g, a.tokens, a.V, a.rows, p.most, p.scale);
+        row_grads_kernel<<<dim3((unsigned)((a.rows + 255) / 256)), 256, 0, st>>>(
+            g, a.tokens, a.V, a.rows, bf16 ? nullptr : p.most, p.rows, p.factor, bf16 ? nullptr : p.row_scale);
+        CF_HIP(hipGetLastError());
+        CF_HIP(launch_pack(a.x.p, a.x.ld, a.rows, a.C, p.factor, p.xs, bf16, st));
+    }
+    const Matrix xs = {p.xs, up8(a.C), up8(a.C)};
+    for (int i = 0; i < p.pieces; i++) {
+        const int v0 = i * p.piece, n = a.V - v0 < p.piece ? a.V - v0 : p.piece, pad = up8(n);
+        const Matrix w = {p.w.m.p + (int64_t)v0 * p.w.m.ld, p.w.m.ld, p.w.m.ext}, dz = {p.dz, pad, pad};
+        if (a.rows > 0) {
+            CF_HIP(launch_dz<T>(args_of(p.z, a.rows, n, a.C, p.x.m, a.rows, w, n), DzArgs{p.rows, p.dz, pad, v0}, p.z.tile,
+                                st));
+            StoreArgs s = {};
+            s.out[0] = s.out[1] = (uint16_t *)g.dx;
+            s.ldo = g.lddx;
+            s.row_scale = bf16 ? nullptr : p.row_scale;
+            s.acc = p.acc;
+            s.acc_in = i > 0;
+            s.acc_out = i + 1 < p.pieces;
+            CF_HIP((run_store<KC, RC>(args_of(p.dx, a.rows, a.C, n, dz, a.rows, w, w.ext), s, p.dx, p.part, bf16, st)));
+        }
+        StoreArgs s = {};
+        s.out[0] = s.out[1] = (uint16_t *)g.dw + (int64_t)v0 * a.C;
+        s.ldo = a.C;
+        s.scale = bf16 || a.rows == 0 ? nullptr : p.scale;
+        CF_HIP((run_store<RC, RC>(args_of(p.dw, n, a.C, a.rows, dz, pad, xs, xs.ext), s, p.dw, p.part, bf16, st)));
+    }
+    return hipSuccess;
+}
+
+}  // namespace
+
+bool linear_fits(int64_t rows, int C, int V) {
+    return rows < (int64_t)1 << 30 && C <= 1 << 20 && V <= 1 << 30 && grid_fits(rows, V) && grid_fits(V, C) &&
+           grid_fits(rows, C) && pack_fits(rows, C) && pack_fits(V, C);
+}
+
+size_t linear_workspace_bytes(int64_t rows, int C, int V, bool aligned) {
+    LinearLogProbs a = {};
+    a.rows = (int)rows;
+    a.C = C;
+    a.V = V;
+    const bool copy = C % 8 || !aligned;
+    return forward_plan(a, copy, copy, nullptr).room.used;
+}
+
+size_t linear_backward_workspace_bytes(int64_t rows, int C, int V, bool aligned) {
+    LinearLogProbs a = {};
+    a.rows = (int)rows;
+    a.C = C;
+    a.V = V;
+    const bool copy = C % 8 || !aligned;
+    return backward_plan(a, copy, copy, nullptr).room.used;
+}
+
+hipError_t launch_linear_log_probs(const LinearLogProbs &a, float *logp, float *lse, int bf16, void *ws,
+                                   hipStream_t st) {
+    const ForwardPlan p = forward_plan(a, !fits(a.x.p, a.x.ld, a.C), !fits(a.w.p, a.w.ld, a.C), ws);
+    return bf16 ? forward<BF16>(a, p, logp, lse, bf16, st) : forward<F16>(a, p, logp, lse, bf16, st);
+}
+
+hipError_t launch_linear_log_probs_backward(const LinearLogProbs &a, const LinearGrads &g, int bf16, void *ws,
+                                            hipStream_t st) {
+    const bool some = a.rows > 0;  // else nothing is read
+    const BackwardPlan p = backward_plan(a, some && !fits(a.x.p, a.x.ld, a.C), some && !fits(a.w.p, a.w.ld, a.C), ws);
+    return bf16 ? backward<BF16>(a, p, g, bf16, st) : backward<F16>(a, p, g, bf16, st);
+}
+
+}  // namespace cf

@@ -1,0 +1,17 @@
+// cf_mm_logits_f16.hip -- products of cf_mm.h whose results are logits, fp16.
+#include "cf_mm_run.h"
+
+namespace cf {
+namespace mm {
+
+template <>
+hipError_t launch_lse<F16>(const Args &a, const LseArgs &e, int tile, hipStream_t st) {
+    return launch_tile<F16, KC, KC, Lse>(a, e, tile, st);
+}
+template <>
+hipError_t launch_dz<F16>(const Args &a, const DzArgs &e, int tile, hipStream_t st) {
+    return launch_tile<F16, KC, KC, Dz>(a, e, tile, st);
+}
+
+}  // namespace mm
+}  // namespace cf

@@ -1,0 +1,120 @@
+// cf_mm_run.h -- host side of the products of cf_mm.h: operands, plans and
+// launches.  Each kernel is instantiated in one of the files cf_mm_*.hip.
+#pragma once
+
+#include "cf_mm_epi.h"
+
+namespace cf {
+namespace mm {
+
+template <typename T, int LA, int LB>
+hipError_t launch_store(const Args &a, const StoreArgs &e, int tile, hipStream_t st);
+template <typename T>
+hipError_t launch_gated(const Args &a, const GatedArgs &e, int tile, hipStream_t st);
+template <typename T>
+hipError_t launch_gated_back(const Args &a, const GatedBackArgs &e, int tile, hipStream_t st);
+template <typename T>
+hipError_t launch_lse(const Args &a, const LseArgs &e, int tile, hipStream_t st);
+template <typename T>
+hipError_t launch_dz(const Args &a, const DzArgs &e, int tile, hipStream_t st);
+
+// Sums of split products, and what follows.
+hipError_t launch_join(const Args &a, const StoreArgs &e, int bf16, hipStream_t st);
+
+// A matrix as the tiles read it: 16-byte aligned rows that hold `ext` columns,
+// a multiple of 8.
+struct Matrix {
+    const uint16_t *p;
+    int64_t ld;
+    int ext;
+};
+inline int up8(int n) { return (n + 7) & ~7; }
+// whether rows of `cols` can be read where they are
+inline bool fits(const void *p, int64_t ld, int cols) {
+    return cols % 8 == 0 && ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && ld < (int64_t)1 << 22;
+}
+// bytes of a packed copy, whose rows are padded with zeros
+inline size_t packed_bytes(int64_t rows, int cols) { return ((size_t)rows * up8(cols) * 2 + 255) & ~(size_t)255; }
+// whether the copy's vectors can be numbered
+inline bool pack_fits(int64_t rows, int cols) { return (double)rows * (up8(cols) / 8) < 2147483648.0; }
+// row m times factor[m] (1 if null), rows of factor 0 as zeros
+hipError_t launch_pack(const void *src, int64_t ld, int64_t rows, int cols, const float *factor, void *dst, int bf16,
+                       hipStream_t st);
+
+inline Plan plan(int64_t M, int64_t N, int64_t K, bool may_split, int batch = 1, int segments = 1) {
+    return plan_of(M, N, steps_of(K) * segments, batch, may_split, device_cu_count());
+}
+// a workgroup a tile: a launch holds 2^32 threads
+inline bool grid_fits(int64_t M, int64_t N) { return (double)((M + 127) / 128) * (double)((N + 127) / 128) < 4.0e6; }
+
+inline Args args_of(const Plan &p, int M, int N, int K, const Matrix &a, int ext_a, const Matrix &b, int ext_b,
+                    bool two_segments = false, int batch = 1) {
+    Args r;
+    r.a[0] = r.a[1] = a.p;
+    r.b[0] = r.b[1] = b.p;
+    r.lda = a.ld;
+    r.ldb = b.ld;
+    r.M = M;
+    r.N = N;
+    r.K = K;
+    r.ext_a = ext_a;
+    r.ext_b = ext_b;
+    r.seg = (int)steps_of(K);
+    r.steps = two_segments ? 2 * r.seg : r.seg;
+    if (!two_segments)
+        r.seg = 1 << 30;
+    r.per = p.per;
+    r.tiles_m = (M + TILES[p.tile].m - 1) / TILES[p.tile].m;
+    r.tiles_n = (N + TILES[p.tile].n - 1) / TILES[p.tile].n;
+    r.splits = p.splits;
+    r.batch = batch;
+    return r;
+}
+
+// Pieces of a workspace, one after the other; without one, their size.
+struct Room {
+    uint8_t *p;
+    size_t used = 0;
+    void *take(size_t n) {
+        uint8_t *const r = p ? p + used : nullptr;
+        used += (n + 255) & ~(size_t)255;
+        return r;
+    }
+};
+
+// An operand where it is, or room for a packed copy of it.
+struct Operand {
+    Matrix m;
+    const void *from;
+    int64_t ld, rows;
+    int cols;
+    void *copy;
+};
+inline Operand operand(const void *from, int64_t ld, int64_t rows, int cols, bool copied, Room &room) {
+    Operand o = {Matrix{(const uint16_t *)from, ld, cols}, from, ld, rows, cols, nullptr};
+    if (copied) {
+        o.copy = room.take(packed_bytes(rows, cols));
+        o.m = Matrix{(const uint16_t *)o.copy, up8(cols), up8(cols)};
+    }
+    return o;
+}
+inline hipError_t pack(const Operand &o, int bf16, hipStream_t st) {
+    return o.copy ? launch_pack(o.from, o.ld, o.rows, o.cols, nullptr, o.copy, bf16, st) : hipSuccess;
+}
+
+#define CF_HIP(call)                                                                                                   \
+    do {                                                                                                               \
+        const hipError_t e_ = (call);                                                                                  \
+        if (e_ != hipSuccess)                                                                                          \
+            return e_;                                                                                                 \
+    } while (0)
+
+template <int LA, int LB>
+hipError_t run_store(const Args &a, StoreArgs e, const Plan &p, void *part, int bf16, hipStream_t st) {
+    e.part = (float *)part;
+    const hipError_t r = bf16 ? launch_store<BF16, LA, LB>(a, e, p.tile, st) : launch_store<F16, LA, LB>(a, e, p.tile, st);
+    return r != hipSuccess || a.splits == 1 ? r : launch_join(a, e, bf16, st);
+}
+
+}  // namespace mm
+}  // namespace cf

@@ -1,0 +1,255 @@
+"""Log probabilities from features, forward and backward, against 64 bits.  A
+logit is a sum of C exact products in fp32, off by at most C 2^-24 of the sum of
+their magnitudes; dz is rounded to 16 bits once, and so are the gradients."""
+import pytest
+import torch
+
+import paper_2404_03617_amd as cf
+
+from _rows import DT, F32, ROUND, TINY, assert_within, randn, rows_in
+
+pytestmark = pytest.mark.gpu
+
+
+def mm(a, b):
+    return torch.mm(a.contiguous(), b.contiguous())
+
+
+def case(seed, rows, C, V, dt, scale=2.5):
+    x, w = randn(seed, (rows, C), dt), randn(seed + 1, (V, C), dt, scale * C**-0.5)
+    g = torch.Generator().manual_seed(seed + 2)
+    t = torch.randint(0, V, (rows,), generator=g)
+    t[torch.rand(rows, generator=g) < 0.1] = -1
+    return x, w, t, randn(seed + 3, (rows,)), 0.1 * randn(seed + 4, (rows,))
+
+
+def reference(x, w, t, gl, gs, dt):
+    """(value, tolerance) of logp, lse, dx, dw; all arguments in 64 bits but t."""
+    R, T = ROUND[dt], TINY[dt]
+    rows, C = x.shape
+    z, size = mm(x, w.t()), mm(x.abs(), w.abs().t())
+    ez = C * F32 * size
+    lse = torch.logsumexp(z, 1)
+    p = torch.exp(z - lse[:, None])
+    # sums of V terms in tiles: chains of 300 additions at most, an exponential 4 units of its argument's size
+    top = z.amax(1, keepdim=True)
+    e_lse = (p * (ez + (300 + 4 * (z - top).abs()) * F32)).sum(1) + 4 * F32 * (lse.abs() + top[:, 0].abs() + 1)
+    some, at = t >= 0, t.clamp_min(0)[:, None]
+    logp = torch.where(some, z.gather(1, at)[:, 0] - lse, 0.0)
+    e_logp = torch.where(some, ez.gather(1, at)[:, 0] + e_lse + 4 * F32 * (logp.abs() + z.gather(1, at)[:, 0].abs()), 0.0)
+    if gl is None and gs is None:
+        return (logp, e_logp), (lse, e_lse)
+    gl = torch.zeros(rows, dtype=z.dtype) if gl is None else torch.where(some, gl, 0.0)
+    gs = torch.zeros(rows, dtype=z.dtype) if gs is None else gs
+    c = gs - gl
+    dz = c[:, None] * p
+    dz.scatter_add_(1, at, gl[:, None])
+    ep = p * (ez + e_lse[:, None] + 4 * F32 * ((z - lse[:, None]).abs() + 1))
+    edz = c.abs()[:, None] * ep + 2 * F32 * (dz.abs() + (c[:, None] * p).abs())
+    edz = edz + R * (dz.abs() + edz)
+    # fp16: values below 2^-14 of the row's scale, 2^-13 of the larger of c and gl, lose bits
+    tiny = 2.0**-25 * 2.0**-12 * torch.maximum(c.abs(), gl.abs()) if dt == torch.float16 else torch.zeros_like(c)
+    edz = edz + tiny[:, None]
+    # in dW a row of x is scaled against the largest row
+    share = torch.maximum(c.abs(), gl.abs())
+    lost = 2.0**-25 * 2 * share.max() / share.clamp_min(1e-300) if dt == torch.float16 else torch.zeros_like(c)
+    dx, dw = mm(dz, w), mm(dz.t(), x)
+    edx = mm(edz, w.abs()) + (w.shape[0] + 2) * F32 * mm(dz.abs(), w.abs())
+    edw = mm(edz.t(), x.abs()) + (rows + 2) * F32 * mm(dz.abs().t(), x.abs())
+    edw = edw + (dz.abs().t() @ torch.where(share > 0, lost, 0.0))[:, None]
+    return ((logp, e_logp), (lse, e_lse), (dx, edx + R * (dx.abs() + edx) + T), (dw, edw + R * (dw.abs() + edw) + T))
+
+
+NAMES = ("logp", "lse", "dx", "dw")
+
+
+def check(x, w, t, gl, gs, dt, kind="dense", norm=True):
+    print("linear", tuple(x.shape), w.shape[0], dt, kind, flush=True)
+    ref = reference(x.double(), w.double(), t, None if gl is None else gl.double(), None if gs is None else gs.double(), dt)
+    xg, wg, tg = rows_in(kind, x), rows_in(kind, w), t.cuda()
+    lp = cf.linear_log_probs_forward(xg, wg, tg)
+    only = cf.linear_log_probs_forward(xg, wg)
+    assert only.logp is None and torch.equal(only.lse, lp.lse)
+    args = (xg, wg, tg, lp, None if gl is None else gl.cuda(), None if gs is None else gs.cuda())
+    got = (*lp, *cf.linear_log_probs_backward(*args))
+    again = cf.linear_log_probs_backward(*args)
+    assert all(torch.equal(p, q) for p, q in zip(got[2:], again))
+    for g, (v, e), what in zip(got, ref, NAMES):
+        assert_within(g, v, e, what)
+    if norm:
+        for g, (v, _), what in list(zip(got, ref, NAMES))[2:]:
+            assert float((g.double().cpu() - v).norm()) <= 2 * ROUND[dt] * float(v.norm()) + 1e-12, what
+    return got
+
+
+SIZES = [(1, 8, 10), (1, 1, 1), (3, 5, 7), (16, 64, 1000), (17, 40, 130), (100, 130, 33), (128, 128, 128),
+         (129, 136, 264), (300, 520, 1000), (2, 2048, 96), (64, 24, 3001), (1, 1024, 5000), (260, 16, 260), (40, 1, 9)]
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("rows,C,V", SIZES)
+def test_sizes(rows, C, V, dtype):
+    check(*case(rows + C + V, rows, C, V, DT[dtype]), DT[dtype])
+
+
+@pytest.mark.parametrize("kind", ["slice", "shifted"])
+def test_layouts(kind):
+    check(*case(1, 70, 136, 264, torch.float16), torch.float16, kind)
+    check(*case(2, 9, 45, 130, torch.bfloat16), torch.bfloat16, kind)
+
+
+def test_either_gradient_alone():
+    for dt in (torch.float16, torch.bfloat16):
+        x, w, t, gl, gs = case(3, 50, 64, 200, dt)
+        check(x, w, t, gl, None, dt)
+        check(x, w, t, None, gs, dt)
+        lp = cf.linear_log_probs_forward(x.cuda(), w.cuda())
+        a = cf.linear_log_probs_backward(x.cuda(), w.cuda(), None, lp, None, gs.cuda())
+        b = cf.linear_log_probs_backward(x.cuda(), w.cuda(), t.cuda(), lp, None, gs.cuda())
+        assert all(torch.equal(p, q) for p, q in zip(a, b))
+
+
+def test_a_vocabulary_in_pieces():
+    """Rows enough that dz of all classes does not fit in the workspace at once."""
+    rows, C, V = 30000, 16, 5000
+    for dt in (torch.float16, torch.bfloat16):
+        x, w, t, gl, gs = case(5, rows, C, V, dt)
+        xg, wg, tg, gl, gs = x.cuda(), w.cuda(), t.cuda(), gl.cuda(), gs.cuda()
+        lp = cf.linear_log_probs_forward(xg, wg, tg)
+        dx, dw = cf.linear_log_probs_backward(xg, wg, tg, lp, gl, gs)
+        xd, wd = xg.double(), wg.double()
+        z = mm(xd, wd.t())
+        lse = torch.logsumexp(z, 1)
+        assert float((lp.lse - lse).abs().max()) <= 1e-5  # C = 16 products, lse below 16
+        some = tg >= 0
+        g = torch.where(some, gl, torch.zeros_like(gl)).double()
+        dz = torch.exp(z - lse[:, None]) * (gs.double() - g)[:, None]
+        dz.scatter_add_(1, tg.clamp_min(0)[:, None], g[:, None])
+        for got, want in ((dx, mm(dz, wd)), (dw, mm(dz.t(), xd))):
+            assert float((got.double() - want).norm() / want.norm()) <= 2 * ROUND[dt]
+        # each class and each row by themselves
+        for got, want in ((dx, mm(dz, wd)), (dw, mm(dz.t(), xd))):
+            off, size = (got.double() - want).norm(dim=1), want.norm(dim=1)
+            assert bool((off <= 4 * ROUND[dt] * size + 4 * ROUND[dt] * size.median()).all())
+
+
+def test_logits_of_every_size():
+    """Large logits, rows that are certain of their token, rows that hold no chance for it."""
+    for dt in (torch.float16, torch.bfloat16):
+        x, w, t, gl, gs = case(7, 40, 64, 300, dt, scale=20.0)
+        t[:20] = (x.float() @ w.float().t()).argmax(1)[:20]
+        check(x, w, t, gl, gs, dt, norm=False)
+
+
+def test_small_gradients_keep_their_bits():
+    """Means over many rows without a scaled loss: dz lies far below fp16's smallest numbers."""
+    for dt, down in ((torch.float16, 2.0**-14), (torch.bfloat16, 2.0**-40)):
+        x, w, t, gl, gs = case(9, 64, 32, 500, dt)
+        xg, wg, tg = x.cuda(), w.cuda(), t.cuda()
+        lp = cf.linear_log_probs_forward(xg, wg, tg)
+        big = cf.linear_log_probs_backward(xg, wg, tg, lp, gl.cuda(), gs.cuda())
+        small = cf.linear_log_probs_backward(xg, wg, tg, lp, (gl * down).cuda(), (gs * down).cuda())
+        for b, s in zip(big, small):
+            # the same numbers times a power of two, but for those that pass below the type's normal range
+            want = (b.double() * down).to(dt)
+            assert bool(((s.double() - want.double()).abs() <= TINY[dt] * 2).all())
+
+
+def test_rows_without_a_gradient():
+    """Padding: whatever their features hold, they add nothing."""
+    for dt in (torch.float16, torch.bfloat16):
+        x, w, t, gl, gs = case(11, 60, 48, 130, dt)
+        gs[:] = 0
+        keep = t >= 0
+        x[~keep] = float("nan")
+        x[int((~keep).nonzero()[0])] = float("inf")
+        xg, wg, tg = x.cuda(), w.cuda(), t.cuda()
+        lp = cf.linear_log_probs_forward(xg, wg, tg)
+        for d_lse in (None, gs.cuda()):
+            dx, dw = cf.linear_log_probs_backward(xg, wg, tg, lp, gl.cuda(), d_lse)
+            assert bool((dx[~keep.cuda()] == 0).all())
+            lk = cf.linear_log_probs_forward(xg[keep.cuda()], wg, tg[keep.cuda()])
+            ref = reference(x[keep].double(), w.double(), t[keep], gl[keep].double(), None, dt)
+            assert torch.equal(lk.lse, lp.lse[keep.cuda()])
+            assert_within(dx[keep.cuda()], *ref[2], "dx")
+            assert_within(dw, *ref[3], "dw")
+
+
+def test_tokens_out_of_range_and_rows_that_are_not_finite():
+    dt = torch.bfloat16
+    x, w, t, gl, gs = case(13, 12, 16, 20, dt)
+    t[:] = torch.arange(12)
+    t[3], t[5] = 20, 1 << 40
+    x[7, 0] = float("nan")
+    lp = cf.linear_log_probs_forward(x.cuda(), w.cuda(), t.cuda())
+    bad = torch.zeros(12, dtype=torch.bool)
+    bad[[3, 5, 7]] = True
+    assert torch.equal(lp.logp.cpu().isnan(), bad) and torch.equal(lp.lse.cpu().isnan().nonzero()[:, 0], torch.tensor([7]))
+    dx, dw = cf.linear_log_probs_backward(x.cuda(), w.cuda(), t.cuda(), lp, gl.cuda())
+    assert torch.equal(dx.cpu().isnan().all(1), bad) and torch.equal(dx.cpu().isnan().any(1), bad)
+    assert bool(dw.isnan().all())
+    # rows whose logits are all -inf
+    x, w = torch.ones(3, 8, dtype=dt), torch.ones(6, 8, dtype=dt)
+    w[:] = float("-inf")
+    x[1] = 0.5
+    lp = cf.linear_log_probs_forward(x.cuda(), w.cuda(), torch.tensor([0, -1, 2]).cuda())
+    assert bool((lp.lse == float("-inf")).all())
+    assert lp.logp.tolist() == [float("-inf"), 0.0, float("-inf")]
+
+
+def test_leading_dimensions_workspaces_and_no_rows():
+    dt = torch.float16
+    x, w, t, gl, gs = (v.cuda() for v in case(15, 24, 64, 104, dt))
+    lp = cf.linear_log_probs_forward(x, w, t)
+    dx, dw = cf.linear_log_probs_backward(x, w, t, lp, gl, gs)
+    lp4 = cf.linear_log_probs_forward(x.view(2, 3, 4, 64), w, t.view(2, 3, 4))
+    assert lp4.logp.shape == (2, 3, 4) and torch.equal(lp4.logp.flatten(), lp.logp)
+    for aligned in (True, False):
+        ws = torch.full((cf.heads.linear_log_probs_workspace_bytes(24, 64, 104, aligned),), 255, dtype=torch.uint8,
+                        device="cuda")
+        assert torch.equal(cf.linear_log_probs_forward(x, w, t, ws=ws).logp, lp.logp)
+        ws = torch.full((cf.heads.linear_log_probs_backward_workspace_bytes(24, 64, 104, aligned),), 255,
+                        dtype=torch.uint8, device="cuda")
+        wide = torch.full((24, 80), 7.0, dtype=dt, device="cuda")
+        a, b = cf.linear_log_probs_backward(x, w, t, lp, gl, gs, out=wide[:, 8:72], ws=ws)
+        assert torch.equal(a, dx) and torch.equal(b, dw)
+        wide[:, 8:72] = 7.0
+        assert bool((wide == 7.0).all())
+    e = cf.linear_log_probs_forward(x[:0], w, t[:0])
+    assert e.logp.shape == (0,) and e.lse.shape == (0,)
+    a, b = cf.linear_log_probs_backward(x[:0], w, t[:0], e, gl[:0], gs[:0])
+    assert a.shape == (0, 64) and b.shape == (104, 64) and bool((b == 0).all())
+
+
+def test_agrees_with_log_probs_of_the_logits():
+    x, w, t, gl, _ = (v.cuda() for v in case(17, 200, 64, 1000, torch.bfloat16))
+    z = x.float() @ w.float().t()
+    want = cf.log_probs_forward(z, t)
+    got = cf.linear_log_probs_forward(x, w, t)
+    assert float((got.logp - want.logp).abs().max()) <= 2e-5 and float((got.lse - want.stats.sum(-1)).abs().max()) <= 2e-5
+    dz = cf.log_probs_backward(z, t, want, gl)
+    dx, dw = cf.linear_log_probs_backward(x, w, t, got, gl)
+    for a, b in ((dx, dz @ w.float()), (dw, dz.t().contiguous() @ x.float())):
+        assert float((a.float() - b).norm() / b.norm()) <= 2 * ROUND[torch.bfloat16]
+
+
+def test_gradients_against_differences():
+    dt = torch.float16
+    x, w, t, gl, gs = case(19, 6, 24, 40, dt)
+    lp = cf.linear_log_probs_forward(x.cuda(), w.cuda(), t.cuda())
+    grads = [g.double().cpu() for g in cf.linear_log_probs_backward(x.cuda(), w.cuda(), t.cuda(), lp, gl.cuda(), gs.cuda())]
+    ref = reference(x.double(), w.double(), t, gl.double(), gs.double(), dt)
+
+    def loss(x, w):
+        z = x @ w.t()
+        lse = torch.logsumexp(z, 1)
+        logp = torch.where(t >= 0, z.gather(1, t.clamp_min(0)[:, None])[:, 0] - lse, 0.0)
+        return float((logp * gl.double() + lse * gs.double()).sum())
+
+    at = [x.double(), w.double()]
+    for i, g in enumerate(grads):
+        v = randn(30 + i, g.shape).double()
+        up, down = list(at), list(at)
+        up[i], down[i] = at[i] + 1e-5 * v, at[i] - 1e-5 * v
+        want = (loss(*up) - loss(*down)) / 2e-5
+        assert abs(float((g * v).sum()) - want) <= float((ref[2 + i][1] * v.abs()).sum()) + 1e-6, i

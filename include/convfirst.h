@@ -539,7 +539,7 @@ cf_status cf_log_probs_backward(const void *z, const int64_t *tokens, const floa
  * C / G channels (at most CF_GROUP_MAX).  Over the P * C / G values of each group
  *   mean = avg x,  rstd = 1 / sqrt(avg (x - mean)^2 + eps)
  *   y = act(weight[c] * (x - mean) * rstd + bias[c])
- * weight, bias [C] may be NULL.  stats [N][G][2] (mean and rstd, for the
+ * weight, bias [C] may be NULL.  Row strides are below 2^22.  stats [N][G][2] (mean and rstd, for the
  * backward pass) may be NULL.  y may equal x with ldy = ldx. */
 #define CF_GROUP_MAX 4096
 cf_status cf_group_norm_forward(const void *x, void *y, const float *weight, const float *bias, float *stats, void *ws,

@@ -54,6 +54,9 @@ Args args_of(const GroupNorm &g, const Plan &p) {
     a.V = p.V;
     a.rows = p.rows;
     a.whole = p.chunks == 1;
+    a.by_V = make_fastdiv((uint32_t)p.V);
+    a.by_W = make_fastdiv((uint32_t)p.V * 8);
+    a.by_D = make_fastdiv((uint32_t)a.D);
     return a;
 }
 

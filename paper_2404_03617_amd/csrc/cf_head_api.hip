@@ -27,6 +27,12 @@ cf_status no_images(const char *what, int64_t N, int64_t P, int C, int G) {
     return api_fail(CF_ERR_UNSUPPORTED, "%s: no kernel for N=%lld P=%lld C=%d groups=%d (a group of up to %d channels)",
                     what, (long long)N, (long long)P, C, G, CF_GROUP_MAX);
 }
+// row strides: an image's pixels beside each other are told apart in 32 bits
+cf_status check_near(const char *what, int64_t rows, int64_t ld) {
+    if (rows > 1 && ld >= (int64_t)1 << 22)
+        return api_fail(CF_ERR_UNSUPPORTED, "%s: row strides must be below 2^22, got %lld", what, (long long)ld);
+    return CF_OK;
+}
 bool images_fit(int64_t N, int64_t P, int C, int G) { return C / G <= CF_GROUP_MAX && group_norm_fits(N, P, C, G); }
 
 // whether the matrix products could read these rows in place, were their length
@@ -75,6 +81,8 @@ cf_status cf_group_norm_forward(const void *x, void *y, const float *weight, con
         CF_TRY(check_out(what, t[i], t, i, i == 3 ? t[0].name : ""));
     if (!images_fit(N, P, C, G))
         return no_images(what, N, P, C, G);
+    CF_TRY(check_near(what, rows, ldx));
+    CF_TRY(check_near(what, rows, ldy));
     CF_TRY(check_ws(what, ws, ws_bytes, cf_group_norm_workspace_bytes(N, P, C, G), t, 5));
     const GroupNorm a = {x, ldx, weight, bias, N, P, C, G, (int)act};
     return api_done(launch_group_norm(a, y, ldy, stats, eps, dt == CF_BF16, ws, (hipStream_t)stream), what);
@@ -117,6 +125,9 @@ cf_status cf_group_norm_backward(const void *dy, const void *x, const float *sta
         CF_TRY(check_out(what, t[i], t, i, i == 5 ? t[0].name : ""));
     if (rows > 0 && !images_fit(N, P, C, G))
         return no_images(what, N, P, C, G);
+    CF_TRY(check_near(what, rows, lddy));
+    CF_TRY(check_near(what, rows, ldx));
+    CF_TRY(check_near(what, rows, lddx));
     if (rows == 0 && !dweight)
         return api_done(hipSuccess, what);
     CF_TRY(check_ws(what, ws, ws_bytes, cf_group_norm_backward_workspace_bytes(N, P, C, G), t, 8));

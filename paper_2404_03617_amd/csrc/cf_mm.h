@@ -70,46 +70,37 @@ __device__ __forceinline__ Work work_of(const Args &a) {
 template <int L, int R>
 constexpr int PITCH = L == RC && R == 256 ? 1088 : 1024;
 template <int L, int R>
-constexpr int BYTES = R * 64 / 1024 * PITCH<L, R>;
+constexpr int BYTES = R * STEP * 2 / 1024 * PITCH<L, R>;
 
-template <int TM_, int TN_, int WM_, int WN_, int STAGES_, int OCC_>
+template <int TM_, int TN_, int WM_, int WN_, int OCC_>
 struct Shape {
-    static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, STAGES = STAGES_, OCC = OCC_;
+    static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, OCC = OCC_;
     static constexpr int TH = 64 * WM * WN, FM = TM / WM / 16, FN = TN / WN / 16;
-    static constexpr int COPIES = (TM + TN) * 64 / (TH * 16);  // LDS-DMA instructions of a wave and stage
-    static_assert(TM * 64 % (TH * 16) == 0 && TN * 64 % (TH * 16) == 0, "whole copies");
+    static constexpr int COPIES = (TM + TN) * STEP * 2 / (TH * 16);  // LDS-DMA instructions of a wave and stage
+    static_assert(TM * STEP * 2 % (TH * 16) == 0 && TN * STEP * 2 % (TH * 16) == 0, "whole copies");
 };
 
 static __device__ __attribute__((aligned(16))) const uint32_t zero_page[4] = {0, 0, 0, 0};
 
 // 16 bytes a lane from base + voff to LDS address lds + 16 lane
 __device__ __forceinline__ void copy16(const void *base, uint32_t voff, uint32_t lds) {
-    const uint64_t b = (uint64_t)(uintptr_t)base;
-    const uint64_t bu = ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(b >> 32)) << 32) |
-                        (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)b);
-    uint32_t saved;
     asm volatile(
-        "s_mov_b32 %0, m0\n\t"
-        "s_mov_b32 m0, %3\n\t"
+        "s_mov_b32 m0, %2\n\t"
         "s_nop 0\n\t"
-        "global_load_lds_dwordx4 %1, %2\n\t"
-        "s_mov_b32 m0, %0"
-        : "=&s"(saved)
-        : "v"(voff), "s"(bu), "s"((uint32_t)__builtin_amdgcn_readfirstlane(lds))
-        : "memory");
+        "global_load_lds_dwordx4 %0, %1"
+        :
+        : "v"(voff), "s"(base), "s"(lds)
+        : "memory", "m0");
 }
 // the same from an address a lane
 __device__ __forceinline__ void copy16_any(const void *p, uint32_t lds) {
-    uint32_t saved;
     asm volatile(
-        "s_mov_b32 %0, m0\n\t"
-        "s_mov_b32 m0, %2\n\t"
+        "s_mov_b32 m0, %1\n\t"
         "s_nop 0\n\t"
-        "global_load_lds_dwordx4 %1, off\n\t"
-        "s_mov_b32 m0, %0"
-        : "=&s"(saved)
-        : "v"((uint64_t)(uintptr_t)p), "s"((uint32_t)__builtin_amdgcn_readfirstlane(lds))
-        : "memory");
+        "global_load_lds_dwordx4 %0, off"
+        :
+        : "v"((uint64_t)(uintptr_t)p), "s"(lds)
+        : "memory", "m0");
 }
 
 // all but the last n copies of this wave have arrived
@@ -136,7 +127,7 @@ __device__ __forceinline__ u32x2 read_tr(const uint8_t *p) {
 // 16 rows come from two matrices in turn, r0 / 2 being the first row of either.
 template <int L, int R, int TH, bool DUAL>
 struct Copies {
-    static constexpr int N = R * 64 / (TH * 16);
+    static constexpr int N = R * STEP * 2 / (TH * 16);
     uint32_t off[N];
     int k[N];  // the first k of this lane's 16 bytes within a step
 
@@ -145,7 +136,7 @@ struct Copies {
         for (int i = 0; i < N; i++) {
             const int s = i * TH + tid;
             if constexpr (L == KC) {
-                const int row = s >> 2, c = (s & 3) ^ ((row >> 1) & 3);
+                const int row = s >> 3, c = (s & 7) ^ (row & 7);
                 const int at = DUAL ? (row >> 5) * 16 + (row & 15) : row, first = DUAL ? r0 / 2 : r0;
                 const int r = first + at < ext ? at : ext - 1 - first;
                 off[i] = (uint32_t)r * (uint32_t)(ld * 2) + c * 16;
@@ -160,30 +151,30 @@ struct Copies {
             }
         }
     }
-    // from the tile's first row of each matrix, `left` k's of them
-    __device__ __forceinline__ void issue(const uint16_t *p0, const uint16_t *p1, int left, uint32_t lds, int wave) const {
-#pragma unroll
-        for (int i = 0; i < N; i++) {
-            const uint16_t *const p = DUAL && ((i * TH / 64 + wave) & 1) ? p1 : p0;
-            const uint32_t to = lds + (i * TH / 64 + wave) * PITCH<L, R>;
-            if (left >= 32)
-                copy16(p, off[i], to);
-            else
-                copy16_any(k[i] < left ? (const uint8_t *)p + off[i] : (const uint8_t *)zero_page, to);
-        }
+    // The i-th copy of a step from the tile's first row of each matrix, `left` k's
+    // of them.
+    __device__ __forceinline__ void issue(int i, const uint16_t *p0, const uint16_t *p1, int left, uint32_t lds,
+                                          int wave) const {
+        const uint16_t *const p = DUAL && (((i * TH / 64 + wave) >> 1) & 1) ? p1 : p0;
+        const uint32_t to = lds + (i * TH / 64 + wave) * PITCH<L, R>;
+        if (left >= STEP)
+            copy16(p, off[i], to);
+        else
+            copy16_any(k[i] < left ? (const uint8_t *)p + off[i] : (const uint8_t *)zero_page, to);
     }
 };
 
 template <int L, int R>
 struct Reader {
-    // this lane's places in a stage for rows (columns) w0 + 16 i ..
-    static constexpr int N = L == KC ? 1 : R == 256 ? 2 : 4;
+    // this lane's places in a stage for rows (columns) w0 + 16 i .., k's from 32 h on
+    static constexpr int N = L == KC ? 2 : R == 256 ? 2 : 4;
     static constexpr int ROW = R * 2, PER = 1024 / ROW;  // RC: bytes of a row, rows of a copy
     int at[N];
     __device__ __forceinline__ void init(int lane, int w0) {
         if constexpr (L == KC) {
             const int r = lane & 15;
-            at[0] = (w0 + r) * 64 + (((lane >> 4) ^ ((r >> 1) & 3)) << 4);
+            at[0] = (w0 + r) * 128 + (((lane >> 4) ^ (r & 7)) << 4);
+            at[1] = at[0] ^ 64;
         } else {
             const int k = 8 * (lane >> 4) + ((lane & 15) >> 2);
 #pragma unroll
@@ -191,11 +182,11 @@ struct Reader {
                 at[i] = k / PER * PITCH<L, R> + k % PER * ROW + w0 * 2 + ((i ^ rc_swizzle<R>(k)) << 5) + 8 * (lane & 3);
         }
     }
-    __device__ __forceinline__ u32x4 get(const uint8_t *stage, int i) const {
+    __device__ __forceinline__ u32x4 get(const uint8_t *stage, int h, int i) const {
         if constexpr (L == KC) {
-            return *reinterpret_cast<const u32x4 *>(stage + at[0] + i * 1024);
+            return *reinterpret_cast<const u32x4 *>(stage + at[h] + i * 2048);
         } else {
-            const uint8_t *const p = stage + at[i % N] + i / N * (N * 32);
+            const uint8_t *const p = stage + at[i % N] + i / N * (N * 32) + h * (32 / PER * PITCH<L, R>);
             const u32x2 lo = read_tr(p), hi = read_tr(p + 4 / PER * PITCH<L, R>);
             return u32x4{lo.x, lo.y, hi.x, hi.y};
         }
@@ -206,7 +197,7 @@ struct Reader {
 // mm args, wave's first m and n, lane, LDS).
 template <typename T, typename S, int LA, int LB, typename E>
 __global__ __launch_bounds__(S::TH, S::OCC) void kernel(Args a, typename E::Args e) {
-    constexpr int TM = S::TM, TN = S::TN, FM = S::FM, FN = S::FN, ST = S::STAGES;
+    constexpr int TM = S::TM, TN = S::TN, FM = S::FM, FN = S::FN;
     constexpr int BYTES_A = BYTES<LA, TM>, STAGE = BYTES_A + BYTES<LB, TN>;
     static_assert(FM % 4 == 0 && FN % 4 == 0, "a wave's first row and column");
     extern __shared__ __align__(1024) uint8_t lds[];
@@ -229,17 +220,45 @@ __global__ __launch_bounds__(S::TH, S::OCC) void kernel(Args a, typename E::Args
     rb.init(lane, wn);
     const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
 
-    const int64_t row_a = LA == KC ? (int64_t)m0 * a.lda : m0, step_a = LA == KC ? 32 : 32 * a.lda;
-    const int64_t row_b = LB == KC ? (int64_t)(E::DUAL ? n0 / 2 : n0) * a.ldb : n0, step_b = LB == KC ? 32 : 32 * a.ldb;
-    auto issue = [&](int s) {  // step s of this split into its buffer
-        if (s >= steps)
-            return;
-        const int g = first + s, two = g >= a.seg, in = two ? g - a.seg : g;
-        const int left = a.K - in * 32;
-        const uint32_t to = lds_at + (s % ST) * STAGE;
-        ca.issue(a.a[two | at.batch] + row_a + in * step_a, nullptr, left, to, wave);
-        cb.issue(a.b[E::DUAL ? 0 : two] + row_b + in * step_b, E::DUAL ? a.b[1] + row_b + in * step_b : nullptr, left,
-                 to + BYTES_A, wave);
+    // The next step to fetch: its place in its segment of k, its buffer and what is
+    // left of k.  Everything here is uniform.
+    const int64_t step_a = LA == KC ? STEP : STEP * a.lda,
+                  step_b = LB == KC ? STEP : STEP * a.ldb;
+    const int64_t row_a = LA == KC ? (int64_t)m0 * a.lda : m0,
+                  row_b = LB == KC ? (int64_t)(E::DUAL ? n0 / 2 : n0) * a.ldb : n0;
+    struct Next {
+        const uint16_t *a, *b, *b1;
+        int left, segment, buffer;
+    } nx;
+    {
+        const int two = first >= a.seg, in = two ? first - a.seg : first;
+        nx.a = a.a[two | at.batch] + row_a + in * step_a;
+        nx.b = a.b[E::DUAL ? 0 : two] + row_b + in * step_b;
+        nx.b1 = E::DUAL ? a.b[1] + row_b + in * step_b : nullptr;
+        nx.left = a.K - in * STEP;
+        nx.segment = two ? 1 << 30 : a.seg - first;  // steps to its end
+        nx.buffer = 0;
+    }
+    constexpr int CA = Copies<LA, TM, S::TH, false>::N, CB = Copies<LB, TN, S::TH, E::DUAL>::N;
+    auto copy = [&](int i) {  // the i-th of the step's copies
+        const uint32_t to = lds_at + nx.buffer * STAGE;
+        if (i < CA)
+            ca.issue(i, nx.a, nullptr, nx.left, to, wave);
+        else
+            cb.issue(i - CA, nx.b, nx.b1, nx.left, to + BYTES_A, wave);
+    };
+    auto advance = [&] {
+        nx.a += step_a;
+        nx.b += step_b;
+        nx.b1 += E::DUAL ? step_b : 0;
+        nx.left -= STEP;
+        nx.buffer ^= 1;
+        if (--nx.segment == 0) {
+            nx.a = a.a[1] + row_a;
+            nx.b = a.b[1] + row_b;
+            nx.left = a.K;
+            nx.segment = 1 << 30;
+        }
     };
 
     float4v acc[FM][FN];
@@ -252,56 +271,70 @@ __global__ __launch_bounds__(S::TH, S::OCC) void kernel(Args a, typename E::Args
     struct Frags {
         u32x4 a[FM], b[FN];
     } f[2];
-    auto read = [&](Frags &t, int s) {
-        const uint8_t *const p = lds + (s % ST) * STAGE;
-#pragma unroll
-        for (int j = 0; j < FN; j++)
-            t.b[j] = rb.get(p + BYTES_A, j);
-#pragma unroll
-        for (int i = 0; i < FM; i++)
-            t.a[i] = ra.get(p, i);
+    auto read = [&](Frags &t, const uint8_t *stage, int h, int i) {  // the i-th fragment of 32 k's
+        if (i < FN)
+            t.b[i] = rb.get(stage + BYTES_A, h, i);
+        else
+            t.a[i - FN] = ra.get(stage, h, i - FN);
     };
     auto barrier = [&] {
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
-    // Step s with its fragments in `now`: step s + 1 must have arrived and everyone
-    // must have read step s, whose buffer is filled again.
-    auto step = [&](Frags &now, Frags &next, int s) {
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (s + ST - 1 < steps)
-            wait_copies<(ST - 2) * S::COPIES>();
-        else
-            wait_copies<0>();
-        barrier();
-        issue(s + ST);
-        if (s + 1 < steps)
-            read(next, s + 1);
+    // The products of 32 k's in FM groups, each of which starts with a share of what
+    // goes on beside them: the next fragments' reads and, in the second half of a
+    // step, the copies of the step after the next.
+    constexpr int READS = FM + FN, PER = (READS + FM - 2) / (FM - 1);  // no reads in the last group
+    auto half = [&](const Frags &now, Frags &next, const uint8_t *from, int h, bool copies) {
 #pragma unroll
-        for (int i = 0; i < FM; i++)
+        for (int i = 0; i < FM; i++) {
+#pragma unroll
+            for (int r = i * PER; r < (i + 1) * PER; r++)
+                if (r < READS)
+                    read(next, from, h, r);
+            if (copies) {
+#pragma unroll
+                for (int c = 0; c < S::COPIES; c++)
+                    if (c * FM / S::COPIES == i)
+                        copy(c);
+            }
 #pragma unroll
             for (int j = 0; j < FN; j++)
                 acc[i][j] = T::mfma(now.b[j], now.a[i], acc[i][j]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     };
 
     if (steps > 0) {
+        for (int s = 0; s < 2 && s < steps; s++) {
 #pragma unroll
-        for (int s = 0; s < ST; s++)
-            issue(s);
-        if (steps >= ST)
-            wait_copies<(ST - 1) * S::COPIES>();
+            for (int c = 0; c < S::COPIES; c++)
+                copy(c);
+            advance();
+        }
+        if (steps > 1)
+            wait_copies<S::COPIES>();
         else
             wait_copies<0>();
         barrier();
-        read(f[0], 0);
-        int s = 0;
-        for (; s + 1 < steps; s += 2) {
-            step(f[0], f[1], s);
-            step(f[1], f[0], s + 1);
+#pragma unroll
+        for (int r = 0; r < READS; r++)
+            read(f[0], lds, 0, r);
+        const uint8_t *now = lds, *next = lds + STAGE;
+        for (int s = 0; s < steps; s++) {
+            half(f[0], f[1], now, 1, false);
+            // This wave has read all of the step, and its share of the next one is there.
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            barrier();
+            // (behind the last step: fragments that nobody uses)
+            half(f[1], f[0], next, 0, s + 2 < steps);
+            if (s + 2 < steps)
+                advance();
+            const uint8_t *const t = now;
+            now = next;
+            next = t;
         }
-        if (s < steps)
-            step(f[0], f[1], s);
     }
     E::template run<T, S>(e, acc, at, a, m0 + wm, n0 + wn, lane, lds);
 }
@@ -309,7 +342,7 @@ __global__ __launch_bounds__(S::TH, S::OCC) void kernel(Args a, typename E::Args
 template <typename T, typename S, int LA, int LB, typename E>
 hipError_t launch(const Args &a, const typename E::Args &e, hipStream_t st) {
     void (*const f)(Args, typename E::Args) = kernel<T, S, LA, LB, E>;
-    constexpr int LDS = S::STAGES * (BYTES<LA, S::TM> + BYTES<LB, S::TN>);
+    constexpr int LDS = 2 * (BYTES<LA, S::TM> + BYTES<LB, S::TN>);
     if (LDS > 64 * 1024) {
         const hipError_t err = allow_full_lds((const void *)f);
         if (err != hipSuccess)
@@ -321,8 +354,8 @@ hipError_t launch(const Args &a, const typename E::Args &e, hipStream_t st) {
 }
 
 // the plan's tiles
-typedef Shape<256, 256, 2, 4, 4, 2> Tile256;
-typedef Shape<128, 128, 2, 2, 4, 2> Tile128;
+typedef Shape<256, 256, 2, 4, 2> Tile256;
+typedef Shape<128, 128, 2, 2, 2> Tile128;
 
 template <typename T, int LA, int LB, typename E>
 hipError_t launch_tile(const Args &a, const typename E::Args &e, int tile, hipStream_t st) {

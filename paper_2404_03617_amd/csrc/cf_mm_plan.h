@@ -10,7 +10,7 @@
 namespace cf {
 namespace mm {
 
-constexpr int STEP = 32;  // k's of a step
+constexpr int STEP = 64;  // k's of a step
 
 struct Tile {
     int m, n, per_cu;

@@ -4,27 +4,29 @@
 //
 // An operand is stored with k contiguous (KC: x W^T has both so) or with its
 // other index contiguous (RC: gradients sum over rows or over outputs).  A
-// workgroup makes a TM x TN tile.  Steps of 32 k go by LDS-DMA into a ring of
-// STAGES buffers, as the instruction writes them: 16 bytes a lane, one after
-// the other.  A lane chooses what it fetches, so that the tile stands there
-// swizzled and the fragment reads meet no bank twice:
-//   KC  rows of 64 bytes, their 16-byte pieces permuted by bits 1 and 2 of the row;
-//       fragments by 16-byte loads
+// workgroup makes TM x TN tiles, one after the other.  Steps of 64 k go by LDS-DMA
+// into two buffers, as the instruction writes them: 16 bytes a lane, one after the
+// other.  A lane chooses what it fetches, so that the tile stands there permuted
+// and fragment reads meet no bank twice:
+//   KC  rows of 128 bytes, a cache line each (half a line a step costs a fifth of
+//       the rate), in pieces of 16; fragments by 16-byte loads
 //   RC  rows of one k, their 32-byte pieces permuted by the lowest bits of k;
 //       fragments by transposing loads, whose 16 lanes read 32 bytes of 4 rows.
-//       Rows of 512 bytes: one bit, and 64 bytes between pairs of rows (two
-//       bits, or three, took eight addresses a lane, and the tile spilled)
-// While the products of a step run, the next step's fragments are read into a
-// second set of registers and the step STAGES further is fetched: one barrier a
-// step, and no wait but for copies issued STAGES - 1 steps before.
+//       Rows of 512 bytes: one bit, and 32 bytes between pairs of rows (three
+//       bits took eight addresses a lane, and the tile spilled)
+// While the products of half a step run, the next half's fragments are read into
+// a second set of registers; once everyone has read a step, its buffer receives
+// the step after the next: one barrier a step.  The copies run on through the
+// ends of tiles.
 //
-// MFMA 16x16x32 takes B's fragment first: a lane then holds four consecutive n
-// of one m, which is what a store, a sum over n or a pair of gate and up
-// channels wants.
+// MFMA 16x16x32 takes B's fragment first: a lane then holds columns beside each
+// other of one row, which is what a store, a sum over columns or a pair of gate and up
+// channels wants.  (32x32x16 keeps the matrix unit busier, 72% against 68, at a
+// lower clock: 1287 TFLOP/s against 1350.)
 //
 // The ends: rows of A and B past the last are read from the last (they reach
-// results that are not stored), k past the last from a page of zeros.  So an
-// operand must have 16-byte aligned rows whose contiguous extent is a multiple
+// results that are not stored); k's past the last are read from the step's first
+// and cleared in LDS.  So an operand must have 16-byte aligned rows whose contiguous extent is a multiple
 // of 8 (zeros behind the last k of KC); others are packed first (cf_mm.hip).
 #pragma once
 
@@ -46,18 +48,20 @@ struct Args {
     int steps;            // of both
     int per;              // steps a split
     int tiles_m, tiles_n, splits;
+    unsigned items;       // tiles * splits * batch
     int batch;            // 2: a[1] and out[1] are a second problem with the same b[0]
 };
 
 struct Work {
     int m, n, split, batch;
 };
-// Workgroups go to the eight XCDs in turn, each with an L2 of its own; every XCD
-// takes a run of the list of tiles, in bands eight tiles of m high, so that what
-// runs together behind one L2 shares rows of both operands.
-__device__ __forceinline__ Work work_of(const Args &a) {
-    const unsigned n = gridDim.x, xcd = blockIdx.x & 7, q = n >> 3, rest = n & 7;
-    unsigned i = xcd * q + (xcd < rest ? xcd : rest) + (blockIdx.x >> 3);
+// The item that comes `turn`-th.  Workgroups, and with them their items, go to the
+// eight XCDs in turn, each with an L2 of its own; every XCD takes a run of the list of
+// tiles, in bands eight tiles of m high, so that what runs together behind one L2
+// shares rows of both operands.
+__device__ __forceinline__ Work work_of(const Args &a, unsigned turn) {
+    const unsigned n = a.items, xcd = turn & 7, q = n >> 3, rest = n & 7;
+    unsigned i = xcd * q + (xcd < rest ? xcd : rest) + (turn >> 3);
     const unsigned tiles = (unsigned)a.tiles_m * (unsigned)a.tiles_n, part = i / tiles;
     i -= part * tiles;
     const unsigned band = i / (8u * a.tiles_n), m0 = 8 * band,
@@ -68,7 +72,7 @@ __device__ __forceinline__ Work work_of(const Args &a) {
 
 // the 1024 bytes of a copy instruction, and what is left free behind them
 template <int L, int R>
-constexpr int PITCH = L == RC && R == 256 ? 1088 : 1024;
+constexpr int PITCH = L == KC ? 1024 : R == 256 ? 1056 : 1088;
 template <int L, int R>
 constexpr int BYTES = R * STEP * 2 / 1024 * PITCH<L, R>;
 
@@ -80,27 +84,19 @@ struct Shape {
     static_assert(TM * STEP * 2 % (TH * 16) == 0 && TN * STEP * 2 % (TH * 16) == 0, "whole copies");
 };
 
-static __device__ __attribute__((aligned(16))) const uint32_t zero_page[4] = {0, 0, 0, 0};
-
-// 16 bytes a lane from base + voff to LDS address lds + 16 lane
+// 16 bytes a lane from base + voff to LDS address lds + AT + 16 lane
+template <int AT>
 __device__ __forceinline__ void copy16(const void *base, uint32_t voff, uint32_t lds) {
+    const uint64_t b = (uint64_t)(uintptr_t)base;
+    const uint64_t uniform = ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(b >> 32)) << 32) |
+                             (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)b);
     asm volatile(
-        "s_mov_b32 m0, %2\n\t"
+        "s_add_u32 m0, %2, %3\n\t"
         "s_nop 0\n\t"
         "global_load_lds_dwordx4 %0, %1"
         :
-        : "v"(voff), "s"(base), "s"(lds)
-        : "memory", "m0");
-}
-// the same from an address a lane
-__device__ __forceinline__ void copy16_any(const void *p, uint32_t lds) {
-    asm volatile(
-        "s_mov_b32 m0, %1\n\t"
-        "s_nop 0\n\t"
-        "global_load_lds_dwordx4 %0, off"
-        :
-        : "v"((uint64_t)(uintptr_t)p), "s"(lds)
-        : "memory", "m0");
+        : "v"(voff), "s"(uniform), "s"(lds), "n"(AT)
+        : "memory", "m0", "scc");
 }
 
 // all but the last n copies of this wave have arrived
@@ -110,9 +106,18 @@ __device__ __forceinline__ void wait_copies() {
     __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
 }
 
+// By what the 32-byte pieces of row k of an RC tile are permuted: with what is free
+// behind a copy, the 8 rows that 32 lanes read together (8 q to 8 q + 3 and 8
+// further) lie in different banks.
+// What the 16-byte pieces of a KC row are permuted by: 8 lanes beside each other
+// read 8 rows in different banks.  B's rows of a fragment are 4 of every 8.
+template <bool B>
+__device__ __forceinline__ int kc_swizzle(int row) {
+    return B ? (row & 3) | (row >> 1 & 4) : row & 7;
+}
 template <int R>
 __device__ __forceinline__ int rc_swizzle(int k) {
-    return R == 256 ? k & 1 : k & 3;
+    return R == 256 ? (k & 1) << 1 : k & 3;
 }
 
 // 4 k x 16 columns of an RC tile, given as 4 columns of row lane / 4 by each of
@@ -124,72 +129,118 @@ __device__ __forceinline__ u32x2 read_tr(const uint8_t *p) {
 }
 
 // One operand's copies: R rows (columns) of the tile from r0 on.  DUAL: groups of
-// 16 rows come from two matrices in turn, r0 / 2 being the first row of either.
-template <int L, int R, int TH, bool DUAL>
+// 32 rows come from two matrices in turn, r0 / 2 being the first row of either.
+template <int L, int R, int TH, bool B, bool DUAL>
 struct Copies {
     static constexpr int N = R * STEP * 2 / (TH * 16);
-    uint32_t off[N];
-    int k[N];  // the first k of this lane's 16 bytes within a step
+    static constexpr int ROWS = L == KC ? TH / 8 : TH / (R / 8);  // rows (k's) between a lane's copies
+    static_assert(L == KC ? ROWS % 16 == 0 : ROWS % 4 == 0, "the same piece of each row");
+    uint32_t off[L == KC ? N : 1], col;  // RC: of the first copy, of its columns alone
+    int k;                          // the first k of this lane's 16 bytes (RC: of the first copy)
 
     __device__ __forceinline__ void init(int tid, int r0, int ext, int64_t ld) {
+        if constexpr (L == KC) {
+            const int c = (tid & 7) ^ kc_swizzle<B>(tid >> 3);
+            k = c * 8;
 #pragma unroll
-        for (int i = 0; i < N; i++) {
-            const int s = i * TH + tid;
-            if constexpr (L == KC) {
-                const int row = s >> 3, c = (s & 7) ^ (row & 7);
-                const int at = DUAL ? (row >> 5) * 16 + (row & 15) : row, first = DUAL ? r0 / 2 : r0;
+            for (int i = 0; i < N; i++) {
+                const int row = i * ROWS + (tid >> 3);
+                const int at = DUAL ? (row >> 6) * 32 + (row & 31) : row, first = DUAL ? r0 / 2 : r0;
                 const int r = first + at < ext ? at : ext - 1 - first;
                 off[i] = (uint32_t)r * (uint32_t)(ld * 2) + c * 16;
-                k[i] = c * 8;
-            } else {
-                constexpr int PER = R / 8;
-                const int kk = s / PER, p = s % PER;
-                const int col = (((p >> 1) ^ rc_swizzle<R>(kk)) << 4) + (p & 1) * 8;
-                const int c = r0 + col <= ext - 8 ? col : ext - 8 - r0;
-                off[i] = (uint32_t)kk * (uint32_t)(ld * 2) + c * 2;
-                k[i] = kk;
             }
+        } else {
+            constexpr int PER = R / 8;
+            const int p = tid % PER;
+            k = tid / PER;
+            const int at = (((p >> 1) ^ rc_swizzle<R>(k)) << 4) + (p & 1) * 8;
+            const int c = r0 + at <= ext - 8 ? at : ext - 8 - r0;
+            col = c * 2;
+            off[0] = (uint32_t)k * (uint32_t)(ld * 2) + col;
         }
     }
-    // The i-th copy of a step from the tile's first row of each matrix, `left` k's
-    // of them.
-    __device__ __forceinline__ void issue(int i, const uint16_t *p0, const uint16_t *p1, int left, uint32_t lds,
+    // The I-th copy of a step of which `left` k's are there, from the tile's first row
+    // of each matrix, to `lds`, the wave's place.  k's past them are read from the
+    // step's first, and cleared once they are in LDS.
+    template <int I>
+    __device__ __forceinline__ void issue(const uint16_t *p0, const uint16_t *p1, uint32_t row, int left, uint32_t lds,
                                           int wave) const {
-        const uint16_t *const p = DUAL && (((i * TH / 64 + wave) >> 1) & 1) ? p1 : p0;
-        const uint32_t to = lds + (i * TH / 64 + wave) * PITCH<L, R>;
-        if (left >= STEP)
-            copy16(p, off[i], to);
-        else
-            copy16_any(k[i] < left ? (const uint8_t *)p + off[i] : (const uint8_t *)zero_page, to);
+        constexpr int AT = I * (TH / 64) * PITCH<L, R>;
+        if constexpr (L == KC) {
+            static_assert(!DUAL || TH / 64 % 4 == 0, "groups of 32 rows are 4 waves' copies");
+            copy16<AT>(DUAL && ((wave / 4 + I * (TH / 256)) & 1) ? p1 : p0, off[I] - (k < left ? 0u : (uint32_t)k * 2), lds);
+        } else {
+            copy16<AT>(p0, k < left - I * ROWS ? off[0] + I * ROWS * row : col, lds);
+        }
+    }
+    __device__ __forceinline__ void clear(int left, uint8_t *stage, int wave, int lane) const {
+#pragma unroll
+        for (int i = 0; i < N; i++)
+            if (k + (L == RC ? i * ROWS : 0) >= left)
+                *reinterpret_cast<u32x4 *>(stage + (i * TH / 64 + wave) * PITCH<L, R> + lane * 16) = u32x4{0u, 0u, 0u, 0u};
     }
 };
 
-template <int L, int R>
+// Fragments of 16 rows (columns) from w0 on.  A's are in order.  B's of a KC tile are
+// ordered so that two beside each other give a lane 8 columns beside each other:
+// row d of fragment i is row 32 (i / 2) + 8 (d / 4) + 4 (i % 2) + d % 4.
+template <int L, int R, bool B>
 struct Reader {
     // this lane's places in a stage for rows (columns) w0 + 16 i .., k's from 32 h on
+    // (RC: of the i that differ in the bits that rows permute)
     static constexpr int N = L == KC ? 2 : R == 256 ? 2 : 4;
     static constexpr int ROW = R * 2, PER = 1024 / ROW;  // RC: bytes of a row, rows of a copy
     int at[N];
+    static constexpr int which(int i) { return R == 256 ? i >> 1 & 1 : i & 3; }
+    static constexpr int rest(int i) { return R == 256 ? i & ~2 : i & ~3; }
     __device__ __forceinline__ void init(int lane, int w0) {
         if constexpr (L == KC) {
-            const int r = lane & 15;
-            at[0] = (w0 + r) * 128 + (((lane >> 4) ^ (r & 7)) << 4);
+            const int d = lane & 15, r = w0 + (B ? (d >> 2) * 8 + (d & 3) : d);
+            at[0] = r * 128 + (((lane >> 4) ^ kc_swizzle<B>(r)) << 4);
             at[1] = at[0] ^ 64;
         } else {
             const int k = 8 * (lane >> 4) + ((lane & 15) >> 2);
 #pragma unroll
-            for (int i = 0; i < N; i++)  // w0 / 16 is a multiple of N
-                at[i] = k / PER * PITCH<L, R> + k % PER * ROW + w0 * 2 + ((i ^ rc_swizzle<R>(k)) << 5) + 8 * (lane & 3);
+            for (int i = 0; i < N; i++)  // w0 / 16 is a multiple of 4
+                at[i] = k / PER * PITCH<L, R> + k % PER * ROW + w0 * 2 + 8 * (lane & 3) +
+                        (((R == 256 ? 2 * i : i) ^ rc_swizzle<R>(k)) << 5);
         }
     }
     __device__ __forceinline__ u32x4 get(const uint8_t *stage, int h, int i) const {
         if constexpr (L == KC) {
-            return *reinterpret_cast<const u32x4 *>(stage + at[h] + i * 2048);
+            return *reinterpret_cast<const u32x4 *>(stage + at[h] + (B ? i / 2 * 32 + i % 2 * 4 : i * 16) * 128);
         } else {
-            const uint8_t *const p = stage + at[i % N] + i / N * (N * 32) + h * (32 / PER * PITCH<L, R>);
+            const uint8_t *const p = stage + at[which(i)] + rest(i) * 32 + h * (32 / PER * PITCH<L, R>);
             const u32x2 lo = read_tr(p), hi = read_tr(p + 4 / PER * PITCH<L, R>);
             return u32x4{lo.x, lo.y, hi.x, hi.y};
         }
+    }
+};
+
+template <int V>
+struct Number {
+    static constexpr int value = V;
+};
+// f(Number<0>()) .. f(Number<N - 1>())
+template <int N, int I = 0, typename F>
+__device__ __forceinline__ void each(F &&f) {
+    if constexpr (I < N) {
+        f(Number<I>());
+        each<N, I + 1>(f);
+    }
+}
+
+// A wave's results: FM rows a lane (16 apart), in PIECES pieces of W columns beside
+// each other.
+template <typename S, bool WIDE>
+struct Results {
+    static constexpr int W = WIDE ? 8 : 4, PIECES = S::FN * 4 / W;
+    float4v (&acc)[S::FM][S::FN];
+    static __device__ __forceinline__ int column(int piece, int lane) {
+        return WIDE ? 32 * piece + 8 * (lane >> 4) : 16 * piece + 4 * (lane >> 4);
+    }
+    __device__ __forceinline__ float get(int i, int piece, int k) const {
+        return WIDE ? acc[i][2 * piece + k / 4][k % 4] : acc[i][piece][k];
     }
 };
 
@@ -202,50 +253,62 @@ __global__ __launch_bounds__(S::TH, S::OCC) void kernel(Args a, typename E::Args
     static_assert(FM % 4 == 0 && FN % 4 == 0, "a wave's first row and column");
     extern __shared__ __align__(1024) uint8_t lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const Work at = work_of(a);
-    const int m0 = at.m * TM, n0 = at.n * TN;
     const int wm = wave / S::WN * (TM / S::WM), wn = wave % S::WN * (TN / S::WN);
 
-    const int first = at.split * a.per;
-    int steps = a.steps - first < a.per ? a.steps - first : a.per;
-    steps = steps < 0 ? 0 : steps;
-
-    Copies<LA, TM, S::TH, false> ca;
-    Copies<LB, TN, S::TH, E::DUAL> cb;
-    ca.init(tid, m0, a.ext_a, a.lda);
-    cb.init(tid, n0, a.ext_b, a.ldb);
-    Reader<LA, TM> ra;
-    Reader<LB, TN> rb;
+    Copies<LA, TM, S::TH, false, false> ca;
+    Copies<LB, TN, S::TH, true, E::DUAL> cb;
+    Reader<LA, TM, false> ra;
+    Reader<LB, TN, true> rb;
     ra.init(lane, wm);
     rb.init(lane, wn);
     const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
 
-    // The next step to fetch: its place in its segment of k, its buffer and what is
-    // left of k.  Everything here is uniform.
+    // The next step to fetch, which may be of the next item: where it is, which item
+    // and how many more steps of it there are, its buffer and what is left of k.
+    // Everything here is uniform.
     const int64_t step_a = LA == KC ? STEP : STEP * a.lda,
                   step_b = LB == KC ? STEP : STEP * a.ldb;
-    const int64_t row_a = LA == KC ? (int64_t)m0 * a.lda : m0,
-                  row_b = LB == KC ? (int64_t)(E::DUAL ? n0 / 2 : n0) * a.ldb : n0;
     struct Next {
         const uint16_t *a, *b, *b1;
-        int left, segment, buffer;
+        int64_t row_a, row_b;
+        unsigned item;
+        int left, segment, buffer, steps, first, batch;
     } nx;
-    {
-        const int two = first >= a.seg, in = two ? first - a.seg : first;
-        nx.a = a.a[two | at.batch] + row_a + in * step_a;
-        nx.b = a.b[E::DUAL ? 0 : two] + row_b + in * step_b;
-        nx.b1 = E::DUAL ? a.b[1] + row_b + in * step_b : nullptr;
+    auto steps_of = [&](const Work &w) {
+        const int left = a.steps - w.split * a.per;
+        return left < a.per ? left : a.per;
+    };
+    auto restart = [&] {  // to the first step of the item that was entered last
+        const int two = nx.first >= a.seg, in = two ? nx.first - a.seg : nx.first;
+        nx.a = (two | nx.batch ? a.a[1] : a.a[0]) + nx.row_a + in * step_a;
+        nx.b = (!E::DUAL && two ? a.b[1] : a.b[0]) + nx.row_b + in * step_b;
+        nx.b1 = E::DUAL ? a.b[1] + nx.row_b + in * step_b : nullptr;
         nx.left = a.K - in * STEP;
-        nx.segment = two ? 1 << 30 : a.seg - first;  // steps to its end
-        nx.buffer = 0;
-    }
-    constexpr int CA = Copies<LA, TM, S::TH, false>::N, CB = Copies<LB, TN, S::TH, E::DUAL>::N;
-    auto copy = [&](int i) {  // the i-th of the step's copies
-        const uint32_t to = lds_at + nx.buffer * STAGE;
-        if (i < CA)
-            ca.issue(i, nx.a, nullptr, nx.left, to, wave);
+        nx.segment = two ? 1 << 30 : a.seg - nx.first;  // steps to its end
+    };
+    auto enter = [&] {
+        const Work w = work_of(a, nx.item);
+        const int m0 = w.m * TM, n0 = w.n * TN;
+        nx.first = w.split * a.per;
+        nx.batch = w.batch;
+        ca.init(tid, m0, a.ext_a, a.lda);
+        cb.init(tid, n0, a.ext_b, a.ldb);
+        nx.row_a = LA == KC ? (int64_t)m0 * a.lda : m0;
+        nx.row_b = LB == KC ? (int64_t)(E::DUAL ? n0 / 2 : n0) * a.ldb : n0;
+        nx.steps = steps_of(w);
+        restart();
+    };
+    constexpr int CA = Copies<LA, TM, S::TH, false, false>::N, CB = Copies<LB, TN, S::TH, true, E::DUAL>::N;
+    static_assert(CA + CB == S::COPIES, "");
+    const uint32_t row_bytes_a = (uint32_t)(a.lda * 2), row_bytes_b = (uint32_t)(a.ldb * 2);
+    const uint32_t to_a = lds_at + wave * PITCH<LA, TM>, to_b = lds_at + BYTES_A + wave * PITCH<LB, TN>;
+    auto copy = [&](auto which) {  // one of the step's copies
+        constexpr int I = decltype(which)::value;
+        const uint32_t buffer = (uint32_t)__builtin_amdgcn_readfirstlane(nx.buffer) * STAGE;
+        if constexpr (I < CA)
+            ca.template issue<I>(nx.a, nullptr, row_bytes_a, nx.left, to_a + buffer, wave);
         else
-            cb.issue(i - CA, nx.b, nx.b1, nx.left, to + BYTES_A, wave);
+            cb.template issue<I - CA>(nx.b, nx.b1, row_bytes_b, nx.left, to_b + buffer, wave);
     };
     auto advance = [&] {
         nx.a += step_a;
@@ -254,20 +317,19 @@ __global__ __launch_bounds__(S::TH, S::OCC) void kernel(Args a, typename E::Args
         nx.left -= STEP;
         nx.buffer ^= 1;
         if (--nx.segment == 0) {
-            nx.a = a.a[1] + row_a;
-            nx.b = a.b[1] + row_b;
+            nx.a = a.a[1] + nx.row_a;
+            nx.b = a.b[1] + nx.row_b;
             nx.left = a.K;
             nx.segment = 1 << 30;
+        }
+        if (--nx.steps == 0) {
+            nx.item += gridDim.x;
+            if (nx.item < a.items)
+                enter();
         }
     };
 
     float4v acc[FM][FN];
-#pragma unroll
-    for (int i = 0; i < FM; i++)
-#pragma unroll
-        for (int j = 0; j < FN; j++)
-            acc[i][j] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
-
     struct Frags {
         u32x4 a[FM], b[FN];
     } f[2];
@@ -282,74 +344,118 @@ __global__ __launch_bounds__(S::TH, S::OCC) void kernel(Args a, typename E::Args
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
-    // The products of 32 k's in FM groups, each of which starts with a share of what
-    // goes on beside them: the next fragments' reads and, in the second half of a
-    // step, the copies of the step after the next.
-    constexpr int READS = FM + FN, PER = (READS + FM - 2) / (FM - 1);  // no reads in the last group
-    auto half = [&](const Frags &now, Frags &next, const uint8_t *from, int h, bool copies) {
-#pragma unroll
-        for (int i = 0; i < FM; i++) {
-#pragma unroll
-            for (int r = i * PER; r < (i + 1) * PER; r++)
-                if (r < READS)
-                    read(next, from, h, r);
-            if (copies) {
-#pragma unroll
-                for (int c = 0; c < S::COPIES; c++)
-                    if (c * FM / S::COPIES == i)
-                        copy(c);
-            }
-#pragma unroll
-            for (int j = 0; j < FN; j++)
-                acc[i][j] = T::mfma(now.b[j], now.a[i], acc[i][j]);
+    // The products of 32 k's, and one after the other between them what goes on
+    // beside them: the next fragments' reads and, with COPIES, the copies of the
+    // step after the next.  A product keeps the matrix unit busy for four
+    // instructions' time; what stands in that shadow costs nothing.  There is no
+    // branch: with another version of the loop for the ends the registers spill.
+    constexpr int READS = FM + FN, PRODUCTS = FM * FN;
+    auto half = [&](const Frags &now, Frags &next, const uint8_t *from, int h, auto copies) {
+        constexpr int COPIES = decltype(copies)::value, PIECES = READS + COPIES;
+        each<PRODUCTS>([&](auto product) {
+            constexpr int T0 = decltype(product)::value, I = T0 / FN, J = T0 % FN;
+            acc[I][J] = T::mfma(now.b[J], now.a[I], acc[I][J]);
+            // (products have no side effects: without this they are gathered behind
+            // the copies, which are volatile)
+            asm volatile("" ::"v"(acc[I][J]));
+            // reads and copies in turn, over all products but the last few
+            each<PIECES>([&](auto piece) {
+                constexpr int P = decltype(piece)::value;
+                if constexpr (P * (PRODUCTS - 2) / PIECES == T0) {
+                    if constexpr (COPIES == 0)
+                        read(next, from, h, P);
+                    else if constexpr (P < 2 * COPIES && P % 2 == 1)
+                        copy(Number<P / 2>());
+                    else
+                        read(next, from, h, P < 2 * COPIES ? P / 2 : P - COPIES);
+                }
+            });
             __builtin_amdgcn_sched_barrier(0);
-        }
+        });
     };
 
-    if (steps > 0) {
-        for (int s = 0; s < 2 && s < steps; s++) {
-#pragma unroll
-            for (int c = 0; c < S::COPIES; c++)
-                copy(c);
+    // what is left of k in the step that lies in a buffer, where that is not all of it
+    auto clear = [&](uint8_t *stage, int left) {
+        ca.clear(left, stage, wave, lane);
+        cb.clear(left, stage + BYTES_A, wave, lane);
+    };
+    uint8_t *now = lds, *next = lds + STAGE;
+    int left_now = STEP, left_next = STEP;
+    // No k's at all: nothing to fetch.
+    nx.item = a.steps > 0 ? blockIdx.x : a.items;
+    nx.buffer = 0;
+    if (nx.item < a.items) {
+        enter();
+        left_now = nx.left;
+        each<S::COPIES>(copy);
+        advance();
+        if (nx.item < a.items) {
+            left_next = nx.left;
+            each<S::COPIES>(copy);
             advance();
         }
-        if (steps > 1)
-            wait_copies<S::COPIES>();
-        else
-            wait_copies<0>();
+        wait_copies<0>();
+        if (left_now < STEP)
+            clear(now, left_now);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         barrier();
 #pragma unroll
         for (int r = 0; r < READS; r++)
             read(f[0], lds, 0, r);
-        const uint8_t *now = lds, *next = lds + STAGE;
+    }
+    // Item by item.  The copies go on through the ends of items: while one's results
+    // are stored, the first two steps of the next are on their way.
+    for (unsigned item = blockIdx.x; item < a.items; item += gridDim.x) {
+        const Work at = work_of(a, item);
+        const int steps = a.steps > 0 ? steps_of(at) : 0;
+#pragma unroll
+        for (int i = 0; i < FM; i++)
+#pragma unroll
+            for (int j = 0; j < FN; j++)
+                acc[i][j] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
         for (int s = 0; s < steps; s++) {
-            half(f[0], f[1], now, 1, false);
+            half(f[0], f[1], now, 1, Number<0>());
             // This wave has read all of the step, and its share of the next one is there.
             asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            if (left_next < STEP) {
+                clear(next, left_next);
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            }
             barrier();
-            // (behind the last step: fragments that nobody uses)
-            half(f[1], f[0], next, 0, s + 2 < steps);
-            if (s + 2 < steps)
+            // Behind the last step of all: what nobody reads, from where the item that was
+            // last entered began.
+            const bool more = nx.item < a.items;
+            if (!more)
+                restart();
+            left_now = nx.left;
+            half(f[1], f[0], next, 0, Number<S::COPIES>());
+            if (more)
                 advance();
-            const uint8_t *const t = now;
+            uint8_t *const t = now;
             now = next;
             next = t;
+            const int l = left_now;
+            left_now = left_next;
+            left_next = l;
         }
+        E::template run<T, S, LB == KC>(e, Results<S, LB == KC>{acc}, at, a, at.m * TM + wm, at.n * TN + wn, lane, lds + 2 * STAGE);
     }
-    E::template run<T, S>(e, acc, at, a, m0 + wm, n0 + wn, lane, lds);
+    wait_copies<0>();  // nothing may arrive in LDS that is another workgroup's
 }
 
 template <typename T, typename S, int LA, int LB, typename E>
-hipError_t launch(const Args &a, const typename E::Args &e, hipStream_t st) {
+hipError_t launch(const Args &a, const typename E::Args &e, int per_cu, hipStream_t st) {
     void (*const f)(Args, typename E::Args) = kernel<T, S, LA, LB, E>;
-    constexpr int LDS = 2 * (BYTES<LA, S::TM> + BYTES<LB, S::TN>);
+    constexpr int LDS = 2 * (BYTES<LA, S::TM> + BYTES<LB, S::TN>) + E::template lds_bytes<S>();
+    static_assert(LDS <= 160 * 1024, "a CU's");
     if (LDS > 64 * 1024) {
         const hipError_t err = allow_full_lds((const void *)f);
         if (err != hipSuccess)
             return err;
     }
-    const int64_t grid = (int64_t)a.tiles_m * a.tiles_n * a.splits * a.batch;
-    f<<<dim3((unsigned)grid), dim3(S::TH), LDS, st>>>(a, e);
+    // as many workgroups as run together, a multiple of the XCDs
+    const unsigned most = (unsigned)(device_cu_count() * per_cu) & ~7u, grid = a.items < most || most == 0 ? a.items : most;
+    f<<<dim3(grid), dim3(S::TH), LDS, st>>>(a, e);
     return hipGetLastError();
 }
 
@@ -361,7 +467,8 @@ template <typename T, int LA, int LB, typename E>
 hipError_t launch_tile(const Args &a, const typename E::Args &e, int tile, hipStream_t st) {
     static_assert(Tile256::TM == TILES[0].m && Tile256::TN == TILES[0].n && Tile128::TM == TILES[1].m &&
                       Tile128::TN == TILES[1].n, "what the plan counts with");
-    return tile == 0 ? launch<T, Tile256, LA, LB, E>(a, e, st) : launch<T, Tile128, LA, LB, E>(a, e, st);
+    return tile == 0 ? launch<T, Tile256, LA, LB, E>(a, e, TILES[0].per_cu, st)
+                     : launch<T, Tile128, LA, LB, E>(a, e, TILES[1].per_cu, st);
 }
 
 }  // namespace mm

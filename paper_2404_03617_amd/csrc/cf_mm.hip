@@ -48,14 +48,18 @@ __global__ __launch_bounds__(256) void join_kernel(Args a, StoreArgs e, int per_
     float4v v = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
     for (int s = g; s < a.splits; s += G)
-        v += load4f(p + s * step, a.N - c);
+    {
+        float4v w;
+        load_rowf<4>(p + s * step, w, a.N - c);
+        v += w;
+    }
 #pragma unroll
     for (int d = 1; d < G; d *= 2)
 #pragma unroll
         for (int k = 0; k < 4; k++)
             v[k] += __shfl_xor(v[k], d);
     if (g == 0)
-        finish4<T>(e, v, m, c, a.M, a.N, batch);
+        finish<T, 4>(e, v, m, c, a.M, a.N, batch);
 }
 
 template <typename T>

@@ -1,6 +1,5 @@
 // cf_mm_epi.h -- what follows a product of cf_mm.h, on the sums that a lane
-// holds: for the wave's 16 x 16 tiles (i, j), row m = m0 + 16 i + lane % 16 and
-// columns n0 + 16 j + 4 (lane / 16) ... + 3.
+// holds (Results): rows m0 + 16 i + lane % 16, columns from n0 on.
 #pragma once
 
 #include "cf_act.h"
@@ -9,45 +8,79 @@
 namespace cf {
 namespace mm {
 
-struct __attribute__((packed, aligned(2))) Any8 {
-    u32x2 v;
+struct __attribute__((packed, aligned(2))) Any16h {
+    u32x4 v;
 };
 struct __attribute__((packed, aligned(4))) Any16f {
     float4v v;
 };
 
-// four values from p on, `left` of which are in the row
-template <typename T>
-__device__ __forceinline__ void store4(uint16_t *p, const float4v &v, int left) {
-    const u32x2 w = {T::pack2(v[0], v[1]), T::pack2(v[2], v[3])};
-    if (left >= 4) {
-        reinterpret_cast<Any8 *>(p)->v = w;
-    } else {
+struct __attribute__((packed, aligned(2))) Any8h {
+    u32x2 v;
+};
+
+// N values (4, or a multiple of 8) from p on, `left` of which are in the row
+template <typename T, int N, typename V>
+__device__ __forceinline__ void store_row(uint16_t *p, const V &v, int left) {
+    if constexpr (N == 4) {
+        const u32x2 w = {T::pack2(v[0], v[1]), T::pack2(v[2], v[3])};
+        if (left >= 4) {
+            reinterpret_cast<Any8h *>(p)->v = w;
+        } else {
 #pragma unroll
-        for (int i = 0; i < 3; i++)
-            if (i < left)
-                p[i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
+            for (int i = 0; i < 4; i++)
+                if (i < left)
+                    p[i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
+        }
+        return;
+    }
+#pragma unroll
+    for (int c = 0; c + 8 <= N; c += 8) {
+        u32x4 w;
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+            w[i] = T::pack2(v[c + 2 * i], v[c + 2 * i + 1]);
+        if (left >= c + 8) {
+            reinterpret_cast<Any16h *>(p + c)->v = w;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; i++)
+                if (c + i < left)
+                    p[c + i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
+        }
     }
 }
-__device__ __forceinline__ void store4f(float *p, const float4v &v, int left) {
-    if (left >= 4) {
-        reinterpret_cast<Any16f *>(p)->v = v;
-    } else {
+template <int N, typename V>
+__device__ __forceinline__ void store_rowf(float *p, const V &v, int left) {
 #pragma unroll
-        for (int i = 0; i < 3; i++)
-            if (i < left)
-                p[i] = v[i];
+    for (int c = 0; c < N; c += 4) {
+        if (left >= c + 4) {
+            reinterpret_cast<Any16f *>(p + c)->v = float4v{v[c], v[c + 1], v[c + 2], v[c + 3]};
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+                if (c + i < left)
+                    p[c + i] = v[c + i];
+        }
     }
 }
-__device__ __forceinline__ float4v load4f(const float *p, int left) {
-    if (left >= 4)
-        return reinterpret_cast<const Any16f *>(p)->v;
-    float4v v = {0.0f, 0.0f, 0.0f, 0.0f};
+template <int N, typename V>
+__device__ __forceinline__ void load_rowf(const float *p, V &v, int left) {
 #pragma unroll
-    for (int i = 0; i < 3; i++)
-        if (i < left)
-            v[i] = p[i];
-    return v;
+    for (int c = 0; c < N; c += 4) {
+        float4v w = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (left >= c + 4) {
+            w = reinterpret_cast<const Any16f *>(p + c)->v;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+                if (c + i < left)
+                    w[i] = p[c + i];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+            v[c + i] = w[i];
+    }
 }
 
 // --- the product itself, rounded once -------------------------------------
@@ -61,29 +94,42 @@ struct StoreArgs {
     float *part;             // [splits][batch][M][N] for split sums
 };
 
-template <typename T>
-__device__ __forceinline__ void finish4(const StoreArgs &e, float4v v, int m, int n, int M, int N, int batch) {
-    const int left = N - n;
-    float *const acc = e.acc + (e.acc ? (int64_t)m * N + n : 0);
-    if (e.acc_in)
-        v += load4f(acc, left);
+// N sums of row m from column n on
+template <typename T, int N, typename V>
+__device__ __forceinline__ void finish(const StoreArgs &e, V &v, int m, int n, int M, int cols, int batch) {
+    const int left = cols - n;
+    float *const acc = e.acc + (e.acc ? (int64_t)m * cols + n : 0);
+    if (e.acc_in) {
+        float more[N];
+        load_rowf<N>(acc, more, left);
+#pragma unroll
+        for (int i = 0; i < N; i++)
+            v[i] += more[i];
+    }
     if (e.acc_out) {
-        store4f(acc, v, left);
+        store_rowf<N>(acc, v, left);
         return;
     }
-    if (e.row_scale)
-        v *= e.row_scale[m];
-    if (e.scale)
-        v *= *e.scale;
-    store4<T>(e.out[batch] + (int64_t)m * e.ldo + n, v, left);
+    if (e.row_scale || e.scale) {
+        const float f = (e.row_scale ? e.row_scale[m] : 1.0f) * (e.scale ? *e.scale : 1.0f);
+#pragma unroll
+        for (int i = 0; i < N; i++)
+            v[i] *= f;
+    }
+    store_row<T, N>(e.out[batch] + (int64_t)m * e.ldo + n, v, left);
 }
 
 struct Store {
     static constexpr bool DUAL = false;
+    template <typename S>
+    static constexpr int lds_bytes() {
+        return 0;
+    }
     using Args = StoreArgs;
-    template <typename T, typename S>
-    static __device__ __forceinline__ void run(const StoreArgs &e, float4v (&acc)[S::FM][S::FN], const Work &at,
+    template <typename T, typename S, bool WIDE>
+    static __device__ __forceinline__ void run(const StoreArgs &e, const Results<S, WIDE> &t, const Work &at,
                                                const mm::Args &a, int m0, int n0, int lane, uint8_t *) {
+        constexpr int W = Results<S, WIDE>::W, PIECES = Results<S, WIDE>::PIECES;
         float *const part = a.splits > 1 ? e.part + ((int64_t)at.split * a.batch + at.batch) * a.M * a.N : nullptr;
 #pragma unroll
         for (int i = 0; i < S::FM; i++) {
@@ -91,21 +137,25 @@ struct Store {
             if (m >= a.M)
                 continue;
 #pragma unroll
-            for (int j = 0; j < S::FN; j++) {
-                const int n = n0 + 16 * j + 4 * (lane >> 4);
+            for (int p = 0; p < PIECES; p++) {
+                const int n = n0 + t.column(p, lane);
                 if (n >= a.N)
                     continue;
+                float v[W];
+#pragma unroll
+                for (int k = 0; k < W; k++)
+                    v[k] = t.get(i, p, k);
                 if (part)
-                    store4f(part + (int64_t)m * a.N + n, acc[i][j], a.N - n);
+                    store_rowf<W>(part + (int64_t)m * a.N + n, v, a.N - n);
                 else
-                    finish4<T>(e, acc[i][j], m, n, a.M, a.N, at.batch);
+                    finish<T, W>(e, v, m, n, a.M, a.N, at.batch);
             }
         }
     }
 };
 
 // --- gate and up channels: h = act(g) u ------------------------------------
-// The tile's groups of 16 columns are of the gate and of the up projection in
+// The tile's groups of 32 columns are of the gate and of the up projection in
 // turn.  h has `pad` columns, those past H zero; g and u are kept in fp32 for the
 // backward pass where it is wanted (16 bits there would add two roundings to
 // each gradient).
@@ -118,10 +168,15 @@ struct GatedArgs {
 
 struct Gated {
     static constexpr bool DUAL = true;
+    template <typename S>
+    static constexpr int lds_bytes() {
+        return 0;
+    }
     using Args = GatedArgs;
-    template <typename T, typename S>
-    static __device__ __forceinline__ void run(const GatedArgs &e, float4v (&acc)[S::FM][S::FN], const Work &,
+    template <typename T, typename S, bool WIDE>
+    static __device__ __forceinline__ void run(const GatedArgs &e, const Results<S, WIDE> &t, const Work &,
                                                const mm::Args &a, int m0, int n0, int lane, uint8_t *) {
+        constexpr int PIECES = Results<S, WIDE>::PIECES;
         with_act(e.act, [&](auto tag) {
             constexpr int ACT = decltype(tag)::value;
 #pragma unroll
@@ -130,20 +185,23 @@ struct Gated {
                 if (m >= a.M)
                     continue;
 #pragma unroll
-                for (int j = 0; j < S::FN; j += 2) {
-                    const int n = n0 / 2 + 8 * j + 4 * (lane >> 4);
+                for (int p = 0; p < PIECES; p += 2) {
+                    static_assert(WIDE, "pieces of gate and of up channels in turn");
+                    const int n = n0 / 2 + t.column(p / 2, lane), left = e.H - n;
                     if (n >= e.pad)
                         continue;
-                    const int left = e.H - n;
-                    float4v h;
+                    float g[8], u[8], h[8];
 #pragma unroll
-                    for (int k = 0; k < 4; k++)
-                        h[k] = k < left ? act_pair<ACT>(acc[i][j][k]).f * acc[i][j + 1][k] : 0.0f;
-                    store4<T>(e.h + m * e.ldh + n, h, e.pad - n);
-                    if (e.saved && left > 0) {
+                    for (int k = 0; k < 8; k++) {
+                        g[k] = t.get(i, p, k);
+                        u[k] = t.get(i, p + 1, k);
+                        h[k] = k < left ? act_pair<ACT>(g[k]).f * u[k] : 0.0f;
+                    }
+                    store_row<T, 8>(e.h + m * e.ldh + n, h, 8);
+                    if (e.saved) {
                         float *const s = e.saved + (int64_t)m * 2 * e.H + n;
-                        store4f(s, acc[i][j], left);
-                        store4f(s + e.H, acc[i][j + 1], left);
+                        store_rowf<8>(s, g, left);
+                        store_rowf<8>(s + e.H, u, left);
                     }
                 }
             }
@@ -161,10 +219,15 @@ struct GatedBackArgs {
 
 struct GatedBack {
     static constexpr bool DUAL = false;
+    template <typename S>
+    static constexpr int lds_bytes() {
+        return 0;
+    }
     using Args = GatedBackArgs;
-    template <typename T, typename S>
-    static __device__ __forceinline__ void run(const GatedBackArgs &e, float4v (&acc)[S::FM][S::FN], const Work &,
+    template <typename T, typename S, bool WIDE>
+    static __device__ __forceinline__ void run(const GatedBackArgs &e, const Results<S, WIDE> &t, const Work &,
                                                const mm::Args &a, int m0, int n0, int lane, uint8_t *) {
+        constexpr int W = Results<S, WIDE>::W, PIECES = Results<S, WIDE>::PIECES;
         with_act(e.act, [&](auto tag) {
             constexpr int ACT = decltype(tag)::value;
 #pragma unroll
@@ -173,25 +236,26 @@ struct GatedBack {
                 if (m >= a.M)
                     continue;
 #pragma unroll
-                for (int j = 0; j < S::FN; j++) {
-                    const int n = n0 + 16 * j + 4 * (lane >> 4), left = e.H - n;
+                for (int p = 0; p < PIECES; p++) {
+                    const int n = n0 + t.column(p, lane), left = e.H - n;
                     if (n >= e.pad)
                         continue;
                     const float *const s = e.saved + (int64_t)m * 2 * e.H + n;
-                    const float4v g = load4f(s, left), u = load4f(s + e.H, left);
-                    float4v dg, du, h;
+                    float g[W], u[W], dg[W], du[W], h[W];
+                    load_rowf<W>(s, g, left);
+                    load_rowf<W>(s + e.H, u, left);
 #pragma unroll
-                    for (int k = 0; k < 4; k++) {
-                        const ActPair p = act_pair<ACT>(g[k]);
-                        const float dh = acc[i][j][k];
-                        dg[k] = k < left ? dh * u[k] * p.d : 0.0f;
-                        du[k] = k < left ? dh * p.f : 0.0f;
-                        h[k] = k < left ? p.f * u[k] : 0.0f;
+                    for (int k = 0; k < W; k++) {
+                        const ActPair q = act_pair<ACT>(g[k]);
+                        const float dh = t.get(i, p, k);
+                        dg[k] = k < left ? dh * u[k] * q.d : 0.0f;
+                        du[k] = k < left ? dh * q.f : 0.0f;
+                        h[k] = k < left ? q.f * u[k] : 0.0f;
                     }
                     uint16_t *const d = e.d + (int64_t)m * 2 * e.pad + n;
-                    store4<T>(d, dg, e.pad - n);
-                    store4<T>(d + e.pad, du, e.pad - n);
-                    store4<T>(e.h + (int64_t)m * e.pad + n, h, e.pad - n);
+                    store_row<T, W>(d, dg, W);
+                    store_row<T, W>(d + e.pad, du, W);
+                    store_row<T, W>(e.h + (int64_t)m * e.pad + n, h, W);
                 }
             }
         });
@@ -215,10 +279,15 @@ __device__ __forceinline__ float2 join_lse(float2 a, float2 b) {
 
 struct Lse {
     static constexpr bool DUAL = false;
+    template <typename S>
+    static constexpr int lds_bytes() {
+        return S::WN * S::TM * (int)sizeof(float2);
+    }
     using Args = LseArgs;
-    template <typename T, typename S>
-    static __device__ __forceinline__ void run(const LseArgs &e, float4v (&acc)[S::FM][S::FN], const Work &at,
+    template <typename T, typename S, bool WIDE>
+    static __device__ __forceinline__ void run(const LseArgs &e, const Results<S, WIDE> &t, const Work &at,
                                                const mm::Args &a, int m0, int n0, int lane, uint8_t *lds) {
+        constexpr int W = Results<S, WIDE>::W, PIECES = Results<S, WIDE>::PIECES;
         float2 *const row = reinterpret_cast<float2 *>(lds);  // [WN][TM]
         const int wn = n0 % S::TN / (S::TN / S::WN), local = m0 % S::TM;
 #pragma unroll
@@ -226,25 +295,27 @@ struct Lse {
             const int m = m0 + 16 * i + (lane & 15);
             const int64_t want = e.tokens && m < a.M ? e.tokens[m] : -1;
             float top = -INFINITY;
+            float z[PIECES][W];
 #pragma unroll
-            for (int j = 0; j < S::FN; j++) {
-                const int n = n0 + 16 * j + 4 * (lane >> 4);
+            for (int p = 0; p < PIECES; p++) {
+                const int n = n0 + t.column(p, lane);
 #pragma unroll
-                for (int k = 0; k < 4; k++) {
+                for (int k = 0; k < W; k++) {
+                    z[p][k] = t.get(i, p, k);
                     if (n + k >= a.N)
-                        acc[i][j][k] = -INFINITY;
+                        z[p][k] = -INFINITY;
                     else if (n + k == want)
-                        e.picked[m] = acc[i][j][k];
-                    top = fmaxf(top, acc[i][j][k]);
+                        e.picked[m] = z[p][k];
+                    top = fmaxf(top, z[p][k]);
                 }
             }
             const float base = top == -INFINITY ? 0.0f : top;
             float sum = 0.0f;
 #pragma unroll
-            for (int j = 0; j < S::FN; j++)
+            for (int p = 0; p < PIECES; p++)
 #pragma unroll
-                for (int k = 0; k < 4; k++)
-                    sum += __builtin_amdgcn_exp2f((acc[i][j][k] - base) * LOG2E);
+                for (int k = 0; k < W; k++)
+                    sum += __builtin_amdgcn_exp2f((z[p][k] - base) * LOG2E);
             float2 r = make_float2(top, sum);
             r = join_lse(r, make_float2(__shfl_xor(r.x, 16), __shfl_xor(r.y, 16)));
             r = join_lse(r, make_float2(__shfl_xor(r.x, 32), __shfl_xor(r.y, 32)));
@@ -252,15 +323,16 @@ struct Lse {
                 row[wn * S::TM + local + 16 * i + lane] = r;
         }
         __syncthreads();
-        for (int t = threadIdx.x; t < S::TM; t += S::TH) {
-            float2 r = row[t];
+        for (int l = threadIdx.x; l < S::TM; l += S::TH) {
+            float2 r = row[l];
 #pragma unroll
             for (int w = 1; w < S::WN; w++)
-                r = join_lse(r, row[w * S::TM + t]);
-            const int m = at.m * S::TM + t;
+                r = join_lse(r, row[w * S::TM + l]);
+            const int m = at.m * S::TM + l;
             if (m < a.M)
                 e.part[(int64_t)at.n * a.M + m] = r;
         }
+        __syncthreads();  // before the next item's
     }
 };
 
@@ -277,10 +349,15 @@ struct DzArgs {
 
 struct Dz {
     static constexpr bool DUAL = false;
+    template <typename S>
+    static constexpr int lds_bytes() {
+        return 0;
+    }
     using Args = DzArgs;
-    template <typename T, typename S>
-    static __device__ __forceinline__ void run(const DzArgs &e, float4v (&acc)[S::FM][S::FN], const Work &,
+    template <typename T, typename S, bool WIDE>
+    static __device__ __forceinline__ void run(const DzArgs &e, const Results<S, WIDE> &t, const Work &,
                                                const mm::Args &a, int m0, int n0, int lane, uint8_t *) {
+        constexpr int W = Results<S, WIDE>::W, PIECES = Results<S, WIDE>::PIECES;
 #pragma unroll
         for (int i = 0; i < S::FM; i++) {
             const int m = m0 + 16 * i + (lane & 15);
@@ -290,17 +367,17 @@ struct Dz {
             const int want = r.token - e.v0;
             const bool any = !(r.c == 0.0f && r.g == 0.0f);
 #pragma unroll
-            for (int j = 0; j < S::FN; j++) {
-                const int n = n0 + 16 * j + 4 * (lane >> 4);
+            for (int p = 0; p < PIECES; p++) {
+                const int n = n0 + t.column(p, lane);
                 if (n >= e.pad)
                     continue;
-                float4v d;
+                float d[W];
 #pragma unroll
-                for (int k = 0; k < 4; k++) {
-                    const float p = __builtin_amdgcn_exp2f((acc[i][j][k] - r.lse) * LOG2E);
-                    d[k] = any && n + k < a.N ? fmaf(r.c, p, n + k == want ? r.g : 0.0f) : 0.0f;
+                for (int k = 0; k < W; k++) {
+                    const float q = __builtin_amdgcn_exp2f((t.get(i, p, k) - r.lse) * LOG2E);
+                    d[k] = any && n + k < a.N ? fmaf(r.c, q, n + k == want ? r.g : 0.0f) : 0.0f;
                 }
-                store4<T>(e.dz + (int64_t)m * e.pad + n, d, e.pad - n);
+                store_row<T, W>(e.dz + (int64_t)m * e.pad + n, d, W);
             }
         }
     }

@@ -68,6 +68,7 @@ inline Args args_of(const Plan &p, int M, int N, int K, const Matrix &a, int ext
     r.tiles_n = (N + TILES[p.tile].n - 1) / TILES[p.tile].n;
     r.splits = p.splits;
     r.batch = batch;
+    r.items = (unsigned)r.tiles_m * (unsigned)r.tiles_n * (unsigned)r.splits * (unsigned)batch;
     return r;
 }
 

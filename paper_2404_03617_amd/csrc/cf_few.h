@@ -1,0 +1,165 @@
+// cf_few.h -- products x W^T of a few rows (up to 16: decoded tokens, a handful of
+// features), bound by reading W once.  A workgroup takes 16 or 32 rows of W, its
+// waves share k: each goes through 256 k's at a time, 512 bytes a row, straight
+// from memory into MFMA fragments, 16 or more loads in flight a wave.  The rows of x
+// come from the caches.  The waves' sums meet in LDS in a fixed order, and the
+// first wave does what follows.
+#pragma once
+
+#include "cf_mm_epi.h"
+
+namespace cf {
+namespace few {
+
+using mm::RowGrad;
+using mm::StoreArgs;
+
+constexpr int ROWS = 16, U = 8;  // rows of x at most; steps of 32 k's of a wave
+
+struct Args {
+    const uint16_t *x, *w[2];
+    int64_t ldx, ldw;
+    int M, N, K;  // K: columns that the rows hold, a multiple of 8
+};
+
+// What follows gets `sum(f)`, the four results of fragment f in row lane % 16 of x:
+// rows n0 + 16 f + 4 (lane / 16) .. + 3 of W (DUAL: of either matrix, n0 alone).
+struct Gated {
+    static constexpr bool DUAL = true;
+    using Extra = mm::GatedArgs;
+    template <typename T, int FN>
+    static __device__ __forceinline__ void run(const Extra &e, const float4v (&sum)[FN], const Args &a, int n0, int lane) {
+        const int m = lane & 15, n = n0 + 4 * (lane >> 4), left = e.H - n;
+        if (m >= a.M || n >= e.pad)
+            return;
+        mm::store_rowf<4>(e.saved ? e.saved + (int64_t)m * 2 * e.H + n : nullptr, sum[0], e.saved ? left : 0);
+        mm::store_rowf<4>(e.saved ? e.saved + (int64_t)m * 2 * e.H + e.H + n : nullptr, sum[1], e.saved ? left : 0);
+        with_act(e.act, [&](auto tag) {
+            float4v h;
+#pragma unroll
+            for (int k = 0; k < 4; k++)
+                h[k] = k < left ? act_pair<decltype(tag)::value>(sum[0][k]).f * sum[1][k] : 0.0f;
+            mm::store_row<T, 4>(e.h + m * e.ldh + n, h, 4);
+        });
+    }
+};
+
+struct Store {
+    static constexpr bool DUAL = false;
+    using Extra = mm::StoreArgs;
+    template <typename T, int FN>
+    static __device__ __forceinline__ void run(const Extra &e, const float4v (&sum)[FN], const Args &a, int n0, int lane) {
+        const int m = lane & 15;
+#pragma unroll
+        for (int f = 0; f < FN; f++) {
+            const int n = n0 + 16 * f + 4 * (lane >> 4);
+            if (m < a.M && n < a.N)
+                mm::store_row<T, 4>(e.out[0] + (int64_t)m * e.ldo + n, sum[f], a.N - n);
+        }
+    }
+};
+
+struct Lse {
+    static constexpr bool DUAL = false;
+    using Extra = mm::LseArgs;
+    template <typename T, int FN>
+    static __device__ __forceinline__ void run(const Extra &e, const float4v (&sum)[FN], const Args &a, int n0, int lane) {
+        const int m = lane & 15;
+        const int64_t want = e.tokens && m < a.M ? e.tokens[m] : -1;
+        float top = -INFINITY;
+        float z[FN][4];
+#pragma unroll
+        for (int f = 0; f < FN; f++)
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+                const int n = n0 + 16 * f + 4 * (lane >> 4) + k;
+                z[f][k] = n < a.N ? sum[f][k] : -INFINITY;
+                if (n == want)
+                    e.picked[m] = z[f][k];
+                top = fmaxf(top, z[f][k]);
+            }
+        const float base = top == -INFINITY ? 0.0f : top;
+        float s = 0.0f;
+#pragma unroll
+        for (int f = 0; f < FN; f++)
+#pragma unroll
+            for (int k = 0; k < 4; k++)
+                s += __builtin_amdgcn_exp2f((z[f][k] - base) * mm::LOG2E);
+        float2 r = make_float2(top, s);
+        r = mm::join_lse(r, make_float2(__shfl_xor(r.x, 16), __shfl_xor(r.y, 16)));
+        r = mm::join_lse(r, make_float2(__shfl_xor(r.x, 32), __shfl_xor(r.y, 32)));
+        if (lane < a.M && lane < 16)
+            e.part[(int64_t)blockIdx.x * a.M + lane] = r;
+    }
+};
+
+template <typename T, int WAVES, int FN, typename E>
+__global__ __launch_bounds__(WAVES * 64) void kernel(Args a, typename E::Extra e) {
+    __shared__ float4v red[WAVES][FN][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, q = lane >> 4;
+    const int n0 = blockIdx.x * (E::DUAL ? 16 : 16 * FN);
+    const uint16_t *w[FN];
+#pragma unroll
+    for (int f = 0; f < FN; f++) {
+        const int row = n0 + (E::DUAL ? 0 : 16 * f) + r;
+        w[f] = (E::DUAL && f ? a.w[1] : a.w[0]) + (int64_t)(row < a.N ? row : a.N - 1) * a.ldw + q * 8;
+    }
+    const uint16_t *const x = a.x + (int64_t)(r < a.M ? r : a.M - 1) * a.ldx + q * 8;
+    float4v acc[FN];
+#pragma unroll
+    for (int f = 0; f < FN; f++)
+        acc[f] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+
+    constexpr int SHARE = U * 32;
+    int k0 = wave * SHARE;
+    for (; k0 + SHARE <= a.K; k0 += WAVES * SHARE) {
+        u32x4 fw[FN][U], fx[U];
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+#pragma unroll
+            for (int f = 0; f < FN; f++)
+                fw[f][u] = *reinterpret_cast<const u32x4 *>(w[f] + k0 + 32 * u);
+            fx[u] = *reinterpret_cast<const u32x4 *>(x + k0 + 32 * u);
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++)
+#pragma unroll
+            for (int f = 0; f < FN; f++)
+                acc[f] = T::mfma(fw[f][u], fx[u], acc[f]);
+    }
+    for (; k0 < a.K; k0 += 32) {  // the wave that has the last share of k, where it is not whole
+        const bool in = k0 + q * 8 < a.K;
+        const u32x4 none = {0u, 0u, 0u, 0u}, fx = in ? *reinterpret_cast<const u32x4 *>(x + k0) : none;
+#pragma unroll
+        for (int f = 0; f < FN; f++)
+            acc[f] = T::mfma(in ? *reinterpret_cast<const u32x4 *>(w[f] + k0) : none, fx, acc[f]);
+    }
+#pragma unroll
+    for (int f = 0; f < FN; f++)
+        red[wave][f][lane] = acc[f];
+    __syncthreads();
+    if (wave)
+        return;
+#pragma unroll
+    for (int f = 0; f < FN; f++)
+#pragma unroll
+        for (int v = 1; v < WAVES; v++)
+            acc[f] += red[v][f][lane];
+    E::template run<T, FN>(e, acc, a, n0, lane);
+}
+
+// Waves that share k: enough that each has about one share of it.
+inline int waves_of(int K) { return K > 6144 ? 16 : K > 1536 ? 8 : 4; }
+
+template <typename T, int FN, typename E>
+hipError_t launch(const Args &a, const typename E::Extra &e, hipStream_t st) {
+    const int per = E::DUAL ? 16 : 16 * FN, waves = waves_of(a.K);
+    void (*const f)(Args, typename E::Extra) = waves == 16  ? kernel<T, 16, FN, E>
+                                               : waves == 8 ? kernel<T, 8, FN, E>
+                                                            : kernel<T, 4, FN, E>;
+    f<<<dim3((unsigned)((a.N + per - 1) / per)), dim3(waves * 64), 0, st>>>(a, e);
+    return hipGetLastError();
+}
+
+}  // namespace few
+}  // namespace cf

@@ -10,6 +10,7 @@
 //   dWd = dy^T h;  dWg = dg^T x, dWu = du^T x (one launch);  dx = dg Wg + du Wu (one sum)
 //
 // h, dg and du are rounded to the type of x for the products that read them.
+#include "cf_few.h"
 #include "cf_head.h"
 #include "cf_mm_run.h"
 
@@ -54,7 +55,7 @@ ForwardPlan forward_plan(const GatedFfn &a, const Copied &c, void *ws) {
     p.h = (uint16_t *)p.room.take((size_t)a.rows * p.pad * 2);
     p.up = plan(a.rows, 2 * (int64_t)a.H, a.C, false);
     p.down = plan(a.rows, a.C, a.H, true);
-    p.part = p.room.take(part_bytes(p.down, a.rows, a.C, 1));
+    p.part = a.rows <= few::ROWS ? nullptr : p.room.take(part_bytes(p.down, a.rows, a.C, 1));
     return p;
 }
 
@@ -94,6 +95,15 @@ hipError_t forward(const GatedFfn &a, const ForwardPlan &p, void *y, int64_t ldy
     CF_HIP(pack(p.wg, bf16, st));
     CF_HIP(pack(p.wu, bf16, st));
     CF_HIP(pack(p.wd, bf16, st));
+    if (a.rows <= few::ROWS) {
+        const few::Args up = {p.x.m.p, {p.wg.m.p, p.wu.m.p}, p.x.m.ld, p.wg.m.ld, a.rows, a.H, p.x.m.ext};
+        CF_HIP((few::launch<T, 2, few::Gated>(up, GatedArgs{p.h, p.pad, saved, a.H, p.pad, a.act}, st)));
+        StoreArgs s = {};
+        s.out[0] = (uint16_t *)y;
+        s.ldo = ldy;
+        const few::Args down = {p.h, {p.wd.m.p, p.wd.m.p}, p.pad, p.wd.m.ld, a.rows, a.C, p.pad};
+        return few::launch<T, 1, few::Store>(down, s, st);
+    }
     Args up = args_of(p.up, a.rows, 2 * a.H, a.C, p.x.m, a.rows, p.wg.m, a.H);
     up.b[1] = p.wu.m.p;
     CF_HIP(launch_gated<T>(up, GatedArgs{p.h, p.pad, saved, a.H, p.pad, a.act}, p.up.tile, st));

@@ -22,6 +22,7 @@
 // (exactly, but for what falls below fp16 against the largest row) and the sums
 // back.  The same copy of x leaves out rows without a gradient: what their
 // features hold, NaN included, reaches nothing.
+#include "cf_few.h"
 #include "cf_head.h"
 #include "cf_mm_run.h"
 #include "cf_rows.h"
@@ -33,17 +34,28 @@ using namespace mm;
 namespace {
 
 constexpr double PIECE_BYTES = 256 << 20;
+constexpr int FEW = 2;  // fragments of 16 classes a workgroup where there are few rows
 
+// L lanes join the parts of a row.
+template <int L>
 __global__ __launch_bounds__(256) void join_lse_kernel(const float2 *part, const float *picked, const int64_t *tokens,
                                                        float *logp, float *lse, int rows, int V, int parts) {
-    const int lane = threadIdx.x & 15, r = blockIdx.x * 16 + (threadIdx.x >> 4);
+    const int lane = threadIdx.x % L, r = blockIdx.x * (256 / L) + threadIdx.x / L;
     float2 v = make_float2(-INFINITY, 0.0f);
     if (r < rows)
-        for (int i = lane; i < parts; i += 16)
+#pragma unroll 4
+        for (int i = lane; i < parts; i += L)
             v = join_lse(v, part[(int64_t)i * rows + r]);
 #pragma unroll
-    for (int d = 1; d < 16; d *= 2)
+    for (int d = 1; d < (L < 64 ? L : 64); d *= 2)
         v = join_lse(v, make_float2(__shfl_xor(v.x, d), __shfl_xor(v.y, d)));
+    if constexpr (L == 256) {
+        __shared__ float2 s[4];
+        if ((lane & 63) == 0)
+            s[lane >> 6] = v;
+        __syncthreads();
+        v = join_lse(join_lse(s[0], s[1]), join_lse(s[2], s[3]));
+    }
     if (lane || r >= rows)
         return;
     const float ls = logf(v.y);
@@ -139,7 +151,8 @@ ForwardPlan forward_plan(const LinearLogProbs &a, bool copy_x, bool copy_w, void
     p.x = operand(a.x.p, a.x.ld, a.rows, a.C, copy_x, p.room);
     p.w = operand(a.w.p, a.w.ld, a.V, a.C, copy_w, p.room);
     p.z = plan(a.rows, a.V, a.C, false);
-    p.parts = (a.V + TILES[p.z.tile].n - 1) / TILES[p.z.tile].n;
+    const int n = a.rows <= few::ROWS ? 16 * FEW : TILES[p.z.tile].n;
+    p.parts = (a.V + n - 1) / n;
     p.part = (float2 *)p.room.take((size_t)p.parts * a.rows * sizeof(float2));
     p.picked = (float *)p.room.take((size_t)a.rows * 4);
     return p;
@@ -187,10 +200,19 @@ template <typename T>
 hipError_t forward(const LinearLogProbs &a, const ForwardPlan &p, float *logp, float *lse, int bf16, hipStream_t st) {
     CF_HIP(pack(p.x, bf16, st));
     CF_HIP(pack(p.w, bf16, st));
-    CF_HIP(launch_lse<T>(args_of(p.z, a.rows, a.V, a.C, p.x.m, a.rows, p.w.m, a.V),
-                         LseArgs{p.part, p.picked, logp ? a.tokens : nullptr}, p.z.tile, st));
-    join_lse_kernel<<<dim3((unsigned)((a.rows + 15) / 16)), 256, 0, st>>>(p.part, p.picked, a.tokens, logp, lse, a.rows,
-                                                                          a.V, p.parts);
+    const LseArgs e = {p.part, p.picked, logp ? a.tokens : nullptr};
+    if (a.rows <= few::ROWS)
+        CF_HIP((few::launch<T, FEW, few::Lse>(
+            few::Args{p.x.m.p, {p.w.m.p, p.w.m.p}, p.x.m.ld, p.w.m.ld, a.rows, a.V, p.x.m.ext}, e, st)));
+    else
+        CF_HIP(launch_lse<T>(args_of(p.z, a.rows, a.V, a.C, p.x.m, a.rows, p.w.m, a.V), e, p.z.tile, st));
+    // few rows of many parts: a workgroup each
+    if (a.rows <= 256 && p.parts > 64)
+        join_lse_kernel<256><<<dim3((unsigned)a.rows), 256, 0, st>>>(p.part, p.picked, a.tokens, logp, lse, a.rows, a.V,
+                                                                     p.parts);
+    else
+        join_lse_kernel<16><<<dim3((unsigned)((a.rows + 15) / 16)), 256, 0, st>>>(p.part, p.picked, a.tokens, logp, lse,
+                                                                                  a.rows, a.V, p.parts);
     return hipGetLastError();
 }
 

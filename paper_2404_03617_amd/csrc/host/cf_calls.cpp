@@ -1,4 +1,4 @@
-// cf_calls.cpp -- calls of the training and scoring operators in native code
+// cf_calls.cpp -- calls of the training and scoring operators and of those for heads in native code
 // (part of the module _cf_args): one function checks a call's arguments, makes
 // its outputs with torch's allocator and calls the library on the current
 // stream.  As with the checks of cf_args.cpp, these functions only say yes:
@@ -11,6 +11,7 @@
 #include <Python.h>
 
 #include <ATen/ops/empty.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -36,6 +37,18 @@ struct Library {
     decltype(&cf_log_probs_forward) log_probs;
     decltype(&cf_log_probs_workspace_bytes) log_probs_ws;
     decltype(&cf_log_probs_backward) log_probs_backward;
+    decltype(&cf_group_norm_forward) group_norm;
+    decltype(&cf_group_norm_workspace_bytes) group_norm_ws;
+    decltype(&cf_group_norm_backward) group_norm_backward;
+    decltype(&cf_group_norm_backward_workspace_bytes) group_norm_backward_ws;
+    decltype(&cf_gated_ffn_forward) gated;
+    decltype(&cf_gated_ffn_workspace_bytes) gated_ws;
+    decltype(&cf_gated_ffn_backward) gated_backward;
+    decltype(&cf_gated_ffn_backward_workspace_bytes) gated_backward_ws;
+    decltype(&cf_linear_log_probs_forward) linear;
+    decltype(&cf_linear_log_probs_workspace_bytes) linear_ws;
+    decltype(&cf_linear_log_probs_backward) linear_backward;
+    decltype(&cf_linear_log_probs_backward_workspace_bytes) linear_backward_ws;
 };
 Library lib;
 bool bound = false;
@@ -368,6 +381,163 @@ PyObject *log_probs_backward(PyObject *const *a, Py_ssize_t n) {
     return give(dz.t);
 }
 
+// --- operators for heads ----------------------------------------------------
+
+// These run on their tensors' device: this path is for the current one.
+void on_current(const at::Tensor &x) { must(x.device().index() == c10::hip::current_device()); }
+
+float *data(const at::Tensor &t) { return t.defined() ? static_cast<float *>(t.data_ptr()) : nullptr; }
+
+struct Workspace {
+    at::Tensor t;
+    void *p = nullptr;
+    size_t bytes = 0;
+    Workspace(const at::Tensor &x, size_t n) : bytes(n) {
+        if (n) {
+            t = fresh(x, {(int64_t)n}, at::kByte);
+            p = t.data_ptr();
+        }
+    }
+};
+
+// feature maps [N, .., C]: images and their pixels
+RowsOf images_of(PyObject *o, int64_t *N, int64_t *P) {
+    const RowsOf x = rows_of(o, 2);
+    must(x.t->dim() >= 2);
+    *N = x.t->size(0);
+    *P = *N ? x.n / *N : 0;
+    return x;
+}
+
+// (x, groups, weight, bias, eps, act, save, out) -> (y, stats or None)
+PyObject *group_norm(PyObject *const *a, Py_ssize_t n) {
+    must(n == 8 && PyLong_CheckExact(a[1]));
+    int64_t N, P;
+    const RowsOf x = images_of(a[0], &N, &P);
+    on_current(*x.t);
+    const long G = whole(a[1]), act = whole(a[5]);
+    must(G >= 1 && G <= x.C && x.C % G == 0);
+    const float *w = floats(a[2], *x.t, x.C), *b = floats(a[3], *x.t, x.C), eps = real(a[4]);
+    const Out y = out_of(a[7], *x.t, x.code);
+    at::Tensor stats;
+    if (truth(a[6]))
+        stats = fresh(*x.t, {N, G, 2}, at::kFloat);
+    const Workspace ws(*x.t, lib.group_norm_ws(N, P, x.C, (int)G));
+    check(lib.group_norm(x.p, y.p, w, b, data(stats), ws.p, ws.bytes, N, P, x.C, (int)G, x.ld, y.ld, eps,
+                         (cf_dtype)x.code, (cf_act)act, stream()));
+    return give_all(y.t, stats);
+}
+
+// (dy, x, stats, weight, bias, act, param_grads, out) -> (dx, dweight, dbias)
+PyObject *group_norm_backward(PyObject *const *a, Py_ssize_t n) {
+    must(n == 8);
+    int64_t N, P;
+    const RowsOf dy = images_of(a[0], &N, &P), x = rows_of(a[1], 2);
+    on_current(*dy.t);
+    must(x.code == dy.code && x.t->sizes() == dy.t->sizes() && x.t->device() == dy.t->device());
+    const at::Tensor &st = tensor(a[2]);
+    must(st.dim() == 3 && st.size(1) >= 1 && st.size(1) <= dy.C && dy.C % st.size(1) == 0);
+    const int G = (int)st.size(1);
+    const float *stats = floats(a[2], *dy.t, N * G, 2), *w = floats(a[3], *dy.t, dy.C), *b = floats(a[4], *dy.t, dy.C);
+    const long act = whole(a[5]);
+    const Out dx = out_of(a[7], *dy.t, dy.code);
+    at::Tensor dw, db;
+    if (truth(a[6])) {
+        dw = fresh(*dy.t, {dy.C}, at::kFloat);
+        db = fresh(*dy.t, {dy.C}, at::kFloat);
+    }
+    const Workspace ws(*dy.t, lib.group_norm_backward_ws(N, P, dy.C, G));
+    check(lib.group_norm_backward(dy.p, x.p, stats, w, b, dx.p, data(dw), data(db), ws.p, ws.bytes, N, P, dy.C, G, dy.ld,
+                                  x.ld, dx.ld, (cf_dtype)dy.code, (cf_act)act, stream()));
+    return give_all(dx.t, dw, db);
+}
+
+// a weight matrix [rows (-1: any), cols] of x's type and device
+RowsOf matrix_of(PyObject *o, const RowsOf &x, int64_t rows, int64_t cols) {
+    const RowsOf w = rows_of(o, 2);
+    must(w.t->dim() == 2 && w.code == x.code && w.C == cols && (rows < 0 ? w.n >= 1 : w.n == rows) &&
+         w.n < ((int64_t)1 << 31) && w.t->device() == x.t->device());
+    return w;
+}
+
+// whether the products read these rows in place
+bool readable(const RowsOf &r) { return ((uintptr_t)r.p & 15) == 0 && r.ld % 8 == 0 && r.ld < ((int64_t)1 << 22); }
+
+// (x, w_gate, w_up, w_down, act, save, out) -> (y, saved or None)
+PyObject *gated(PyObject *const *a, Py_ssize_t n) {
+    must(n == 7);
+    const RowsOf x = rows_of(a[0], 2);
+    on_current(*x.t);
+    const RowsOf g = matrix_of(a[1], x, -1, x.C), u = matrix_of(a[2], x, g.n, x.C), d = matrix_of(a[3], x, x.C, g.n);
+    const int H = (int)g.n;
+    const long act = whole(a[4]);
+    const Out y = out_of(a[6], *x.t, x.code);
+    at::Tensor saved;
+    if (truth(a[5]))
+        saved = fresh(*x.t, lead(*x.t, 2 * (int64_t)H), at::kFloat);
+    const bool plain = readable(x) && readable(g) && readable(u) && readable(d) && g.ld == u.ld;
+    const Workspace ws(*x.t, lib.gated_ws(x.n, x.C, H, plain));
+    check(lib.gated(x.p, g.p, u.p, d.p, y.p, data(saved), ws.p, ws.bytes, x.n, x.C, H, x.ld, g.ld, u.ld, d.ld, y.ld,
+                    (cf_dtype)x.code, (cf_act)act, stream()));
+    return give_all(y.t, saved);
+}
+
+// (dy, x, saved, w_gate, w_up, w_down, act, out) -> (dx, dw_gate, dw_up, dw_down)
+PyObject *gated_backward(PyObject *const *a, Py_ssize_t n) {
+    must(n == 8 && a[2] != Py_None);
+    const RowsOf dy = rows_of(a[0], 2), x = rows_of(a[1], 2);
+    on_current(*dy.t);
+    must(x.code == dy.code && x.t->sizes() == dy.t->sizes() && x.t->device() == dy.t->device());
+    const RowsOf g = matrix_of(a[3], dy, -1, dy.C), u = matrix_of(a[4], dy, g.n, dy.C), d = matrix_of(a[5], dy, dy.C, g.n);
+    const int H = (int)g.n;
+    const float *saved = floats(a[2], *dy.t, dy.n, 2 * (int64_t)H);
+    const long act = whole(a[6]);
+    const Out dx = out_of(a[7], *dy.t, dy.code);
+    const at::ScalarType type = type_of(dy.code);
+    const at::Tensor dg = fresh(*dy.t, {H, dy.C}, type), du = fresh(*dy.t, {H, dy.C}, type),
+                     dd = fresh(*dy.t, {dy.C, H}, type);
+    const bool plain = readable(dy) && readable(x) && readable(g) && readable(u) && readable(d) && g.ld == u.ld;
+    const Workspace ws(*dy.t, lib.gated_backward_ws(dy.n, dy.C, H, plain));
+    check(lib.gated_backward(dy.p, x.p, saved, g.p, u.p, d.p, dx.p, dg.data_ptr(), du.data_ptr(), dd.data_ptr(), ws.p,
+                             ws.bytes, dy.n, dy.C, H, dy.ld, x.ld, g.ld, u.ld, d.ld, dx.ld, (cf_dtype)dy.code,
+                             (cf_act)act, stream()));
+    return give_all(dx.t, dg, du, dd);
+}
+
+// (x, weight, tokens or None) -> (logp or None, lse)
+PyObject *linear(PyObject *const *a, Py_ssize_t n) {
+    must(n == 3);
+    const RowsOf x = rows_of(a[0], 2);
+    on_current(*x.t);
+    const RowsOf w = matrix_of(a[1], x, -1, x.C);
+    const int64_t *tokens = flat_of<const int64_t>(a[2], *x.t, at::kLong, x.n, 0);
+    const std::vector<int64_t> shape = lead(*x.t);
+    at::Tensor logp;
+    if (a[2] != Py_None)
+        logp = fresh(*x.t, shape, at::kFloat);
+    const at::Tensor lse = fresh(*x.t, shape, at::kFloat);
+    const Workspace ws(*x.t, lib.linear_ws(x.n, x.C, (int)w.n, readable(x) && readable(w)));
+    check(lib.linear(x.p, w.p, tokens, data(logp), data(lse), ws.p, ws.bytes, x.n, x.C, (int)w.n, x.ld, w.ld,
+                     (cf_dtype)x.code, stream()));
+    return give_all(logp, lse);
+}
+
+// (x, weight, tokens or None, lse, d_logp, d_lse, out) -> (dx, dweight)
+PyObject *linear_backward(PyObject *const *a, Py_ssize_t n) {
+    must(n == 7 && a[3] != Py_None);
+    const RowsOf x = rows_of(a[0], 2);
+    on_current(*x.t);
+    const RowsOf w = matrix_of(a[1], x, -1, x.C);
+    const int64_t *tokens = flat_of<const int64_t>(a[2], *x.t, at::kLong, x.n, 0);
+    const float *lse = floats(a[3], *x.t, x.n), *gl = floats(a[4], *x.t, x.n), *gs = floats(a[5], *x.t, x.n);
+    const Out dx = out_of(a[6], *x.t, x.code);
+    const at::Tensor dw = fresh(*x.t, {w.n, x.C}, type_of(x.code));
+    const Workspace ws(*x.t, lib.linear_backward_ws(x.n, x.C, (int)w.n, readable(x) && readable(w)));
+    check(lib.linear_backward(x.p, w.p, tokens, lse, gl, gs, dx.p, dw.data_ptr(), ws.p, ws.bytes, x.n, x.C, (int)w.n,
+                              x.ld, w.ld, dx.ld, (cf_dtype)x.code, stream()));
+    return give_all(dx.t, dw);
+}
+
 // bind((address, ..)): the library's functions, in the order of Library
 PyObject *bind(PyObject *, PyObject *arg) {
     constexpr Py_ssize_t n = sizeof(Library) / sizeof(void *);
@@ -403,6 +573,12 @@ PyMethodDef calls[] = {CF_CALL("norm_forward", norm_forward),
                        CF_CALL("wgrad", wgrad),
                        CF_CALL("log_probs", log_probs),
                        CF_CALL("log_probs_backward", log_probs_backward),
+                       CF_CALL("group_norm", group_norm),
+                       CF_CALL("group_norm_backward", group_norm_backward),
+                       CF_CALL("gated", gated),
+                       CF_CALL("gated_backward", gated_backward),
+                       CF_CALL("linear", linear),
+                       CF_CALL("linear_backward", linear_backward),
                        {"bind", bind, METH_O, nullptr},
                        {nullptr, nullptr, 0, nullptr}};
 

@@ -18,7 +18,7 @@ import torch
 
 import paper_2404_03617_amd as _cf
 
-from .training import _flat, _like, _out_rows, _rows, _ws
+from .training import _flat, _like, _native, _out_rows, _rows, _ws
 
 ACTS = {"gelu": 0, "relu": 1, "none": 2, "silu": 3}
 
@@ -91,6 +91,10 @@ def _groups(groups, C):
 
 
 def _group_norm(x, groups, weight, bias, eps, act, save, out, ws, stream):
+    if stream is None and ws is None and act in ACTS:
+        r = _native("group_norm", x, groups, weight, bias, eps, ACTS[act], save, out)
+        if r is not None:
+            return r
     xp, N, P, C, ldx, code = _images("x", x)
     G, a = _groups(groups, C), _act(act)
     w, b = _flat("weight", x, weight, 2, C, 0), _flat("bias", x, bias, 2, C, 0)
@@ -139,6 +143,10 @@ def group_norm_backward(dy: torch.Tensor, x: torch.Tensor, stats: torch.Tensor, 
     dtype, dweight and dbias fp32 [C] (None without param_grads), from the forward
     call's x, weight, bias, act and stats.  out may be dy.  ws: a uint8 workspace
     of group_norm_backward_workspace_bytes()."""
+    if stream is None and ws is None and act in ACTS:
+        r = _native("group_norm_backward", dy, x, stats, weight, bias, ACTS[act], param_grads, out)
+        if r is not None:
+            return r
     dyp, N, P, C, lddy, code = _images("dy", dy)
     xp, ldx = _like("x", dy, x, dy.shape, code)
     if not isinstance(stats, torch.Tensor) or stats.dim() != 3:
@@ -179,6 +187,10 @@ def _gated_weights(x, w_gate, w_up, w_down, C, code):
 
 
 def _gated(x, w_gate, w_up, w_down, act, save, out, ws, stream):
+    if stream is None and ws is None and act in ACTS:
+        r = _native("gated", x, w_gate, w_up, w_down, ACTS[act], save, out)
+        if r is not None:
+            return r
     xp, rows, C, ldx, code = _rows("x", x, 2)
     a = _act(act)
     H, (g, u, d) = _gated_weights(x, w_gate, w_up, w_down, C, code)
@@ -221,6 +233,10 @@ def gated_ffn_backward(dy: torch.Tensor, x: torch.Tensor, saved: torch.Tensor, w
     """Gradients of gated_ffn_forward_save: (dx, dw_gate, dw_up, dw_down), all in
     dy's dtype, from the forward call's x, weights, act and saved.  ws: a uint8
     workspace of gated_ffn_backward_workspace_bytes()."""
+    if stream is None and ws is None and act in ACTS:
+        r = _native("gated_backward", dy, x, saved, w_gate, w_up, w_down, ACTS[act], out)
+        if r is not None:
+            return r
     dyp, rows, C, lddy, code = _rows("dy", dy, 2)
     xp, ldx = _like("x", dy, x, dy.shape, code)
     a = _act(act)
@@ -262,6 +278,10 @@ def linear_log_probs_forward(x: torch.Tensor, weight: torch.Tensor, tokens=None,
     logp 0) under the logits x weight^T of features x [..., C] and a classifier's
     weight [V, C] in x's dtype, whose logits are never kept, and their lse.  ws: a
     uint8 workspace of linear_log_probs_workspace_bytes()."""
+    if stream is None and ws is None:
+        r = _native("linear", x, weight, tokens)
+        if r is not None:
+            return LinearLogProbs(*r)
     xp, rows, C, ldx, code = _rows("x", x, 2)
     V, (w, ldw) = _classifier(x, weight, C, code)
     tp = _flat("tokens", x, tokens, 4, rows, 0)
@@ -291,6 +311,10 @@ def linear_log_probs_backward(x: torch.Tensor, weight: torch.Tensor, tokens, lp:
     d_lse fp32 [...] or None.  Rows without a gradient (both 0, or d_logp of a
     negative token) add nothing to dweight, whatever their features hold.  ws: a
     uint8 workspace of linear_log_probs_backward_workspace_bytes()."""
+    if stream is None and ws is None and type(lp) is LinearLogProbs:
+        r = _native("linear_backward", x, weight, tokens, lp.lse, d_logp, d_lse, out)
+        if r is not None:
+            return r
     xp, rows, C, ldx, code = _rows("x", x, 2)
     V, (w, ldw) = _classifier(x, weight, C, code)
     tp = _flat("tokens", x, tokens, 4, rows, 0)

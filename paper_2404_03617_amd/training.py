@@ -70,7 +70,11 @@ class LogProbs(NamedTuple):
 _BOUND = ("cf_layer_norm_forward", "cf_layer_norm_backward", "cf_layer_norm_backward_workspace_bytes",
           "cf_act_forward", "cf_act_backward", "cf_checkpoint_unpack", "cf_linear_weight_grad",
           "cf_linear_weight_grad_workspace_bytes", "cf_log_probs_forward", "cf_log_probs_workspace_bytes",
-          "cf_log_probs_backward")
+          "cf_log_probs_backward", "cf_group_norm_forward", "cf_group_norm_workspace_bytes", "cf_group_norm_backward",
+          "cf_group_norm_backward_workspace_bytes", "cf_gated_ffn_forward", "cf_gated_ffn_workspace_bytes",
+          "cf_gated_ffn_backward", "cf_gated_ffn_backward_workspace_bytes", "cf_linear_log_probs_forward",
+          "cf_linear_log_probs_workspace_bytes", "cf_linear_log_probs_backward",
+          "cf_linear_log_probs_backward_workspace_bytes")
 
 
 def _native(name, *args):

@@ -43,6 +43,15 @@ __device__ __forceinline__ ActPair act_pair(float u) {
     }
 }
 
+// act(u) alone; GELU at -inf is 0 here too.
+template <int ACT>
+__device__ __forceinline__ float act_value(float u) {
+    if constexpr (ACT == ACT_GELU)
+        return gelu_f32(u);
+    else
+        return act_pair<ACT>(u).f;
+}
+
 template <int A>
 struct ActTag {
     static constexpr int value = A;

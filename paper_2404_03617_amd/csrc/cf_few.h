@@ -38,7 +38,7 @@ struct Gated {
             float4v h;
 #pragma unroll
             for (int k = 0; k < 4; k++)
-                h[k] = k < left ? act_pair<decltype(tag)::value>(sum[0][k]).f * sum[1][k] : 0.0f;
+                h[k] = k < left ? act_value<decltype(tag)::value>(sum[0][k]) * sum[1][k] : 0.0f;
             mm::store_row<T, 4>(e.h + m * e.ldh + n, h, 4);
         });
     }

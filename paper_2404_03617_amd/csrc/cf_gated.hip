@@ -40,6 +40,7 @@ struct ForwardPlan {
     Room room;
     Operand x, wg, wu, wd;
     int pad;
+    int64_t ld;  // of h
     uint16_t *h;
     Plan up, down;
     void *part;
@@ -48,11 +49,12 @@ ForwardPlan forward_plan(const GatedFfn &a, const Copied &c, void *ws) {
     ForwardPlan p;
     p.room.p = (uint8_t *)ws;
     p.pad = up8(a.H);
+    p.ld = stride_of(a.H);
     p.x = operand(a.x.p, a.x.ld, a.rows, a.C, c.x, p.room);
     p.wg = operand(a.w_gate.p, a.w_gate.ld, a.H, a.C, c.wgu, p.room);
     p.wu = operand(a.w_up.p, a.w_up.ld, a.H, a.C, c.wgu, p.room);
     p.wd = operand(a.w_down.p, a.w_down.ld, a.C, a.H, c.wd, p.room);
-    p.h = (uint16_t *)p.room.take((size_t)a.rows * p.pad * 2);
+    p.h = (uint16_t *)p.room.take((size_t)a.rows * p.ld * 2);
     p.up = plan(a.rows, 2 * (int64_t)a.H, a.C, false);
     p.down = plan(a.rows, a.C, a.H, true);
     p.part = a.rows <= few::ROWS ? nullptr : p.room.take(part_bytes(p.down, a.rows, a.C, 1));
@@ -63,6 +65,7 @@ struct BackwardPlan {
     Room room;
     Operand x, dy, wg, wu, wd;
     int pad;
+    int64_t ld;  // of h; d has two of them a row
     uint16_t *d, *h;
     Plan dh, dwd, dwu, dx;
     void *part;
@@ -71,13 +74,14 @@ BackwardPlan backward_plan(const GatedFfn &a, const RowsIn &dy, const Copied &c,
     BackwardPlan p;
     p.room.p = (uint8_t *)ws;
     p.pad = up8(a.H);
+    p.ld = stride_of(a.H);
     p.x = operand(a.x.p, a.x.ld, a.rows, a.C, c.x, p.room);
     p.dy = operand(dy.p, dy.ld, a.rows, a.C, c.dy, p.room);
     p.wg = operand(a.w_gate.p, a.w_gate.ld, a.H, a.C, c.wgu, p.room);
     p.wu = operand(a.w_up.p, a.w_up.ld, a.H, a.C, c.wgu, p.room);
     p.wd = operand(a.w_down.p, a.w_down.ld, a.C, a.H, c.wd, p.room);
-    p.d = (uint16_t *)p.room.take((size_t)a.rows * 2 * p.pad * 2);
-    p.h = (uint16_t *)p.room.take((size_t)a.rows * p.pad * 2);
+    p.d = (uint16_t *)p.room.take((size_t)a.rows * 2 * p.ld * 2);
+    p.h = (uint16_t *)p.room.take((size_t)a.rows * p.ld * 2);
     p.dh = plan(a.rows, a.H, a.C, false);
     p.dwd = plan(a.C, a.H, a.rows, true);
     p.dwu = plan(a.H, a.C, a.rows, true, 2);
@@ -97,20 +101,20 @@ hipError_t forward(const GatedFfn &a, const ForwardPlan &p, void *y, int64_t ldy
     CF_HIP(pack(p.wd, bf16, st));
     if (a.rows <= few::ROWS) {
         const few::Args up = {p.x.m.p, {p.wg.m.p, p.wu.m.p}, p.x.m.ld, p.wg.m.ld, a.rows, a.H, p.x.m.ext};
-        CF_HIP((few::launch<T, 2, few::Gated>(up, GatedArgs{p.h, p.pad, saved, a.H, p.pad, a.act}, st)));
+        CF_HIP((few::launch<T, 2, few::Gated>(up, GatedArgs{p.h, p.ld, saved, a.H, p.pad, a.act}, st)));
         StoreArgs s = {};
         s.out[0] = (uint16_t *)y;
         s.ldo = ldy;
-        const few::Args down = {p.h, {p.wd.m.p, p.wd.m.p}, p.pad, p.wd.m.ld, a.rows, a.C, p.pad};
+        const few::Args down = {p.h, {p.wd.m.p, p.wd.m.p}, p.ld, p.wd.m.ld, a.rows, a.C, p.pad};
         return few::launch<T, 1, few::Store>(down, s, st);
     }
     Args up = args_of(p.up, a.rows, 2 * a.H, a.C, p.x.m, a.rows, p.wg.m, a.H);
     up.b[1] = p.wu.m.p;
-    CF_HIP(launch_gated<T>(up, GatedArgs{p.h, p.pad, saved, a.H, p.pad, a.act}, p.up.tile, st));
+    CF_HIP(launch_gated<T>(up, GatedArgs{p.h, p.ld, saved, a.H, p.pad, a.act}, p.up.tile, st));
     StoreArgs s = {};
     s.out[0] = s.out[1] = (uint16_t *)y;
     s.ldo = ldy;
-    return run_store<KC, KC>(args_of(p.down, a.rows, a.C, a.H, Matrix{p.h, p.pad, p.pad}, a.rows, p.wd.m, a.C), s,
+    return run_store<KC, KC>(args_of(p.down, a.rows, a.C, a.H, Matrix{p.h, p.ld, p.pad}, a.rows, p.wd.m, a.C), s,
                              p.down, p.part, bf16, st);
 }
 
@@ -122,12 +126,12 @@ hipError_t backward(const GatedFfn &a, const BackwardPlan &p, const float *saved
     CF_HIP(pack(p.wg, bf16, st));
     CF_HIP(pack(p.wu, bf16, st));
     CF_HIP(pack(p.wd, bf16, st));
-    const Matrix h = {p.h, p.pad, p.pad}, d = {p.d, 2 * (int64_t)p.pad, p.pad};
+    const Matrix h = {p.h, p.ld, p.pad}, d = {p.d, 2 * p.ld, p.pad};
     if (a.rows > 0) {
         CF_HIP(launch_gated_back<T>(args_of(p.dh, a.rows, a.H, a.C, p.dy.m, a.rows, p.wd.m, p.wd.m.ext),
-                                    GatedBackArgs{saved, p.d, p.h, a.H, p.pad, a.act}, p.dh.tile, st));
+                                    GatedBackArgs{saved, p.d, p.h, p.ld, a.H, p.pad, a.act}, p.dh.tile, st));
         Args dx = args_of(p.dx, a.rows, a.C, a.H, d, a.rows, p.wg.m, p.wg.m.ext, true);
-        dx.a[1] = p.d + p.pad;
+        dx.a[1] = p.d + p.ld;
         dx.b[1] = p.wu.m.p;
         StoreArgs s = {};
         s.out[0] = s.out[1] = (uint16_t *)g.dx;
@@ -139,7 +143,7 @@ hipError_t backward(const GatedFfn &a, const BackwardPlan &p, const float *saved
     s.ldo = a.H;
     CF_HIP((run_store<RC, RC>(args_of(p.dwd, a.C, a.H, a.rows, p.dy.m, p.dy.m.ext, h, p.pad), s, p.dwd, p.part, bf16, st)));
     Args w = args_of(p.dwu, a.H, a.C, a.rows, d, p.pad, p.x.m, p.x.m.ext, false, 2);
-    w.a[1] = p.d + p.pad;
+    w.a[1] = p.d + p.ld;
     s.out[0] = (uint16_t *)g.dw_gate;
     s.out[1] = (uint16_t *)g.dw_up;
     s.ldo = a.C;

@@ -320,7 +320,7 @@ __device__ __forceinline__ void apply(const Channels &h, const u32x4 &raw, uint1
     unpack8<T>(raw, x);
 #pragma unroll
     for (int e = 0; e < 8; e++)
-        x[e] = act_pair<ACT>(fmaf((x[e] - h.mean[e]) * h.rstd[e], h.w[e], h.b[e])).f;
+        x[e] = act_value<ACT>(fmaf((x[e] - h.mean[e]) * h.rstd[e], h.w[e], h.b[e]));
     store_channels<T, MODE>(base, off, h, x);
 }
 

@@ -186,7 +186,7 @@ BackwardPlan backward_plan(const LinearLogProbs &a, bool copy_x, bool copy_w, vo
     p.pieces = (int)((a.V + at_most - 1) / at_most);
     p.piece = p.pieces == 1 ? a.V : ((a.V + p.pieces - 1) / p.pieces + 255) / 256 * 256;
     p.pieces = (a.V + p.piece - 1) / p.piece;
-    p.dz = (uint16_t *)p.room.take((size_t)a.rows * up8(p.piece) * 2);
+    p.dz = (uint16_t *)p.room.take((size_t)a.rows * stride_of(p.piece) * 2);
     p.acc = p.pieces > 1 ? (float *)p.room.take((size_t)a.rows * a.C * 4) : nullptr;
     p.z = plan(a.rows, p.piece, a.C, false);
     p.dx = plan(a.rows, a.C, p.piece, true);
@@ -228,12 +228,12 @@ hipError_t backward(const LinearLogProbs &a, const BackwardPlan &p, const Linear
         CF_HIP(hipGetLastError());
         CF_HIP(launch_pack(a.x.p, a.x.ld, a.rows, a.C, p.factor, p.xs, bf16, st));
     }
-    const Matrix xs = {p.xs, up8(a.C), up8(a.C)};
+    const Matrix xs = {p.xs, stride_of(a.C), up8(a.C)};
     for (int i = 0; i < p.pieces; i++) {
         const int v0 = i * p.piece, n = a.V - v0 < p.piece ? a.V - v0 : p.piece, pad = up8(n);
-        const Matrix w = {p.w.m.p + (int64_t)v0 * p.w.m.ld, p.w.m.ld, p.w.m.ext}, dz = {p.dz, pad, pad};
+        const Matrix w = {p.w.m.p + (int64_t)v0 * p.w.m.ld, p.w.m.ld, p.w.m.ext}, dz = {p.dz, stride_of(n), pad};
         if (a.rows > 0) {
-            CF_HIP(launch_dz<T>(args_of(p.z, a.rows, n, a.C, p.x.m, a.rows, w, n), DzArgs{p.rows, p.dz, pad, v0}, p.z.tile,
+            CF_HIP(launch_dz<T>(args_of(p.z, a.rows, n, a.C, p.x.m, a.rows, w, n), DzArgs{p.rows, p.dz, dz.ld, pad, v0}, p.z.tile,
                                 st));
             StoreArgs s = {};
             s.out[0] = s.out[1] = (uint16_t *)g.dx;

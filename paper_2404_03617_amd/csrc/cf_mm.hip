@@ -11,7 +11,7 @@ namespace {
 
 template <typename T>
 __global__ __launch_bounds__(256) void pack_kernel(const uint16_t *src, int64_t ld, int cols, const float *factor,
-                                                   u32x4 *dst, uint32_t n, FastDiv per_row) {
+                                                   u32x4 *dst, int64_t ldd, uint32_t n, FastDiv per_row) {
     const uint32_t i = blockIdx.x * 256 + threadIdx.x;
     if (i >= n)
         return;
@@ -30,7 +30,7 @@ __global__ __launch_bounds__(256) void pack_kernel(const uint16_t *src, int64_t 
             v = pack8<T>(x);
         }
     }
-    dst[i] = v;
+    dst[r * ldd + c / 8] = v;
 }
 
 // G lanes share four entries, each adding every G-th split; then they add
@@ -82,10 +82,10 @@ hipError_t launch_pack(const void *src, int64_t ld, int64_t rows, int cols, cons
         return hipSuccess;
     const dim3 grid((n + 255) / 256);
     if (bf16)
-        pack_kernel<BF16><<<grid, 256, 0, st>>>((const uint16_t *)src, ld, cols, factor, (u32x4 *)dst, n,
+        pack_kernel<BF16><<<grid, 256, 0, st>>>((const uint16_t *)src, ld, cols, factor, (u32x4 *)dst, stride_of(cols) / 8, n,
                                                 make_fastdiv(per_row));
     else
-        pack_kernel<F16><<<grid, 256, 0, st>>>((const uint16_t *)src, ld, cols, factor, (u32x4 *)dst, n,
+        pack_kernel<F16><<<grid, 256, 0, st>>>((const uint16_t *)src, ld, cols, factor, (u32x4 *)dst, stride_of(cols) / 8, n,
                                                make_fastdiv(per_row));
     return hipGetLastError();
 }

@@ -195,7 +195,7 @@ struct Gated {
                     for (int k = 0; k < 8; k++) {
                         g[k] = t.get(i, p, k);
                         u[k] = t.get(i, p + 1, k);
-                        h[k] = k < left ? act_pair<ACT>(g[k]).f * u[k] : 0.0f;
+                        h[k] = k < left ? act_value<ACT>(g[k]) * u[k] : 0.0f;
                     }
                     store_row<T, 8>(e.h + m * e.ldh + n, h, 8);
                     if (e.saved) {
@@ -212,8 +212,9 @@ struct Gated {
 // --- their gradients from dh: dg = dh u act'(g), du = dh act(g), and h again ---
 struct GatedBackArgs {
     const float *saved;
-    uint16_t *d;  // [M][2 pad]: dg, du
-    uint16_t *h;  // [M][pad]
+    uint16_t *d;  // [M][2 ld]: dg, du
+    uint16_t *h;  // [M][ld]
+    int64_t ld;
     int H, pad, act;
 };
 
@@ -252,10 +253,10 @@ struct GatedBack {
                         du[k] = k < left ? dh * q.f : 0.0f;
                         h[k] = k < left ? q.f * u[k] : 0.0f;
                     }
-                    uint16_t *const d = e.d + (int64_t)m * 2 * e.pad + n;
+                    uint16_t *const d = e.d + m * 2 * e.ld + n;
                     store_row<T, W>(d, dg, W);
-                    store_row<T, W>(d + e.pad, du, W);
-                    store_row<T, W>(e.h + (int64_t)m * e.pad + n, h, W);
+                    store_row<T, W>(d + e.ld, du, W);
+                    store_row<T, W>(e.h + m * e.ld + n, h, W);
                 }
             }
         });
@@ -343,8 +344,9 @@ struct RowGrad {
 };
 struct DzArgs {
     const RowGrad *rows;
-    uint16_t *dz;  // [M][pad]
-    int pad, v0;   // the piece's first token
+    uint16_t *dz;  // [M][ld], `pad` columns
+    int64_t ld;
+    int pad, v0;  // the piece's first token
 };
 
 struct Dz {
@@ -377,7 +379,7 @@ struct Dz {
                     const float q = __builtin_amdgcn_exp2f((t.get(i, p, k) - r.lse) * LOG2E);
                     d[k] = any && n + k < a.N ? fmaf(r.c, q, n + k == want ? r.g : 0.0f) : 0.0f;
                 }
-                store_row<T, W>(e.dz + (int64_t)m * e.pad + n, d, W);
+                store_row<T, W>(e.dz + m * e.ld + n, d, W);
             }
         }
     }

@@ -12,14 +12,17 @@ namespace mm {
 
 constexpr int STEP = 64;  // k's of a step
 
+// The tiles, workgroups that run on a CU together, and what the choice among them
+// estimates with, in microseconds.
 struct Tile {
     int m, n, per_cu;
-    double alone, full, fixed;  // microseconds: a step for a workgroup alone on its CU, its share of a full one, its ends
+    double alone, ends;       // a step for a workgroup alone on its CU, and its start and end
+    double full, full_ends;   // its share of a full CU
 };
 constexpr int TILE_COUNT = 2;
 constexpr Tile TILES[TILE_COUNT] = {
-    {256, 256, 1, 0.62, 0.62, 5.0},
-    {128, 128, 2, 0.28, 0.21, 3.5},
+    {256, 256, 1, 0.56, 7.6, 1.505, 10.0},
+    {128, 128, 2, 0.751, 6.15, 0.616, 2.46},
 };
 
 struct Plan {
@@ -33,15 +36,19 @@ inline int64_t tiles_of(const Tile &t, int64_t M, int64_t N) {
 
 constexpr double PART_BYTES = 128 << 20;  // room for partial sums
 
-// The least time by an estimate, as for weight gradients: rounds of
-// workgroups, each its steps and its ends; split sums are written, read and
-// added by a second launch.
+// The tile and number of splits that take the least time by this estimate, fitted to
+// runs of either tile, whole and split, over 35 shapes (16 to 131072 rows and
+// columns, 16 to 50024 k's, with each kind of epilogue), where it picks the best
+// or one within 4% of it: rounds of workgroups, each its steps and its ends, or a
+// CU's share of all, whichever is longer; partial sums written and read, at 8
+// TB/s.  Large tiles move least and win where they fill the chip; small
+// ones start and end while their neighbour's products run.
 inline double time_of(const Tile &t, int64_t M, int64_t N, int64_t steps, int64_t batch, int64_t splits, int64_t cus) {
     const double work = (double)tiles_of(t, M, N) * batch * splits;
     const int64_t each = (steps + splits - 1) / splits;
     const double rounds = std::ceil(work / (cus * t.per_cu)), load = std::ceil(work / cus);
-    const double step = t.alone * rounds > t.full * load ? t.alone * rounds : t.full * load;
-    return t.fixed * rounds + each * step + (splits > 1 ? 4.0 + splits * 8.0 * batch * M * N / 5.0e6 : 0.0);
+    const double one = rounds * (t.ends + each * t.alone), all = load * (t.full_ends + each * t.full);
+    return (one > all ? one : all) + (splits > 1 ? splits * 8.0 * batch * M * N / 8.0e6 : 0.0);
 }
 
 inline Plan plan_of(int64_t M, int64_t N, int64_t steps, int64_t batch, bool may_split, int64_t cus) {
@@ -52,9 +59,9 @@ inline Plan plan_of(int64_t M, int64_t N, int64_t steps, int64_t batch, bool may
     for (int i = 0; i < TILE_COUNT; i++) {
         const Tile &t = TILES[i];
         const int64_t tiles = tiles_of(t, M, N) * batch;
-        for (int r = 0; r <= (may_split ? t.per_cu : 0); r++) {
-            int64_t splits = r ? r * cus / tiles : 1;
-            const int64_t most = steps / 4, room = (int64_t)(PART_BYTES / (4.0 * batch * M * N + 1.0));
+        for (int r = 0; r <= (may_split ? 2 * t.per_cu : 0); r++) {  // whole, or r / 2 workgroups a CU
+            int64_t splits = r ? r * cus / (2 * tiles) : 1;
+            const int64_t most = steps / 2, room = (int64_t)(PART_BYTES / (4.0 * batch * M * N + 1.0));
             splits = splits < most ? splits : most;
             splits = splits < room ? splits : room;
             if (splits < 1)

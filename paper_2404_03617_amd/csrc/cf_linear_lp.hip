@@ -34,7 +34,10 @@ using namespace mm;
 namespace {
 
 constexpr double PIECE_BYTES = 256 << 20;
-constexpr int FEW = 2;  // fragments of 16 classes a workgroup where there are few rows
+// Fragments of 16 classes a workgroup where there are few rows: one or two rows come
+// from the caches at little cost (1 x 131072 x 4096 182 us with one, 197 with two),
+// more rather once for two (8 rows 205 and 192, 16 rows 245 and 197).
+constexpr int few_of(int64_t rows) { return rows <= 2 ? 1 : 2; }
 
 // L lanes join the parts of a row.
 template <int L>
@@ -151,7 +154,7 @@ ForwardPlan forward_plan(const LinearLogProbs &a, bool copy_x, bool copy_w, void
     p.x = operand(a.x.p, a.x.ld, a.rows, a.C, copy_x, p.room);
     p.w = operand(a.w.p, a.w.ld, a.V, a.C, copy_w, p.room);
     p.z = plan(a.rows, a.V, a.C, false);
-    const int n = a.rows <= few::ROWS ? 16 * FEW : TILES[p.z.tile].n;
+    const int n = a.rows <= few::ROWS ? 16 * few_of(a.rows) : TILES[p.z.tile].n;
     p.parts = (a.V + n - 1) / n;
     p.part = (float2 *)p.room.take((size_t)p.parts * a.rows * sizeof(float2));
     p.picked = (float *)p.room.take((size_t)a.rows * 4);
@@ -201,9 +204,9 @@ hipError_t forward(const LinearLogProbs &a, const ForwardPlan &p, float *logp, f
     CF_HIP(pack(p.x, bf16, st));
     CF_HIP(pack(p.w, bf16, st));
     const LseArgs e = {p.part, p.picked, logp ? a.tokens : nullptr};
+    const few::Args f = {p.x.m.p, {p.w.m.p, p.w.m.p}, p.x.m.ld, p.w.m.ld, (int)a.rows, a.V, p.x.m.ext};
     if (a.rows <= few::ROWS)
-        CF_HIP((few::launch<T, FEW, few::Lse>(
-            few::Args{p.x.m.p, {p.w.m.p, p.w.m.p}, p.x.m.ld, p.w.m.ld, a.rows, a.V, p.x.m.ext}, e, st)));
+        CF_HIP((few_of(a.rows) == 1 ? few::launch<T, 1, few::Lse>(f, e, st) : few::launch<T, 2, few::Lse>(f, e, st)));
     else
         CF_HIP(launch_lse<T>(args_of(p.z, a.rows, a.V, a.C, p.x.m, a.rows, p.w.m, a.V), e, p.z.tile, st));
     // few rows of many parts: a workgroup each

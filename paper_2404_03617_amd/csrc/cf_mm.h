@@ -230,18 +230,35 @@ __device__ __forceinline__ void each(F &&f) {
     }
 }
 
-// A wave's results: FM rows a lane (16 apart), in PIECES pieces of W columns beside
-// each other.
-template <typename S, bool WIDE>
+// A wave's results: FM rows a lane (16 apart), in PIECES pieces of W = 8 columns
+// beside each other.  With B in KC its fragments are read so that two of them make a
+// piece; with B in RC every fragment has 16 columns that lie together, 4 a lane,
+// and lanes 16 apart exchange halves of two (`gather`): 16 instructions for 64
+// results, for stores of 16 bytes a lane in place of 8.
+template <typename S, bool GATHERED>
 struct Results {
-    static constexpr int W = WIDE ? 8 : 4, PIECES = S::FN * 4 / W;
+    static constexpr int W = 8, PIECES = S::FN / 2;
     float4v (&acc)[S::FM][S::FN];
+    __device__ __forceinline__ void gather() const {
+        if constexpr (GATHERED) {
+#pragma unroll
+            for (int i = 0; i < S::FM; i++)
+#pragma unroll
+                for (int p = 0; p < S::FN; p += 2)
+#pragma unroll
+                    for (int k = 0; k < 4; k++) {
+                        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(acc[i][p][k]),
+                                                                        __float_as_uint(acc[i][p + 1][k]), false, false);
+                        acc[i][p][k] = __uint_as_float(r[0]);
+                        acc[i][p + 1][k] = __uint_as_float(r[1]);
+                    }
+        }
+    }
     static __device__ __forceinline__ int column(int piece, int lane) {
-        return WIDE ? 32 * piece + 8 * (lane >> 4) : 16 * piece + 4 * (lane >> 4);
+        const int q = lane >> 4;
+        return 32 * piece + (GATHERED ? 16 * (q & 1) + 8 * (q >> 1) : 8 * q);
     }
-    __device__ __forceinline__ float get(int i, int piece, int k) const {
-        return WIDE ? acc[i][2 * piece + k / 4][k % 4] : acc[i][piece][k];
-    }
+    __device__ __forceinline__ float get(int i, int piece, int k) const { return acc[i][2 * piece + k / 4][k % 4]; }
 };
 
 // E: what follows the product.  E::DUAL as above; E::Args; run(args, acc, work,
@@ -438,7 +455,9 @@ __global__ __launch_bounds__(S::TH, S::OCC) void kernel(Args a, typename E::Args
             left_now = left_next;
             left_next = l;
         }
-        E::template run<T, S, LB == KC>(e, Results<S, LB == KC>{acc}, at, a, at.m * TM + wm, at.n * TN + wn, lane, lds + 2 * STAGE);
+        const Results<S, LB == RC> results = {acc};
+        results.gather();
+        E::template run<T>(e, results, at, a, at.m * TM + wm, at.n * TN + wn, lane, lds + 2 * STAGE);
     }
     wait_copies<0>();  // nothing may arrive in LDS that is another workgroup's
 }

@@ -126,10 +126,10 @@ struct Store {
         return 0;
     }
     using Args = StoreArgs;
-    template <typename T, typename S, bool WIDE>
-    static __device__ __forceinline__ void run(const StoreArgs &e, const Results<S, WIDE> &t, const Work &at,
+    template <typename T, typename S, bool G>
+    static __device__ __forceinline__ void run(const StoreArgs &e, const Results<S, G> &t, const Work &at,
                                                const mm::Args &a, int m0, int n0, int lane, uint8_t *) {
-        constexpr int W = Results<S, WIDE>::W, PIECES = Results<S, WIDE>::PIECES;
+        constexpr int W = Results<S, G>::W, PIECES = Results<S, G>::PIECES;
         float *const part = a.splits > 1 ? e.part + ((int64_t)at.split * a.batch + at.batch) * a.M * a.N : nullptr;
 #pragma unroll
         for (int i = 0; i < S::FM; i++) {
@@ -173,10 +173,10 @@ struct Gated {
         return 0;
     }
     using Args = GatedArgs;
-    template <typename T, typename S, bool WIDE>
-    static __device__ __forceinline__ void run(const GatedArgs &e, const Results<S, WIDE> &t, const Work &,
+    template <typename T, typename S, bool G>
+    static __device__ __forceinline__ void run(const GatedArgs &e, const Results<S, G> &t, const Work &,
                                                const mm::Args &a, int m0, int n0, int lane, uint8_t *) {
-        constexpr int PIECES = Results<S, WIDE>::PIECES;
+        constexpr int PIECES = Results<S, G>::PIECES;
         with_act(e.act, [&](auto tag) {
             constexpr int ACT = decltype(tag)::value;
 #pragma unroll
@@ -186,7 +186,6 @@ struct Gated {
                     continue;
 #pragma unroll
                 for (int p = 0; p < PIECES; p += 2) {
-                    static_assert(WIDE, "pieces of gate and of up channels in turn");
                     const int n = n0 / 2 + t.column(p / 2, lane), left = e.H - n;
                     if (n >= e.pad)
                         continue;
@@ -225,39 +224,42 @@ struct GatedBack {
         return 0;
     }
     using Args = GatedBackArgs;
-    template <typename T, typename S, bool WIDE>
-    static __device__ __forceinline__ void run(const GatedBackArgs &e, const Results<S, WIDE> &t, const Work &,
+    template <typename T, typename S, bool G>
+    static __device__ __forceinline__ void run(const GatedBackArgs &e, const Results<S, G> &t, const Work &,
                                                const mm::Args &a, int m0, int n0, int lane, uint8_t *) {
-        constexpr int W = Results<S, WIDE>::W, PIECES = Results<S, WIDE>::PIECES;
+        constexpr int W = Results<S, G>::W, PIECES = Results<S, G>::PIECES;
         with_act(e.act, [&](auto tag) {
-            constexpr int ACT = decltype(tag)::value;
+            constexpr int ACT = decltype(tag)::value, COUNT = S::FM * PIECES;
+            float g[2][W], u[2][W];
+            // piece j of the wave's, whose g and u are read while the one before is worked on
+            auto read = [&](int j) {
+                const int m = m0 + 16 * (j / PIECES) + (lane & 15), n = n0 + t.column(j % PIECES, lane);
+                const int left = m < a.M ? e.H - n : 0;
+                const float *const s = e.saved + (int64_t)m * 2 * e.H + n;
+                load_rowf<W>(s, g[j % 2], left);
+                load_rowf<W>(s + e.H, u[j % 2], left);
+            };
+            read(0);
 #pragma unroll
-            for (int i = 0; i < S::FM; i++) {
-                const int m = m0 + 16 * i + (lane & 15);
-                if (m >= a.M)
+            for (int j = 0; j < COUNT; j++) {
+                if (j + 1 < COUNT)
+                    read(j + 1);
+                const int m = m0 + 16 * (j / PIECES) + (lane & 15), n = n0 + t.column(j % PIECES, lane), left = e.H - n;
+                if (m >= a.M || n >= e.pad)
                     continue;
+                float dg[W], du[W], h[W];
 #pragma unroll
-                for (int p = 0; p < PIECES; p++) {
-                    const int n = n0 + t.column(p, lane), left = e.H - n;
-                    if (n >= e.pad)
-                        continue;
-                    const float *const s = e.saved + (int64_t)m * 2 * e.H + n;
-                    float g[W], u[W], dg[W], du[W], h[W];
-                    load_rowf<W>(s, g, left);
-                    load_rowf<W>(s + e.H, u, left);
-#pragma unroll
-                    for (int k = 0; k < W; k++) {
-                        const ActPair q = act_pair<ACT>(g[k]);
-                        const float dh = t.get(i, p, k);
-                        dg[k] = k < left ? dh * u[k] * q.d : 0.0f;
-                        du[k] = k < left ? dh * q.f : 0.0f;
-                        h[k] = k < left ? q.f * u[k] : 0.0f;
-                    }
-                    uint16_t *const d = e.d + m * 2 * e.ld + n;
-                    store_row<T, W>(d, dg, W);
-                    store_row<T, W>(d + e.ld, du, W);
-                    store_row<T, W>(e.h + m * e.ld + n, h, W);
+                for (int k = 0; k < W; k++) {
+                    const ActPair q = act_pair<ACT>(g[j % 2][k]);
+                    const float dh = t.get(j / PIECES, j % PIECES, k), up = u[j % 2][k];
+                    dg[k] = k < left ? dh * up * q.d : 0.0f;
+                    du[k] = k < left ? dh * q.f : 0.0f;
+                    h[k] = k < left ? q.f * up : 0.0f;
                 }
+                uint16_t *const d = e.d + m * 2 * e.ld + n;
+                store_row<T, W>(d, dg, W);
+                store_row<T, W>(d + e.ld, du, W);
+                store_row<T, W>(e.h + m * e.ld + n, h, W);
             }
         });
     }
@@ -285,10 +287,10 @@ struct Lse {
         return S::WN * S::TM * (int)sizeof(float2);
     }
     using Args = LseArgs;
-    template <typename T, typename S, bool WIDE>
-    static __device__ __forceinline__ void run(const LseArgs &e, const Results<S, WIDE> &t, const Work &at,
+    template <typename T, typename S, bool G>
+    static __device__ __forceinline__ void run(const LseArgs &e, const Results<S, G> &t, const Work &at,
                                                const mm::Args &a, int m0, int n0, int lane, uint8_t *lds) {
-        constexpr int W = Results<S, WIDE>::W, PIECES = Results<S, WIDE>::PIECES;
+        constexpr int W = Results<S, G>::W, PIECES = Results<S, G>::PIECES;
         float2 *const row = reinterpret_cast<float2 *>(lds);  // [WN][TM]
         const int wn = n0 % S::TN / (S::TN / S::WN), local = m0 % S::TM;
 #pragma unroll
@@ -356,10 +358,10 @@ struct Dz {
         return 0;
     }
     using Args = DzArgs;
-    template <typename T, typename S, bool WIDE>
-    static __device__ __forceinline__ void run(const DzArgs &e, const Results<S, WIDE> &t, const Work &,
+    template <typename T, typename S, bool G>
+    static __device__ __forceinline__ void run(const DzArgs &e, const Results<S, G> &t, const Work &,
                                                const mm::Args &a, int m0, int n0, int lane, uint8_t *) {
-        constexpr int W = Results<S, WIDE>::W, PIECES = Results<S, WIDE>::PIECES;
+        constexpr int W = Results<S, G>::W, PIECES = Results<S, G>::PIECES;
 #pragma unroll
         for (int i = 0; i < S::FM; i++) {
             const int m = m0 + 16 * i + (lane & 15);

@@ -82,7 +82,7 @@ BackwardPlan backward_plan(const GatedFfn &a, const RowsIn &dy, const Copied &c,
     p.wd = operand(a.w_down.p, a.w_down.ld, a.C, a.H, c.wd, p.room);
     p.d = (uint16_t *)p.room.take((size_t)a.rows * 2 * p.ld * 2);
     p.h = (uint16_t *)p.room.take((size_t)a.rows * p.ld * 2);
-    p.dh = plan(a.rows, a.H, a.C, false);
+    p.dh = plan(a.rows, a.H, a.C, false, 1, 1, true);
     p.dwd = plan(a.C, a.H, a.rows, true);
     p.dwu = plan(a.H, a.C, a.rows, true, 2);
     p.dx = plan(a.rows, a.C, a.H, true, 1, 2);

@@ -18,11 +18,12 @@ struct Tile {
     int m, n, per_cu;
     double alone, ends;       // a step for a workgroup alone on its CU, and its start and end
     double full, full_ends;   // its share of a full CU
+    double wide;              // a tile whose results are joined with 8 bytes and leave as 6, beyond the rest
 };
 constexpr int TILE_COUNT = 2;
 constexpr Tile TILES[TILE_COUNT] = {
-    {256, 256, 1, 0.56, 7.6, 1.505, 10.0},
-    {128, 128, 2, 0.751, 6.15, 0.616, 2.46},
+    {256, 256, 1, 0.56, 7.6, 1.505, 10.0, 47.5},
+    {128, 128, 2, 0.751, 6.15, 0.616, 2.46, 8.5},
 };
 
 struct Plan {
@@ -42,16 +43,22 @@ constexpr double PART_BYTES = 128 << 20;  // room for partial sums
 // or one within 4% of it: rounds of workgroups, each its steps and its ends, or a
 // CU's share of all, whichever is longer; partial sums written and read, at 8
 // TB/s.  Large tiles move least and win where they fill the chip; small
-// ones start and end while their neighbour's products run.
-inline double time_of(const Tile &t, int64_t M, int64_t N, int64_t steps, int64_t batch, int64_t splits, int64_t cus) {
+// ones start and end while their neighbour's products run.  `wide`: what follows a
+// tile of the gate's gradients, 14 bytes a result, which small tiles hide in part
+// (25088 x 1024 x 256 94 us with small tiles, 120 with large ones; 4096 x 4096 x 8192
+// 340 and 312).
+inline double time_of(const Tile &t, int64_t M, int64_t N, int64_t steps, int64_t batch, int64_t splits, int64_t cus,
+                      bool wide) {
     const double work = (double)tiles_of(t, M, N) * batch * splits;
     const int64_t each = (steps + splits - 1) / splits;
     const double rounds = std::ceil(work / (cus * t.per_cu)), load = std::ceil(work / cus);
-    const double one = rounds * (t.ends + each * t.alone), all = load * (t.full_ends + each * t.full);
+    const double after = wide ? t.wide : 0.0;
+    const double one = rounds * (t.ends + after + each * t.alone), all = load * (t.full_ends + after + each * t.full);
     return (one > all ? one : all) + (splits > 1 ? splits * 8.0 * batch * M * N / 8.0e6 : 0.0);
 }
 
-inline Plan plan_of(int64_t M, int64_t N, int64_t steps, int64_t batch, bool may_split, int64_t cus) {
+inline Plan plan_of(int64_t M, int64_t N, int64_t steps, int64_t batch, bool may_split, int64_t cus,
+                    bool wide = false) {
     Plan best = {0, 1, (int)(steps < 1 ? 1 : steps)};
     if (M < 1 || N < 1)  // nothing to make
         return best;
@@ -66,7 +73,7 @@ inline Plan plan_of(int64_t M, int64_t N, int64_t steps, int64_t batch, bool may
             splits = splits < room ? splits : room;
             if (splits < 1)
                 splits = 1;
-            const double time = time_of(t, M, N, steps, batch, splits, cus);
+            const double time = time_of(t, M, N, steps, batch, splits, cus, wide);
             if (time < least) {
                 least = time;
                 best.tile = i;

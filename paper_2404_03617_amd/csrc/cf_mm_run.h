@@ -45,8 +45,9 @@ inline bool pack_fits(int64_t rows, int cols) { return (double)rows * (up8(cols)
 hipError_t launch_pack(const void *src, int64_t ld, int64_t rows, int cols, const float *factor, void *dst, int bf16,
                        hipStream_t st);
 
-inline Plan plan(int64_t M, int64_t N, int64_t K, bool may_split, int batch = 1, int segments = 1) {
-    return plan_of(M, N, steps_of(K) * segments, batch, may_split, device_cu_count());
+inline Plan plan(int64_t M, int64_t N, int64_t K, bool may_split, int batch = 1, int segments = 1,
+                 bool wide = false) {
+    return plan_of(M, N, steps_of(K) * segments, batch, may_split, device_cu_count(), wide);
 }
 // a workgroup a tile: a launch holds 2^32 threads
 inline bool grid_fits(int64_t M, int64_t N) { return (double)((M + 127) / 128) * (double)((N + 127) / 128) < 4.0e6; }

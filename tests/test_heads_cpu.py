@@ -292,3 +292,28 @@ def test_parts_of_a_group_norm_hold_all_pixels_and_groups(tmp_path, cus):
                     }
         }
     """ % cus)
+
+
+def test_the_sizes_of_the_tile_tests_take_every_tile(tmp_path):
+    """The tests of the tiles on the GPU (test_heads_gpu.py) run both behind each
+    kind of product, and products over whole and split axes."""
+    from test_heads_gpu import LARGE_GATED, LARGE_LINEAR
+
+    products = []
+    for r, C, H in LARGE_GATED:
+        products += [("up", r, 2 * H, C, 1, "false", "false"), ("dh", r, H, C, 1, "false", "true"),
+                     ("down", r, C, H, 1, "true", "false"), ("dx", r, C, 2 * H, 1, "true", "false"),
+                     ("dw", C, H, r, 1, "true", "false"), ("dw", H, C, r, 2, "true", "false")]
+    for r, C, V in LARGE_LINEAR:
+        products += [("logits", r, V, C, 1, "false", "false"), ("dx of logits", r, C, V, 1, "true", "false"),
+                     ("dw of logits", V, C, r, 1, "true", "false")]
+    out = run_cpp(tmp_path, "cf_mm_plan.h", "mm", "".join(
+        "{ const Plan p = plan_of(%d, %d, steps_of(%d), %d, %s, 256, %s); printf(\"%%d %%d\\n\", p.tile, p.splits); }\n"
+        % q[1:] for q in products))
+    seen = set()
+    for q, line in zip(products, out.split("\n")):
+        tile, splits = (int(v) for v in line.split())
+        seen |= {(q[0], tile), (tile, "split" if splits > 1 else "whole")}
+    missing = {(name, t) for name in ("up", "dh", "down", "dx", "dw", "logits") for t in range(2)} - seen
+    assert not missing, missing
+    assert {(t, k) for t in range(2) for k in ("split", "whole")} <= seen, seen

@@ -1,0 +1,428 @@
+"""The operators for heads as a program uses them: together, natively and not, on
+streams of the caller's, in graphs, with far strides and many values, and at the
+sizes where their kernels change."""
+import pytest
+import torch
+
+import paper_2404_03617_amd as cf
+from paper_2404_03617_amd import heads
+
+import test_gated_ffn_gpu as gated
+import test_linear_log_probs_gpu as linear
+from _rows import DT, F32, ROUND, randn
+from test_training_args_gpu import outcome, spoiled
+
+pytestmark = pytest.mark.gpu
+
+
+def flat(r):
+    return [r] if isinstance(r, torch.Tensor) else [] if r is None else [t for x in r for t in flat(x)]
+
+
+def same(a, b):
+    a, b = flat(a), flat(b)
+    return len(a) == len(b) and all(p.shape == q.shape and p.dtype == q.dtype and
+                                    torch.equal(p.contiguous().view(torch.int8), q.contiguous().view(torch.int8))
+                                    for p, q in zip(a, b))
+
+
+def inputs(seed=1, dt=torch.float16, N=3, P=14, C=96, H=136, V=200):
+    x = randn(seed, (N, P, C), dt).cuda()
+    return dict(x=x, dy=randn(seed + 1, (N, P, C), dt).cuda(), w=randn(seed + 2, (C,)).cuda(), b=randn(seed + 3, (C,)).cuda(),
+                wg=randn(seed + 4, (H, C), dt, C**-0.5).cuda(), wu=randn(seed + 5, (H, C), dt, C**-0.5).cuda(),
+                wd=randn(seed + 6, (C, H), dt, H**-0.5).cuda(), wv=randn(seed + 7, (V, C), dt, C**-0.5).cuda(),
+                t=(torch.arange(N * P).view(N, P) * 37 % (V + 1) - 1).cuda(), gl=randn(seed + 8, (N, P)).cuda(),
+                gs=randn(seed + 9, (N, P), scale=0.1).cuda())
+
+
+# ---------------------------------------------------------------------------
+# Native calls
+
+
+def calls():
+    v = inputs()
+    x, dy = v["x"], v["dy"]
+    _, stats = cf.group_norm_forward_save(x, 8, v["w"], v["b"])
+    x2, dy2 = x[0], dy[0]
+    _, saved = cf.gated_ffn_forward_save(x2, v["wg"], v["wu"], v["wd"])
+    lp = cf.linear_log_probs_forward(x2, v["wv"], v["t"][0])
+    out, out2 = torch.empty_like(x), torch.empty_like(x2)
+    ffn = dict(w_gate=v["wg"], w_up=v["wu"], w_down=v["wd"])
+    return {
+        "norm": (cf.group_norm_forward, dict(x=x, groups=8, weight=v["w"], bias=v["b"], eps=1e-5, act="gelu", out=out)),
+        "norm_save": (cf.group_norm_forward_save, dict(x=x, groups=8, weight=v["w"], bias=v["b"], act="silu", out=out)),
+        "norm_backward": (cf.group_norm_backward, dict(dy=dy, x=x, stats=stats, weight=v["w"], bias=v["b"], act="none",
+                                                       out=out)),
+        "norm_backward, dx alone": (cf.group_norm_backward, dict(dy=dy, x=x, stats=stats, param_grads=False)),
+        "gated": (cf.gated_ffn_forward, dict(x=x2, **ffn, act="silu", out=out2)),
+        "gated_save": (cf.gated_ffn_forward_save, dict(x=x2, **ffn, act="gelu")),
+        "gated_backward": (cf.gated_ffn_backward, dict(dy=dy2, x=x2, saved=saved, **ffn, act="relu", out=out2)),
+        "linear": (cf.linear_log_probs_forward, dict(x=x2, weight=v["wv"], tokens=v["t"][0])),
+        "linear_backward": (cf.linear_log_probs_backward, dict(x=x2, weight=v["wv"], tokens=v["t"][0], lp=lp,
+                                                               d_logp=v["gl"][0], d_lse=v["gs"][0], out=out2)),
+    }
+
+
+@pytest.mark.parametrize("name", list(calls()) if torch.cuda.is_available() else ["none"])
+def test_native_calls_accept_and_refuse_alike(name, monkeypatch):
+    assert cf._args is not None
+    call, args = calls()[name]
+    variants = [args, {k: v for k, v in args.items() if k != "out"}]
+    for key, value in args.items():
+        variants += [{**args, key: s} for s in spoiled(value)]
+    if "eps" in args:
+        variants += [{**args, "eps": e} for e in (-1.0, float("nan"), float("inf"), 0.0)]
+    if "groups" in args:
+        variants += [{**args, "groups": g} for g in (0, -1, 7, 96, 1, True, 8.0)]
+    if "act" in args:
+        variants += [{**args, "act": a} for a in ("silu", "gelu", "relu", "none", "tanh", 0)]
+    if "lp" in args:
+        lp = args["lp"]
+        variants += [{**args, "lp": cf.LinearLogProbs(lp.logp, s)} for s in spoiled(lp.lse)]
+        variants += [{**args, "d_logp": None}, {**args, "d_lse": None}, {**args, "d_logp": None, "d_lse": None},
+                     {**args, "tokens": None, "d_logp": None}]
+    cf.lib()
+    native = [outcome(call, v) for v in variants]
+    monkeypatch.setattr(cf, "_args", None)
+    accepted = 0
+    for i, v in enumerate(variants):
+        want = outcome(call, v)
+        if isinstance(want, list):
+            assert isinstance(native[i], list), (i, native[i])
+            assert same(native[i], want), i
+            accepted += 1
+        else:
+            assert native[i] == want, (i, native[i], want)
+    assert accepted >= 2 and isinstance(native[0], list)
+
+
+def test_outputs_that_overlap_inputs_are_refused():
+    v = inputs()
+    x, ffn = v["x"][0], (v["wg"], v["wu"], v["wd"])
+    with pytest.raises(RuntimeError, match="overlap"):
+        cf.gated_ffn_forward(x, *ffn, out=x)
+    wide = torch.zeros(x.shape[0] + 1, x.shape[1], dtype=x.dtype, device="cuda")
+    with pytest.raises(RuntimeError, match="overlap"):
+        cf.group_norm_forward(wide[:-1].view(2, 7, 96), 8, out=wide[1:].view(2, 7, 96))
+    lp = cf.linear_log_probs_forward(x, v["wv"], v["t"][0])
+    with pytest.raises(RuntimeError, match="overlap"):
+        cf.linear_log_probs_backward(x, v["wv"], v["t"][0], lp, v["gl"][0], out=x)
+
+
+def test_the_same_tensor_in_two_places():
+    v = inputs(3)
+    x, w, wd = v["x"][0], v["wg"], v["wd"]
+    assert same(cf.gated_ffn_forward(x, w, w, wd), cf.gated_ffn_forward(x, w, w.clone(), wd))
+    _, saved = cf.gated_ffn_forward_save(x, w, w, wd)
+    assert same(cf.gated_ffn_backward(x, x, saved, w, w, wd), cf.gated_ffn_backward(x.clone(), x, saved, w.clone(), w, wd))
+    # features that are the classifier's own rows
+    few = v["wv"][:14]
+    lp = cf.linear_log_probs_forward(few, v["wv"], v["t"][0])
+    assert same(lp, cf.linear_log_probs_forward(few.clone(), v["wv"], v["t"][0]))
+    assert same(cf.linear_log_probs_backward(few, v["wv"], v["t"][0], lp, v["gl"][0]),
+                cf.linear_log_probs_backward(few.clone(), v["wv"], v["t"][0], lp, v["gl"][0]))
+    _, stats = cf.group_norm_forward_save(v["x"], 8)
+    assert same(cf.group_norm_backward(v["x"], v["x"], stats), cf.group_norm_backward(v["x"].clone(), v["x"], stats))
+
+
+# ---------------------------------------------------------------------------
+# Streams and graphs
+
+
+def step(v, ws=None, stream=None):
+    """Forward and backward of a head: norm, gated block, log probabilities.  ws:
+    one workspace for all of its calls, one after the other."""
+    kw = dict(ws=ws, stream=stream)
+    n, stats = cf.group_norm_forward_save(v["x"], 8, v["w"], v["b"], act="gelu", **kw)
+    h, saved = cf.gated_ffn_forward_save(n, v["wg"], v["wu"], v["wd"], **kw)
+    lp = cf.linear_log_probs_forward(h, v["wv"], v["t"], **kw)
+    dh, dwv = cf.linear_log_probs_backward(h, v["wv"], v["t"], lp, v["gl"], v["gs"], **kw)
+    dn, *dw = cf.gated_ffn_backward(dh, n, saved, v["wg"], v["wu"], v["wd"], **kw)
+    dx, dgamma, dbeta = cf.group_norm_backward(dn, v["x"], stats, v["w"], v["b"], act="gelu", **kw)
+    return [n, h, *lp, dh, dwv, dn, *dw, dx, dgamma, dbeta]
+
+
+def room(v):
+    N, P, C = v["x"].shape
+    H, V = v["wg"].shape[0], v["wv"].shape[0]
+    need = max(heads.group_norm_workspace_bytes((N, P, C), 8), heads.group_norm_backward_workspace_bytes((N, P, C), 8),
+               heads.gated_ffn_workspace_bytes(N * P, C, H), heads.gated_ffn_backward_workspace_bytes(N * P, C, H),
+               heads.linear_log_probs_workspace_bytes(N * P, C, V),
+               heads.linear_log_probs_backward_workspace_bytes(N * P, C, V))
+    return torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+
+
+SHAPES = [dict(), dict(N=1, P=1), dict(N=2, P=400, C=104, H=264, V=1000), dict(N=1, P=17, C=72, H=70, V=33, dt=torch.bfloat16)]
+
+
+@pytest.mark.parametrize("n", range(len(SHAPES)))
+def test_a_workspace_of_the_callers_and_another_stream(n):
+    v = inputs(5, **SHAPES[n])
+    want = step(v)
+    torch.cuda.synchronize()
+    assert same(step(v, ws=room(v)), want)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = step(v, stream=side)
+    got_ws = step(v, ws=room(v), stream=side)
+    side.synchronize()
+    assert same(got, want) and same(got_ws, want)
+    with torch.cuda.stream(side):
+        side.wait_stream(torch.cuda.default_stream())
+        got = step(v)
+    side.synchronize()
+    assert same(got, want)
+
+
+def test_two_streams_at_once():
+    v, u = inputs(6, N=4, P=300, C=128, H=256, V=700), inputs(7, N=2, P=500, C=256, H=264, V=900, dt=torch.bfloat16)
+    want = step(v), step(u)
+    torch.cuda.synchronize()
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    got = []
+    for _ in range(4):
+        with torch.cuda.stream(a):
+            p = step(v)
+        with torch.cuda.stream(b):
+            q = step(u)
+        got.append((p, q))
+    torch.cuda.synchronize()
+    for p, q in got:
+        assert same(p, want[0]) and same(q, want[1])
+
+
+def captured(v, ws=None):
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(v, ws=ws)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        r = step(v, ws=ws)
+    return g, r
+
+
+@pytest.mark.parametrize("shared", [False, True])
+def test_graphs_replayed_with_eager_work_between(shared):
+    """Two captured steps, with memory of their own or one workspace for both, that
+    take turns with eager calls while their inputs change."""
+    v, u = inputs(8), inputs(9, N=2, P=200, C=256, H=520, V=3000, dt=torch.bfloat16)
+    ws = None
+    if shared:
+        ws = max(room(v), room(u), key=torch.Tensor.numel)
+    graphs = [(*captured(t, ws), t) for t in (v, u)]
+    for turn in range(4):
+        for t in (v, u):
+            t["x"].copy_(randn(20 + turn, tuple(t["x"].shape), t["x"].dtype))
+            t["t"].copy_((t["t"] + 1) % 33)
+        for g, r, t in graphs:
+            g.replay()
+            eager = step(t)
+            torch.cuda.synchronize()
+            assert same(r, eager), turn
+        junk = torch.randn(1 << 20, device="cuda").sum().item()
+        assert junk == junk
+        graphs[0][0].replay()
+        graphs[1][0].replay()
+        graphs[0][0].replay()
+        torch.cuda.synchronize()
+        for g, r, t in graphs:
+            assert same(r, step(t)), turn
+
+
+# ---------------------------------------------------------------------------
+# Where the kernels change
+
+
+# rows up to 16 go another way than more; 4, 8 or 16 waves share k
+FEW = [(r, c) for r in (1, 2, 3, 8, 15, 16, 17) for c in (8, 250, 1536, 1544, 6144, 6160)]
+
+
+@pytest.mark.parametrize("rows,C", FEW)
+def test_few_rows(rows, C):
+    dt = torch.float16 if rows % 2 else torch.bfloat16
+    gated.exact_case(rows, C, 40, dt, "relu", rows + C)
+    gated.exact_case(rows, 40, C, dt, "none", rows + C)
+    x, w, t, gl, gs = linear.case(rows + C, rows, C, 77, dt)
+    linear.check(x, w, t, gl, gs, dt)
+
+
+# both tiles behind each product, with ragged ends (test_heads_cpu.py holds them to it)
+LARGE_GATED = [(4090, 8200, 4090), (2100, 4104, 2100), (4100, 1032, 2050), (300, 264, 520)]
+LARGE_LINEAR = [(1030, 520, 20001), (2050, 1032, 5001), (4100, 264, 5001)]
+
+
+@pytest.mark.parametrize("n", range(len(LARGE_GATED)))
+def test_both_tiles_of_the_gated_block(n):
+    gated.exact_case(*LARGE_GATED[n], torch.float16 if n % 2 else torch.bfloat16, "none" if n % 2 else "relu", n)
+
+
+@pytest.mark.parametrize("n", range(len(LARGE_LINEAR)))
+def test_both_tiles_of_log_probabilities(n):
+    dt = torch.bfloat16 if n % 2 else torch.float16
+    linear.check(*linear.case(n, *LARGE_LINEAR[n], dt), dt)
+
+
+def far(t, stride):
+    """t [rows, C] as rows `stride` apart, NaN behind each."""
+    wide = torch.empty(t.shape[0] * stride, dtype=t.dtype, device="cuda").as_strided(t.shape, (stride, 1))
+    wide.as_strided((t.shape[0], t.shape[1] + 64), (stride, 1)).fill_(float("nan"))
+    return wide.copy_(t)
+
+
+@pytest.mark.parametrize("stride", [(1 << 22) - 8, (1 << 22) + 8])
+def test_rows_far_apart(stride):
+    """The longest strides that are read in place, and longer ones: offsets of 2^32
+    bytes and more."""
+    rows, C, H, V = 530, 72, 72, 530
+    dt = torch.float16
+    x, dy, wv = randn(1, (rows, C), dt).cuda(), randn(2, (rows, C), dt).cuda(), randn(3, (V, C), dt, 0.2).cuda()
+    wg, wu, wd = (randn(4 + i, (H, C), dt, 0.1).cuda() for i in range(3))
+    t, gl = (torch.arange(rows) * 7 % V).cuda(), randn(9, (rows,)).cuda()
+    fx = far(x, stride)
+    y, saved = cf.gated_ffn_forward_save(x, wg, wu, wd)
+    assert same(cf.gated_ffn_forward_save(fx, wg, wu, wd), (y, saved))
+    want = cf.gated_ffn_backward(dy, x, saved, wg, wu, wd)
+    assert same(cf.gated_ffn_backward(dy, fx, saved, wg, wu, wd), want)
+    lp = cf.linear_log_probs_forward(x, wv, t)
+    grads = cf.linear_log_probs_backward(x, wv, t, lp, gl)
+    assert same(cf.linear_log_probs_forward(fx, wv, t), lp)
+    out = torch.empty(rows * stride, dtype=dt, device="cuda").as_strided((rows, C), (stride, 1))
+    assert same(cf.linear_log_probs_backward(fx, wv, t, lp, gl, out=out), grads)
+    del out
+    fw = far(wv, stride)
+    assert same(cf.linear_log_probs_forward(fx, fw, t), lp)
+    assert same(cf.linear_log_probs_backward(fx, fw, t, lp, gl), grads)
+    del fw
+    fg, fu, fd = far(wg, stride), far(wu, stride), far(wd, stride)
+    assert same(cf.gated_ffn_forward_save(x, fg, fu, fd), (y, saved))
+    assert same(cf.gated_ffn_backward(dy, x, saved, fg, fu, fd), want)
+    del fg, fu, fd
+    if stride < 1 << 22:
+        for shape in ((530, 1, C), (1, 530, C), (2, 265, C)):
+            g, s = cf.group_norm_forward_save(x.view(shape), 9)
+            fv = fx.as_strided(shape, (shape[1] * stride, stride, 1))
+            assert same(cf.group_norm_forward_save(fv, 9), (g, s))
+            assert same(cf.group_norm_backward(dy.view(shape), fv, s), cf.group_norm_backward(dy.view(shape), x.view(shape), s))
+    else:
+        with pytest.raises(RuntimeError, match="2\\^22"):
+            cf.group_norm_forward(fx.as_strided((1, rows, C), (stride, stride, 1)), 9)
+
+
+def test_more_values_than_32_bits_count():
+    """Feature maps and kept values of more than 2^32 bytes: the last rows are those
+    of a call of their own."""
+    dt = torch.bfloat16
+    x = torch.empty(50000, 49, 1024, dtype=dt, device="cuda")
+    x.normal_(generator=torch.Generator("cuda").manual_seed(1))
+    w, b = randn(2, (1024,)).cuda(), randn(3, (1024,)).cuda()
+    y, s = cf.group_norm_forward_save(x, 32, w, b, act="silu")
+    at = slice(46000, 50000)
+    assert same(cf.group_norm_forward_save(x[at], 32, w, b, act="silu"), (y[at], s[at]))
+    assert same(cf.group_norm_forward_save(x[:4000], 32, w, b, act="silu"), (y[:4000], s[:4000]))
+    dx, *_ = cf.group_norm_backward(y, x, s, w, b, act="silu", out=y)
+    y2 = cf.group_norm_forward(x[at], 32, w, b, act="silu")
+    dx2, *_ = cf.group_norm_backward(y2, x[at], s[at], w, b, act="silu", param_grads=False)
+    assert same(dx[at], dx2)
+    del x, y, dx
+    torch.cuda.empty_cache()
+    rows, C, H = 140000, 64, 8200  # 2^31 kept values and more
+    x = torch.randint(-1, 2, (rows, C), device="cuda", generator=torch.Generator("cuda").manual_seed(4)).to(dt)
+    wg, wu, wd = (gated.signs(5 + i, *size, 3).to(dt) for i, size in enumerate(((H, C), (H, C), (C, H))))
+    y, saved = cf.gated_ffn_forward_save(x, wg, wu, wd, act="relu")
+    last = x[-300:].clone()
+    y2, saved2 = cf.gated_ffn_forward_save(last, wg, wu, wd, act="relu")
+    assert same((y[-300:], saved[-300:]), (y2, saved2))  # whole numbers: exact in any order
+    dy = gated.signs(9, rows, C, 2).to(dt)
+    dx = cf.gated_ffn_backward(dy, x, saved, wg, wu, wd, act="relu")[0]
+    dx2 = cf.gated_ffn_backward(dy[-300:].clone(), last, saved2, wg, wu, wd, act="relu")[0]
+    assert same(dx[-300:], dx2)
+
+
+def test_a_long_vocabulary():
+    """2^27 classes of 8 channels, more logits for 40 rows than 32 bits count; some of
+    the classes against 64 bits."""
+    rows, C, V = 40, 8, 1 << 27
+    w = torch.empty(V, C, dtype=torch.float16, device="cuda")
+    w.normal_(0, 0.3, generator=torch.Generator("cuda").manual_seed(2))
+    x = randn(3, (rows, C), torch.float16).cuda()
+    t = torch.tensor([0, V - 1, V - 2, V // 2] * 10).cuda()
+    lp = cf.linear_log_probs_forward(x, w, t)
+    xd, total = x.double(), torch.zeros(rows, dtype=torch.float64, device="cuda")
+    for lo in range(0, V, 1 << 23):
+        total += torch.exp(torch.mm(xd, w[lo:lo + (1 << 23)].double().t().contiguous())).sum(1)
+    lse = total.log()
+    # in units of 2^-24: 2^20 tiles of 128 join by 256 lanes in chains of 2^12 additions, each half a
+    # unit of the sum so far; 300 more in a tile; 24 of the logits' products; 4 of an exponential; the
+    # rounding of numbers up to 20
+    assert float((lp.lse - lse).abs().max()) <= (2**12 + 700) * F32
+    z = (xd * w[t].double()).sum(1)
+    assert float((lp.logp - (z - lse)).abs().max()) <= (2**12 + 900) * F32
+    dx, dw = cf.linear_log_probs_backward(x, w, t, lp, torch.ones(rows, device="cuda"))
+    at = torch.cat([torch.arange(5), V - 1 - torch.arange(5), V // 2 + torch.arange(3)]).cuda()
+    p = torch.exp(torch.mm(xd, w[at].double().t().contiguous()) - lp.lse.double()[:, None])
+    dz = -p + (t[:, None] == at[None]).double()
+    want = torch.mm(dz.t().contiguous(), xd)
+    got = dw[at].double()
+    assert float((got - want).abs().max()) <= 2 * 2.0**-11 * float(want.abs().max()) + 2.0**-25
+    assert bool(torch.isfinite(dx).all())
+
+
+# ---------------------------------------------------------------------------
+# Together
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_a_head_from_features_to_the_loss(dtype):
+    """Norm, gated block with a residual, log probabilities, and all gradients of a
+    weighted loss, against 64 bits.  The largest gain between neighbours is about 2
+    (a norm's slope, a softmax under logits of size 1, an activation's), and on the
+    way to the first gradient there are 10 roundings of at most one R each."""
+    dt = DT[dtype]
+    v = inputs(11, dt, N=4, P=49, C=128, H=264, V=300)
+    p = {k: t.double().cpu() if t.is_floating_point() else t.cpu() for k, t in v.items()}
+    leaves = ("x", "w", "b", "wg", "wu", "wd", "wv")
+    for k in leaves:
+        p[k].requires_grad_()
+    n = torch.nn.functional.group_norm(p["x"].transpose(1, 2), 8, p["w"], p["b"], 1e-6).transpose(1, 2)
+    n = n * torch.special.ndtr(n)
+    h = n + (torch.nn.functional.silu(n @ p["wg"].t()) * (n @ p["wu"].t())) @ p["wd"].t()
+    z = h @ p["wv"].t()
+    lse = torch.logsumexp(z, -1)
+    some = p["t"] >= 0
+    logp = torch.where(some, z.gather(-1, p["t"].clamp_min(0)[..., None])[..., 0] - lse, 0.0)
+    ((p["gl"] * logp).sum() + (p["gs"] * lse).sum()).backward()
+
+    n1, stats = cf.group_norm_forward_save(v["x"], 8, v["w"], v["b"], act="gelu")
+    f, saved = cf.gated_ffn_forward_save(n1, v["wg"], v["wu"], v["wd"])
+    h1 = n1 + f
+    lp = cf.linear_log_probs_forward(h1, v["wv"], v["t"])
+    dh, dwv = cf.linear_log_probs_backward(h1, v["wv"], v["t"], lp, v["gl"], v["gs"])
+    dn, dwg, dwu, dwd = cf.gated_ffn_backward(dh, n1, saved, v["wg"], v["wu"], v["wd"])
+    dx, dw, db = cf.group_norm_backward(dn + dh, v["x"], stats, v["w"], v["b"], act="gelu")
+    R = ROUND[dt]
+    for got, want in ((lp.logp, logp.detach()), (lp.lse, lse.detach())):
+        assert float((got.double().cpu() - want).norm() / want.norm()) <= 8 * R
+    for got, key in zip((dx, dw, db, dwg, dwu, dwd, dwv), leaves):
+        want = p[key].grad
+        assert float((got.double().cpu() - want).norm() / want.norm()) <= 20 * R, key
+
+
+def test_tokens_one_at_a_time_agree_with_all_at_once():
+    """A head asked for one row a call, as a decoder does: the rows of one call over
+    all of them, whose sums go in another order."""
+    v = inputs(12, torch.bfloat16, N=1, P=40, C=256, H=520, V=1000)
+    x = v["x"][0]
+    y = cf.gated_ffn_forward(x, v["wg"], v["wu"], v["wd"])
+    lp = cf.linear_log_probs_forward(x, v["wv"], v["t"][0])
+    R = ROUND[torch.bfloat16]
+    for i in range(0, 40, 3):
+        one = cf.gated_ffn_forward(x[i:i + 1], v["wg"], v["wu"], v["wd"])
+        # h and y are rounded to neighbours at most: 2 R each, h's through a product
+        assert float((one.double() - y[i:i + 1].double()).norm() / y[i].double().norm()) <= 4 * R
+        l = cf.linear_log_probs_forward(x[i:i + 1], v["wv"], v["t"][0, i:i + 1])
+        # logits below 5 of 256 products, sums of 1000
+        assert float((l.lse - lp.lse[i:i + 1]).abs()) <= (2 * 256 * 5 + 1000) * F32
+        assert float((l.logp - lp.logp[i:i + 1]).abs()) <= (4 * 256 * 5 + 1000) * F32

@@ -289,28 +289,37 @@ __device__ __forceinline__ void group_sums(const Args &a, const Item &t, A &&add
     }
 }
 
-// mean and rstd of the groups of this item from the parts of the image
+// mean and rstd of the groups of this item from the parts of the image: a wave a
+// group, lanes beside each other take parts (1 x 256 x 256 x 64 in 128 parts,
+// forward 14.3 us against 50.5 by a thread a group)
+template <int TH>
 __device__ __forceinline__ void join_parts(const Args &a, const Item &t, float *gm, float *gr) {
-    each_group(t, [&](int g) {
+    const int lane = threadIdx.x & 63;
+    for (int g = threadIdx.x >> 6; g < t.groups; g += TH / 64) {
         const float2 *const p = a.part + t.n * a.chunks * a.G + t.g0 + g;
         const float all = (float)a.P;
+        auto pixels = [&](int i) {
+            const int64_t left = a.P - i * a.px;
+            return (float)(left < a.px ? left : a.px);
+        };
         float mean = 0.0f;
-        for (int i = 0; i < a.chunks; i++) {
-            const int64_t left = a.P - i * a.px;
-            mean += p[(int64_t)i * a.G].x * ((float)(left < a.px ? left : a.px) / all);
-        }
+        for (int i = lane; i < a.chunks; i += 64)
+            mean = fmaf(p[(int64_t)i * a.G].x, pixels(i) / all, mean);
+        mean = lanes<Add, 64>(mean);
         float m2 = 0.0f;
-        for (int i = 0; i < a.chunks; i++) {
-            const int64_t left = a.P - i * a.px;
+        for (int i = lane; i < a.chunks; i += 64) {
             const float2 v = p[(int64_t)i * a.G];
-            const float d = v.x - mean, count = (float)(left < a.px ? left : a.px) * (float)a.D;
-            m2 += fmaf(d * d, count, v.y);
+            const float d = v.x - mean;
+            m2 += fmaf(d * d, pixels(i) * (float)a.D, v.y);
         }
-        gm[g] = mean;
-        gr[g] = 1.0f / sqrtf(m2 / (all * (float)a.D) + a.eps);
-        if (t.chunk == 0 && a.stats)
-            a.stats[t.n * a.G + t.g0 + g] = make_float2(gm[g], gr[g]);
-    });
+        m2 = lanes<Add, 64>(m2);
+        if (lane == 0) {
+            gm[g] = mean;
+            gr[g] = 1.0f / sqrtf(m2 / (all * (float)a.D) + a.eps);
+            if (t.chunk == 0 && a.stats)
+                a.stats[t.n * a.G + t.g0 + g] = make_float2(gm[g], gr[g]);
+        }
+    }
     __syncthreads();
 }
 
@@ -414,7 +423,7 @@ __global__ __launch_bounds__(TH) void forward_apply_kernel(Args a) {
     extern __shared__ __align__(16) float lds[];
     CF_GN_PLACES
     float *const gm = groups_at(a, lds), *const gr = gm + a.per_block;
-    join_parts(a, t, gm, gr);
+    join_parts<TH>(a, t, gm, gr);
     set_stats(h, gm, gr);
 #pragma unroll 4
     for (int i = 0; i * a.rows < left; i++)
@@ -549,15 +558,26 @@ __global__ __launch_bounds__(TH) void backward_apply_kernel(Args a) {
     const uint16_t *const dy = a.dy + first * a.lddy;
     const uint32_t at_d = (uint32_t)row * (uint32_t)a.lddy * 2 + (uint32_t)h.c * 2;
     const int64_t step_d = a.rows * a.lddy;
-    for (int c = threadIdx.x; c < t.channels; c += TH) {
-        float s1 = 0.0f, s2 = 0.0f;
-        for (int i = 0; i < a.chunks; i++) {
-            const float2 v = a.part[(t.n * a.chunks + i) * a.C + t.c0 + c];
-            s1 += v.x;
-            s2 += v.y;
+    int share = 1;  // lanes of a channel, which add its parts together
+    while (share < 64 && share < a.chunks && 2 * share * t.channels <= TH)
+        share *= 2;
+    for (int i = threadIdx.x; i < t.channels * share; i += TH) {
+        const int c = i / share;
+        float2 s = make_float2(0.0f, 0.0f);
+#pragma unroll 4
+        for (int k = i % share; k < a.chunks; k += share) {
+            const float2 v = a.part[(t.n * a.chunks + k) * a.C + t.c0 + c];
+            s.x += v.x;
+            s.y += v.y;
         }
-        tot[c] = s1;
-        tot[a.V * 8 + c] = s2;
+        for (int d = 1; d < share; d *= 2) {
+            s.x += __shfl_xor(s.x, d);
+            s.y += __shfl_xor(s.y, d);
+        }
+        if (i % share == 0) {
+            tot[c] = s.x;
+            tot[a.V * 8 + c] = s.y;
+        }
     }
     __syncthreads();
     group_means(a, t, tot, ga, gb);

@@ -22,7 +22,7 @@ struct Plan {
 
 // The channels of a workgroup are a run of whole groups, at least `want` bytes
 // of each pixel.
-inline Plan shape(int64_t P, int C, int G, int want, int most_nv) {
+inline Plan shape(int64_t N, int64_t P, int C, int G, int want, int most_nv, int64_t cus) {
     const int D = C / G;
     Plan p;
     p.per_block = (want + 2 * D - 1) / (2 * D);
@@ -30,7 +30,9 @@ inline Plan shape(int64_t P, int C, int G, int want, int most_nv) {
     p.blocks = (G + p.per_block - 1) / p.per_block;
     p.V = (p.per_block * D + 7) / 8;
     const int64_t vectors = P * p.V;
-    p.threads = vectors > 4096 || p.V > 256 ? 512 : 256;
+    // a workgroup that has its CU to itself is better large (32 x 28 x 28 x 192 in 6 groups, forward
+    // 10.0 us against 12.5)
+    p.threads = vectors > 4096 || (vectors > 2048 && N * p.blocks <= cus && N * p.blocks >= cus / 2) || p.V > 256 ? 512 : 256;
     p.rows = p.threads / p.V;
     const int64_t hold = p.rows > 0 ? (int64_t)p.rows * most_nv : 0;  // pixels that fit
     p.chunks = hold ? (int)((P + hold - 1) / hold) : 0;
@@ -43,10 +45,13 @@ inline Plan shape(int64_t P, int C, int G, int want, int most_nv) {
 // same L2 at about the same time, makes twice the workgroups that 128 bytes do
 // (128 x 14 x 14 x 256, forward 12.1 us against 13.7, backward 20.4 against 22.1).
 inline Plan plan_of(int64_t N, int64_t P, int C, int G, int most_nv, int64_t cus) {
-    Plan p = shape(P, C, G, 64, most_nv);
-    // few workgroups with much to do each: parts of at least 4 vectors a thread
-    if (p.chunks >= 1 && N * p.blocks * p.chunks < cus / 2 && p.nv > 4) {
-        int64_t chunks = (cus + N * p.blocks - 1) / (N * p.blocks);
+    Plan p = shape(N, P, C, G, 64, most_nv, cus);
+    // Few workgroups with much to do each: parts of at least 4 vectors a thread, as many as make a
+    // workgroup a CU.  What is in parts anyhow is cut further (8 x 64 x 64 x 320 in 32 groups, forward
+    // 22.6 us against 31.4; a few workgroups more than CUs cost a second round).
+    const int64_t now = N * p.blocks * p.chunks;
+    if (p.nv > 4 && now < (p.chunks > 1 ? cus : cus / 2)) {
+        int64_t chunks = cus / (N * p.blocks);
         const int64_t most = (P + 4 * p.rows - 1) / (4 * p.rows);
         chunks = chunks < most ? chunks : most;
         if (chunks > p.chunks) {

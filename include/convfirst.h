@@ -531,16 +531,18 @@ cf_status cf_log_probs_backward(const void *z, const int64_t *tokens, const floa
  * The matrix products read rows in place that start at 16-byte aligned
  * addresses, with strides that are multiples of 8 elements and below 2^22, and
  * whose length is a multiple of 8; other operands are copied into the workspace
- * first.  The queries' `aligned` says (not 0) that the call's 16-bit inputs
- * have such addresses and strides, and w_gate and w_up one stride; without it they
+ * first, but for forward calls of up to 16 rows, which read all of theirs in
+ * place.  The queries' `aligned` says (not 0) that the call's 16-bit inputs have
+ * such addresses and strides, and w_gate and w_up one stride; without it they
  * leave room for copies of all of them. */
 
 /* Group norm over NHWC feature maps: x [N][P][C], P pixels an image, G groups of
  * C / G channels (at most CF_GROUP_MAX).  Over the P * C / G values of each group
  *   mean = avg x,  rstd = 1 / sqrt(avg (x - mean)^2 + eps)
  *   y = act(weight[c] * (x - mean) * rstd + bias[c])
- * weight, bias [C] may be NULL.  Row strides are below 2^22.  stats [N][G][2] (mean and rstd, for the
- * backward pass) may be NULL.  y may equal x with ldy = ldx. */
+ * weight, bias [C] may be NULL.  Row strides are below 2^22.  stats [N][G][2]
+ * (mean and rstd, for the backward pass) may be NULL.  y may equal x with ldy =
+ * ldx. */
 #define CF_GROUP_MAX 4096
 cf_status cf_group_norm_forward(const void *x, void *y, const float *weight, const float *bias, float *stats, void *ws,
                                 size_t ws_bytes, int64_t N, int64_t P, int C, int G, int64_t ldx, int64_t ldy,

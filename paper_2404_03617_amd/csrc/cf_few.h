@@ -4,12 +4,14 @@
 // memory into MFMA fragments, eight loads in flight a wave.  A row's loads are issued
 // one after the other, so that both halves of a cache line are asked for together: 16
 // rows x 131072 x 4096 take 200 us, with the matrices' loads among each other 247.
-// The rows of x come from the caches.  The waves' sums meet in LDS in a fixed order,
+// The rows of x come from the caches.  Rows may start anywhere and have any length:
+// what is left of k goes element by element.  The waves' sums meet in LDS in a fixed order,
 // and the first wave does what follows.  1 x 131072 x 4096 takes 182 us, 5.9 TB/s; a
 // gated block of 1 x 4096 x 12288 59 us, 5.1 TB/s.
 #pragma once
 
 #include "cf_mm_epi.h"
+#include "cf_rows.h"
 
 namespace cf {
 namespace few {
@@ -21,9 +23,21 @@ constexpr int ROWS = 16;  // rows of x at most
 
 struct Args {
     const uint16_t *x, *w[2];
-    int64_t ldx, ldw;
-    int M, N, K;  // K: columns that the rows hold, a multiple of 8
+    int64_t ldx, ldw[2];
+    int M, N, K;
 };
+
+// 8 k's of a row that has `left` of them from here on
+__device__ __forceinline__ u32x4 load_k(const uint16_t *p, int left) {
+    if (left >= 8)
+        return reinterpret_cast<const Any16 *>(p)->v;
+    u32x4 r = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int i = 0; i < 7; i++)
+        if (i < left)
+            r[i / 2] |= (uint32_t)p[i] << (16 * (i & 1));
+    return r;
+}
 
 // What follows gets `sum(f)`, the four results of fragment f in row lane % 16 of x:
 // rows n0 + 16 f + 4 (lane / 16) .. + 3 of W (DUAL: of either matrix, n0 alone).
@@ -105,7 +119,7 @@ __global__ __launch_bounds__(WAVES * 64) void kernel(Args a, typename E::Extra e
 #pragma unroll
     for (int f = 0; f < FN; f++) {
         const int row = n0 + (E::DUAL ? 0 : 16 * f) + r;
-        w[f] = (E::DUAL && f ? a.w[1] : a.w[0]) + (int64_t)(row < a.N ? row : a.N - 1) * a.ldw + q * 8;
+        w[f] = (E::DUAL && f ? a.w[1] : a.w[0]) + (row < a.N ? row : a.N - 1) * (E::DUAL && f ? a.ldw[1] : a.ldw[0]) + q * 8;
     }
     const uint16_t *const x = a.x + (int64_t)(r < a.M ? r : a.M - 1) * a.ldx + q * 8;
     float4v acc[FN];
@@ -121,10 +135,10 @@ __global__ __launch_bounds__(WAVES * 64) void kernel(Args a, typename E::Extra e
         for (int f = 0; f < FN; f++)
 #pragma unroll
             for (int u = 0; u < U; u++)
-                fw[f][u] = *reinterpret_cast<const u32x4 *>(w[f] + k0 + 32 * u);
+                fw[f][u] = reinterpret_cast<const Any16 *>(w[f] + k0 + 32 * u)->v;
 #pragma unroll
         for (int u = 0; u < U; u++)
-            fx[u] = *reinterpret_cast<const u32x4 *>(x + k0 + 32 * u);
+            fx[u] = reinterpret_cast<const Any16 *>(x + k0 + 32 * u)->v;
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int u = 0; u < U; u++)
@@ -133,11 +147,11 @@ __global__ __launch_bounds__(WAVES * 64) void kernel(Args a, typename E::Extra e
                 acc[f] = T::mfma(fw[f][u], fx[u], acc[f]);
     }
     for (; k0 < a.K; k0 += 32) {  // the wave that has the last share of k, where it is not whole
-        const bool in = k0 + q * 8 < a.K;
-        const u32x4 none = {0u, 0u, 0u, 0u}, fx = in ? *reinterpret_cast<const u32x4 *>(x + k0) : none;
+        const int left = a.K - k0 - q * 8;
+        const u32x4 fx = load_k(x + k0, left);
 #pragma unroll
         for (int f = 0; f < FN; f++)
-            acc[f] = T::mfma(in ? *reinterpret_cast<const u32x4 *>(w[f] + k0) : none, fx, acc[f]);
+            acc[f] = T::mfma(load_k(w[f] + k0, left), fx, acc[f]);
     }
 #pragma unroll
     for (int f = 0; f < FN; f++)

@@ -45,8 +45,10 @@ struct ForwardPlan {
     Plan up, down;
     void *part;
 };
-ForwardPlan forward_plan(const GatedFfn &a, const Copied &c, void *ws) {
+ForwardPlan forward_plan(const GatedFfn &a, Copied c, void *ws) {
     ForwardPlan p;
+    if (a.rows <= few::ROWS)  // read wherever they are
+        c = {};
     p.room.p = (uint8_t *)ws;
     p.pad = up8(a.H);
     p.ld = stride_of(a.H);
@@ -100,12 +102,12 @@ hipError_t forward(const GatedFfn &a, const ForwardPlan &p, void *y, int64_t ldy
     CF_HIP(pack(p.wu, bf16, st));
     CF_HIP(pack(p.wd, bf16, st));
     if (a.rows <= few::ROWS) {
-        const few::Args up = {p.x.m.p, {p.wg.m.p, p.wu.m.p}, p.x.m.ld, p.wg.m.ld, a.rows, a.H, p.x.m.ext};
+        const few::Args up = {p.x.m.p, {p.wg.m.p, p.wu.m.p}, p.x.m.ld, {p.wg.m.ld, p.wu.m.ld}, a.rows, a.H, a.C};
         CF_HIP((few::launch<T, 2, few::Gated>(up, GatedArgs{p.h, p.ld, saved, a.H, p.pad, a.act}, st)));
         StoreArgs s = {};
         s.out[0] = (uint16_t *)y;
         s.ldo = ldy;
-        const few::Args down = {p.h, {p.wd.m.p, p.wd.m.p}, p.ld, p.wd.m.ld, a.rows, a.C, p.pad};
+        const few::Args down = {p.h, {p.wd.m.p, p.wd.m.p}, p.ld, {p.wd.m.ld, p.wd.m.ld}, a.rows, a.C, a.H};
         return few::launch<T, 1, few::Store>(down, s, st);
     }
     Args up = args_of(p.up, a.rows, 2 * a.H, a.C, p.x.m, a.rows, p.wg.m, a.H);

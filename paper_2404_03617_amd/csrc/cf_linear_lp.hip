@@ -150,6 +150,8 @@ struct ForwardPlan {
 };
 ForwardPlan forward_plan(const LinearLogProbs &a, bool copy_x, bool copy_w, void *ws) {
     ForwardPlan p;
+    copy_x &= a.rows > few::ROWS;  // fewer are read wherever they are
+    copy_w &= a.rows > few::ROWS;
     p.room.p = (uint8_t *)ws;
     p.x = operand(a.x.p, a.x.ld, a.rows, a.C, copy_x, p.room);
     p.w = operand(a.w.p, a.w.ld, a.V, a.C, copy_w, p.room);
@@ -204,7 +206,7 @@ hipError_t forward(const LinearLogProbs &a, const ForwardPlan &p, float *logp, f
     CF_HIP(pack(p.x, bf16, st));
     CF_HIP(pack(p.w, bf16, st));
     const LseArgs e = {p.part, p.picked, logp ? a.tokens : nullptr};
-    const few::Args f = {p.x.m.p, {p.w.m.p, p.w.m.p}, p.x.m.ld, p.w.m.ld, (int)a.rows, a.V, p.x.m.ext};
+    const few::Args f = {p.x.m.p, {p.w.m.p, p.w.m.p}, p.x.m.ld, {p.w.m.ld, p.w.m.ld}, (int)a.rows, a.V, a.C};
     if (a.rows <= few::ROWS)
         CF_HIP((few_of(a.rows) == 1 ? few::launch<T, 1, few::Lse>(f, e, st) : few::launch<T, 2, few::Lse>(f, e, st)));
     else

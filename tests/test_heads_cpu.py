@@ -151,7 +151,8 @@ def test_silu_is_of_these_operators_alone():
 def test_workspace_queries():
     """0 for what has no kernel, room for what the formulas keep there (h, its
     gradients, a piece of dz), and without alignment for copies of the inputs too
-    (which are there with it where rows are no multiple of 8 long)."""
+    (which are there with it where rows are no multiple of 8 long; up to 16 rows of a
+    forward call need none)."""
     L = cf.lib()
     assert L.cf_group_norm_workspace_bytes(2, 100, 64, 7) == 0
     assert L.cf_group_norm_workspace_bytes(2, 100, 8192, 1) == 0
@@ -160,11 +161,13 @@ def test_workspace_queries():
     for rows, C, H in ((1, 64, 96), (300, 100, 77), (5000, 512, 1365), (8192, 4096, 12288)):
         for f, least in ((L.cf_gated_ffn_workspace_bytes, 2), (L.cf_gated_ffn_backward_workspace_bytes, 6)):
             tight, loose = f(rows, C, H, 1), f(rows, C, H, 0)
-            assert tight >= least * rows * H and loose >= tight + (C % 8 == 0 and H % 8 == 0) * 2 * (rows * C + 3 * C * H), (rows, C, H)
+            copied = C % 8 == 0 and H % 8 == 0 and (rows > 16 or least == 6)
+            assert tight >= least * rows * H and loose >= tight + copied * 2 * (rows * C + 3 * C * H), (rows, C, H)
     for rows, C, V in ((1, 64, 1000), (300, 100, 77), (2047, 1000, 50021), (8192, 4096, 131072)):
         for f in (L.cf_linear_log_probs_workspace_bytes, L.cf_linear_log_probs_backward_workspace_bytes):
             tight, loose = f(rows, C, V, 1), f(rows, C, V, 0)
-            assert tight > 0 and loose >= tight + (C % 8 == 0) * 2 * (rows * C + V * C), (rows, C, V)
+            copied = C % 8 == 0 and (rows > 16 or f == L.cf_linear_log_probs_backward_workspace_bytes)
+            assert tight > 0 and loose >= tight + copied * 2 * (rows * C + V * C), (rows, C, V)
     dz = L.cf_linear_log_probs_backward_workspace_bytes(8192, 4096, 131072, 1)
     assert dz < 2 << 30  # the logits alone would be 2 GiB
     for f in (L.cf_gated_ffn_workspace_bytes, L.cf_linear_log_probs_workspace_bytes,

@@ -293,25 +293,39 @@ struct Lse {
         constexpr int W = Results<S, G>::W, PIECES = Results<S, G>::PIECES;
         float2 *const row = reinterpret_cast<float2 *>(lds);  // [WN][TM]
         const int wn = n0 % S::TN / (S::TN / S::WN), local = m0 % S::TM;
+        constexpr int COLUMNS = 16 * S::FN;  // of a wave
 #pragma unroll
         for (int i = 0; i < S::FM; i++) {
             const int m = m0 + 16 * i + (lane & 15);
             const int64_t want = e.tokens && m < a.M ? e.tokens[m] : -1;
-            float top = -INFINITY;
+            const bool here = want >= n0 && want < n0 + COLUMNS && want < a.N;
             float z[PIECES][W];
 #pragma unroll
-            for (int p = 0; p < PIECES; p++) {
-                const int n = n0 + t.column(p, lane);
+            for (int p = 0; p < PIECES; p++)
 #pragma unroll
-                for (int k = 0; k < W; k++) {
+                for (int k = 0; k < W; k++)
                     z[p][k] = t.get(i, p, k);
-                    if (n + k >= a.N)
-                        z[p][k] = -INFINITY;
-                    else if (n + k == want)
-                        e.picked[m] = z[p][k];
+            // Both seldom, and the same for a wave: two comparisons a logit less.
+            if (n0 + COLUMNS > a.N)
+#pragma unroll
+                for (int p = 0; p < PIECES; p++)
+#pragma unroll
+                    for (int k = 0; k < W; k++)
+                        if (n0 + t.column(p, lane) + k >= a.N)
+                            z[p][k] = -INFINITY;
+            if (__any(here))
+#pragma unroll
+                for (int p = 0; p < PIECES; p++)
+#pragma unroll
+                    for (int k = 0; k < W; k++)
+                        if (here && n0 + t.column(p, lane) + k == want)
+                            e.picked[m] = z[p][k];
+            float top = -INFINITY;
+#pragma unroll
+            for (int p = 0; p < PIECES; p++)
+#pragma unroll
+                for (int k = 0; k < W; k++)
                     top = fmaxf(top, z[p][k]);
-                }
-            }
             const float base = top == -INFINITY ? 0.0f : top;
             float sum = 0.0f;
 #pragma unroll
@@ -369,7 +383,7 @@ struct Dz {
                 continue;
             const RowGrad r = e.rows[m];
             const int want = r.token - e.v0;
-            const bool any = !(r.c == 0.0f && r.g == 0.0f);
+            const bool any = !(r.c == 0.0f && r.g == 0.0f), mine = __any(any && want >= n0 && want < n0 + 16 * S::FN);
 #pragma unroll
             for (int p = 0; p < PIECES; p++) {
                 const int n = n0 + t.column(p, lane);
@@ -378,9 +392,18 @@ struct Dz {
                 float d[W];
 #pragma unroll
                 for (int k = 0; k < W; k++) {
-                    const float q = __builtin_amdgcn_exp2f((t.get(i, p, k) - r.lse) * LOG2E);
-                    d[k] = any && n + k < a.N ? fmaf(r.c, q, n + k == want ? r.g : 0.0f) : 0.0f;
+                    const float q = r.c * __builtin_amdgcn_exp2f((t.get(i, p, k) - r.lse) * LOG2E);
+                    d[k] = any ? q : 0.0f;
                 }
+                // both seldom, and the same for a wave
+                if (mine)
+#pragma unroll
+                    for (int k = 0; k < W; k++)
+                        d[k] += any && n + k == want ? r.g : 0.0f;
+                if (n0 + 16 * S::FN > a.N)
+#pragma unroll
+                    for (int k = 0; k < W; k++)
+                        d[k] = n + k < a.N ? d[k] : 0.0f;
                 store_row<T, W>(e.dz + m * e.ld + n, d, W);
             }
         }

@@ -194,8 +194,12 @@ struct Gated {
                     for (int k = 0; k < 8; k++) {
                         g[k] = t.get(i, p, k);
                         u[k] = t.get(i, p + 1, k);
-                        h[k] = k < left ? act_value<ACT>(g[k]) * u[k] : 0.0f;
+                        h[k] = act_value<ACT>(g[k]) * u[k];
                     }
+                    if (n0 / 2 + 8 * S::FN > e.H)  // the same for a wave
+#pragma unroll
+                        for (int k = 0; k < 8; k++)
+                            h[k] = k < left ? h[k] : 0.0f;
                     store_row<T, 8>(e.h + m * e.ldh + n, h, 8);
                     if (e.saved) {
                         float *const s = e.saved + (int64_t)m * 2 * e.H + n;

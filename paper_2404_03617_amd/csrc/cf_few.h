@@ -11,7 +11,6 @@
 #pragma once
 
 #include "cf_mm_epi.h"
-#include "cf_rows.h"
 
 namespace cf {
 namespace few {

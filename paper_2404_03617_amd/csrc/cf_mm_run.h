@@ -18,8 +18,15 @@ hipError_t launch_lse(const Args &a, const LseArgs &e, int tile, hipStream_t st)
 template <typename T>
 hipError_t launch_dz(const Args &a, const DzArgs &e, int tile, hipStream_t st);
 
-// Sums of split products, and what follows.
+// Sums of split products, and what follows: a store, h of the gate (batch 0) and
+// up channels (batch 1), their gradients, the largest logits and sums of
+// JOIN_CLASSES classes each, the logits' gradients.
+constexpr int JOIN_CLASSES = 2048;
 hipError_t launch_join(const Args &a, const StoreArgs &e, int bf16, hipStream_t st);
+hipError_t launch_join(const Args &a, const float *part, const GatedArgs &e, int bf16, hipStream_t st);
+hipError_t launch_join(const Args &a, const float *part, const GatedBackArgs &e, int bf16, hipStream_t st);
+hipError_t launch_join(const Args &a, const float *part, const LseArgs &e, int bf16, hipStream_t st);
+hipError_t launch_join(const Args &a, const float *part, const DzArgs &e, int bf16, hipStream_t st);
 
 // A matrix as the tiles read it: 16-byte aligned rows that hold `ext` columns,
 // a multiple of 8.
@@ -46,8 +53,8 @@ hipError_t launch_pack(const void *src, int64_t ld, int64_t rows, int cols, cons
                        hipStream_t st);
 
 inline Plan plan(int64_t M, int64_t N, int64_t K, bool may_split, int batch = 1, int segments = 1,
-                 bool wide = false) {
-    return plan_of(M, N, steps_of(K) * segments, batch, may_split, device_cu_count(), wide);
+                 After what = STORE) {
+    return plan_of(M, N, steps_of(K) * segments, batch, may_split, device_cu_count(), what);
 }
 // a workgroup a tile: a launch holds 2^32 threads
 inline bool grid_fits(int64_t M, int64_t N) { return (double)((M + 127) / 128) * (double)((N + 127) / 128) < 4.0e6; }
@@ -120,6 +127,15 @@ hipError_t run_store(const Args &a, StoreArgs e, const Plan &p, void *part, int 
     e.part = (float *)part;
     const hipError_t r = bf16 ? launch_store<BF16, LA, LB>(a, e, p.tile, st) : launch_store<F16, LA, LB>(a, e, p.tile, st);
     return r != hipSuccess || a.splits == 1 ? r : launch_join(a, e, bf16, st);
+}
+
+// The parts alone of a split product, and what follows.
+template <int LA, int LB, typename E>
+hipError_t run_split(const Args &a, const E &e, const Plan &p, void *part, int bf16, hipStream_t st) {
+    StoreArgs s = {};
+    s.part = (float *)part;
+    CF_HIP((bf16 ? launch_store<BF16, LA, LB>(a, s, p.tile, st) : launch_store<F16, LA, LB>(a, s, p.tile, st)));
+    return launch_join(a, s.part, e, bf16, st);
 }
 
 }  // namespace mm

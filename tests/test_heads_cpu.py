@@ -242,7 +242,7 @@ def test_splits_of_the_products_hold_all_steps_and_fit_the_room(tmp_path, cus):
             for (int64_t steps = 0; steps < 1 << 22; steps += steps / 2 + 1)
                 for (int batch = 1; batch < 3; batch++)
                     for (int split = 0; split < 2; split++) {
-                        const Plan p = plan_of(M, N, steps, batch, split, %d, M %% 2 == 0);
+                        const Plan p = plan_of(M, N, steps, batch, split, %d, M %% 3 == 0 ? STORE : M %% 3 == 1 ? MORE : GATE);
                         const bool ok = p.tile >= 0 && p.tile < TILE_COUNT && p.splits >= 1 && p.per >= 1 &&
                                         (int64_t)p.splits * p.per >= steps && (split || p.splits == 1) &&
                                         (p.splits == 1 || (int64_t)(p.splits - 1) * p.per < steps) &&
@@ -304,19 +304,23 @@ def test_the_sizes_of_the_tile_tests_take_every_tile(tmp_path):
 
     products = []
     for r, C, H in LARGE_GATED:
-        products += [("up", r, 2 * H, C, 1, "false", "false"), ("dh", r, H, C, 1, "false", "true"),
-                     ("down", r, C, H, 1, "true", "false"), ("dx", r, C, 2 * H, 1, "true", "false"),
-                     ("dw", C, H, r, 1, "true", "false"), ("dw", H, C, r, 2, "true", "false")]
+        products += [("up", r, 2 * H, C, 1, "true", "MORE"), ("dh", r, H, C, 1, "true", "GATE"),
+                     ("down", r, C, H, 1, "true", "STORE"), ("dx", r, C, 2 * H, 1, "true", "STORE"),
+                     ("dw", C, H, r, 1, "true", "STORE"), ("dw", H, C, r, 2, "true", "STORE")]
     for r, C, V in LARGE_LINEAR:
-        products += [("logits", r, V, C, 1, "false", "false"), ("dx of logits", r, C, V, 1, "true", "false"),
-                     ("dw of logits", V, C, r, 1, "true", "false")]
+        products += [("logits", r, V, C, 1, "true", "MORE"), ("dx of logits", r, C, V, 1, "true", "STORE"),
+                     ("dw of logits", V, C, r, 1, "true", "STORE")]
     out = run_cpp(tmp_path, "cf_mm_plan.h", "mm", "".join(
         "{ const Plan p = plan_of(%d, %d, steps_of(%d), %d, %s, 256, %s); printf(\"%%d %%d\\n\", p.tile, p.splits); }\n"
         % q[1:] for q in products))
     seen = set()
     for q, line in zip(products, out.split("\n")):
         tile, splits = (int(v) for v in line.split())
-        seen |= {(q[0], tile), (tile, "split" if splits > 1 else "whole")}
+        # behind a split sum of gates or logits the tile's own end does not run
+        if splits == 1 or q[0] not in ("up", "dh", "logits"):
+            seen.add((q[0], tile))
+        seen |= {(tile, "split" if splits > 1 else "whole"), (q[0], "split" if splits > 1 else "whole")}
     missing = {(name, t) for name in ("up", "dh", "down", "dx", "dw", "logits") for t in range(2)} - seen
+    missing |= {(name, "split") for name in ("up", "dh", "logits")} - seen
     assert not missing, missing
     assert {(t, k) for t in range(2) for k in ("split", "whole")} <= seen, seen

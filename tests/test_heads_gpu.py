@@ -249,9 +249,10 @@ def test_few_rows(rows, C):
     linear.check(x, w, t, gl, gs, dt)
 
 
-# both tiles behind each product, with ragged ends (test_heads_cpu.py holds them to it)
-LARGE_GATED = [(4090, 8200, 4090), (2100, 4104, 2100), (4100, 1032, 2050), (300, 264, 520)]
-LARGE_LINEAR = [(1030, 520, 20001), (2050, 1032, 5001), (4100, 264, 5001)]
+# both tiles behind each product and split sums of each, with ragged ends (test_heads_cpu.py holds
+# them to it)
+LARGE_GATED = [(4090, 8200, 4090), (2100, 4104, 2100), (4100, 1032, 2050), (300, 264, 520), (95, 4104, 1031), (33, 1030, 250)]
+LARGE_LINEAR = [(1030, 520, 20001), (2050, 1032, 5001), (4100, 264, 5001), (95, 4104, 2061), (260, 2055, 5003)]
 
 
 @pytest.mark.parametrize("n", range(len(LARGE_GATED)))

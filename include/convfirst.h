@@ -599,9 +599,11 @@ cf_status cf_linear_log_probs_forward(const void *x, const void *weight, const i
 size_t cf_linear_log_probs_workspace_bytes(int64_t rows, int C, int V, int aligned);
 
 /* The gradients of sum(d_logp * logp) + sum(d_lse * lse), either of which may be
- * NULL (d_logp needs tokens); lse is the forward call's:
+ * NULL (d_logp needs tokens and logp); logp and lse are the forward call's:
  *   dz[r][v] = (d_lse[r] - d_logp[r]) p_v + d_logp[r] 1[v = token],  p = exp(z - lse)
  *   dx = dz weight,  dweight = dz^T x
+ * At the token, p = exp(logp) and 1 - p = -expm1(logp), which keeps what is left of
+ * a gradient where p is nearly 1.
  * The logits are made again, a piece of the vocabulary at a time (dz of a piece,
  * in dt, is in the workspace: 256 MiB, or rows * 8 KiB if that is more); in fp16 dz
  * is scaled by a power of two a row, so that small probabilities keep their
@@ -610,10 +612,10 @@ size_t cf_linear_log_probs_workspace_bytes(int64_t rows, int C, int V, int align
  * their features hold.  A token of V or more makes the gradients NaN.  dx
  * [rows][C] and dweight [V][C], dense, in dt; rows = 0 gives zeros in dweight.  No
  * output may overlap an input. */
-cf_status cf_linear_log_probs_backward(const void *x, const void *weight, const int64_t *tokens, const float *lse,
-                                       const float *d_logp, const float *d_lse, void *dx, void *dweight, void *ws,
-                                       size_t ws_bytes, int64_t rows, int C, int V, int64_t ldx, int64_t ldw,
-                                       int64_t lddx, cf_dtype dt, void *stream);
+cf_status cf_linear_log_probs_backward(const void *x, const void *weight, const int64_t *tokens, const float *logp,
+                                       const float *lse, const float *d_logp, const float *d_lse, void *dx,
+                                       void *dweight, void *ws, size_t ws_bytes, int64_t rows, int C, int V,
+                                       int64_t ldx, int64_t ldw, int64_t lddx, cf_dtype dt, void *stream);
 size_t cf_linear_log_probs_backward_workspace_bytes(int64_t rows, int C, int V, int aligned);
 
 /* Thread-local message describing the most recent non-CF_OK status. */

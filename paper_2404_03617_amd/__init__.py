@@ -244,7 +244,7 @@ def lib():
             "cf_gated_ffn_backward_workspace_bytes": (sz, [l, i, i, i]),
             "cf_linear_log_probs_forward": (i, [vp] * 6 + [sz, l, i, i, l, l, i, vp]),
             "cf_linear_log_probs_workspace_bytes": (sz, [l, i, i, i]),
-            "cf_linear_log_probs_backward": (i, [vp] * 9 + [sz, l, i, i, l, l, l, i, vp]),
+            "cf_linear_log_probs_backward": (i, [vp] * 10 + [sz, l, i, i, l, l, l, i, vp]),
             "cf_linear_log_probs_backward_workspace_bytes": (sz, [l, i, i, i]),
         })
         for name, (res, args) in sig.items():

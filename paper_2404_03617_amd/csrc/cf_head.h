@@ -62,7 +62,7 @@ hipError_t launch_linear_log_probs(const LinearLogProbs &a, float *logp, float *
                                    hipStream_t st);
 size_t linear_backward_workspace_bytes(int64_t rows, int C, int V, bool aligned);
 struct LinearGrads {
-    const float *lse, *d_logp, *d_lse;  // d_* may be null
+    const float *logp, *lse, *d_logp, *d_lse;  // logp for d_logp; d_* may be null
     void *dx;
     int64_t lddx;
     void *dw;  // [V][C] dense

@@ -268,8 +268,8 @@ size_t cf_linear_log_probs_backward_workspace_bytes(int64_t rows, int C, int V, 
                : linear_backward_workspace_bytes(rows, C, V, aligned != 0);
 }
 
-cf_status cf_linear_log_probs_backward(const void *x, const void *weight, const int64_t *tokens, const float *lse,
-                                       const float *d_logp, const float *d_lse, void *dx, void *dweight, void *ws,
+cf_status cf_linear_log_probs_backward(const void *x, const void *weight, const int64_t *tokens, const float *logp,
+                                       const float *lse, const float *d_logp, const float *d_lse, void *dx, void *dweight, void *ws,
                                        size_t ws_bytes, int64_t rows, int C, int V, int64_t ldx, int64_t ldw,
                                        int64_t lddx, cf_dtype dt, void *stream) {
     const char *const what = "cf_linear_log_probs_backward";
@@ -285,25 +285,26 @@ cf_status cf_linear_log_probs_backward(const void *x, const void *weight, const 
         return api_fail(CF_ERR_INVALID, "%s: x, weight, lse and dx must be non-NULL", what);
     if (rows > 0 && !d_logp && !d_lse)
         return api_fail(CF_ERR_INVALID, "%s: d_logp or d_lse must be non-NULL", what);
-    if (rows > 0 && d_logp && !tokens)
-        return api_fail(CF_ERR_INVALID, "%s: d_logp needs tokens", what);
+    if (rows > 0 && d_logp && (!tokens || !logp))
+        return api_fail(CF_ERR_INVALID, "%s: d_logp needs tokens and their logp", what);
     const Span t[] = {{"x", x, rows, C, ldx, 2},
                       {"weight", weight, V, C, ldw, 2},
                       dense("tokens", tokens, rows, 1, 8),
+                      dense("logp", logp, rows, 1, 4),
                       dense("lse", lse, rows, 1, 4),
                       dense("d_logp", d_logp, rows, 1, 4),
                       dense("d_lse", d_lse, rows, 1, 4),
                       {"dx", dx, rows, C, lddx, 2},
                       dense("dweight", dweight, V, C, 2)};
-    CF_TRY(check_aligned(what, t, 8));
-    for (int i = 6; i < 8; i++)
+    CF_TRY(check_aligned(what, t, 9));
+    for (int i = 7; i < 9; i++)
         CF_TRY(check_out(what, t[i], t, i));
     if (!linear_fits(rows, C, V))
         return too_large(what);
     const bool plain = readable(x, ldx) && readable(weight, ldw);
-    CF_TRY(check_ws(what, ws, ws_bytes, cf_linear_log_probs_backward_workspace_bytes(rows, C, V, plain), t, 8));
+    CF_TRY(check_ws(what, ws, ws_bytes, cf_linear_log_probs_backward_workspace_bytes(rows, C, V, plain), t, 9));
     const LinearLogProbs a = {{x, ldx}, {weight, ldw}, tokens, (int)rows, C, V};
-    const LinearGrads g = {lse, d_logp, d_lse, dx, lddx, dweight};
+    const LinearGrads g = {logp, lse, d_logp, d_lse, dx, lddx, dweight};
     return api_done(launch_linear_log_probs_backward(a, g, dt == CF_BF16, ws, (hipStream_t)stream), what);
 }
 

@@ -18,8 +18,8 @@
 // over the pieces in fp32.
 //
 // A gradient in 16 bits: in bf16 its range is that of fp32.  In fp16 a row's
-// values are scaled by a power of two, so that the largest of c and d_logp lies
-// in [2^13, 2^14) and a probability of 4e-9 still has all bits; dx is scaled
+// values are scaled by a power of two, so that the largest of c and the token's value
+// lies in [2^13, 2^14) and a probability of 4e-9 still has all bits; dx is scaled
 // back by row, and the rows of x that dW sums are scaled against each other
 // (exactly, but for what falls below fp16 against the largest row) and the sums
 // back.  The same copy of x leaves out rows without a gradient: what their
@@ -80,22 +80,23 @@ __global__ __launch_bounds__(256) void join_lse_kernel(const float2 *part, const
     }
 }
 
-// What a row's gradient is made of; none for c = g = 0.
+// What a row's gradient is made of; none for c = at = 0.  At the token, c p + d_logp
+// is d_lse p + d_logp (1 - p) with both factors from logp: where p is nearly 1, lse in
+// fp32 has lost what is left of 1 - p (a row with lse = 15 and 1 - p = 5e-7: all of it).
 __device__ __forceinline__ RowGrad grad_of(const LinearGrads &g, const int64_t *tokens, int V, int r) {
-    const int64_t t = tokens ? tokens[r] : -1;
-    float gl = g.d_logp && t >= 0 ? g.d_logp[r] : 0.0f;
-    if (t >= V && g.d_logp)
-        gl = NAN;
-    const float lse = g.lse[r];
-    RowGrad w = {(g.d_lse ? g.d_lse[r] : 0.0f) - gl, gl, lse, t < V ? (int)t : -1};
+    const int64_t t = g.d_logp ? tokens[r] : -1;
+    const float gl = t >= V ? NAN : t >= 0 ? g.d_logp[r] : 0.0f, gs = g.d_lse ? g.d_lse[r] : 0.0f, lse = g.lse[r];
+    RowGrad w = {gs - gl, 0.0f, lse, t < V ? (int)t : -1};
+    if (w.token >= 0)
+        w.at = gs * expf(g.logp[r]) - gl * expm1f(g.logp[r]);
     if (lse == -INFINITY)
-        w.c = w.g = 0.0f;
+        w.c = w.at = 0.0f;
     return w;
 }
-// 2^e <= the larger of |c| and |g| < 2^(e+1), within what fp32 can be scaled by
+// 2^e <= the larger of |c| and |at| < 2^(e+1), within what fp32 can be scaled by
 constexpr int E_MIN = -100, E_MAX = 100;
 __device__ __forceinline__ int exponent_of(const RowGrad &w) {
-    const float a = fmaxf(fabsf(w.c), fabsf(w.g));
+    const float a = fmaxf(fabsf(w.c), fabsf(w.at));
     const int e = (int)(__float_as_uint(a) >> 23) - 127;
     return e < E_MIN ? E_MIN : e > E_MAX ? E_MAX : e;
 }
@@ -133,12 +134,12 @@ __global__ __launch_bounds__(256) void row_grads_kernel(LinearGrads g, const int
     if (r >= rows)
         return;
     RowGrad w = grad_of(g, tokens, V, r);
-    const bool none = w.c == 0.0f && w.g == 0.0f;
+    const bool none = w.c == 0.0f && w.at == 0.0f;
     float f = none ? 0.0f : 1.0f;
     if (most) {
         const int e = exponent_of(w);
         w.c *= pow2(13 - e);
-        w.g *= pow2(13 - e);
+        w.at *= pow2(13 - e);
         row_scale[r] = pow2(e - 13);
         f = none ? 0.0f : pow2(e - *most);
     }

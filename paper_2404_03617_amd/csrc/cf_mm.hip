@@ -1,7 +1,7 @@
 // cf_mm.hip -- what stands around the products of cf_mm.h: packed copies of
 // operands that the tiles cannot read where they are, and the joining of split
-// sums, in a fixed order, with what follows them.  Both are bound by memory: 100 MB of
-// features are copied in 21 us, 4.8 TB/s with the write; the joins are 4 to 13 us.
+// sums, in a fixed order, with what follows them.  Both are bound by memory: 67 MB of
+// features are copied in 21 us; the joins take 4 to 13 us.
 #include "cf_mm_run.h"
 #include "cf_rows.h"
 

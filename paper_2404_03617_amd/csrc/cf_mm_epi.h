@@ -378,10 +378,10 @@ struct Lse {
     }
 };
 
-// --- logits again: their gradients, c p + g 1[token], times a power of two ----
+// --- logits again: their gradients, c p and another at the token, times a power of two
 struct RowGrad {
-    float c, g, lse;  // all 0 (and what multiplies them skipped) for a row without a gradient
-    int token;
+    float c, at, lse;  // c and at are 0 (and what multiplies them skipped) for a row without a gradient
+    int token;         // or -1
 };
 struct DzArgs {
     const RowGrad *rows;
@@ -402,7 +402,7 @@ struct Dz {
     static __device__ __forceinline__ void piece(const DzArgs &e, const RowGrad &r, const float (&z)[8], int m, int n, int N,
                                                  bool mine, bool ends) {
         const int want = r.token - e.v0;
-        const bool any = !(r.c == 0.0f && r.g == 0.0f);
+        const bool any = !(r.c == 0.0f && r.at == 0.0f);
         float d[8];
 #pragma unroll
         for (int k = 0; k < 8; k++) {
@@ -412,7 +412,7 @@ struct Dz {
         if (mine)
 #pragma unroll
             for (int k = 0; k < 8; k++)
-                d[k] += any && n + k == want ? r.g : 0.0f;
+                d[k] = any && n + k == want ? r.at : d[k];
         if (ends)
 #pragma unroll
             for (int k = 0; k < 8; k++)

@@ -524,17 +524,18 @@ PyObject *linear(PyObject *const *a, Py_ssize_t n) {
 
 // (x, weight, tokens or None, lse, d_logp, d_lse, out) -> (dx, dweight)
 PyObject *linear_backward(PyObject *const *a, Py_ssize_t n) {
-    must(n == 7 && a[3] != Py_None);
+    must(n == 8 && a[4] != Py_None);
     const RowsOf x = rows_of(a[0], 2);
     on_current(*x.t);
     const RowsOf w = matrix_of(a[1], x, -1, x.C);
     const int64_t *tokens = flat_of<const int64_t>(a[2], *x.t, at::kLong, x.n, 0);
-    const float *lse = floats(a[3], *x.t, x.n), *gl = floats(a[4], *x.t, x.n), *gs = floats(a[5], *x.t, x.n);
-    const Out dx = out_of(a[6], *x.t, x.code);
+    const float *logp = floats(a[3], *x.t, x.n), *lse = floats(a[4], *x.t, x.n);
+    const float *gl = floats(a[5], *x.t, x.n), *gs = floats(a[6], *x.t, x.n);
+    const Out dx = out_of(a[7], *x.t, x.code);
     const at::Tensor dw = fresh(*x.t, {w.n, x.C}, type_of(x.code));
     const Workspace ws(*x.t, lib.linear_backward_ws(x.n, x.C, (int)w.n, readable(x) && readable(w)));
-    check(lib.linear_backward(x.p, w.p, tokens, lse, gl, gs, dx.p, dw.data_ptr(), ws.p, ws.bytes, x.n, x.C, (int)w.n,
-                              x.ld, w.ld, dx.ld, (cf_dtype)x.code, stream()));
+    check(lib.linear_backward(x.p, w.p, tokens, logp, lse, gl, gs, dx.p, dw.data_ptr(), ws.p, ws.bytes, x.n, x.C,
+                              (int)w.n, x.ld, w.ld, dx.ld, (cf_dtype)x.code, stream()));
     return give_all(dx.t, dw);
 }
 

@@ -307,18 +307,18 @@ def linear_log_probs_workspace_bytes(rows: int, C: int, V: int, aligned: bool = 
 def linear_log_probs_backward(x: torch.Tensor, weight: torch.Tensor, tokens, lp: LinearLogProbs, d_logp=None,
                               d_lse=None, out=None, ws=None, stream=None):
     """The gradients (dx, dweight), in x's dtype, of sum(d_logp * lp.logp) +
-    sum(d_lse * lp.lse); lp is what linear_log_probs_forward returned, d_logp and
-    d_lse fp32 [...] or None.  Rows without a gradient (both 0, or d_logp of a
+    sum(d_lse * lp.lse); lp is what linear_log_probs_forward returned (for d_logp,
+    with these tokens), d_logp and d_lse fp32 [...] or None.  Rows without a gradient (both 0, or d_logp of a
     negative token) add nothing to dweight, whatever their features hold.  ws: a
     uint8 workspace of linear_log_probs_backward_workspace_bytes()."""
     if stream is None and ws is None and type(lp) is LinearLogProbs:
-        r = _native("linear_backward", x, weight, tokens, lp.lse, d_logp, d_lse, out)
+        r = _native("linear_backward", x, weight, tokens, lp.logp, lp.lse, d_logp, d_lse, out)
         if r is not None:
             return r
     xp, rows, C, ldx, code = _rows("x", x, 2)
     V, (w, ldw) = _classifier(x, weight, C, code)
     tp = _flat("tokens", x, tokens, 4, rows, 0)
-    sp = _some("lp.lse", x, lp.lse, 2, rows, 0)
+    pp, sp = _flat("lp.logp", x, lp.logp, 2, rows, 0), _some("lp.lse", x, lp.lse, 2, rows, 0)
     gl, gs = _flat("d_logp", x, d_logp, 2, rows, 0), _flat("d_lse", x, d_lse, 2, rows, 0)
     with _on(x):
         dx, dxp, lddx = _out_rows(x, out, x.shape, code, stream)
@@ -326,8 +326,8 @@ def linear_log_probs_backward(x: torch.Tensor, weight: torch.Tensor, tokens, lp:
         L = _cf.lib()
         need = L.cf_linear_log_probs_backward_workspace_bytes(rows, C, V, _readable((xp, ldx), (w, ldw)))
         keep, wp, nbytes = _ws(x, ws, need, stream)
-        _cf._check(L.cf_linear_log_probs_backward(xp, w, tp, sp, gl, gs, dxp, dw.data_ptr(), wp, nbytes, rows, C, V,
-                                                  ldx, ldw, lddx, code, _cf._stream(stream)))
+        _cf._check(L.cf_linear_log_probs_backward(xp, w, tp, pp, sp, gl, gs, dxp, dw.data_ptr(), wp, nbytes, rows, C,
+                                                  V, ldx, ldw, lddx, code, _cf._stream(stream)))
     return dx, dw
 
 

@@ -125,14 +125,15 @@ def test_linear_log_probs_forward_rejects(kw, status):
     assert status_of("cf_linear_log_probs_forward", LINEAR, kw) == status
 
 
-LINEAR_BACK = dict(x=A, w=B, tokens=C1, lse=S, gl=G1, gs=G2, dx=OUT, dw=O2, ws=WS, nbytes=BIG, rows=50, C=64, V=1000,
+LINEAR_BACK = dict(x=A, w=B, tokens=C1, logp=C2, lse=S, gl=G1, gs=G2, dx=OUT, dw=O2, ws=WS, nbytes=BIG, rows=50, C=64, V=1000,
                    ldx=64, ldw=64, lddx=64, dt=0)
 
 
 @needs_library
 @pytest.mark.parametrize("kw,status", [
     (dict(x=None), INVALID), (dict(w=None), INVALID), (dict(lse=None), INVALID), (dict(dx=None), INVALID),
-    (dict(dw=None), INVALID), (dict(gl=None, gs=None), INVALID), (dict(tokens=None), INVALID), (dict(lddx=63), INVALID),
+    (dict(dw=None), INVALID), (dict(gl=None, gs=None), INVALID), (dict(tokens=None), INVALID), (dict(logp=None), INVALID), (dict(lddx=63), INVALID),
+    (dict(logp=C2 + 2), INVALID), (dict(dx=C2), INVALID),
     (dict(dx=A), INVALID), (dict(dw=B), INVALID), (dict(dw=OUT), INVALID), (dict(dx=G1), INVALID),
     (dict(gs=G2 + 2), INVALID), (dict(ws=None, nbytes=0), WORKSPACE), (dict(ws=WS + 8), INVALID),
     (dict(ws=O2), INVALID), (dict(rows=1 << 30), UNSUPPORTED), (dict(rows=0, dw=None), INVALID),

@@ -79,6 +79,7 @@ def test_native_calls_accept_and_refuse_alike(name, monkeypatch):
     if "lp" in args:
         lp = args["lp"]
         variants += [{**args, "lp": cf.LinearLogProbs(lp.logp, s)} for s in spoiled(lp.lse)]
+        variants += [{**args, "lp": cf.LinearLogProbs(s, lp.lse)} for s in spoiled(lp.logp)]
         variants += [{**args, "d_logp": None}, {**args, "d_lse": None}, {**args, "d_logp": None, "d_lse": None},
                      {**args, "tokens": None, "d_logp": None}]
     cf.lib()

@@ -221,6 +221,37 @@ def test_leading_dimensions_workspaces_and_no_rows():
     assert a.shape == (0, 64) and b.shape == (104, 64) and bool((b == 0).all())
 
 
+@pytest.mark.parametrize("rows", [1, 5, 40])
+def test_tokens_that_are_nearly_certain(rows):
+    """What a gradient has left where 1 - p is 1e-3 to 4e-7.  Off in fp32: at the token,
+    10 additions to a sum of 1 at most, half a unit of 1 each, and with the rest the
+    errors of its logits; elsewhere, relative to p, those of two logits, lse (17,
+    rounded) and the exponential's argument (17 times two roundings)."""
+    dt, C, V = torch.float16, 48, 10
+    w = randn(1, (V, C), dt, C**-0.5)
+    t = torch.arange(rows) % V
+    gap = torch.linspace(16.8, 9, rows).double()
+    wd = w.double()
+    x = (gap[:, None] * torch.linalg.pinv(wd).t()[t]).to(dt)  # logits: the gap at the token, 0 elsewhere
+    gl, xd = -1000.0 * torch.ones(rows), x.double()
+    z, ez = mm(xd, wd.t()), C * F32 * mm(xd.abs(), wd.abs().t()).amax(1)
+    at = torch.zeros(rows, V, dtype=torch.bool).scatter(1, t[:, None], True)
+    logp = torch.log_softmax(z, 1)
+    rest = -torch.expm1(logp[at])
+    assert 2e-7 < float(rest.min()) < 1e-6 and float(rest.max()) < 0.01
+    dz = 1000 * logp.exp()
+    dz[at] = -1000 * rest
+    edz = dz.abs() * (2 * ez[:, None] + 66 * F32)
+    edz[at] = 1000 * (10 * F32 + rest * (2 * ez + 10 * F32))
+    edz = edz + ROUND[dt] * (dz.abs() + edz)
+    lp = cf.linear_log_probs_forward(x.cuda(), w.cuda(), t.cuda())
+    dx, dw = cf.linear_log_probs_backward(x.cuda(), w.cuda(), t.cuda(), lp, gl.cuda())
+    for got, a, b, ea, n, what in ((dx, dz, wd, edz, V, "dx"), (dw, dz.t(), xd, edz.t(), rows, "dw")):
+        want = mm(a, b)
+        e = mm(ea, b.abs()) + (n + 2) * F32 * mm(a.abs(), b.abs())
+        assert_within(got, want, e + ROUND[dt] * (want.abs() + e) + TINY[dt], what)
+
+
 def test_agrees_with_log_probs_of_the_logits():
     x, w, t, gl, _ = (v.cuda() for v in case(17, 200, 64, 1000, torch.bfloat16))
     z = x.float() @ w.float().t()

@@ -82,26 +82,15 @@ struct Lse {
     static __device__ __forceinline__ void run(const Extra &e, const float4v (&sum)[FN], const Args &a, int n0, int lane) {
         const int m = lane & 15;
         const int64_t want = e.tokens && m < a.M ? e.tokens[m] : -1;
-        float top = -INFINITY;
-        float z[FN][4];
+        float z[4 * FN];
 #pragma unroll
-        for (int f = 0; f < FN; f++)
-#pragma unroll
-            for (int k = 0; k < 4; k++) {
-                const int n = n0 + 16 * f + 4 * (lane >> 4) + k;
-                z[f][k] = n < a.N ? sum[f][k] : -INFINITY;
-                if (n == want)
-                    e.picked[m] = z[f][k];
-                top = fmaxf(top, z[f][k]);
-            }
-        const float base = top == -INFINITY ? 0.0f : top;
-        float s = 0.0f;
-#pragma unroll
-        for (int f = 0; f < FN; f++)
-#pragma unroll
-            for (int k = 0; k < 4; k++)
-                s += __builtin_amdgcn_exp2f((z[f][k] - base) * mm::LOG2E);
-        float2 r = make_float2(top, s);
+        for (int k = 0; k < 4 * FN; k++) {
+            const int n = n0 + 16 * (k / 4) + 4 * (lane >> 4) + k % 4;
+            z[k] = n < a.N ? sum[k / 4][k % 4] : -INFINITY;
+            if (n == want)
+                e.picked[m] = z[k];
+        }
+        float2 r = mm::sum_exp(z);
         r = mm::join_lse(r, make_float2(__shfl_xor(r.x, 16), __shfl_xor(r.y, 16)));
         r = mm::join_lse(r, make_float2(__shfl_xor(r.x, 32), __shfl_xor(r.y, 32)));
         if (lane < a.M && lane < 16)

@@ -50,7 +50,7 @@ template <int L>
 __global__ __launch_bounds__(256) void join_lse_kernel(const float2 *part, const float *picked, const int64_t *tokens,
                                                        float *logp, float *lse, int rows, int V, int parts) {
     const int lane = threadIdx.x % L, r = blockIdx.x * (256 / L) + threadIdx.x / L;
-    float2 v = make_float2(-INFINITY, 0.0f);
+    float2 v = make_float2(-INFINITY, -1.0f);
     if (r < rows)
 #pragma unroll 4
         for (int i = lane; i < parts; i += L)
@@ -67,7 +67,7 @@ __global__ __launch_bounds__(256) void join_lse_kernel(const float2 *part, const
     }
     if (lane || r >= rows)
         return;
-    const float ls = logf(v.y);
+    const float ls = log1pf(v.y);
     lse[r] = v.x + ls;
     if (logp) {
         const int64_t t = tokens[r];

@@ -132,7 +132,7 @@ __global__ __launch_bounds__(JOIN_CLASSES / 8) void join_kernel(Args a, const fl
     __shared__ float2 s[WAVES];
     const int m = (int)(blockIdx.x / (unsigned)chunks), chunk = (int)(blockIdx.x - (unsigned)m * chunks),
               n = chunk * JOIN_CLASSES + threadIdx.x * 8;
-    float2 r = make_float2(-INFINITY, 0.0f);
+    float2 r = make_float2(-INFINITY, -1.0f);
     if (n < a.N) {
         const int64_t want = e.tokens ? e.tokens[m] : -1;
         float z[8];
@@ -143,12 +143,8 @@ __global__ __launch_bounds__(JOIN_CLASSES / 8) void join_kernel(Args a, const fl
                 z[k] = -INFINITY;
             else if (n + k == want)
                 e.picked[m] = z[k];
-            r.x = fmaxf(r.x, z[k]);
         }
-        const float base = r.x == -INFINITY ? 0.0f : r.x;
-#pragma unroll
-        for (int k = 0; k < 8; k++)
-            r.y += __builtin_amdgcn_exp2f((z[k] - base) * LOG2E);
+        r = sum_exp(z);
     }
 #pragma unroll
     for (int d = 1; d < 64; d *= 2)

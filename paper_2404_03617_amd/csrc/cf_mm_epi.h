@@ -291,6 +291,8 @@ struct GatedBack {
 };
 
 // --- logits: largest and sum of exp(z - largest) of each row in the tile -------
+// A sum is kept without the 1 of its largest term (-1: without any term), which
+// would hide what is left where a class is nearly certain.
 struct LseArgs {
     float2 *part;  // [tiles_n][M]
     float *picked;  // [M]: the logit of the row's token
@@ -300,9 +302,28 @@ struct LseArgs {
 constexpr float LOG2E = 1.44269504088896f;
 
 __device__ __forceinline__ float2 join_lse(float2 a, float2 b) {
-    const float m = fmaxf(a.x, b.x), base = m == -INFINITY ? 0.0f : m;
-    return make_float2(m, a.y * __builtin_amdgcn_exp2f((a.x - base) * LOG2E) +
-                              b.y * __builtin_amdgcn_exp2f((b.x - base) * LOG2E));
+    const bool first = a.x >= b.x;  // NaN: either way it stays
+    const float2 hi = first ? a : b, lo = first ? b : a;
+    const float base = hi.x == -INFINITY ? 0.0f : hi.x;
+    return make_float2(hi.x, fmaf(1.0f + lo.y, __builtin_amdgcn_exp2f((lo.x - base) * LOG2E), hi.y));
+}
+// of N logits, exactly
+template <int N>
+__device__ __forceinline__ float2 sum_exp(const float (&z)[N]) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < N; k++)
+        top = fmaxf(top, z[k]);
+    const float base = top == -INFINITY ? 0.0f : top;
+    float rest = 0.0f, ones = 0.0f;
+#pragma unroll
+    for (int k = 0; k < N; k++) {
+        const float e = __builtin_amdgcn_exp2f((z[k] - base) * LOG2E);
+        const bool one = z[k] == base;
+        rest += one ? e - 1.0f : e;  // NaN at +inf
+        ones += one ? 1.0f : 0.0f;
+    }
+    return make_float2(top, rest + (top == -INFINITY ? -1.0f : ones - 1.0f));
 }
 
 struct Lse {
@@ -324,43 +345,39 @@ struct Lse {
             const int m = m0 + 16 * i + (lane & 15);
             const int64_t want = e.tokens && m < a.M ? e.tokens[m] : -1;
             const bool here = want >= n0 && want < n0 + COLUMNS && want < a.N;
-            float z[PIECES][W];
+            constexpr int N = PIECES * W;
+            float z[N];
 #pragma unroll
-            for (int p = 0; p < PIECES; p++)
-#pragma unroll
-                for (int k = 0; k < W; k++)
-                    z[p][k] = t.get(i, p, k);
+            for (int k = 0; k < N; k++)
+                z[k] = t.get(i, k / W, k % W);
+            auto at_column = [&](int k) { return n0 + t.column(k / W, lane) + k % W; };
             // Both seldom, and the same for a wave: two comparisons a logit less.
             if (n0 + COLUMNS > a.N)
 #pragma unroll
-                for (int p = 0; p < PIECES; p++)
-#pragma unroll
-                    for (int k = 0; k < W; k++)
-                        if (n0 + t.column(p, lane) + k >= a.N)
-                            z[p][k] = -INFINITY;
+                for (int k = 0; k < N; k++)
+                    if (at_column(k) >= a.N)
+                        z[k] = -INFINITY;
             if (__any(here))
 #pragma unroll
-                for (int p = 0; p < PIECES; p++)
-#pragma unroll
-                    for (int k = 0; k < W; k++)
-                        if (here && n0 + t.column(p, lane) + k == want)
-                            e.picked[m] = z[p][k];
+                for (int k = 0; k < N; k++)
+                    if (here && at_column(k) == want)
+                        e.picked[m] = z[k];
             float top = -INFINITY;
 #pragma unroll
-            for (int p = 0; p < PIECES; p++)
-#pragma unroll
-                for (int k = 0; k < W; k++)
-                    top = fmaxf(top, z[p][k]);
+            for (int k = 0; k < N; k++)
+                top = fmaxf(top, z[k]);
             const float base = top == -INFINITY ? 0.0f : top;
-            float sum = 0.0f;
+            float sum = -1.0f;
 #pragma unroll
-            for (int p = 0; p < PIECES; p++)
-#pragma unroll
-                for (int k = 0; k < W; k++)
-                    sum += __builtin_amdgcn_exp2f((z[p][k] - base) * LOG2E);
-            float2 r = make_float2(top, sum);
-            r = join_lse(r, make_float2(__shfl_xor(r.x, 16), __shfl_xor(r.y, 16)));
-            r = join_lse(r, make_float2(__shfl_xor(r.x, 32), __shfl_xor(r.y, 32)));
+            for (int k = 0; k < N; k++)
+                sum += __builtin_amdgcn_exp2f((z[k] - base) * LOG2E);
+            auto over_lanes = [&](float2 r) {
+                r = join_lse(r, make_float2(__shfl_xor(r.x, 16), __shfl_xor(r.y, 16)));
+                return join_lse(r, make_float2(__shfl_xor(r.x, 32), __shfl_xor(r.y, 32)));
+            };
+            float2 r = over_lanes(make_float2(top, sum));
+            if (__any(r.y < 0x1p-8f))  // a row with one large logit, the same for a wave: as exactly as it goes
+                r = over_lanes(sum_exp(z));
             if (lane < 16)
                 row[wn * S::TM + local + 16 * i + lane] = r;
         }

@@ -9,14 +9,15 @@ using namespace gnorm;
 
 namespace {
 
-// dweight and dbias: 16 lanes a channel add the images' parts, then each other
-__global__ __launch_bounds__(256) void params_kernel(const float2 *part, int64_t parts, int C, float *dw, float *db) {
-    __shared__ float2 s[16][17];
+// dweight and dbias: L lanes a channel add the images' parts, then each other
+template <int L>
+__global__ __launch_bounds__(16 * L) void params_kernel(const float2 *part, int64_t parts, int C, float *dw, float *db) {
+    __shared__ float2 s[L][17];
     const int c = blockIdx.x * 16 + (threadIdx.x & 15), l = threadIdx.x >> 4;
     float2 v = make_float2(0.0f, 0.0f);
     if (c < C)
 #pragma unroll 4
-        for (int64_t i = l; i < parts; i += 16) {
+        for (int64_t i = l; i < parts; i += L) {
             const float2 p = part[i * C + c];
             v.x += p.x;
             v.y += p.y;
@@ -25,7 +26,7 @@ __global__ __launch_bounds__(256) void params_kernel(const float2 *part, int64_t
     __syncthreads();
     if (threadIdx.x < 16 && c < C) {
         float2 r = s[0][threadIdx.x];
-        for (int i = 1; i < 16; i++) {
+        for (int i = 1; i < L; i++) {
             r.x += s[i][threadIdx.x].x;
             r.y += s[i][threadIdx.x].y;
         }
@@ -113,8 +114,12 @@ hipError_t launch_group_norm_backward(const GroupNorm &g, const void *dy, int64_
     }
     if (!dweight)
         return hipSuccess;
-    params_kernel<<<dim3((unsigned)((g.C + 15) / 16)), 256, 0, st>>>((const float2 *)ws, some ? g.N * p.chunks : 0, g.C,
-                                                                     dweight, dbias);
+    const int64_t parts = some ? g.N * p.chunks : 0;
+    const dim3 grid((unsigned)((g.C + 15) / 16));
+    if (parts < 512)
+        params_kernel<16><<<grid, 256, 0, st>>>((const float2 *)ws, parts, g.C, dweight, dbias);
+    else  // (20000 images of 64 channels 36 us against 105)
+        params_kernel<64><<<grid, 1024, 0, st>>>((const float2 *)ws, parts, g.C, dweight, dbias);
     return hipGetLastError();
 }
 

@@ -143,6 +143,18 @@ def test_linear_log_probs_backward_rejects(kw, status):
 
 
 @needs_library
+def test_launches_of_more_than_32_bits_are_refused():
+    """Rows, classes and images whose launches would have 2^32 threads."""
+    big = dict(C=8, ldx=8, ldw=8)
+    assert status_of("cf_linear_log_probs_forward", LINEAR, dict(rows=1, V=1 << 28, **big)) == UNSUPPORTED
+    assert status_of("cf_linear_log_probs_forward", LINEAR, dict(rows=1 << 28, V=10, **big)) == UNSUPPORTED
+    big["lddx"] = 8
+    assert status_of("cf_linear_log_probs_backward", LINEAR_BACK, dict(rows=1 << 28, V=10, **big)) == UNSUPPORTED
+    assert status_of("cf_group_norm_forward", NORM, dict(N=1 << 25, P=1, G=64)) == UNSUPPORTED
+    assert cf.lib().cf_linear_log_probs_workspace_bytes(1, 8, (1 << 28) - 1, 1) > 0
+
+
+@needs_library
 def test_silu_is_of_these_operators_alone():
     """The activations of training keep their list."""
     assert cf.lib().cf_act_forward(A, B, C1, C2, None, None, 4, 70, 70, 70, 0, 3, None) == INVALID

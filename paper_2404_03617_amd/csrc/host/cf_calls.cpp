@@ -522,7 +522,7 @@ PyObject *linear(PyObject *const *a, Py_ssize_t n) {
     return give_all(logp, lse);
 }
 
-// (x, weight, tokens or None, lse, d_logp, d_lse, out) -> (dx, dweight)
+// (x, weight, tokens or None, logp or None, lse, d_logp, d_lse, out) -> (dx, dweight)
 PyObject *linear_backward(PyObject *const *a, Py_ssize_t n) {
     must(n == 8 && a[4] != Py_None);
     const RowsOf x = rows_of(a[0], 2);

@@ -267,15 +267,20 @@ struct GatedBack {
         with_act(e.act, [&](auto tag) {
             constexpr int COUNT = S::FM * PIECES;
             float g[2][8], u[2][8];
-            // piece j of the wave's, whose g and u are read while the one before is worked on
+            // piece j of the wave's, whose g and u are read while the one before is worked on, but
+            // for large tiles, whose registers spill then (8192 x 4096 x 1024 175 us, ahead 183)
+            constexpr bool AHEAD = S::TM < 256;
             auto ask = [&](int j) {
                 const int m = m0 + 16 * (j / PIECES) + (lane & 15), n = n0 + t.column(j % PIECES, lane);
                 read(e, m, n, m < a.M ? e.H - n : 0, g[j % 2], u[j % 2]);
             };
-            ask(0);
+            if (AHEAD)
+                ask(0);
 #pragma unroll
             for (int j = 0; j < COUNT; j++) {
-                if (j + 1 < COUNT)
+                if (!AHEAD)
+                    ask(j);
+                else if (j + 1 < COUNT)
                     ask(j + 1);
                 const int m = m0 + 16 * (j / PIECES) + (lane & 15), n = n0 + t.column(j % PIECES, lane);
                 if (m >= a.M || n >= e.pad)
@@ -285,6 +290,8 @@ struct GatedBack {
                 for (int k = 0; k < 8; k++)
                     dh[k] = t.get(j / PIECES, j % PIECES, k);
                 piece<T, decltype(tag)::value>(e, dh, g[j % 2], u[j % 2], m, n);
+                if (!AHEAD)
+                    __builtin_amdgcn_sched_barrier(0);
             }
         });
     }

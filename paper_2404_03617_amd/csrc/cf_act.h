@@ -22,20 +22,19 @@ struct ActPair {
 template <int ACT>
 __device__ __forceinline__ ActPair act_pair(float u) {
     if constexpr (ACT == ACT_GELU) {
-        const float v = u < -32.0f ? -32.0f : u > 32.0f ? 32.0f : u;  // where the exponential is 0
-        const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(v), 0.32f, 1.0f));
+        const float v = __builtin_amdgcn_fmed3f(u, -32.0f, 32.0f);  // where the exponential is 0
+        const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(u), 0.32f, 1.0f));
         float q = fmaf(-0.129858347f, t, 0.495794653f);
         q = fmaf(q, t, -0.265561934f);
         q = fmaf(q, t, 0.314940331f);
         q = fmaf(q, t, 0.079603797f);
         q = fmaf(q, t, 0.005081451f);
-        const float e = __builtin_amdgcn_exp2f(v * v * -0.721347520f), tail = q * e;
-        return {fmaf(-fabsf(v), tail, u < 0.0f ? 0.0f : u), fmaf(v, e * 0.398942280f, v > 0.0f ? 1.0f - tail : tail)};
+        const float e = __builtin_amdgcn_exp2f(u * u * -0.721347520f), tail = q * e;  // NaN where u is
+        return {fmaf(-fabsf(v), tail, fmaxf(u, 0.0f)), fmaf(v, e * 0.398942280f, v > 0.0f ? 1.0f - tail : tail)};
     } else if constexpr (ACT == ACT_SILU) {
-        const float v = u < -128.0f ? -128.0f : u;
-        const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v * -1.44269504f));
-        const float f = v * s;
-        return {f, fmaf(f, v > 128.0f ? 0.0f : 1.0f - s, s)};
+        const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u * -1.44269504f));  // NaN where u is
+        const float f = fmaxf(u, -128.0f) * s;
+        return {f, fmaf(fminf(f, 128.0f), 1.0f - s, s)};
     } else if constexpr (ACT == ACT_RELU) {
         return {u < 0.0f ? 0.0f : u, u > 0.0f ? 1.0f : u <= 0.0f ? 0.0f : u};
     } else {

@@ -564,8 +564,9 @@ size_t cf_group_norm_backward_workspace_bytes(int64_t N, int64_t P, int C, int G
 /* Gated feed-forward block, x and y [rows][C]:
  *   a = x w_gate^T,  u = x w_up^T,  h = act(a) * u,  y = h w_down^T
  * w_gate, w_up [H][C] and w_down [C][H] in dt, rows ld_* apart.  Sums are fp32; h is
- * rounded to dt for its product.  saved [rows][2 H] fp32 receives a and u of each
- * row for the backward pass; NULL for inference.  y may not overlap x. */
+ * rounded to dt for its product, or for up to 16 rows kept in two numbers of dt.
+ * saved [rows][2 H] fp32 receives a and u of each row for the backward pass; NULL
+ * for inference.  y may not overlap x. */
 cf_status cf_gated_ffn_forward(const void *x, const void *w_gate, const void *w_up, const void *w_down, void *y,
                                float *saved, void *ws, size_t ws_bytes, int64_t rows, int C, int H, int64_t ldx,
                                int64_t ld_gate, int64_t ld_up, int64_t ld_down, int64_t ldy, cf_dtype dt, cf_act act,
@@ -576,7 +577,8 @@ size_t cf_gated_ffn_workspace_bytes(int64_t rows, int C, int H, int aligned);
  *   dh = dy w_down,  da = dh * u * act'(a),  du = dh * act(a)
  *   dx = da w_gate + du w_up
  *   dw_gate = da^T x,  dw_up = du^T x,  dw_down = dy^T h
- * da, du and h are rounded to dt for their products.  dw_gate, dw_up [H][C] and
+ * da, du and h are rounded to dt for their products, or for up to 16 rows kept in two
+ * numbers of dt.  dw_gate, dw_up [H][C] and
  * dw_down [C][H] in dt, dense; rows = 0 gives zeros.  No output may overlap an
  * input. */
 cf_status cf_gated_ffn_backward(const void *dy, const void *x, const float *saved, const void *w_gate, const void *w_up,
@@ -586,8 +588,8 @@ cf_status cf_gated_ffn_backward(const void *dy, const void *x, const float *save
 size_t cf_gated_ffn_backward_workspace_bytes(int64_t rows, int C, int H, int aligned);
 
 /* Log probabilities from features x [rows][C] and a classifier's weight [V][C]
- * in dt, without its logits z = x weight^T, which stay in fp32 and are never
- * stored:
+ * in dt, without its logits z = x weight^T, which stay in fp32 and are not kept
+ * (parts of split sums of few rows' pass through the workspace, 128 MiB at most):
  *   lse[r] = log sum_v exp(z[r][v])
  *   logp[r] = z[r][token] - lse[r]   (tokens, logp: both or neither NULL; 0 for a
  *             negative token, NaN for one of V or more)
@@ -605,7 +607,8 @@ size_t cf_linear_log_probs_workspace_bytes(int64_t rows, int C, int V, int align
  * At the token, p = exp(logp) and 1 - p = -expm1(logp), which keeps what is left of
  * a gradient where p is nearly 1.
  * The logits are made again, a piece of the vocabulary at a time (dz of a piece,
- * in dt, is in the workspace: 256 MiB, or rows * 8 KiB if that is more); in fp16 dz
+ * in dt, or for up to 16 rows in two numbers of dt, is in the workspace: 256 MiB, or
+ * rows * 8 KiB if that is more); in fp16 dz
  * is scaled by a power of two a row, so that small probabilities keep their
  * bits.  Rows whose d_logp and d_lse are 0 (d_logp counts as 0 for a negative token)
  * or whose lse is -inf have no gradient and add nothing to dweight, whatever

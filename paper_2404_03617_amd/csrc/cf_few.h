@@ -7,7 +7,7 @@
 // The rows of x come from the caches.  Rows may start anywhere and have any length:
 // what is left of k goes element by element.  The waves' sums meet in LDS in a fixed order,
 // and the first wave does what follows.  1 x 131072 x 4096 takes 182 us, 5.9 TB/s; a
-// gated block of 1 x 4096 x 12288 59 us, 5.1 TB/s.
+// gated block of 1 x 4096 x 12288 62 us, 4.8 TB/s (58 without the second number of h).
 #pragma once
 
 #include "cf_mm_epi.h"
@@ -22,7 +22,7 @@ constexpr int ROWS = 16;  // rows of x at most
 
 struct Args {
     const uint16_t *x, *w[2];
-    int64_t ldx, ldw[2];
+    int64_t ldx, ldw[2], lo;  // lo: from x to what rounding it took, where a kernel has that
     int M, N, K;
 };
 
@@ -41,7 +41,7 @@ __device__ __forceinline__ u32x4 load_k(const uint16_t *p, int left) {
 // What follows gets `sum(f)`, the four results of fragment f in row lane % 16 of x:
 // rows n0 + 16 f + 4 (lane / 16) .. + 3 of W (DUAL: of either matrix, n0 alone).
 struct Gated {
-    static constexpr bool DUAL = true;
+    static constexpr bool DUAL = true, LO = false;
     using Extra = mm::GatedArgs;
     template <typename T, int FN>
     static __device__ __forceinline__ void run(const Extra &e, const float4v (&sum)[FN], const Args &a, int n0, int lane) {
@@ -56,12 +56,19 @@ struct Gated {
             for (int k = 0; k < 4; k++)
                 h[k] = k < left ? act_value<decltype(tag)::value>(sum[0][k]) * sum[1][k] : 0.0f;
             mm::store_row<T, 4>(e.h + m * e.ldh + n, h, 4);
+            const u32x4 r = {T::pack2(h[0], h[1]), T::pack2(h[2], h[3]), 0u, 0u};
+            float f[8];
+            unpack8<T>(r, f);
+#pragma unroll
+            for (int k = 0; k < 4; k++)
+                f[k] = fabsf(f[k]) < INFINITY ? h[k] - f[k] : 0.0f;
+            mm::store_row<T, 4>(e.h + e.lo + m * e.ldh + n, f, 4);
         });
     }
 };
 
 struct Store {
-    static constexpr bool DUAL = false;
+    static constexpr bool DUAL = false, LO = true;
     using Extra = mm::StoreArgs;
     template <typename T, int FN>
     static __device__ __forceinline__ void run(const Extra &e, const float4v (&sum)[FN], const Args &a, int n0, int lane) {
@@ -76,7 +83,7 @@ struct Store {
 };
 
 struct Lse {
-    static constexpr bool DUAL = false;
+    static constexpr bool DUAL = false, LO = false;
     using Extra = mm::LseArgs;
     template <typename T, int FN>
     static __device__ __forceinline__ void run(const Extra &e, const float4v (&sum)[FN], const Args &a, int n0, int lane) {
@@ -118,7 +125,7 @@ __global__ __launch_bounds__(WAVES * 64) void kernel(Args a, typename E::Extra e
     constexpr int U = 8 / FN, SHARE = U * 32;
     int k0 = wave * SHARE;
     for (; k0 + SHARE <= a.K; k0 += WAVES * SHARE) {
-        u32x4 fw[FN][U], fx[U];
+        u32x4 fw[FN][U], fx[U], fl[E::LO ? U : 1];
 #pragma unroll
         for (int f = 0; f < FN; f++)
 #pragma unroll
@@ -127,19 +134,32 @@ __global__ __launch_bounds__(WAVES * 64) void kernel(Args a, typename E::Extra e
 #pragma unroll
         for (int u = 0; u < U; u++)
             fx[u] = reinterpret_cast<const Any16 *>(x + k0 + 32 * u)->v;
+        if constexpr (E::LO)
+#pragma unroll
+            for (int u = 0; u < U; u++)
+                fl[u] = reinterpret_cast<const Any16 *>(x + a.lo + k0 + 32 * u)->v;
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int u = 0; u < U; u++)
 #pragma unroll
             for (int f = 0; f < FN; f++)
+            {
                 acc[f] = T::mfma(fw[f][u], fx[u], acc[f]);
+                if constexpr (E::LO)
+                    acc[f] = T::mfma(fw[f][u], fl[u], acc[f]);
+            }
     }
     for (; k0 < a.K; k0 += 32) {  // the wave that has the last share of k, where it is not whole
         const int left = a.K - k0 - q * 8;
         const u32x4 fx = load_k(x + k0, left);
 #pragma unroll
         for (int f = 0; f < FN; f++)
-            acc[f] = T::mfma(load_k(w[f] + k0, left), fx, acc[f]);
+        {
+            const u32x4 fw = load_k(w[f] + k0, left);
+            acc[f] = T::mfma(fw, fx, acc[f]);
+            if constexpr (E::LO)
+                acc[f] = T::mfma(fw, load_k(x + a.lo + k0, left), acc[f]);
+        }
     }
 #pragma unroll
     for (int f = 0; f < FN; f++)

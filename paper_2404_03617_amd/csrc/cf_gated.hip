@@ -47,7 +47,7 @@ struct ForwardPlan {
     Room room;
     Operand x, wg, wu, wd;
     int pad;
-    int64_t ld;  // of h
+    int64_t ld, lo;  // of h; to what rounding it takes, or 0
     uint16_t *h;
     Plan up, down;
     void *part;
@@ -63,10 +63,13 @@ ForwardPlan forward_plan(const GatedFfn &a, Copied c, void *ws) {
     p.wg = operand(a.w_gate.p, a.w_gate.ld, a.H, a.C, c.wgu, p.room);
     p.wu = operand(a.w_up.p, a.w_up.ld, a.H, a.C, c.wgu, p.room);
     p.wd = operand(a.w_down.p, a.w_down.ld, a.C, a.H, c.wd, p.room);
-    p.h = (uint16_t *)p.room.take((size_t)a.rows * p.ld * 2);
+    const bool lo = in_parts(a.rows);
+    const int64_t rows = lo ? 2 * a.rows : a.rows;
+    p.lo = lo ? a.rows * p.ld : 0;
+    p.h = (uint16_t *)p.room.take((size_t)rows * p.ld * 2);
     p.up = plan(a.rows, 2 * (int64_t)a.H, a.C, true, 1, 1, MORE);
-    p.down = plan(a.rows, a.C, a.H, true);
-    const size_t one = part_bytes(p.up, a.rows, a.H, 2), two = part_bytes(p.down, a.rows, a.C, 1);
+    p.down = plan(rows, a.C, a.H, true);
+    const size_t one = joined_bytes(p.up, a.rows, a.H, 2, lo), two = joined_bytes(p.down, rows, a.C, 1, lo);
     p.part = a.rows <= few::ROWS ? nullptr : p.room.take(one > two ? one : two);
     return p;
 }
@@ -75,7 +78,7 @@ struct BackwardPlan {
     Room room;
     Operand x, dy, wg, wu, wd;
     int pad;
-    int64_t ld;  // of h; d has two of them a row
+    int64_t ld, lo;  // of h; to what rounding it takes, or 0; d has two of them a row
     uint16_t *d, *h;
     Plan dh, dwd, dwu, dx;
     void *part;
@@ -90,18 +93,21 @@ BackwardPlan backward_plan(const GatedFfn &a, const RowsIn &dy, const Copied &c,
     p.wg = operand(a.w_gate.p, a.w_gate.ld, a.H, a.C, c.wgu, p.room);
     p.wu = operand(a.w_up.p, a.w_up.ld, a.H, a.C, c.wgu, p.room);
     p.wd = operand(a.w_down.p, a.w_down.ld, a.C, a.H, c.wd, p.room);
-    p.d = (uint16_t *)p.room.take((size_t)a.rows * 2 * p.ld * 2);
-    p.h = (uint16_t *)p.room.take((size_t)a.rows * p.ld * 2);
+    const bool lo = in_parts(a.rows);
+    const int64_t rows = lo ? 2 * a.rows : a.rows;
+    p.lo = lo ? a.rows * p.ld : 0;
+    p.d = (uint16_t *)p.room.take((size_t)rows * 2 * p.ld * 2);
+    p.h = (uint16_t *)p.room.take((size_t)rows * p.ld * 2);
     p.dh = plan(a.rows, a.H, a.C, true, 1, 1, GATE);
-    p.dwd = plan(a.C, a.H, a.rows, true);
-    p.dwu = plan(a.H, a.C, a.rows, true, 2);
-    p.dx = plan(a.rows, a.C, a.H, true, 1, 2);
+    p.dwd = plan(a.C, a.H, a.rows, true, 1, lo ? 2 : 1);
+    p.dwu = plan(a.H, a.C, a.rows, true, lo ? 1 : 2, lo ? 2 : 1);
+    p.dx = plan(rows, a.C, a.H, true, 1, 2);
     size_t part = part_bytes(p.dwd, a.C, a.H, 1);
-    const size_t two = part_bytes(p.dwu, a.H, a.C, 2), three = part_bytes(p.dx, a.rows, a.C, 1);
-    part = part > two ? part : two;
-    const size_t four = part_bytes(p.dh, a.rows, a.H, 1);
-    part = part > three ? part : three;
-    p.part = p.room.take(part > four ? part : four);
+    const size_t more[] = {part_bytes(p.dwu, a.H, a.C, lo ? 1 : 2), joined_bytes(p.dx, rows, a.C, 1, lo),
+                           joined_bytes(p.dh, a.rows, a.H, 1, lo)};
+    for (size_t m : more)
+        part = part > m ? part : m;
+    p.part = p.room.take(part);
     return p;
 }
 
@@ -112,16 +118,16 @@ hipError_t forward(const GatedFfn &a, const ForwardPlan &p, void *y, int64_t ldy
     CF_HIP(pack(p.wu, bf16, st));
     CF_HIP(pack(p.wd, bf16, st));
     if (a.rows <= few::ROWS) {
-        const few::Args up = {p.x.m.p, {p.wg.m.p, p.wu.m.p}, p.x.m.ld, {p.wg.m.ld, p.wu.m.ld}, a.rows, a.H, a.C};
-        CF_HIP((few::launch<T, 2, few::Gated>(up, GatedArgs{p.h, p.ld, saved, a.H, p.pad, a.act}, st)));
+        const few::Args up = {p.x.m.p, {p.wg.m.p, p.wu.m.p}, p.x.m.ld, {p.wg.m.ld, p.wu.m.ld}, 0, a.rows, a.H, a.C};
+        CF_HIP((few::launch<T, 2, few::Gated>(up, GatedArgs{p.h, p.ld, p.lo, saved, a.H, p.pad, a.act}, st)));
         StoreArgs s = {};
         s.out[0] = (uint16_t *)y;
         s.ldo = ldy;
-        const few::Args down = {p.h, {p.wd.m.p, p.wd.m.p}, p.ld, {p.wd.m.ld, p.wd.m.ld}, a.rows, a.C, a.H};
+        const few::Args down = {p.h, {p.wd.m.p, p.wd.m.p}, p.ld, {p.wd.m.ld, p.wd.m.ld}, p.lo, a.rows, a.C, a.H};
         return few::launch<T, 1, few::Store>(down, s, st);
     }
-    const GatedArgs gate = {p.h, p.ld, saved, a.H, p.pad, a.act};
-    const bool split = p.up.splits > 1;
+    const GatedArgs gate = {p.h, p.ld, p.lo, saved, a.H, p.pad, a.act};
+    const bool split = p.up.splits > 1 || p.lo;
     Args up = args_of(p.up, a.rows, split ? a.H : 2 * a.H, a.C, p.x.m, a.rows, p.wg.m, a.H, false, split ? 2 : 1);
     up.b[1] = p.wu.m.p;
     if (split)
@@ -131,8 +137,10 @@ hipError_t forward(const GatedFfn &a, const ForwardPlan &p, void *y, int64_t ldy
     StoreArgs s = {};
     s.out[0] = s.out[1] = (uint16_t *)y;
     s.ldo = ldy;
-    return run_store<KC, KC>(args_of(p.down, a.rows, a.C, a.H, Matrix{p.h, p.ld, p.pad}, a.rows, p.wd.m, a.C), s,
-                             p.down, p.part, bf16, st);
+    s.fold = p.lo ? a.rows : 0;
+    const int rows = p.lo ? 2 * a.rows : a.rows;
+    return run_store<KC, KC>(args_of(p.down, rows, a.C, a.H, Matrix{p.h, p.ld, p.pad}, rows, p.wd.m, a.C), s, p.down, p.part,
+                             bf16, st);
 }
 
 template <typename T>
@@ -146,28 +154,42 @@ hipError_t backward(const GatedFfn &a, const BackwardPlan &p, const float *saved
     const Matrix h = {p.h, p.ld, p.pad}, d = {p.d, 2 * p.ld, p.pad};
     if (a.rows > 0) {
         const Args dh = args_of(p.dh, a.rows, a.H, a.C, p.dy.m, a.rows, p.wd.m, p.wd.m.ext);
-        const GatedBackArgs e = {saved, p.d, p.h, p.ld, a.H, p.pad, a.act};
-        if (p.dh.splits > 1)
+        const GatedBackArgs e = {saved, p.d, p.h, p.ld, p.lo, a.H, p.pad, a.act};
+        if (p.dh.splits > 1 || p.lo)
             CF_HIP((run_split<KC, RC>(dh, e, p.dh, p.part, bf16, st)));
         else
             CF_HIP(launch_gated_back<T>(dh, e, p.dh.tile, st));
-        Args dx = args_of(p.dx, a.rows, a.C, a.H, d, a.rows, p.wg.m, p.wg.m.ext, true);
+        const int rows = p.lo ? 2 * a.rows : a.rows;
+        Args dx = args_of(p.dx, rows, a.C, a.H, d, rows, p.wg.m, p.wg.m.ext, true);
         dx.a[1] = p.d + p.ld;
         dx.b[1] = p.wu.m.p;
         StoreArgs s = {};
         s.out[0] = s.out[1] = (uint16_t *)g.dx;
         s.ldo = g.lddx;
+        s.fold = p.lo ? a.rows : 0;
         CF_HIP((run_store<KC, RC>(dx, s, p.dx, p.part, bf16, st)));
     }
     StoreArgs s = {};
     s.out[0] = s.out[1] = (uint16_t *)g.dw_down;
     s.ldo = a.H;
-    CF_HIP((run_store<RC, RC>(args_of(p.dwd, a.C, a.H, a.rows, p.dy.m, p.dy.m.ext, h, p.pad), s, p.dwd, p.part, bf16, st)));
+    Args down = args_of(p.dwd, a.C, a.H, a.rows, p.dy.m, p.dy.m.ext, h, p.pad, p.lo != 0);
+    down.b[1] = p.h + p.lo;
+    CF_HIP((run_store<RC, RC>(down, s, p.dwd, p.part, bf16, st)));
+    s.ldo = a.C;
+    if (p.lo) {
+        for (int i = 0; i < 2; i++) {
+            const Matrix di = {p.d + i * p.ld, 2 * p.ld, p.pad};
+            Args w = args_of(p.dwu, a.H, a.C, a.rows, di, p.pad, p.x.m, p.x.m.ext, true);
+            w.a[1] = di.p + 2 * p.lo;
+            s.out[0] = (uint16_t *)(i ? g.dw_up : g.dw_gate);
+            CF_HIP((run_store<RC, RC>(w, s, p.dwu, p.part, bf16, st)));
+        }
+        return hipSuccess;
+    }
     Args w = args_of(p.dwu, a.H, a.C, a.rows, d, p.pad, p.x.m, p.x.m.ext, false, 2);
     w.a[1] = p.d + p.ld;
     s.out[0] = (uint16_t *)g.dw_gate;
     s.out[1] = (uint16_t *)g.dw_up;
-    s.ldo = a.C;
     return run_store<RC, RC>(w, s, p.dwu, p.part, bf16, st);
 }
 

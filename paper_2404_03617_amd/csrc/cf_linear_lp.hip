@@ -205,18 +205,20 @@ BackwardPlan backward_plan(const LinearLogProbs &a, bool copy_x, bool copy_w, vo
     p.scale = (float *)p.room.take(4);
     p.most = (int *)p.room.take(EXPONENTS * 4);
     // Pieces of at least 4096 columns, all but the last a multiple of a tile.
-    const double most = PIECE_BYTES / (2.0 * (a.rows > 0 ? a.rows : 1));
+    const bool lo = in_parts(a.rows);
+    const int64_t rows = lo ? 2 * a.rows : a.rows;
+    const double most = (lo ? PART_BYTES / 2 : PIECE_BYTES) / (2.0 * (a.rows > 0 ? a.rows : 1));
     const int64_t at_most = most < 4096 ? 4096 : most > (1 << 30) ? 1 << 30 : (int64_t)most;
     p.pieces = (int)((a.V + at_most - 1) / at_most);
     p.piece = p.pieces == 1 ? a.V : ((a.V + p.pieces - 1) / p.pieces + 255) / 256 * 256;
     p.pieces = (a.V + p.piece - 1) / p.piece;
-    p.dz = (uint16_t *)p.room.take((size_t)a.rows * stride_of(p.piece) * 2);
+    p.dz = (uint16_t *)p.room.take((size_t)rows * stride_of(p.piece) * 2);
     p.acc = p.pieces > 1 ? (float *)p.room.take((size_t)a.rows * a.C * 4) : nullptr;
     p.z = plan(a.rows, p.piece, a.C, true, 1, 1, MORE);
-    p.dx = plan(a.rows, a.C, p.piece, true);
-    p.dw = plan(p.piece, a.C, a.rows, true);
-    const size_t one = part_bytes(p.dx, a.rows, a.C, 1), two = part_bytes(p.dw, p.piece, a.C, 1);
-    const size_t three = part_bytes(p.z, a.rows, p.piece, 1), most_of = one > two ? one : two;
+    p.dx = plan(rows, a.C, p.piece, true);
+    p.dw = plan(p.piece, a.C, a.rows, true, 1, lo ? 2 : 1);
+    const size_t one = joined_bytes(p.dx, rows, a.C, 1, lo), two = part_bytes(p.dw, p.piece, a.C, 1);
+    const size_t three = joined_bytes(p.z, a.rows, p.piece, 1, lo), most_of = one > two ? one : two;
     p.part = p.room.take(most_of > three ? most_of : three);
     return p;
 }
@@ -226,7 +228,7 @@ hipError_t forward(const LinearLogProbs &a, const ForwardPlan &p, float *logp, f
     CF_HIP(pack(p.x, bf16, st));
     CF_HIP(pack(p.w, bf16, st));
     const LseArgs e = {p.part, p.picked, logp ? a.tokens : nullptr};
-    const few::Args f = {p.x.m.p, {p.w.m.p, p.w.m.p}, p.x.m.ld, {p.w.m.ld, p.w.m.ld}, (int)a.rows, a.V, a.C};
+    const few::Args f = {p.x.m.p, {p.w.m.p, p.w.m.p}, p.x.m.ld, {p.w.m.ld, p.w.m.ld}, 0, a.rows, a.V, a.C};
     if (a.rows <= few::ROWS) {
         CF_HIP((few_of(a.rows) == 1 ? few::launch<T, 1, few::Lse>(f, e, st) : few::launch<T, 2, few::Lse>(f, e, st)));
     } else {
@@ -265,10 +267,11 @@ hipError_t backward(const LinearLogProbs &a, const BackwardPlan &p, const Linear
     for (int i = 0; i < p.pieces; i++) {
         const int v0 = i * p.piece, n = a.V - v0 < p.piece ? a.V - v0 : p.piece, pad = up8(n);
         const Matrix w = {p.w.m.p + (int64_t)v0 * p.w.m.ld, p.w.m.ld, p.w.m.ext}, dz = {p.dz, stride_of(n), pad};
+        const int64_t lo = in_parts(a.rows) ? a.rows * dz.ld : 0;
         if (a.rows > 0) {
             const Args z = args_of(p.z, a.rows, n, a.C, p.x.m, a.rows, w, n);
-            const DzArgs e = {p.rows, p.dz, dz.ld, pad, v0};
-            if (p.z.splits > 1)
+            const DzArgs e = {p.rows, p.dz, dz.ld, lo, pad, v0};
+            if (p.z.splits > 1 || lo)
                 CF_HIP((run_split<KC, KC>(z, e, p.z, p.part, bf16, st)));
             else
                 CF_HIP(launch_dz<T>(z, e, p.z.tile, st));
@@ -276,16 +279,20 @@ hipError_t backward(const LinearLogProbs &a, const BackwardPlan &p, const Linear
             s.out[0] = s.out[1] = (uint16_t *)g.dx;
             s.ldo = g.lddx;
             s.row_scale = bf16 ? nullptr : p.row_scale;
+            s.fold = lo ? a.rows : 0;
             s.acc = p.acc;
             s.acc_in = i > 0;
             s.acc_out = i + 1 < p.pieces;
-            CF_HIP((run_store<KC, RC>(args_of(p.dx, a.rows, a.C, n, dz, a.rows, w, w.ext), s, p.dx, p.part, bf16, st)));
+            const int rows = lo ? 2 * a.rows : a.rows;
+            CF_HIP((run_store<KC, RC>(args_of(p.dx, rows, a.C, n, dz, rows, w, w.ext), s, p.dx, p.part, bf16, st)));
         }
         StoreArgs s = {};
         s.out[0] = s.out[1] = (uint16_t *)g.dw + (int64_t)v0 * a.C;
         s.ldo = a.C;
         s.scale = bf16 || a.rows == 0 ? nullptr : p.scale;
-        CF_HIP((run_store<RC, RC>(args_of(p.dw, n, a.C, a.rows, dz, pad, xs, xs.ext), s, p.dw, p.part, bf16, st)));
+        Args dw = args_of(p.dw, n, a.C, a.rows, dz, pad, xs, xs.ext, lo != 0);
+        dw.a[1] = p.dz + lo;
+        CF_HIP((run_store<RC, RC>(dw, s, p.dw, p.part, bf16, st)));
     }
     return hipSuccess;
 }

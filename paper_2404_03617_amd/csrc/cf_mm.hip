@@ -42,17 +42,21 @@ __global__ __launch_bounds__(256) void join_kernel(Args a, StoreArgs e, int per_
     const int g = threadIdx.x % G;
     if (i >= n)  // whole groups of lanes
         return;
-    const int64_t row = i / per_row;  // of batch * M
-    const int batch = (int)(row / a.M), m = (int)(row - (int64_t)batch * a.M), c = (int)(i - row * per_row) * 4;
+    const int64_t row = i / per_row;  // of the batch's
+    const int rows = e.fold ? e.fold : a.M;
+    const int batch = (int)(row / rows), m = (int)(row - (int64_t)batch * rows), c = (int)(i - row * per_row) * 4;
     const int64_t step = (int64_t)a.batch * a.M * a.N;
     const float *p = e.part + ((int64_t)batch * a.M + m) * a.N + c;
     float4v v = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
-    for (int s = g; s < a.splits; s += G)
-    {
+    for (int s = g; s < a.splits; s += G) {
         float4v w;
         load_rowf<4>(p + s * step, w, a.N - c);
         v += w;
+        if (e.fold) {
+            load_rowf<4>(p + s * step + (int64_t)e.fold * a.N, w, a.N - c);
+            v += w;
+        }
     }
 #pragma unroll
     for (int d = 1; d < G; d *= 2)
@@ -66,7 +70,7 @@ __global__ __launch_bounds__(256) void join_kernel(Args a, StoreArgs e, int per_
 template <typename T>
 hipError_t join(const Args &a, const StoreArgs &e, hipStream_t st) {
     const int per_row = (a.N + 3) / 4;
-    const int64_t n = (int64_t)a.batch * a.M * per_row;
+    const int64_t n = (int64_t)a.batch * (e.fold ? e.fold : a.M) * per_row;
     if (n >= 65536 || a.splits < 8)
         join_kernel<T, 1><<<dim3((unsigned)((n + 255) / 256)), 256, 0, st>>>(a, e, per_row, n);
     else
@@ -101,7 +105,12 @@ __global__ __launch_bounds__(256) void join_kernel(Args a, const float *part, Ga
     float g[8], u[8];
     sum_parts(a, part, 0, m, n, g);
     sum_parts(a, part, 1, m, n, u);
-    with_act(e.act, [&](auto tag) { Gated::piece<T, decltype(tag)::value>(e, g, u, m, n, true); });
+    with_act(e.act, [&](auto tag) {
+        if (e.lo)
+            Gated::piece<T, decltype(tag)::value, true>(e, g, u, m, n, true);
+        else
+            Gated::piece<T, decltype(tag)::value>(e, g, u, m, n, true);
+    });
 }
 template <typename T>
 __global__ __launch_bounds__(256) void join_kernel(Args a, const float *part, GatedBackArgs e, FastDiv vectors,
@@ -113,7 +122,12 @@ __global__ __launch_bounds__(256) void join_kernel(Args a, const float *part, Ga
     float g[8], u[8], dh[8];
     GatedBack::read(e, m, n, e.H - n, g, u);
     sum_parts(a, part, 0, m, n, dh);
-    with_act(e.act, [&](auto tag) { GatedBack::piece<T, decltype(tag)::value>(e, dh, g, u, m, n); });
+    with_act(e.act, [&](auto tag) {
+        if (e.lo)
+            GatedBack::piece<T, decltype(tag)::value, true>(e, dh, g, u, m, n);
+        else
+            GatedBack::piece<T, decltype(tag)::value>(e, dh, g, u, m, n);
+    });
 }
 template <typename T>
 __global__ __launch_bounds__(256) void join_kernel(Args a, const float *part, DzArgs e, FastDiv vectors, uint32_t all) {
@@ -123,7 +137,10 @@ __global__ __launch_bounds__(256) void join_kernel(Args a, const float *part, Dz
     const int m = (int)fdiv(i, vectors), n = (int)(i - (uint32_t)m * vectors.d) * 8;
     float z[8];
     sum_parts(a, part, 0, m, n, z);
-    Dz::piece<T>(e, e.rows[m], z, m, n, a.N, true, true);
+    if (e.lo)
+        Dz::piece<T, true>(e, e.rows[m], z, m, n, a.N, true, true);
+    else
+        Dz::piece<T>(e, e.rows[m], z, m, n, a.N, true, true);
 }
 
 // A workgroup JOIN_CLASSES classes of a row, a thread 8 of them.

@@ -80,6 +80,23 @@ __device__ __forceinline__ void load_rowf(const float *p, V &v, int left) {
     }
 }
 
+// 8 values from p on, and with LO what rounding took from them `lo` elements further
+// on: where there are few rows, one rounding counts, and a product of twice the
+// rows costs nothing.
+template <typename T, bool LO>
+__device__ __forceinline__ void store_parts(uint16_t *p, int64_t lo, const float (&v)[8]) {
+    const u32x4 r = pack8<T>(v);
+    reinterpret_cast<Any16 *>(p)->v = r;
+    if constexpr (LO) {
+        float f[8];
+        unpack8<T>(r, f);
+#pragma unroll
+        for (int k = 0; k < 8; k++)
+            f[k] = fabsf(f[k]) < INFINITY ? v[k] - f[k] : 0.0f;
+        reinterpret_cast<Any16 *>(p + lo)->v = pack8<T>(f);
+    }
+}
+
 // --- the product itself, rounded once -------------------------------------
 struct StoreArgs {
     uint16_t *out[2];
@@ -88,7 +105,8 @@ struct StoreArgs {
     const float *scale;      // one number, or null
     float *acc;              // [M][N] running sums of several products
     int acc_in, acc_out;     // whether to add them, and to leave them there instead of a result
-    float *part;             // [splits][batch][M][N] for split sums
+    float *part;             // [splits][batch][M][N] for sums that a launch of their own joins, or null
+    int fold;                // there: the rows of the result, each the sum of rows m and m + fold; 0: of one each
 };
 
 // N sums of row m from column n on
@@ -127,7 +145,7 @@ struct Store {
     static __device__ __forceinline__ void run(const StoreArgs &e, const Results<S, G> &t, const Work &at,
                                                const mm::Args &a, int m0, int n0, int lane, uint8_t *) {
         constexpr int W = Results<S, G>::W, PIECES = Results<S, G>::PIECES;
-        float *const part = a.splits > 1 ? e.part + ((int64_t)at.split * a.batch + at.batch) * a.M * a.N : nullptr;
+        float *const part = e.part ? e.part + ((int64_t)at.split * a.batch + at.batch) * a.M * a.N : nullptr;
 #pragma unroll
         for (int i = 0; i < S::FM; i++) {
             const int m = m0 + 16 * i + (lane & 15);
@@ -158,7 +176,7 @@ struct Store {
 // each gradient).
 struct GatedArgs {
     uint16_t *h;
-    int64_t ldh;
+    int64_t ldh, lo;  // lo: to what rounding h takes, or 0
     float *saved;  // [M][2 H], g then u, or null
     int H, pad, act;
 };
@@ -171,7 +189,7 @@ struct Gated {
     }
     using Args = GatedArgs;
     // 8 channels of row m from n on; ends: H may be among them
-    template <typename T, int ACT>
+    template <typename T, int ACT, bool LO = false>
     static __device__ __forceinline__ void piece(const GatedArgs &e, const float (&g)[8], const float (&u)[8], int m, int n,
                                                  bool ends) {
         const int left = e.H - n;
@@ -183,7 +201,7 @@ struct Gated {
 #pragma unroll
             for (int k = 0; k < 8; k++)
                 h[k] = k < left ? h[k] : 0.0f;
-        store_row<T, 8>(e.h + m * e.ldh + n, h, 8);
+        store_parts<T, LO>(e.h + m * e.ldh + n, e.lo, h);
         if (e.saved) {
             float *const s = e.saved + (int64_t)m * 2 * e.H + n;
             store_rowf<8>(s, g, left);
@@ -226,7 +244,7 @@ struct GatedBackArgs {
     const float *saved;
     uint16_t *d;  // [M][2 ld]: dg, du
     uint16_t *h;  // [M][ld]
-    int64_t ld;
+    int64_t ld, lo;  // lo: to what rounding h takes (d: twice that), or 0
     int H, pad, act;
 };
 
@@ -243,7 +261,7 @@ struct GatedBack {
         load_rowf<8>(s, g, left);
         load_rowf<8>(s + e.H, u, left);
     }
-    template <typename T, int ACT>
+    template <typename T, int ACT, bool LO = false>
     static __device__ __forceinline__ void piece(const GatedBackArgs &e, const float (&dh)[8], const float (&g)[8],
                                                  const float (&u)[8], int m, int n) {
         const int left = e.H - n;
@@ -256,9 +274,9 @@ struct GatedBack {
             h[k] = k < left ? q.f * u[k] : 0.0f;
         }
         uint16_t *const d = e.d + m * 2 * e.ld + n;
-        store_row<T, 8>(d, dg, 8);
-        store_row<T, 8>(d + e.ld, du, 8);
-        store_row<T, 8>(e.h + m * e.ld + n, h, 8);
+        store_parts<T, LO>(d, 2 * e.lo, dg);
+        store_parts<T, LO>(d + e.ld, 2 * e.lo, du);
+        store_parts<T, LO>(e.h + m * e.ld + n, e.lo, h);
     }
     template <typename T, typename S, bool G>
     static __device__ __forceinline__ void run(const GatedBackArgs &e, const Results<S, G> &t, const Work &,
@@ -410,7 +428,7 @@ struct RowGrad {
 struct DzArgs {
     const RowGrad *rows;
     uint16_t *dz;  // [M][ld], `pad` columns
-    int64_t ld;
+    int64_t ld, lo;  // lo: to what rounding dz takes, or 0
     int pad, v0;  // the piece's first token
 };
 
@@ -422,7 +440,7 @@ struct Dz {
     }
     using Args = DzArgs;
     // 8 classes of row m from n on; mine: the row's token may be among them, ends: the last class
-    template <typename T>
+    template <typename T, bool LO = false>
     static __device__ __forceinline__ void piece(const DzArgs &e, const RowGrad &r, const float (&z)[8], int m, int n, int N,
                                                  bool mine, bool ends) {
         const int want = r.token - e.v0;
@@ -441,7 +459,7 @@ struct Dz {
 #pragma unroll
             for (int k = 0; k < 8; k++)
                 d[k] = n + k < N ? d[k] : 0.0f;
-        store_row<T, 8>(e.dz + m * e.ld + n, d, 8);
+        store_parts<T, LO>(e.dz + m * e.ld + n, e.lo, d);
     }
     template <typename T, typename S, bool G>
     static __device__ __forceinline__ void run(const DzArgs &e, const Results<S, G> &t, const Work &,

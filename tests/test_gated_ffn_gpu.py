@@ -88,9 +88,10 @@ def test_whole_numbers_over_large_tiles_and_many_rows():
     exact_case(20000, 256, 512, torch.float16, "none")
 
 
-def bounds(x, wg, wu, wd, dy, act, dt):
+def bounds(x, wg, wu, wd, dy, act, dt, inner=None):
     """Results in 64 bits and tolerances: errors of the sums, propagated, and of each rounding to 16 bits."""
     R, T = ROUND[dt], TINY[dt]
+    inner = R if inner is None else inner
     C, H, rows = x.shape[1], wg.shape[0], x.shape[0]
 
     def product(a, ea, b, eb, n):  # of a b with errors ea, eb in the factors
@@ -110,14 +111,14 @@ def bounds(x, wg, wu, wd, dy, act, dt):
     es = 0.8 * ea + 4e-7 * size + ((a.abs() <= ea).double() if act == "relu" else 0)
     h = f * u
     eh = ef * u.abs() + f.abs() * eu + 2 * F32 * h.abs()
-    eh = eh + R * (h.abs() + eh) + T
+    eh = eh + inner * (h.abs() + eh) + T
     y, ey = product(h, None, wd.t(), None, H)
     ey = ey + mm(eh, wd.t().abs())
     dh, edh = product(dy, None, wd, None, C)
     da, du = dh * u * s, dh * f
     eda = edh * (u * s).abs() + dh.abs() * (eu * s.abs() + u.abs() * es) + 3 * F32 * da.abs()
     edu = edh * f.abs() + dh.abs() * ef + 2 * F32 * du.abs()
-    eda, edu = eda + R * (da.abs() + eda) + T, edu + R * (du.abs() + edu) + T
+    eda, edu = eda + inner * (da.abs() + eda) + T, edu + inner * (du.abs() + edu) + T
     g1, e1 = product(da, eda, wg, None, 2 * H)
     g2, e2 = product(du, edu, wu, None, 2 * H)
     dwg, edwg = product(da.t(), eda.t(), x, None, rows)
@@ -151,6 +152,22 @@ def test_random_numbers(rows, C, H, dtype, act):
         assert_within(g, t, e, what)
         # two roundings of 2^-9 (2^-12) at most, the inner ones independent of each other
         assert float((g.double().cpu() - t).norm() / t.norm()) <= 2 * ROUND[dt], what
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("rows,C,H", [(1, 96, 200), (16, 64, 130), (7, 33, 77), (2, 1032, 24)])
+def test_few_rows_are_rounded_once(rows, C, H, dtype):
+    """Up to 16 rows h, da and du are kept in two numbers of 16 bits: off by the
+    square of a rounding (in fp16 by half of its least number, which is in the
+    tolerance anyway)."""
+    dt = DT[dtype]
+    given = random_case(rows, C, H, dt, 21)
+    ref = bounds(*(t.double() for t in given), "silu", dt, inner=ROUND[dt] ** 2)
+    x, wg, wu, wd, dy = (t.cuda() for t in given)
+    y, saved = cf.gated_ffn_forward_save(x, wg, wu, wd)
+    got = (y, *cf.gated_ffn_backward(dy, x, saved, wg, wu, wd))
+    for g, (t, e), what in zip(got, ref, NAMES):
+        assert_within(g, t, e, what)
 
 
 def test_leading_dimensions_outputs_and_workspaces():

@@ -23,7 +23,7 @@ def case(seed, rows, C, V, dt, scale=2.5):
     return x, w, t, randn(seed + 3, (rows,)), 0.1 * randn(seed + 4, (rows,))
 
 
-def reference(x, w, t, gl, gs, dt):
+def reference(x, w, t, gl, gs, dt, inner=None):
     """(value, tolerance) of logp, lse, dx, dw; all arguments in 64 bits but t."""
     R, T = ROUND[dt], TINY[dt]
     rows, C = x.shape
@@ -46,7 +46,7 @@ def reference(x, w, t, gl, gs, dt):
     dz.scatter_add_(1, at, gl[:, None])
     ep = p * (ez + e_lse[:, None] + 4 * F32 * ((z - lse[:, None]).abs() + 1))
     edz = c.abs()[:, None] * ep + 2 * F32 * (dz.abs() + (c[:, None] * p).abs())
-    edz = edz + R * (dz.abs() + edz)
+    edz = edz + (R if inner is None else inner) * (dz.abs() + edz)
     # fp16: values below 2^-14 of the row's scale, 2^-13 of the larger of c and gl, lose bits
     tiny = 2.0**-25 * 2.0**-12 * torch.maximum(c.abs(), gl.abs()) if dt == torch.float16 else torch.zeros_like(c)
     edz = edz + tiny[:, None]
@@ -90,6 +90,20 @@ SIZES = [(1, 8, 10), (1, 1, 1), (3, 5, 7), (16, 64, 1000), (17, 40, 130), (100, 
 @pytest.mark.parametrize("rows,C,V", SIZES)
 def test_sizes(rows, C, V, dtype):
     check(*case(rows + C + V, rows, C, V, DT[dtype]), DT[dtype])
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("rows,C,V", [(1, 48, 10), (16, 64, 300), (5, 33, 77)])
+def test_few_rows_are_rounded_once(rows, C, V, dtype):
+    """Up to 16 rows dz is kept in two numbers of 16 bits."""
+    dt = DT[dtype]
+    x, w, t, gl, gs = case(31, rows, C, V, dt)
+    t = t.abs()
+    ref = reference(x.double(), w.double(), t, gl.double(), gs.double(), dt, inner=ROUND[dt] ** 2)
+    lp = cf.linear_log_probs_forward(x.cuda(), w.cuda(), t.cuda())
+    got = (*lp, *cf.linear_log_probs_backward(x.cuda(), w.cuda(), t.cuda(), lp, gl.cuda(), gs.cuda()))
+    for g, (v, e), what in zip(got, ref, NAMES):
+        assert_within(g, v, e, what)
 
 
 @pytest.mark.parametrize("kind", ["slice", "shifted"])

@@ -7,7 +7,7 @@
 // The rows of x come from the caches.  Rows may start anywhere and have any length:
 // what is left of k goes element by element.  The waves' sums meet in LDS in a fixed order,
 // and the first wave does what follows.  1 x 131072 x 4096 takes 182 us, 5.9 TB/s; a
-// gated block of 1 x 4096 x 12288 62 us, 4.8 TB/s (58 without the second number of h).
+// gated block of 1 x 4096 x 12288 60 us, 5.0 TB/s (59 without the second number of h).
 #pragma once
 
 #include "cf_mm_epi.h"
@@ -41,7 +41,7 @@ __device__ __forceinline__ u32x4 load_k(const uint16_t *p, int left) {
 // What follows gets `sum(f)`, the four results of fragment f in row lane % 16 of x:
 // rows n0 + 16 f + 4 (lane / 16) .. + 3 of W (DUAL: of either matrix, n0 alone).
 struct Gated {
-    static constexpr bool DUAL = true, LO = false;
+    static constexpr bool DUAL = true, LO = false, FOLD = false;
     using Extra = mm::GatedArgs;
     template <typename T, int FN>
     static __device__ __forceinline__ void run(const Extra &e, const float4v (&sum)[FN], const Args &a, int n0, int lane) {
@@ -67,8 +67,12 @@ struct Gated {
     }
 };
 
+// x in two numbers: the second ones' rows in a fragment of their own, or FOLDED, for up
+// to 8 rows, beside the first ones in the same (1 x 12288 in 4096 rows of W 25 us in
+// two fragments, 23 in one).
+template <bool FOLDED>
 struct Store {
-    static constexpr bool DUAL = false, LO = true;
+    static constexpr bool DUAL = false, LO = !FOLDED, FOLD = FOLDED;
     using Extra = mm::StoreArgs;
     template <typename T, int FN>
     static __device__ __forceinline__ void run(const Extra &e, const float4v (&sum)[FN], const Args &a, int n0, int lane) {
@@ -83,7 +87,7 @@ struct Store {
 };
 
 struct Lse {
-    static constexpr bool DUAL = false, LO = false;
+    static constexpr bool DUAL = false, LO = false, FOLD = false;
     using Extra = mm::LseArgs;
     template <typename T, int FN>
     static __device__ __forceinline__ void run(const Extra &e, const float4v (&sum)[FN], const Args &a, int n0, int lane) {
@@ -116,7 +120,9 @@ __global__ __launch_bounds__(WAVES * 64) void kernel(Args a, typename E::Extra e
         const int row = n0 + (E::DUAL ? 0 : 16 * f) + r;
         w[f] = (E::DUAL && f ? a.w[1] : a.w[0]) + (row < a.N ? row : a.N - 1) * (E::DUAL && f ? a.ldw[1] : a.ldw[0]) + q * 8;
     }
-    const uint16_t *const x = a.x + (int64_t)(r < a.M ? r : a.M - 1) * a.ldx + q * 8;
+    const int row_x = E::FOLD ? r & 7 : r;
+    const uint16_t *const x =
+        a.x + (int64_t)(row_x < a.M ? row_x : a.M - 1) * a.ldx + q * 8 + (E::FOLD && r >= 8 ? a.lo : 0);
     float4v acc[FN];
 #pragma unroll
     for (int f = 0; f < FN; f++)
@@ -142,8 +148,7 @@ __global__ __launch_bounds__(WAVES * 64) void kernel(Args a, typename E::Extra e
 #pragma unroll
         for (int u = 0; u < U; u++)
 #pragma unroll
-            for (int f = 0; f < FN; f++)
-            {
+            for (int f = 0; f < FN; f++) {
                 acc[f] = T::mfma(fw[f][u], fx[u], acc[f]);
                 if constexpr (E::LO)
                     acc[f] = T::mfma(fw[f][u], fl[u], acc[f]);
@@ -153,8 +158,7 @@ __global__ __launch_bounds__(WAVES * 64) void kernel(Args a, typename E::Extra e
         const int left = a.K - k0 - q * 8;
         const u32x4 fx = load_k(x + k0, left);
 #pragma unroll
-        for (int f = 0; f < FN; f++)
-        {
+        for (int f = 0; f < FN; f++) {
             const u32x4 fw = load_k(w[f] + k0, left);
             acc[f] = T::mfma(fw, fx, acc[f]);
             if constexpr (E::LO)
@@ -172,6 +176,12 @@ __global__ __launch_bounds__(WAVES * 64) void kernel(Args a, typename E::Extra e
 #pragma unroll
         for (int v = 1; v < WAVES; v++)
             acc[f] += red[v][f][lane];
+    if constexpr (E::FOLD)
+#pragma unroll
+        for (int f = 0; f < FN; f++)
+#pragma unroll
+            for (int k = 0; k < 4; k++)
+                acc[f][k] += __shfl_xor(acc[f][k], 8);
     E::template run<T, FN>(e, acc, a, n0, lane);
 }
 

@@ -124,7 +124,8 @@ hipError_t forward(const GatedFfn &a, const ForwardPlan &p, void *y, int64_t ldy
         s.out[0] = (uint16_t *)y;
         s.ldo = ldy;
         const few::Args down = {p.h, {p.wd.m.p, p.wd.m.p}, p.ld, {p.wd.m.ld, p.wd.m.ld}, p.lo, a.rows, a.C, a.H};
-        return few::launch<T, 1, few::Store>(down, s, st);
+        return a.rows <= 8 ? few::launch<T, 1, few::Store<true>>(down, s, st)
+                           : few::launch<T, 1, few::Store<false>>(down, s, st);
     }
     const GatedArgs gate = {p.h, p.ld, p.lo, saved, a.H, p.pad, a.act};
     const bool split = p.up.splits > 1 || p.lo;

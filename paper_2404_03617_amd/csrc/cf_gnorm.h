@@ -15,7 +15,7 @@
 // joins them and reads x (and dy) again.
 //
 // 128 x 56 x 56 x 64 in 16 groups, ReLU, takes 24 us forward (4.3 TB/s); 128 x 28 x 28
-// x 128 in 32 groups, GELU, 20.5 forward and 31 backward, whose vector units are 80%
+// x 128 in 32 groups, GELU, 20.5 forward and 31 backward, whose vector units are 84%
 // busy (du is made twice: keeping it takes a second workgroup off the CU); rows that
 // start at any 2 bytes and groups of 11 channels cost twice that a byte.
 #pragma once

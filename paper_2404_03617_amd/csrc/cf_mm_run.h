@@ -118,8 +118,8 @@ inline hipError_t pack(const Operand &o, int bf16, hipStream_t st) {
 // Up to PART_ROWS rows, what a product rounds for the next one is kept with what the
 // rounding takes, as rows of their own: a single row's rounding is not evened out by
 // others (dW of one row in bf16 was up to twice as far off as a rounded exact one), and a
-// tile is one high with them too.  A gated block of 1 x 4096 x 12288 takes 61 us, without
-// them 58, backward 201 and 182; of 64 rows 97 and 83, 221 and 192.
+// tile is one high with them too.  A gated block of 1 x 4096 x 12288 takes 60 us, without
+// them 59, backward 201 and 182; of 64 rows it would be 97 and 83, 221 and 192.
 constexpr int PART_ROWS = 16;
 inline bool in_parts(int64_t rows) { return rows > 0 && rows <= PART_ROWS; }
 // room for the sums of a product that a launch of its own joins

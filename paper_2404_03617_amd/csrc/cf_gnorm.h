@@ -614,15 +614,16 @@ hipError_t launch(void (*f)(Args), const Args &a, const Plan &p, int64_t N, int 
     return hipGetLastError();
 }
 
-// The kernel that holds p.nv vectors a thread.
+// The kernel that holds p.nv vectors a thread, as the plan counts on (`held`).
 template <typename T, int ACT, int MODE>
 hipError_t forward_act(const Args &a, const Plan &p, int64_t N, hipStream_t st) {
     const bool big = p.threads == 512;
-    void (*const f)(Args) = big ? (p.nv <= 16 ? forward_kernel<T, ACT, 512, 16, MODE> : forward_kernel<T, ACT, 512, FORWARD_NV, MODE>)
-                            : p.nv <= 1 ? forward_kernel<T, ACT, 256, 1, MODE>
-                            : p.nv <= 4 ? forward_kernel<T, ACT, 256, 4, MODE>
-                            : p.nv <= 8 ? forward_kernel<T, ACT, 256, 8, MODE>
-                                        : forward_kernel<T, ACT, 256, 16, MODE>;
+    const int nv = held(p, FORWARD_NV);
+    void (*const f)(Args) = big ? (nv == 16 ? forward_kernel<T, ACT, 512, 16, MODE> : forward_kernel<T, ACT, 512, FORWARD_NV, MODE>)
+                            : nv == 1 ? forward_kernel<T, ACT, 256, 1, MODE>
+                            : nv == 4 ? forward_kernel<T, ACT, 256, 4, MODE>
+                            : nv == 8 ? forward_kernel<T, ACT, 256, 8, MODE>
+                                      : forward_kernel<T, ACT, 256, SMALL_NV, MODE>;
     const hipError_t e = launch(f, a, p, N, 1, st);
     if (e != hipSuccess || a.whole)
         return e;
@@ -632,11 +633,12 @@ hipError_t forward_act(const Args &a, const Plan &p, int64_t N, hipStream_t st) 
 template <typename T, int ACT, int MODE>
 hipError_t backward_act(const Args &a, const Plan &p, int64_t N, hipStream_t st) {
     const bool big = p.threads == 512;
+    const int nv = held(p, BACKWARD_NV);
     void (*const f)(Args) = big ? backward_kernel<T, ACT, 512, BACKWARD_NV, MODE>
-                            : p.nv <= 1 ? backward_kernel<T, ACT, 256, 1, MODE>
-                            : p.nv <= 4 ? backward_kernel<T, ACT, 256, 4, MODE>
-                            : p.nv <= 8 ? backward_kernel<T, ACT, 256, 8, MODE>
-                                        : backward_kernel<T, ACT, 256, BACKWARD_NV, MODE>;
+                            : nv == 1 ? backward_kernel<T, ACT, 256, 1, MODE>
+                            : nv == 4 ? backward_kernel<T, ACT, 256, 4, MODE>
+                            : nv == 8 ? backward_kernel<T, ACT, 256, 8, MODE>
+                                      : backward_kernel<T, ACT, 256, SMALL_NV, MODE>;
     const hipError_t e = launch(f, a, p, N, 2, st);
     if (e != hipSuccess || a.whole)
         return e;

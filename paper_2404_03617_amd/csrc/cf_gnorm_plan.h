@@ -8,7 +8,9 @@
 namespace cf {
 namespace gnorm {
 
-constexpr int FORWARD_NV = 28, BACKWARD_NV = 16;  // the most vectors that registers hold (backward: of x and of dy)
+// The most vectors that a thread's registers hold (backward: of x and of dy), and that the kernels
+// of 256 threads have.
+constexpr int FORWARD_NV = 28, BACKWARD_NV = 16, SMALL_NV = 16;
 
 // A workgroup takes `per_block` groups of one image, or a part of its pixels,
 // and holds them in registers: `nv` vectors of 8 channels a thread.
@@ -19,6 +21,13 @@ struct Plan {
     int V, rows;            // vectors beside each other, pixels at a time
     int threads, nv;
 };
+
+// The vectors of a thread that the kernel launched for a plan holds.
+inline int held(const Plan &p, int most_nv) {
+    if (p.threads == 256)
+        return p.nv <= 1 ? 1 : p.nv <= 4 ? 4 : p.nv <= 8 ? 8 : SMALL_NV;
+    return p.nv <= 16 ? 16 : most_nv;
+}
 
 // The channels of a workgroup are a run of whole groups, at least `want` bytes
 // of each pixel.
@@ -33,6 +42,9 @@ inline Plan shape(int64_t N, int64_t P, int C, int G, int want, int most_nv, int
     // a workgroup that has its CU to itself is better large (32 x 28 x 28 x 192 in 6 groups, forward
     // 10.0 us against 12.5)
     p.threads = vectors > 4096 || (vectors > 2048 && N * p.blocks <= cus && N * p.blocks >= cus / 2) || p.V > 256 ? 512 : 256;
+    // and has to be where 256 threads, of which V leaves some without a vector, do not hold what 512 do
+    if (p.threads == 256 && most_nv > SMALL_NV && P > (int64_t)SMALL_NV * (256 / p.V))
+        p.threads = 512;
     p.rows = p.threads / p.V;
     const int64_t hold = p.rows > 0 ? (int64_t)p.rows * most_nv : 0;  // pixels that fit
     p.chunks = hold ? (int)((P + hold - 1) / hold) : 0;

@@ -157,6 +157,20 @@ def test_images_in_parts(shape, groups):
         check(x, dy, groups, w, b, "silu", "slice")
 
 
+@pytest.mark.parametrize("dtype,shape,groups,act", [
+    ("f16", (260, 17, 1032), 1, "gelu"), ("bf16", (33, 26, 26, 384), 8, "silu"), ("f16", (30, 26, 26, 387), 9, "none"),
+    ("bf16", (33, 819, 320), 8, "relu"), ("f16", (40, 31, 1032), 8, "silu"), ("bf16", (33, 14, 14, 1280), 8, "gelu")],
+    ids=str)
+def test_widths_that_leave_threads_without_a_vector(dtype, shape, groups, act):
+    """More groups than workgroups run at once, of up to 4096 vectors, more than 16
+    of them a thread if 256 threads took them."""
+    x, dy, w, b = inputs(sum(shape), shape, DT[dtype])
+    out = torch.full(shape, float("nan"), dtype=DT[dtype], device="cuda")
+    cf.group_norm_forward(x.cuda(), groups, w.cuda(), b.cuda(), act=act, out=out)
+    assert not bool(out.isnan().any()), "pixels that were not written"
+    check(x, dy, groups, w, b, act)
+
+
 def test_offsets_are_taken_off_before_squares():
     """Values far from 0: the variance is of their differences."""
     for shape, groups in (((2, 30, 30, 32), 4), ((1, 40000, 16), 2)):

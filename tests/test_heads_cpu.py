@@ -310,6 +310,34 @@ def test_parts_of_a_group_norm_hold_all_pixels_and_groups(tmp_path, cus):
     """ % cus)
 
 
+@pytest.mark.parametrize("cus", [256, 80])
+def test_the_kernel_of_a_group_norm_holds_every_pixel(tmp_path, cus):
+    """The vectors of a thread that the launched kernel has registers for reach the
+    last pixel of the workgroup's part, for every width of a workgroup and every
+    image of up to 4096 vectors, beyond which workgroups are large."""
+    run_cpp(tmp_path, "cf_gnorm_plan.h", "gnorm", """
+    bool small[2] = {false, false};
+    for (int D = 8; D <= 4096; D += D < 520 ? 1 : 72)
+        for (int64_t P = 1; P * ((D + 7) / 8) <= 4600; P++)
+            for (int64_t groups : {1, 2, 100, 300, 3000})
+                for (int most : {FORWARD_NV, BACKWARD_NV}) {
+                    const int G = groups < 100 ? (int)groups : 4;
+                    const Plan p = plan_of((groups + G - 1) / G, P, D * G, G, most, %d);
+                    if (p.rows < 1)
+                        continue;
+                    const int has = held(p, most);
+                    small[most == BACKWARD_NV] |= p.threads == 256 && p.nv > 8;
+                    if (has < p.nv || (int64_t)has * p.rows < p.px || (p.threads == 256 && has > SMALL_NV)) {
+                        printf("%%d channels a group, P %%lld, %%lld groups: %%d threads, nv %%d, held %%d\\n", D, (long long)P,
+                               (long long)groups, p.threads, p.nv, has);
+                        return 1;
+                    }
+                }
+    if (!small[0] || !small[1])
+        return 1;
+    """ % cus)
+
+
 def test_the_sizes_of_the_tile_tests_take_every_tile(tmp_path):
     """The tests of the tiles on the GPU (test_heads_gpu.py) run both behind each
     kind of product, and products over whole and split axes."""

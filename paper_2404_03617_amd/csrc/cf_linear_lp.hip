@@ -39,7 +39,6 @@ using namespace mm;
 
 namespace {
 
-constexpr double PIECE_BYTES = 256 << 20;
 // Fragments of 16 classes a workgroup where there are few rows: one or two rows come
 // from the caches at little cost (1 x 131072 x 4096 182 us with one, 197 with two),
 // more rather once for two (8 rows 205 and 192, 16 rows 245 and 197).
@@ -204,14 +203,11 @@ BackwardPlan backward_plan(const LinearLogProbs &a, bool copy_x, bool copy_w, vo
     p.row_scale = (float *)p.room.take((size_t)a.rows * 4);
     p.scale = (float *)p.room.take(4);
     p.most = (int *)p.room.take(EXPONENTS * 4);
-    // Pieces of at least 4096 columns, all but the last a multiple of a tile.
     const bool lo = in_parts(a.rows);
     const int64_t rows = lo ? 2 * a.rows : a.rows;
-    const double most = (lo ? PART_BYTES / 2 : PIECE_BYTES) / (2.0 * (a.rows > 0 ? a.rows : 1));
-    const int64_t at_most = most < 4096 ? 4096 : most > (1 << 30) ? 1 << 30 : (int64_t)most;
-    p.pieces = (int)((a.V + at_most - 1) / at_most);
-    p.piece = p.pieces == 1 ? a.V : ((a.V + p.pieces - 1) / p.pieces + 255) / 256 * 256;
-    p.pieces = (a.V + p.piece - 1) / p.piece;
+    const Pieces cut = pieces_of(a.rows, a.V);
+    p.piece = cut.columns;
+    p.pieces = cut.count;
     p.dz = (uint16_t *)p.room.take((size_t)rows * stride_of(p.piece) * 2);
     p.acc = p.pieces > 1 ? (float *)p.room.take((size_t)a.rows * a.C * 4) : nullptr;
     p.z = plan(a.rows, p.piece, a.C, true, 1, 1, MORE);

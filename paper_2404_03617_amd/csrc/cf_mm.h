@@ -44,19 +44,6 @@ namespace mm {
 
 enum { KC = 0, RC = 1 };
 
-struct Args {
-    const uint16_t *a[2], *b[2];
-    int64_t lda, ldb;     // of both
-    int M, N, K;          // K of one segment
-    int ext_a, ext_b;     // rows of a (KC), or the columns that its rows hold (RC); the same of b
-    int seg;              // steps of the first segment of k (behind it a[1], b[1]), or all
-    int steps;            // of both
-    int per;              // steps a split
-    int tiles_m, tiles_n, splits;
-    unsigned items;       // tiles * splits * batch
-    int batch;            // 2: a[1], b[1] and out[1] are a second problem
-};
-
 struct Work {
     int m, n, split, batch;
 };

@@ -1,6 +1,6 @@
-// cf_mm_plan.h -- which tile a matrix product (cf_mm.h) takes and over how many
-// workgroups its sums are split, in plain C++ so that a test can ask without a
-// GPU.
+// cf_mm_plan.h -- which tile a matrix product (cf_mm.h) takes, over how many
+// workgroups its sums are split, what its kernel is given of that, and the pieces
+// that a vocabulary goes by, in plain C++ so that a test can ask without a GPU.
 #pragma once
 
 #include <cmath>
@@ -94,6 +94,81 @@ inline Plan plan_of(int64_t M, int64_t N, int64_t steps, int64_t batch, bool may
 }
 inline size_t part_bytes(const Plan &p, int64_t M, int64_t N, int64_t batch) {
     return p.splits > 1 ? (size_t)p.splits * batch * M * N * 4 : 0;
+}
+
+// A matrix as the tiles read it: 16-byte aligned rows that hold `ext` columns,
+// a multiple of 8.
+struct Matrix {
+    const uint16_t *p;
+    int64_t ld;
+    int ext;
+};
+
+// A product as its kernel is given it.
+struct Args {
+    const uint16_t *a[2], *b[2];
+    int64_t lda, ldb;     // of both
+    int M, N, K;          // K of one segment
+    int ext_a, ext_b;     // rows of a (KC), or the columns that its rows hold (RC); the same of b
+    int seg;              // steps of the first segment of k (behind it a[1], b[1]), or all
+    int steps;            // of both
+    int per;              // steps a split
+    int tiles_m, tiles_n, splits;
+    unsigned items;       // tiles * splits * batch
+    int batch;            // 2: a[1], b[1] and out[1] are a second problem
+};
+
+// A plan's product, or one with fewer k's than it was made for (the last piece of a
+// vocabulary): as many splits as those fill, since the kernel reads the first steps of
+// every split before it asks whether there are any.
+inline Args args_of(const Plan &p, int M, int N, int K, const Matrix &a, int ext_a, const Matrix &b, int ext_b,
+                    bool two_segments = false, int batch = 1) {
+    Args r;
+    r.a[0] = r.a[1] = a.p;
+    r.b[0] = r.b[1] = b.p;
+    r.lda = a.ld;
+    r.ldb = b.ld;
+    r.M = M;
+    r.N = N;
+    r.K = K;
+    r.ext_a = ext_a;
+    r.ext_b = ext_b;
+    r.seg = (int)steps_of(K);
+    r.steps = two_segments ? 2 * r.seg : r.seg;
+    if (!two_segments)
+        r.seg = 1 << 30;
+    r.per = p.per;
+    r.tiles_m = (M + TILES[p.tile].m - 1) / TILES[p.tile].m;
+    r.tiles_n = (N + TILES[p.tile].n - 1) / TILES[p.tile].n;
+    r.splits = r.steps > p.per ? (r.steps + p.per - 1) / p.per : 1;
+    r.batch = batch;
+    r.items = (unsigned)r.tiles_m * (unsigned)r.tiles_n * (unsigned)r.splits * (unsigned)batch;
+    return r;
+}
+
+// Up to PART_ROWS rows, what a product rounds for the next one is kept with what the
+// rounding takes, as rows of their own: a single row's rounding is not evened out by
+// others (dW of one row in bf16 was up to twice as far off as a rounded exact one), and a
+// tile is one high with them too.  A gated block of 1 x 4096 x 12288 takes 60 us, without
+// them 59, backward 201 and 182; of 64 rows it would be 97 and 83, 221 and 192.
+constexpr int PART_ROWS = 16;
+inline bool in_parts(int64_t rows) { return rows > 0 && rows <= PART_ROWS; }
+
+// The vocabulary of a gradient (cf_linear_lp.hip) goes by pieces, of which dz is in the
+// workspace: of at most PIECE_BYTES (two numbers of few rows: of PART_BYTES), but of at
+// least 4096 columns, all but the last a multiple of 256.  The last is shorter.
+constexpr double PIECE_BYTES = 256 << 20;
+struct Pieces {
+    int columns, count;
+};
+inline Pieces pieces_of(int64_t rows, int V) {
+    const double most = (in_parts(rows) ? PART_BYTES / 2 : PIECE_BYTES) / (2.0 * (rows > 0 ? rows : 1));
+    const int64_t at_most = most < 4096 ? 4096 : most > (1 << 30) ? 1 << 30 : (int64_t)most;
+    Pieces p;
+    p.count = (int)((V + at_most - 1) / at_most);
+    p.columns = p.count == 1 ? V : ((V + p.count - 1) / p.count + 255) / 256 * 256;
+    p.count = (V + p.columns - 1) / p.columns;
+    return p;
 }
 
 }  // namespace mm

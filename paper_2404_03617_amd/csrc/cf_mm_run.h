@@ -28,13 +28,6 @@ hipError_t launch_join(const Args &a, const float *part, const GatedBackArgs &e,
 hipError_t launch_join(const Args &a, const float *part, const LseArgs &e, int bf16, hipStream_t st);
 hipError_t launch_join(const Args &a, const float *part, const DzArgs &e, int bf16, hipStream_t st);
 
-// A matrix as the tiles read it: 16-byte aligned rows that hold `ext` columns,
-// a multiple of 8.
-struct Matrix {
-    const uint16_t *p;
-    int64_t ld;
-    int ext;
-};
 inline int up8(int n) { return (n + 7) & ~7; }
 // whether rows of `cols` can be read where they are
 inline bool fits(const void *p, int64_t ld, int cols) {
@@ -58,31 +51,6 @@ inline Plan plan(int64_t M, int64_t N, int64_t K, bool may_split, int batch = 1,
 }
 // a workgroup a tile: a launch holds 2^32 threads
 inline bool grid_fits(int64_t M, int64_t N) { return (double)((M + 127) / 128) * (double)((N + 127) / 128) < 4.0e6; }
-
-inline Args args_of(const Plan &p, int M, int N, int K, const Matrix &a, int ext_a, const Matrix &b, int ext_b,
-                    bool two_segments = false, int batch = 1) {
-    Args r;
-    r.a[0] = r.a[1] = a.p;
-    r.b[0] = r.b[1] = b.p;
-    r.lda = a.ld;
-    r.ldb = b.ld;
-    r.M = M;
-    r.N = N;
-    r.K = K;
-    r.ext_a = ext_a;
-    r.ext_b = ext_b;
-    r.seg = (int)steps_of(K);
-    r.steps = two_segments ? 2 * r.seg : r.seg;
-    if (!two_segments)
-        r.seg = 1 << 30;
-    r.per = p.per;
-    r.tiles_m = (M + TILES[p.tile].m - 1) / TILES[p.tile].m;
-    r.tiles_n = (N + TILES[p.tile].n - 1) / TILES[p.tile].n;
-    r.splits = p.splits;
-    r.batch = batch;
-    r.items = (unsigned)r.tiles_m * (unsigned)r.tiles_n * (unsigned)r.splits * (unsigned)batch;
-    return r;
-}
 
 // Pieces of a workspace, one after the other; without one, their size.
 struct Room {
@@ -115,13 +83,6 @@ inline hipError_t pack(const Operand &o, int bf16, hipStream_t st) {
     return o.copy ? launch_pack(o.from, o.ld, o.rows, o.cols, nullptr, o.copy, bf16, st) : hipSuccess;
 }
 
-// Up to PART_ROWS rows, what a product rounds for the next one is kept with what the
-// rounding takes, as rows of their own: a single row's rounding is not evened out by
-// others (dW of one row in bf16 was up to twice as far off as a rounded exact one), and a
-// tile is one high with them too.  A gated block of 1 x 4096 x 12288 takes 60 us, without
-// them 59, backward 201 and 182; of 64 rows it would be 97 and 83, 221 and 192.
-constexpr int PART_ROWS = 16;
-inline bool in_parts(int64_t rows) { return rows > 0 && rows <= PART_ROWS; }
 // room for the sums of a product that a launch of its own joins
 inline size_t joined_bytes(const Plan &p, int64_t M, int64_t N, int64_t batch, bool always) {
     return always ? (size_t)p.splits * batch * M * N * 4 : part_bytes(p, M, N, batch);

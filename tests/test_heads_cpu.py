@@ -269,6 +269,52 @@ def test_splits_of_the_products_hold_all_steps_and_fit_the_room(tmp_path, cus):
     """ % cus)
 
 
+@pytest.mark.parametrize("cus", [256, 80])
+def test_no_split_of_a_launched_product_is_empty(tmp_path, cus):
+    """What the kernel of a gradient's product over the classes is given, for each
+    piece of the vocabulary, the last and shortest among them, by the plan for whole
+    ones: every split begins before the last step (its reads would be behind the
+    weights), together they are all steps, and their sums have room."""
+    run_cpp(tmp_path, "cf_mm_plan.h", "mm", """
+    int shorter = 0;
+    const int64_t rows_of[] = {1, 16, 17, 40, 922, 4096, 8192, 20000, 32768, 50000, 262144};
+    const int columns[] = {8, 16, 24, 64, 256, 512, 1000, 1024, 4096};
+    for (int64_t rows : rows_of)
+        for (int C : columns)
+            for (int64_t V = 1; V < (1 << 28); V += V / 37 + 1) {
+                const Pieces cut = pieces_of(rows, (int)V);
+                const bool lo = in_parts(rows);
+                const int64_t M = lo ? 2 * rows : rows;
+                const Plan p = plan_of(M, C, steps_of(cut.columns), 1, true, %d);
+                const int last = (int)(V - (int64_t)(cut.count - 1) * cut.columns);
+                if (last < 1 || last > cut.columns) {
+                    printf("%%lld rows, %%lld classes: the last piece has %%d\\n", (long long)rows, (long long)V, last);
+                    return 1;
+                }
+                for (int n : {cut.columns, last}) {
+                    const Args a = args_of(p, (int)M, C, n, Matrix{}, 0, Matrix{}, 0);
+                    shorter += a.splits < p.splits;
+                    if (a.splits < 1 || (int64_t)(a.splits - 1) * a.per >= a.steps || (int64_t)a.splits * a.per < a.steps ||
+                        a.splits > p.splits || a.items != (unsigned)(a.tiles_m * a.tiles_n * a.splits)) {
+                        printf("%%lld rows of %%d, a piece of %%d of %%lld: %%d splits of %%d, %%d steps\\n", (long long)rows, C, n,
+                               (long long)V, a.splits, a.per, a.steps);
+                        return 1;
+                    }
+                }
+            }
+    if (!shorter)
+        return 1;
+    // and for one plan, products of any length up to its own
+    const Plan p = {1, 7, 13};
+    for (int K = 0; K <= 7 * 12 * STEP; K += 5)
+        for (int two = 0; two < 2; two++) {
+            const Args a = args_of(p, 100, 100, two ? K / 2 : K, Matrix{}, 0, Matrix{}, 0, two);
+            if (a.splits < 1 || (a.steps > 0 && (a.splits - 1) * a.per >= a.steps) || a.splits * a.per < a.steps)
+                return 1;
+        }
+    """ % cus)
+
+
 def test_both_tiles_and_splits_are_chosen(tmp_path):
     """Few tiles over a long axis are split, a chip full of large ones is not."""
     out = run_cpp(tmp_path, "cf_mm_plan.h", "mm", "".join(

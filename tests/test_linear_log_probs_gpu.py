@@ -147,6 +147,50 @@ def test_a_vocabulary_in_pieces():
             assert bool((off <= 4 * ROUND[dt] * size + 4 * ROUND[dt] * size.median()).all())
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("rows,C,V", [(922, 24, 174691), (32768, 16, 50257), (16, 8, 3037700), (40000, 16, 4100)])
+def test_a_last_piece_with_fewer_splits(rows, C, V, dtype):
+    """dx over a last piece whose k's do not fill the splits of a whole one (for the last size they
+    are whole in either), with NaN behind the weights.  In units of 2^-24: logits of C products whose
+    magnitudes add up to less than 16, here and in lse; sums of exponentials in chains of fewer than
+    700 additions, exponentials of arguments below 30 to 10 units of those; dx's chains of fewer than
+    2^13 additions, dW's of one a row."""
+    dt = DT[dtype]
+    R, p_off = ROUND[dt], (2 * C * 16 + 700 + 300) * F32
+    print("linear in pieces", rows, C, V, dt, flush=True)
+    g = torch.Generator("cuda").manual_seed(rows)
+    room = torch.full((V + 8192, C), float("nan"), dtype=dt, device="cuda")
+    w = room[:V]
+    w.normal_(0, C**-0.5, generator=g)
+    x = torch.randn((rows, C), generator=g, device="cuda").to(dt)
+    t = torch.randint(0, V, (rows,), generator=g, device="cuda")
+    t[-1] = V - 1
+    gl = torch.randn((rows,), generator=g, device="cuda")
+    lp = cf.linear_log_probs_forward(x, w, t)
+    dx, dw = cf.linear_log_probs_backward(x, w, t, lp, gl)
+    xd, gd = x.double(), gl.double()[:, None]
+    few = rows <= 16 and dt == torch.bfloat16  # two numbers; in fp16 their least numbers count too
+    least = 2.0**-37 * gd.abs() if dt == torch.float16 else 0 * gd  # of dz
+    lost = 2.0**-24 * gd.abs().max() / gd.abs() if dt == torch.float16 else 0 * gd  # of the scaled x
+    step = max(1, (1 << 27) // rows)
+    lse = torch.stack([torch.logsumexp(mm(xd, w[lo:lo + step].double().t()), 1) for lo in range(0, V, step)]).logsumexp(0)
+    want, off = torch.zeros((2, rows, C), dtype=torch.float64, device="cuda")
+    for lo in range(0, V, step):
+        wd = w[lo:lo + step].double()
+        q = torch.exp(mm(xd, wd.t()) - lse[:, None]) * gd.abs()
+        dz = -q * gd.sign()
+        here = ((t >= lo) & (t < lo + step)).nonzero()[:, 0]
+        dz[here, t[here] - lo] += gd[here, 0]
+        e = p_off * (q + dz.abs())
+        e = e + (R * R if few else R) * (dz.abs() + e) + least
+        want += mm(dz, wd)
+        off += mm(e + 2**13 * F32 * dz.abs(), wd.abs())
+        part = mm(dz.t(), xd)
+        e = mm((e + (rows + 2) * F32 * dz.abs()).t(), xd.abs()) + mm(dz.abs().t(), lost)
+        assert_within(dw[lo:lo + step], part.cpu(), (e + R * (part.abs() + e) + TINY[dt]).cpu(), "dw from %d on" % lo)
+    assert_within(dx, want.cpu(), (off + R * (want.abs() + off) + TINY[dt]).cpu(), "dx")
+
+
 def test_logits_of_every_size():
     """Large logits, rows that are certain of their token, rows that hold no chance for it."""
     for dt in (torch.float16, torch.bfloat16):

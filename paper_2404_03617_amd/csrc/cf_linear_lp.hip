@@ -82,12 +82,13 @@ __global__ __launch_bounds__(256) void join_lse_kernel(const float2 *part, const
 // What a row's gradient is made of; none for c = at = 0.  At the token, c p + d_logp
 // is d_lse p + d_logp (1 - p) with both factors from logp: where p is nearly 1, lse in
 // fp32 has lost what is left of 1 - p (a row with lse = 15 and 1 - p = 5e-7: all of it).
+// A weight of 0 takes nothing from a log probability that may be NaN.
 __device__ __forceinline__ RowGrad grad_of(const LinearGrads &g, const int64_t *tokens, int V, int r) {
     const int64_t t = g.d_logp ? tokens[r] : -1;
     const float gl = t >= V ? NAN : t >= 0 ? g.d_logp[r] : 0.0f, gs = g.d_lse ? g.d_lse[r] : 0.0f, lse = g.lse[r];
     RowGrad w = {gs - gl, 0.0f, lse, t < V ? (int)t : -1};
     if (w.token >= 0)
-        w.at = gs * expf(g.logp[r]) - gl * expm1f(g.logp[r]);
+        w.at = (gs != 0.0f ? gs * expf(g.logp[r]) : 0.0f) - (gl != 0.0f ? gl * expm1f(g.logp[r]) : 0.0f);
     if (lse == -INFINITY)
         w.c = w.at = 0.0f;
     return w;

@@ -233,6 +233,28 @@ def test_rows_without_a_gradient():
             assert_within(dw, *ref[3], "dw")
 
 
+@pytest.mark.parametrize("rows", [12, 60])
+def test_rows_of_weight_0_with_a_token(rows):
+    """Padding whose token is one of the classes: gradients of 0 for its logp and lse, which are NaN
+    where its features are."""
+    for dt in (torch.float16, torch.bfloat16):
+        x, w, t, gl, gs = case(12, rows, 48, 130, dt)
+        t = t.abs()
+        out = torch.arange(rows) % 4 == 1
+        gl[out], gs[out] = 0, 0
+        x[out] = float("nan")
+        x[1], x[5] = float("inf"), 60000
+        xg, wg, tg, keep = x.cuda(), w.cuda(), t.cuda(), ~out
+        lp = cf.linear_log_probs_forward(xg, wg, tg)
+        for a, b in ((gl, gs), (gl, None), (None, gs)):
+            dx, dw = cf.linear_log_probs_backward(xg, wg, tg, lp, None if a is None else a.cuda(), None if b is None else b.cuda())
+            assert bool((dx[out.cuda()] == 0).all())
+            ref = reference(x[keep].double(), w.double(), t[keep], None if a is None else a[keep].double(),
+                            None if b is None else b[keep].double(), dt)
+            assert_within(dx[keep.cuda()], *ref[2], "dx")
+            assert_within(dw, *ref[3], "dw")
+
+
 def test_tokens_out_of_range_and_rows_that_are_not_finite():
     dt = torch.bfloat16
     x, w, t, gl, gs = case(13, 12, 16, 20, dt)

@@ -608,9 +608,10 @@ size_t cf_linear_log_probs_workspace_bytes(int64_t rows, int C, int V, int align
  * a gradient where p is nearly 1.
  * The logits are made again, a piece of the vocabulary at a time (dz of a piece,
  * in dt, or for up to 16 rows in two numbers of dt, is in the workspace: 256 MiB, or
- * rows * 8 KiB if that is more); in fp16 dz
- * is scaled by a power of two a row, so that small probabilities keep their
- * bits.  Rows whose d_logp and d_lse are 0 (d_logp counts as 0 for a negative token)
+ * rows * 8 KiB if that is more).  In fp16 dz is scaled by a power of two a row, so
+ * that small probabilities keep their bits, and for dweight the rows of x are scaled
+ * so that gradients times features keep theirs down to 2^-28 of the largest such
+ * product; what smaller ones lose is below 2^-38 of it.  Rows whose d_logp and d_lse are 0 (d_logp counts as 0 for a negative token)
  * or whose lse is -inf have no gradient and add nothing to dweight, whatever
  * their features hold.  A token of V or more makes the gradients NaN.  dx
  * [rows][C] and dweight [V][C], dense, in dt; rows = 0 gives zeros in dweight.  No

@@ -20,10 +20,12 @@
 // A gradient in 16 bits: in bf16 its range is that of fp32.  In fp16 a row's
 // values are scaled by a power of two, so that the largest of c and the token's value
 // lies in [2^13, 2^14) and a probability of 4e-9 still has all bits; dx is scaled
-// back by row, and the rows of x that dW sums are scaled against each other
-// (exactly, but for what falls below fp16 against the largest row) and the sums
-// back.  The same copy of x leaves out rows without a gradient: what their
-// features hold, NaN included, reaches nothing.
+// back by row, and the rows of x that dW sums are scaled against each other, so that
+// the largest product of a row's gradient and one of its features becomes a number in
+// [2^14, 2^15): products down to 2^-28 of it keep all bits, and what smaller ones lose
+// is below 2^-38 of it, about as far as fp16's least number lies below its largest.
+// The same copy of x leaves out rows without a gradient: what their features hold,
+// NaN included, reaches nothing.
 //
 // Bound by the matrix unit: 8192 x 4096 x 131072 in bf16 6.5 ms forward (1350 TFLOP/s);
 // backward 8 pieces of dz 0.88, dx 0.87 and dW 0.85 ms (1256, 1261, 1297).  Pieces of
@@ -111,15 +113,39 @@ __device__ __forceinline__ int wave_max(int e) {
     return e;
 }
 
-// fp16: the largest exponent of each workgroup's rows, EXPONENTS workgroups at most
-// (262144 rows 5.8 us, by one workgroup 209)
-constexpr int EXPONENTS = 64;
-__global__ __launch_bounds__(1024) void exponents_kernel(LinearGrads g, const int64_t *tokens, int V, int rows, int *most) {
+// The exponent of a magnitude in fp16, or less than any for 0; the largest finite one of 8.
+constexpr int NO_EXPONENT = -1000;
+__device__ __forceinline__ int feature_exponent(uint32_t bits) {
+    return bits ? (int)(__float_as_uint(F16::lo(bits)) >> 23) - 127 : NO_EXPONENT;
+}
+__device__ __forceinline__ uint32_t largest_of(const u32x4 &v, uint32_t most) {
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        const uint32_t h = v[i / 2] >> (16 * (i & 1)) & 0x7fffu;
+        most = h < 0x7c00u && h > most ? h : most;
+    }
+    return most;
+}
+
+// fp16: the largest exponent of a gradient and a feature among each workgroup's rows
+// (those without a gradient left out), EXPONENTS workgroups at most.  x as the products
+// read it, `vectors` a row, which 2^log_lanes threads share.  1 to 2 us of a call's 113
+// (64 x 7680 x 6864) or 69 (6272 x 512 x 1000) are for the features.
+constexpr int EXPONENTS = 512;
+__global__ __launch_bounds__(1024) void exponents_kernel(LinearGrads g, const int64_t *tokens, int V, int rows,
+                                                         const uint16_t *x, int64_t ldx, int vectors, int log_lanes,
+                                                         int *most) {
     __shared__ int s[16];
+    const int lane = threadIdx.x & ((1 << log_lanes) - 1), beside = 1024 >> log_lanes;
     int e = E_MIN;
 #pragma unroll 2
-    for (int r = blockIdx.x * 1024 + threadIdx.x; r < rows; r += gridDim.x * 1024) {
-        const int k = exponent_of(grad_of(g, tokens, V, r));
+    for (int r = blockIdx.x * beside + (threadIdx.x >> log_lanes); r < rows; r += gridDim.x * beside) {
+        const u32x4 *const p = reinterpret_cast<const u32x4 *>(x + r * ldx);
+        uint32_t top = 0;
+        for (int i = lane; i < vectors; i += 1 << log_lanes)
+            top = largest_of(p[i], top);
+        const RowGrad w = grad_of(g, tokens, V, r);
+        const int k = w.c == 0.0f && w.at == 0.0f ? E_MIN : exponent_of(w) + feature_exponent(top);
         e = k > e ? k : e;
     }
     e = wave_max(e);
@@ -137,10 +163,14 @@ __global__ __launch_bounds__(1024) void exponents_kernel(LinearGrads g, const in
 __global__ __launch_bounds__(256) void row_grads_kernel(LinearGrads g, const int64_t *tokens, int V, int rows,
                                                         const int *exponents, int counts, RowGrad *out, float *factor,
                                                         float *row_scale, float *scale) {
-    const int r = blockIdx.x * 256 + threadIdx.x, lane = threadIdx.x & 63;
-    const int most = counts ? wave_max(lane < counts ? exponents[lane] : E_MIN) : 0;
+    const int r = blockIdx.x * 256 + threadIdx.x;
+    int most = E_MIN;
+#pragma unroll 4
+    for (int i = threadIdx.x & 63; i < counts; i += 64)
+        most = exponents[i] > most ? exponents[i] : most;
+    most = wave_max(most);
     if (r == 0 && counts)
-        *scale = pow2(most - 13);
+        *scale = pow2(most - 13 - 14);
     if (r >= rows)
         return;
     RowGrad w = grad_of(g, tokens, V, r);
@@ -151,7 +181,8 @@ __global__ __launch_bounds__(256) void row_grads_kernel(LinearGrads g, const int
         w.c *= pow2(13 - e);
         w.at *= pow2(13 - e);
         row_scale[r] = pow2(e - 13);
-        f = none ? 0.0f : pow2(e - most);
+        const int up = e - most + 14;  // below -126 nothing of x is left but NaN; above 126 x is 0
+        f = none ? 0.0f : pow2(up < -126 ? -126 : up > 126 ? 126 : up);
     }
     out[r] = w;
     factor[r] = f;
@@ -252,8 +283,13 @@ hipError_t backward(const LinearLogProbs &a, const BackwardPlan &p, const Linear
     if (a.rows > 0) {
         int counts = 0;
         if (!bf16) {
-            counts = (a.rows + 1023) / 1024 < EXPONENTS ? (a.rows + 1023) / 1024 : EXPONENTS;
-            exponents_kernel<<<counts, 1024, 0, st>>>(g, a.tokens, a.V, a.rows, p.most);
+            int log_lanes = 0;
+            while (log_lanes < 10 && 8 << log_lanes < a.C)
+                log_lanes++;
+            const int beside = 1024 >> log_lanes, groups = (a.rows + beside - 1) / beside;
+            counts = groups < EXPONENTS ? groups : EXPONENTS;
+            exponents_kernel<<<counts, 1024, 0, st>>>(g, a.tokens, a.V, a.rows, p.x.m.p, p.x.m.ld, p.x.m.ext / 8, log_lanes,
+                                                      p.most);
         }
         row_grads_kernel<<<dim3((unsigned)((a.rows + 255) / 256)), 256, 0, st>>>(
             g, a.tokens, a.V, a.rows, p.most, counts, p.rows, p.factor, p.row_scale, p.scale);

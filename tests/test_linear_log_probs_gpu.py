@@ -213,6 +213,43 @@ def test_small_gradients_keep_their_bits():
             assert bool(((s.double() - want.double()).abs() <= TINY[dt] * 2).all())
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("rows,C", [(2, 40), (16, 64), (24, 72), (300, 129)])
+def test_small_gradients_beside_large_ones(rows, C, dtype):
+    """Rows whose gradients are 2^22 apart, each with a class of its own: that class's row of dw
+    is the row's features times its gradient, whatever the others'.  The first has a larger
+    gradient than all, but no features; the second's features are 2^-9 of the others'.  Off: the
+    rounding of dz and of the result, 16 units of fp32 for the token's gradient, e^-30 of each other
+    row's, and in fp16 half of its least number: of a scaled feature, with a dz below 2^14 and a
+    factor of 2^-27 of the largest product of a gradient and a feature, and of the result."""
+    dt = DT[dtype]
+    x = randn(41, (rows, C)).clamp(-4, 4)
+    x[0], x[1:, 0] = 0.0, 1.0
+    x[1, 1:] *= 2.0**-9 if rows > 2 else 1.0
+    x = x.to(dt)
+    w = torch.zeros(rows + 1, C, dtype=dt)
+    w[0, 0] = 30.0  # the class that all but the first row are near, and nobody's token
+    t = torch.arange(rows) + 1
+    gl = torch.exp2(12.0 - 22.0 * torch.arange(rows) / (rows - 1))
+    gl[0] = 2.0**15
+    lp = cf.linear_log_probs_forward(x.cuda(), w.cuda(), t.cuda())
+    _, dw = cf.linear_log_probs_backward(x.cuda(), w.cuda(), t.cuda(), lp, gl.cuda())
+    xd, gd = x.double(), gl.double()[:, None]
+    p = torch.softmax(mm(xd, w.double().t()), 1)
+    dz = -gd * p
+    dz[torch.arange(rows), t] += gd[:, 0]
+    want = mm(dz.t(), xd)
+    R, most = ROUND[dt], float((gd * xd.abs()).max())
+    e = (R + (16 + rows) * F32) * mm(dz.abs().t(), xd.abs()) + rows * 1e-13 * most
+    e = e + (2.0**-38 * most if dt == torch.float16 else 0.0)
+    e = e + R * (want.abs() + e) + TINY[dt]
+    assert_within(dw[1:], want[1:], e[1:], "dw")
+    # half a step for dz, half a step for the result, but for numbers below fp16's normal ones
+    size = want[1:].norm(dim=1)
+    off = (dw[1:].double().cpu() - want[1:]).norm(dim=1)
+    assert bool((off <= 2 * R * size + C**0.5 * 2.0**-23).all())
+
+
 def test_rows_without_a_gradient():
     """Padding: whatever their features hold, they add nothing."""
     for dt in (torch.float16, torch.bfloat16):

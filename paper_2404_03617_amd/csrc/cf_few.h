@@ -15,9 +15,6 @@
 namespace cf {
 namespace few {
 
-using mm::RowGrad;
-using mm::StoreArgs;
-
 constexpr int ROWS = 16;  // rows of x at most
 
 struct Args {

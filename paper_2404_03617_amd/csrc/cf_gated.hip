@@ -47,14 +47,16 @@ struct ForwardPlan {
     Room room;
     Operand x, wg, wu, wd;
     int pad;
-    int64_t ld, lo;  // of h; to what rounding it takes, or 0
+    int64_t ld, lo;  // of h; to what rounding it takes (few rows)
     uint16_t *h;
-    Plan up, down;
+    Plan up, down;  // of more rows
     void *part;
 };
 ForwardPlan forward_plan(const GatedFfn &a, Copied c, void *ws) {
-    ForwardPlan p;
-    if (a.rows <= few::ROWS)  // read wherever they are
+    static_assert(PART_ROWS == few::ROWS, "products of few rows write h in two numbers, those of more in one");
+    ForwardPlan p = {};
+    const bool few = a.rows <= few::ROWS;
+    if (few)  // read wherever they are
         c = {};
     p.room.p = (uint8_t *)ws;
     p.pad = up8(a.H);
@@ -63,14 +65,14 @@ ForwardPlan forward_plan(const GatedFfn &a, Copied c, void *ws) {
     p.wg = operand(a.w_gate.p, a.w_gate.ld, a.H, a.C, c.wgu, p.room);
     p.wu = operand(a.w_up.p, a.w_up.ld, a.H, a.C, c.wgu, p.room);
     p.wd = operand(a.w_down.p, a.w_down.ld, a.C, a.H, c.wd, p.room);
-    const bool lo = in_parts(a.rows);
-    const int64_t rows = lo ? 2 * a.rows : a.rows;
-    p.lo = lo ? a.rows * p.ld : 0;
-    p.h = (uint16_t *)p.room.take((size_t)rows * p.ld * 2);
+    p.lo = few ? a.rows * p.ld : 0;
+    p.h = (uint16_t *)p.room.take((size_t)(few ? 2 : 1) * a.rows * p.ld * 2);
+    if (few)
+        return p;
     p.up = plan(a.rows, 2 * (int64_t)a.H, a.C, true, 1, 1, MORE);
-    p.down = plan(rows, a.C, a.H, true);
-    const size_t one = joined_bytes(p.up, a.rows, a.H, 2, lo), two = joined_bytes(p.down, rows, a.C, 1, lo);
-    p.part = a.rows <= few::ROWS ? nullptr : p.room.take(one > two ? one : two);
+    p.down = plan(a.rows, a.C, a.H, true);
+    const size_t one = part_bytes(p.up, a.rows, a.H, 2), two = part_bytes(p.down, a.rows, a.C, 1);
+    p.part = p.room.take(one > two ? one : two);
     return p;
 }
 
@@ -127,8 +129,8 @@ hipError_t forward(const GatedFfn &a, const ForwardPlan &p, void *y, int64_t ldy
         return a.rows <= 8 ? few::launch<T, 1, few::Store<true>>(down, s, st)
                            : few::launch<T, 1, few::Store<false>>(down, s, st);
     }
-    const GatedArgs gate = {p.h, p.ld, p.lo, saved, a.H, p.pad, a.act};
-    const bool split = p.up.splits > 1 || p.lo;
+    const GatedArgs gate = {p.h, p.ld, 0, saved, a.H, p.pad, a.act};
+    const bool split = p.up.splits > 1;
     Args up = args_of(p.up, a.rows, split ? a.H : 2 * a.H, a.C, p.x.m, a.rows, p.wg.m, a.H, false, split ? 2 : 1);
     up.b[1] = p.wu.m.p;
     if (split)
@@ -138,10 +140,8 @@ hipError_t forward(const GatedFfn &a, const ForwardPlan &p, void *y, int64_t ldy
     StoreArgs s = {};
     s.out[0] = s.out[1] = (uint16_t *)y;
     s.ldo = ldy;
-    s.fold = p.lo ? a.rows : 0;
-    const int rows = p.lo ? 2 * a.rows : a.rows;
-    return run_store<KC, KC>(args_of(p.down, rows, a.C, a.H, Matrix{p.h, p.ld, p.pad}, rows, p.wd.m, a.C), s, p.down, p.part,
-                             bf16, st);
+    return run_store<KC, KC>(args_of(p.down, a.rows, a.C, a.H, Matrix{p.h, p.ld, p.pad}, a.rows, p.wd.m, a.C), s, p.down,
+                             p.part, bf16, st);
 }
 
 template <typename T>

@@ -105,12 +105,7 @@ __global__ __launch_bounds__(256) void join_kernel(Args a, const float *part, Ga
     float g[8], u[8];
     sum_parts(a, part, 0, m, n, g);
     sum_parts(a, part, 1, m, n, u);
-    with_act(e.act, [&](auto tag) {
-        if (e.lo)
-            Gated::piece<T, decltype(tag)::value, true>(e, g, u, m, n, true);
-        else
-            Gated::piece<T, decltype(tag)::value>(e, g, u, m, n, true);
-    });
+    with_act(e.act, [&](auto tag) { Gated::piece<T, decltype(tag)::value>(e, g, u, m, n, true); });
 }
 template <typename T>
 __global__ __launch_bounds__(256) void join_kernel(Args a, const float *part, GatedBackArgs e, FastDiv vectors,

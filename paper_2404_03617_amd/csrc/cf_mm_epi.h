@@ -176,7 +176,7 @@ struct Store {
 // each gradient).
 struct GatedArgs {
     uint16_t *h;
-    int64_t ldh, lo;  // lo: to what rounding h takes, or 0
+    int64_t ldh, lo;  // lo: to what rounding h takes (few rows, cf_few.h)
     float *saved;  // [M][2 H], g then u, or null
     int H, pad, act;
 };
@@ -189,7 +189,7 @@ struct Gated {
     }
     using Args = GatedArgs;
     // 8 channels of row m from n on; ends: H may be among them
-    template <typename T, int ACT, bool LO = false>
+    template <typename T, int ACT>
     static __device__ __forceinline__ void piece(const GatedArgs &e, const float (&g)[8], const float (&u)[8], int m, int n,
                                                  bool ends) {
         const int left = e.H - n;
@@ -201,7 +201,7 @@ struct Gated {
 #pragma unroll
             for (int k = 0; k < 8; k++)
                 h[k] = k < left ? h[k] : 0.0f;
-        store_parts<T, LO>(e.h + m * e.ldh + n, e.lo, h);
+        store_parts<T, false>(e.h + m * e.ldh + n, 0, h);
         if (e.saved) {
             float *const s = e.saved + (int64_t)m * 2 * e.H + n;
             store_rowf<8>(s, g, left);

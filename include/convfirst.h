@@ -564,7 +564,8 @@ size_t cf_group_norm_backward_workspace_bytes(int64_t N, int64_t P, int C, int G
 /* Gated feed-forward block, x and y [rows][C]:
  *   a = x w_gate^T,  u = x w_up^T,  h = act(a) * u,  y = h w_down^T
  * w_gate, w_up [H][C] and w_down [C][H] in dt, rows ld_* apart.  Sums are fp32; h is
- * rounded to dt for its product, or for up to 16 rows kept in two numbers of dt.
+ * rounded to dt for its product (fp16: infinite beyond 65504), or for up to 16 rows
+ * kept in two numbers of dt.
  * saved [rows][2 H] fp32 receives a and u of each row for the backward pass; NULL
  * for inference.  y may not overlap x. */
 cf_status cf_gated_ffn_forward(const void *x, const void *w_gate, const void *w_up, const void *w_down, void *y,
@@ -608,11 +609,12 @@ size_t cf_linear_log_probs_workspace_bytes(int64_t rows, int C, int V, int align
  * a gradient where p is nearly 1.
  * The logits are made again, a piece of the vocabulary at a time (dz of a piece,
  * in dt, or for up to 16 rows in two numbers of dt, is in the workspace: 256 MiB, or
- * rows * 8 KiB if that is more).  In fp16 dz is scaled by a power of two a row, so
- * that small probabilities keep their bits, and for dweight the rows of x are scaled
- * so that gradients times features keep theirs down to 2^-28 of the largest such
- * product; what smaller ones lose is below 2^-38 of it.  Rows whose d_logp and d_lse are 0 (d_logp counts as 0 for a negative token)
- * or whose lse is -inf have no gradient and add nothing to dweight, whatever
+ * rows * 8 KiB if that is more, for pieces of a multiple of 256 tokens).  In fp16 dz
+ * is scaled by a power of two a row, so that small probabilities keep their bits,
+ * and for dweight the rows of x are scaled so that gradients times features keep
+ * theirs down to 2^-28 of the largest such product; what smaller ones lose is below
+ * 2^-38 of it.  Rows whose d_logp and d_lse are 0 (d_logp counts as 0 for a negative
+ * token) or whose lse is -inf have no gradient and add nothing to dweight, whatever
  * their features hold.  A token of V or more makes the gradients NaN.  dx
  * [rows][C] and dweight [V][C], dense, in dt; rows = 0 gives zeros in dweight.  No
  * output may overlap an input. */

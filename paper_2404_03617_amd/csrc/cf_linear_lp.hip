@@ -14,8 +14,8 @@
 //   dz = c p + d_logp 1[token];  dx = dz W;  dW = dz^T x
 //
 // piece by piece of the vocabulary: the piece's logits are made again and become dz
-// in 16 bits (at most PIECE_BYTES of them), which two products read.  dx runs
-// over the pieces in fp32.
+// in 16 bits (pieces_of: PIECE_BYTES, or 4096 classes of many rows), which two
+// products read.  dx runs over the pieces in fp32.
 //
 // A gradient in 16 bits: in bf16 its range is that of fp32.  In fp16 a row's
 // values are scaled by a power of two, so that the largest of c and the token's value

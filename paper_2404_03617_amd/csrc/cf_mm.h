@@ -98,15 +98,15 @@ __device__ __forceinline__ void wait_copies() {
     __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
 }
 
-// By what the 32-byte pieces of row k of an RC tile are permuted: with what is free
-// behind a copy, the 8 rows that 32 lanes read together (8 q to 8 q + 3 and 8
-// further) lie in different banks.
 // What the 16-byte pieces of a KC row are permuted by: 8 lanes beside each other
 // read 8 rows in different banks.  B's rows of a fragment are 4 of every 8.
 template <bool B>
 __device__ __forceinline__ int kc_swizzle(int row) {
     return B ? (row & 3) | (row >> 1 & 4) : row & 7;
 }
+// By what the 32-byte pieces of row k of an RC tile are permuted: with what is free
+// behind a copy, the 8 rows that 32 lanes read together (8 q to 8 q + 3 and 8
+// further) lie in different banks.
 template <int R>
 __device__ __forceinline__ int rc_swizzle(int k) {
     return R == 256 ? (k & 1) << 1 : k & 3;

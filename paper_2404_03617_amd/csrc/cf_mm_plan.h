@@ -154,9 +154,10 @@ inline Args args_of(const Plan &p, int M, int N, int K, const Matrix &a, int ext
 constexpr int PART_ROWS = 16;
 inline bool in_parts(int64_t rows) { return rows > 0 && rows <= PART_ROWS; }
 
-// The vocabulary of a gradient (cf_linear_lp.hip) goes by pieces, of which dz is in the
-// workspace: of at most PIECE_BYTES (two numbers of few rows: of PART_BYTES), but of at
-// least 4096 columns, all but the last a multiple of 256.  The last is shorter.
+// The vocabulary of a gradient (cf_linear_lp.hip) goes by pieces, whose dz is in the
+// workspace: PIECE_BYTES of it (two numbers of few rows: PART_BYTES), or 4096 columns if
+// that is more, rounded up so that all but the last are multiples of 256.  The last
+// may be shorter.
 constexpr double PIECE_BYTES = 256 << 20;
 struct Pieces {
     int columns, count;

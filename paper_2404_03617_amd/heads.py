@@ -308,9 +308,11 @@ def linear_log_probs_backward(x: torch.Tensor, weight: torch.Tensor, tokens, lp:
                               d_lse=None, out=None, ws=None, stream=None):
     """The gradients (dx, dweight), in x's dtype, of sum(d_logp * lp.logp) +
     sum(d_lse * lp.lse); lp is what linear_log_probs_forward returned (for d_logp,
-    with these tokens), d_logp and d_lse fp32 [...] or None.  Rows without a gradient (both 0, or d_logp of a
-    negative token) add nothing to dweight, whatever their features hold.  ws: a
-    uint8 workspace of linear_log_probs_backward_workspace_bytes()."""
+    with these tokens), d_logp and d_lse fp32 [...] or None.  Rows without a
+    gradient (both 0, or d_logp of a negative token) add nothing to dweight, whatever
+    their features hold.  In fp16 a row adds to dweight with all bits where gradient
+    times feature is at least 2^-28 of the largest such product.  ws: a uint8
+    workspace of linear_log_probs_backward_workspace_bytes()."""
     if stream is None and ws is None and type(lp) is LinearLogProbs:
         r = _native("linear_backward", x, weight, tokens, lp.logp, lp.lse, d_logp, d_lse, out)
         if r is not None:
